@@ -21,6 +21,10 @@
  *   reco_penalty_sample  the same penalty, then the next token drawn
  *                        from softmax(z~ / T), one pass per row      (Eq. 4, Sec. 3.3)
  *   reco_answer_ppl      answer perplexity and stop flag             (Eq. 5, 6)
+ *   reco_paged_decode_attn
+ *                        decode attention over a paged cache, with an
+ *                        optional sliding window, sinks and accumulated
+ *                        attention weights                           (Sec. 1)
  *
  * Conventions shared by every call
  * --------------------------------
@@ -83,7 +87,8 @@ enum {
   RECO_DEV_BAD_SCORE = 3,        /* NaN or negative importance score */
   RECO_DEV_BAD_TOKEN_ID = 4,     /* reflection id or answer token outside [0, vocab) */
   RECO_DEV_BAD_LENGTH = 5,       /* stored len outside [0, capacity] */
-  RECO_DEV_BAD_LOGIT = 6         /* a logit row with no non-NaN value to sample */
+  RECO_DEV_BAD_LOGIT = 6,        /* a logit row with no non-NaN value to sample */
+  RECO_DEV_BAD_PAGE = 7          /* a page id of a cached row outside [0, n_pages) */
 };
 
 /* reco_score flags */
@@ -101,6 +106,32 @@ typedef struct reco_kv_cache {
   int32_t head_dim;     /* 64 or 128 */
   int32_t dtype;        /* reco_dtype_t; every cache-typed tensor uses it */
 } reco_kv_cache_t;
+
+/* [host] description of a paged KV cache; read during the call, not retained.
+ * A page holds page_rows rows of one unit; a unit's row j is row j % page_rows
+ * of page pages[unit][j / page_rows], so a unit can hold
+ * capacity = max_pages * page_rows rows, and pages that its rows do not reach
+ * need not exist: only the first ceil(len / page_rows) ids of a unit (and the
+ * ids of rows that a call appends) are ever read.  Ids outside [0, n_pages) among
+ * these set RECO_DEV_BAD_PAGE.  Several units may share pages that no call
+ * writes to; what a call writes (appended rows, evicted units) has to lie in
+ * pages of one unit, each once in its list. */
+typedef struct reco_paged_cache {
+  void *k;              /* [n_pages][page_rows][head_dim], 16-byte aligned */
+  void *v;              /* same layout as k */
+  const int32_t *pages; /* [n_layers][batch][n_kv_heads][max_pages] page ids */
+  int32_t *len;         /* [n_layers][batch][n_kv_heads], valid rows per unit (in/out) */
+  float *weight;        /* nullable [n_layers][batch][n_kv_heads][capacity], accumulated
+                           attention weight of every row (in/out), 16-byte aligned */
+  int32_t n_layers;     /* layers held by the cache (>= 1) */
+  int32_t batch;        /* sequences (>= 1) */
+  int32_t n_kv_heads;   /* KV heads per layer (>= 1) */
+  int32_t n_pages;      /* pages in k and v (>= 1) */
+  int32_t page_rows;    /* rows of a page: a power of two, 16 .. 4096 */
+  int32_t max_pages;    /* pages of a unit (>= 1); capacity <= 2^29 */
+  int32_t head_dim;     /* 64 or 128 */
+  int32_t dtype;        /* reco_dtype_t; every cache-typed tensor uses it */
+} reco_paged_cache_t;
 
 /* ------------------------------------------------------------------------ */
 /* Eq. 2 (Section 3.2, attention-guided selection): importance of every cached
@@ -231,6 +262,35 @@ reco_status_t reco_decode_attn_noalloc(const reco_kv_cache_t *cache, int32_t lay
                                        const void *q, int32_t n_q_heads, float scale, const void *k_new,
                                        const void *v_new, void *out, float *lse, float *row_stats,
                                        int32_t *dev_err, hipStream_t stream);
+
+/* ------------------------------------------------------------------------ */
+/* Decode attention over a paged cache: reco_decode_attn's computation, append
+ * and errors on the units of a reco_paged_cache_t.  With n = len[unit] (plus the
+ * new row where k_new != NULL) the token at row n - 1 sees the rows j < n with
+ *   j < sinks  or  j >= n - window       (all of them where window = 0),
+ * so a window counts the token's own row.
+ *   q            : [n_layers][batch][n_q_heads][head_dim], cache dtype
+ *   k_new, v_new : both NULL (no append) or [n_layers][batch][n_kv_heads][head_dim]
+ *   sinks, window: >= 0; sinks have no effect where window = 0
+ *   out          : [n_layers][batch][n_q_heads][head_dim], cache dtype (output)
+ *   lse          : nullable [n_layers][batch][n_q_heads] fp32 (output)
+ * Where cache->weight is given, every seen row's weight grows by its attention
+ * probabilities summed over the n_q_heads / n_kv_heads query heads of its group,
+ * and an appended row's weight is set to its own (nothing has to be cleared for
+ * it); weights of rows that are not seen are left as they are.
+ * A unit with no rows to see gets out = 0 and lse = -inf.  Rows whose page id is bad
+ * are taken from page 0; an append whose own page id is bad is not performed (the
+ * token still takes part in the attention).  Tensors are 16-byte aligned; the
+ * workspace, whose size depends on the current device and on whether weights are
+ * kept, 256-byte aligned.  Sizes whose grid would pass 2^32 threads (far beyond any
+ * pool that fits the device): RECO_ERR_UNSUPPORTED. */
+size_t reco_paged_decode_attn_workspace_size(const reco_paged_cache_t *cache, int32_t n_layers,
+                                             int32_t n_q_heads);
+reco_status_t reco_paged_decode_attn(const reco_paged_cache_t *cache, int32_t layer0, int32_t n_layers,
+                                     const void *q, int32_t n_q_heads, float scale, int32_t sinks,
+                                     int32_t window, const void *k_new, const void *v_new, void *out,
+                                     float *lse, void *ws, size_t ws_bytes, int32_t *dev_err,
+                                     hipStream_t stream);
 
 /* ------------------------------------------------------------------------ */
 /* Eq. 3 and Eq. 4 (Section 3.3, reward-banded reflection penalty): for every

@@ -8,6 +8,7 @@ computes a result.  The library must have been built in-tree
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import math
 import os
@@ -29,13 +30,14 @@ RECO_SCORE_CAUSAL = 1
 RECO_POOL_MAX = 0
 RECO_POOL_MEAN = 1
 DEV_ERRORS = {0: "ok", 1: "append overflow", 2: "bad retention", 3: "bad score", 4: "bad token id",
-              5: "bad length", 6: "bad logit row"}
+              5: "bad length", 6: "bad logit row", 7: "bad page"}
 
 EXPORTED = [
     "reco_score_workspace_size", "reco_score", "reco_select_compact_workspace_size", "reco_select_compact",
     "reco_pool_scores", "reco_layer_retention",
     "reco_decode_attn_workspace_size", "reco_decode_attn", "reco_decode_attn_noalloc", "reco_logit_penalty",
     "reco_penalty_sample_workspace_size", "reco_penalty_sample",
+    "reco_paged_decode_attn_workspace_size", "reco_paged_decode_attn",
     "reco_answer_ppl_workspace_size", "reco_answer_ppl", "reco_retention_from_reward", "reco_retention_eq1",
     "reco_kept_count", "reco_status_str", "reco_abi_version",
 ]
@@ -45,6 +47,14 @@ class RecoKVCache(ctypes.Structure):
     _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("len", ctypes.c_void_p),
                 ("n_layers", ctypes.c_int32), ("batch", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32),
                 ("capacity", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("dtype", ctypes.c_int32)]
+
+
+class RecoPagedCache(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("pages", ctypes.c_void_p), ("len", ctypes.c_void_p),
+                ("weight", ctypes.c_void_p),
+                ("n_layers", ctypes.c_int32), ("batch", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32),
+                ("n_pages", ctypes.c_int32), ("page_rows", ctypes.c_int32), ("max_pages", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("dtype", ctypes.c_int32)]
 
 
 _lib = None
@@ -61,6 +71,7 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
     P, I32, I64, F32, F64, SZ, U32, U64 = (ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_float,
                                            ctypes.c_double, ctypes.c_size_t, ctypes.c_uint32, ctypes.c_uint64)
     C = ctypes.POINTER(RecoKVCache)
+    PC = ctypes.POINTER(RecoPagedCache)
     sig = {
         "reco_score_workspace_size": (SZ, [C, I32, I32, I32]),
         "reco_score": (I32, [C, I32, I32, P, I32, I32, F32, U32, P, P, P, SZ, P, P]),
@@ -71,6 +82,8 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
         "reco_decode_attn_workspace_size": (SZ, [C, I32, I32]),
         "reco_decode_attn": (I32, [C, I32, I32, P, I32, F32, P, P, P, P, P, P, SZ, P, P]),
         "reco_decode_attn_noalloc": (I32, [C, I32, I32, P, I32, F32, P, P, P, P, P, P, P]),
+        "reco_paged_decode_attn_workspace_size": (SZ, [PC, I32, I32]),
+        "reco_paged_decode_attn": (I32, [PC, I32, I32, P, I32, F32, I32, I32, P, P, P, P, P, SZ, P, P]),
         "reco_logit_penalty": (I32, [P, I32, I32, I64, P, I32, P, F32, F32, F32, F32, F32, P, P]),
         "reco_penalty_sample_workspace_size": (SZ, [I32, I32]),
         "reco_penalty_sample": (I32, [P, I32, I32, I64, P, I32, P, F32, F32, F32, F32, F32, F32, U64, U64, P, P, SZ,
@@ -183,6 +196,49 @@ class KVCache:
         return ctypes.byref(self.struct)
 
 
+class PagedKVCache:
+    """A KV cache in pages: K and V ``[n_pages][page_rows][D]`` (fp32 or bf16; a
+    page holds rows of one unit), the page ids of every unit ``pages``
+    ``[NL][B][H][max_pages]`` int32, ``length`` ``[NL][B][H]`` int32 and, where
+    attention weights are kept, ``weight`` ``[NL][B][H][max_pages * page_rows]``
+    fp32, all on the GPU.  Allocating pages and listing them is the caller's; a
+    unit's list has to reach the rows that a call appends."""
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor, pages: torch.Tensor, length: torch.Tensor,
+                 weight: Optional[torch.Tensor] = None):
+        if k.shape != v.shape or k.dim() != 3 or k.dtype != v.dtype:
+            raise ValueError("k and v must share a [n_pages][page_rows][D] shape and dtype")
+        if k.dtype not in (torch.float32, torch.bfloat16):
+            raise ValueError("cache dtype must be float32 or bfloat16")
+        if pages.dtype != torch.int32 or pages.dim() != 4:
+            raise ValueError("pages must be int32 [NL][B][H][max_pages]")
+        if length.dtype != torch.int32 or tuple(length.shape) != tuple(pages.shape[:3]):
+            raise ValueError("length must be int32 [NL][B][H]")
+        n_pages, page_rows, D = k.shape
+        NL, B, H, max_pages = pages.shape
+        _expect(weight, "weight", (NL, B, H, max_pages * page_rows), torch.float32)
+        _need_cuda(k, v, pages, length, weight)
+        self.k, self.v, self.pages, self.length, self.weight = k, v, pages, length, weight
+        self.struct = RecoPagedCache(k.data_ptr(), v.data_ptr(), pages.data_ptr(), length.data_ptr(),
+                                     None if weight is None else weight.data_ptr(), NL, B, H, n_pages, page_rows,
+                                     max_pages, D, RECO_F32 if k.dtype == torch.float32 else RECO_BF16)
+
+    @property
+    def shape(self):
+        """(NL, B, H, capacity of a unit, D)"""
+        return tuple(self.pages.shape[:3]) + (self.pages.shape[3] * self.k.shape[1], self.k.shape[2])
+
+    def ref(self):
+        return ctypes.byref(self.struct)
+
+
+def _on(t: torch.Tensor):
+    """The tensor's GPU as the current one: launches and compute-unit counts go by that."""
+    if torch.cuda.current_device() == t.get_device():
+        return contextlib.nullcontext()
+    return torch.cuda.device(t.get_device())
+
+
 def _layers(cache: KVCache, layer0: int, n_layers: Optional[int]):
     layer0 = int(layer0)
     nl = (cache.shape[0] - layer0) if n_layers is None else int(n_layers)
@@ -206,6 +262,12 @@ def decode_attn_workspace_size(cache: KVCache, n_q_heads: int, n_layers: Optiona
     return int(load_library().reco_decode_attn_workspace_size(cache.ref(), nl, n_q_heads))
 
 
+def paged_decode_attn_workspace_size(cache: PagedKVCache, n_q_heads: int, n_layers: Optional[int] = None) -> int:
+    nl = cache.shape[0] if n_layers is None else n_layers
+    with _on(cache.k):
+        return int(load_library().reco_paged_decode_attn_workspace_size(cache.ref(), nl, n_q_heads))
+
+
 def penalty_sample_workspace_size(rows: int, vocab: int) -> int:
     return int(load_library().reco_penalty_sample_workspace_size(rows, vocab))
 
@@ -226,6 +288,12 @@ def decode_workspace(cache: "KVCache", n_q_heads: int, n_layers: Optional[int] =
     """A decode workspace (contents need not be initialised).  Do not share
     one between overlapping calls."""
     return _ws(lambda: decode_attn_workspace_size(cache, n_q_heads, n_layers), cache.k.device, None)
+
+
+def paged_decode_workspace(cache: PagedKVCache, n_q_heads: int, n_layers: Optional[int] = None) -> torch.Tensor:
+    """A workspace for reco_paged_decode_attn (contents need not be initialised).
+    Do not share one between overlapping calls."""
+    return _ws(lambda: paged_decode_attn_workspace_size(cache, n_q_heads, n_layers), cache.k.device, None)
 
 
 def _score_shapes(cache: KVCache, nl: int, q_win: torch.Tensor, w: int, scores, row_stats):
@@ -437,6 +505,97 @@ class PreparedDecode:
                       *self._fixed_tail, _ptr(row_stats), *self._ws, _stream(self._dev))
         if st != RECO_OK:
             _check(st, "reco_decode_attn")
+        return self.out, self.lse
+
+
+def _paged_decode_shapes(cache: PagedKVCache, nl: int, q: torch.Tensor, k_new, v_new, out, lse):
+    NL, B, H, Cap, D = cache.shape
+    if q.dim() != 4 or q.shape[0] != nl or q.shape[1] != B or q.shape[3] != D or q.dtype != cache.k.dtype:
+        raise ValueError("q must be [n_layers][B][Hq][D] in the cache dtype")
+    hq = q.shape[2]
+    if (k_new is None) != (v_new is None):
+        raise ValueError("k_new and v_new must be given together")
+    _expect(k_new, "k_new", (nl, B, H, D), cache.k.dtype)
+    _expect(v_new, "v_new", (nl, B, H, D), cache.k.dtype)
+    _expect(out, "out", (nl, B, hq, D), cache.k.dtype)
+    _expect(lse, "lse", (nl, B, hq), torch.float32)
+    return hq
+
+
+def reco_paged_decode_attn(cache: PagedKVCache, q: torch.Tensor, k_new: Optional[torch.Tensor] = None,
+                           v_new: Optional[torch.Tensor] = None, sinks: int = 0, window: int = 0,
+                           scale: Optional[float] = None, out: Optional[torch.Tensor] = None,
+                           lse: Optional[torch.Tensor] = None, want_lse: bool = True, layer0: int = 0,
+                           n_layers: Optional[int] = None, ws: Optional[torch.Tensor] = None,
+                           dev_err: Optional[torch.Tensor] = None):
+    """GQA decode attention over a paged cache (optionally appending the new
+    token); returns (out, lse).  ``window`` > 0: the token sees its last
+    ``window`` rows (its own among them) and the first ``sinks``.  A cache with
+    weights accumulates them."""
+    layer0, nl = _layers(cache, layer0, n_layers)
+    hq = _paged_decode_shapes(cache, nl, q, k_new, v_new, out, lse)
+    _expect_dev_err(dev_err)
+    _need_cuda(cache.k, q, k_new, v_new, out, lse, ws, dev_err)
+    NL, B, H, Cap, D = cache.shape
+    if out is None:
+        out = torch.empty_like(q)
+    if lse is None and want_lse:
+        lse = torch.empty((nl, B, hq), dtype=torch.float32, device=q.device)
+    ws = _ws(lambda: paged_decode_attn_workspace_size(cache, hq, nl), q.device, ws)
+    scale = 1.0 / math.sqrt(D) if scale is None else float(scale)
+    with _on(q):
+        st = load_library().reco_paged_decode_attn(cache.ref(), layer0, nl, _ptr(q), hq, scale, int(sinks),
+                                                   int(window), _ptr(k_new), _ptr(v_new), _ptr(out), _ptr(lse),
+                                                   _ptr(ws), _nbytes(ws), _ptr(dev_err), _stream(q.device))
+    _check(st, "reco_paged_decode_attn")
+    return out, lse
+
+
+class PreparedPagedDecode:
+    """reco_paged_decode_attn for a loop that calls it again and again with the
+    same cache, outputs, workspace and error word, as PreparedDecode is for
+    reco_decode_attn: those are checked once here, each call checks the tensors
+    that change from token to token."""
+
+    def __init__(self, cache: PagedKVCache, n_q_heads: int, out: torch.Tensor, lse: Optional[torch.Tensor],
+                 ws: torch.Tensor, dev_err: Optional[torch.Tensor] = None, sinks: int = 0, window: int = 0,
+                 scale: Optional[float] = None, layer0: int = 0, n_layers: Optional[int] = None):
+        layer0, nl = _layers(cache, layer0, n_layers)
+        NL, Bsz, H, Cap, D = cache.shape
+        hq = int(n_q_heads)
+        if out is None or ws is None:
+            raise ValueError("out and ws must be given")
+        _expect(out, "out", (nl, Bsz, hq, D), cache.k.dtype)
+        _expect(lse, "lse", (nl, Bsz, hq), torch.float32)
+        _expect_dev_err(dev_err)
+        _need_cuda(cache.k, out, lse, ws, dev_err)
+        if _nbytes(ws) < paged_decode_attn_workspace_size(cache, hq, nl):
+            raise ValueError("ws is smaller than reco_paged_decode_attn_workspace_size")
+        self.cache, self.out, self.lse = cache, out, lse
+        self._keep = (ws, dev_err)
+        self._fn = load_library().reco_paged_decode_attn
+        self._dev, self._dt = cache.k.device, cache.k.dtype
+        self._q_shape, self._kv_shape = (nl, Bsz, hq, D), (nl, Bsz, H, D)
+        scale = 1.0 / math.sqrt(D) if scale is None else float(scale)
+        self._head = (cache.ref(), layer0, nl)
+        self._mid = (hq, scale, int(sinks), int(window))
+        self._tail = (_ptr(out), _ptr(lse), _ptr(ws), _nbytes(ws), _ptr(dev_err))
+
+    def _check_t(self, t: torch.Tensor, what: str, shape):
+        if tuple(t.shape) != shape or t.dtype != self._dt or t.device != self._dev or not t.is_contiguous():
+            raise ValueError(f"{what} must be a contiguous {_DT[self._dt]} {list(shape)} tensor on {self._dev}")
+
+    def __call__(self, q: torch.Tensor, k_new: Optional[torch.Tensor] = None, v_new: Optional[torch.Tensor] = None):
+        self._check_t(q, "q", self._q_shape)
+        if (k_new is None) != (v_new is None):
+            raise ValueError("k_new and v_new must be given together")
+        if k_new is not None:
+            self._check_t(k_new, "k_new", self._kv_shape)
+            self._check_t(v_new, "v_new", self._kv_shape)
+        with _on(q):
+            st = self._fn(*self._head, _ptr(q), *self._mid, _ptr(k_new), _ptr(v_new), *self._tail, _stream(self._dev))
+        if st != RECO_OK:
+            _check(st, "reco_paged_decode_attn")
         return self.out, self.lse
 
 

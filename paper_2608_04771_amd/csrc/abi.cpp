@@ -6,11 +6,14 @@
 #include <hip/hip_runtime.h>
 #include <math.h>
 
-#include <atomic>
 #include <stddef.h>
 #include <stdint.h>
 
+#include "abi_common.hpp"
 #include "reco_kernels.hpp"
+
+using reco::current_compute_units;
+using reco::hip_status;
 
 namespace {
 
@@ -46,23 +49,6 @@ bool units_ok(const reco_kv_cache_t *c, int32_t n_layers) {
 int group_of(const reco_kv_cache_t *c, int32_t n_q_heads) {
   if (n_q_heads < 1 || n_q_heads % c->n_kv_heads != 0) return -1;
   return n_q_heads / c->n_kv_heads;
-}
-
-reco_status_t hip_status(hipError_t e) { return e == hipSuccess ? RECO_OK : RECO_ERR_HIP; }
-
-// Compute units of the current device, read once per device (256 on a whole
-// MI355X; a partitioned GPU shows fewer).  Falls back to 256 if the query
-// fails, which only changes the split count, never correctness.
-int current_compute_units() {
-  constexpr int kMaxDevices = 64;
-  static std::atomic<int> cached[kMaxDevices];
-  int dev = 0;
-  if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= kMaxDevices) return 256;
-  int n = cached[dev].load(std::memory_order_relaxed);
-  if (n > 0) return n;
-  if (hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || n < 1) n = 256;
-  cached[dev].store(n, std::memory_order_relaxed);
-  return n;
 }
 
 }  // namespace

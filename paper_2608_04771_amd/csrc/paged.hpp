@@ -1,0 +1,53 @@
+// Launch interface of the kernels over a paged KV cache (paged_decode.hip,
+// paged_prefill.hip, paged_evict.hip).  Not part of the public ABI.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stddef.h>
+#include <stdint.h>
+
+namespace reco {
+
+// A page holds 1 << page_shift rows (16 or more) of one unit; cap = max_pages << page_shift.
+struct PagedCache {
+  void *k;                // [n_pages][page rows][D]
+  void *v;
+  const int32_t *pages;   // [cache layers][batch][hkv][max_pages]
+  int32_t *len;           // [cache layers][batch][hkv]
+  float *weight;          // nullable [cache layers][batch][hkv][cap]
+  int32_t *dev_err;
+  int layer0, n_layers, batch, hkv, n_pages, page_shift, max_pages, cap;
+};
+
+// ---- attention of one new token ---------------------------------------------
+struct PagedDecodeParams {
+  PagedCache c;
+  const void *q;          // [n_layers][batch][hq][D]
+  const void *k_new;      // nullable [n_layers][batch][hkv][D]
+  const void *v_new;
+  void *out;              // [n_layers][batch][hq][D]
+  float *lse;             // nullable [n_layers][batch][hq]
+  float *part_o;          // [units][splits][group][D]
+  float *part_ml;         // [units][splits][2][group]  (maxima, sums)
+  int32_t *len_in;        // [units]  lengths before the append, for the weights
+  float *logits;          // [units][group][logit_pitch]  log2-domain logits, where weights are kept
+  int64_t logit_pitch;
+  int group, hq, splits, cus;
+  int sinks, window;      // window 0: every row is visible
+  float scale_log2;       // logit scale * log2(e)
+};
+// Most tiles of kPagedTile rows that a call's tokens see.
+constexpr int kPagedTile = 32;
+constexpr int kPagedMaxSplits = 128;
+int paged_span_tiles(int capacity, int sinks, int window);
+int paged_decode_splits(int units, int span_tiles, int compute_units);
+size_t paged_decode_workspace_bytes(int units, int capacity, int group, int head_dim, bool weights, int compute_units);
+// Places the parts of a call's workspace; p.splits, p.group and p.c.cap are set.
+void paged_decode_place(PagedDecodeParams &p, int head_dim, void *ws);
+// Workgroups that the weights of a call's unit take, and whether they fit a grid.
+constexpr int kPagedWeightRows = 1024;
+int paged_weight_chunks(const PagedDecodeParams &p);
+bool paged_decode_fits_grid(const PagedDecodeParams &p);
+hipError_t launch_paged_decode(const PagedDecodeParams &p, int dtype, int head_dim, hipStream_t s);
+
+}  // namespace reco

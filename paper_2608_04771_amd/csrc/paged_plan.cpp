@@ -1,0 +1,63 @@
+// Work split of the kernels over a paged cache and the workspaces it implies
+// (host code).
+#include "paged.hpp"
+
+#include "decode_plan.hpp"
+
+namespace reco {
+
+namespace {
+size_t aligned(size_t bytes) { return (bytes + 255) / 256 * 256; }
+size_t logit_pitch(int capacity) { return (static_cast<size_t>(capacity) + 1 + kPagedTile - 1) / kPagedTile * kPagedTile; }
+size_t partial_bytes(int units, int splits, int group, int head_dim) {
+  return aligned(static_cast<size_t>(units) * splits * group * (static_cast<size_t>(head_dim) + 2) * sizeof(float));
+}
+}  // namespace
+
+int paged_span_tiles(int capacity, int sinks, int window) {
+  const int64_t all = (static_cast<int64_t>(capacity) + 1 + kPagedTile - 1) / kPagedTile;
+  if (window == 0) return static_cast<int>(all);
+  // the sinks' tiles, and a window's, which may begin and end inside a tile
+  const int64_t seen = (static_cast<int64_t>(sinks) + kPagedTile - 1) / kPagedTile +
+                       (static_cast<int64_t>(window) + 2 * kPagedTile - 2) / kPagedTile;
+  return static_cast<int>(seen < all ? seen : all);
+}
+
+// The rule of the dense cache (decode_plan.cpp) on the rows that can be visible.
+int paged_decode_splits(int units, int span_tiles, int compute_units) {
+  return decode_splits(units, span_tiles * kDecodeTile - 1, compute_units);
+}
+
+size_t paged_decode_workspace_bytes(int units, int capacity, int group, int head_dim, bool weights,
+                                    int compute_units) {
+  // a window takes no more splits than the whole cache does
+  const int splits = paged_decode_splits(units, paged_span_tiles(capacity, 0, 0), compute_units);
+  size_t bytes = partial_bytes(units, splits, group, head_dim) + aligned(static_cast<size_t>(units) * sizeof(int32_t));
+  if (weights) bytes += static_cast<size_t>(units) * group * logit_pitch(capacity) * sizeof(float);
+  return bytes;
+}
+
+int paged_weight_chunks(const PagedDecodeParams &p) {
+  if (!p.c.weight) return 0;
+  const int64_t rows = static_cast<int64_t>(paged_span_tiles(p.c.cap, p.sinks, p.window)) * kPagedTile;
+  return static_cast<int>((rows + kPagedWeightRows - 1) / kPagedWeightRows);
+}
+
+bool paged_decode_fits_grid(const PagedDecodeParams &p) {
+  const int64_t units = static_cast<int64_t>(p.c.n_layers) * p.c.batch * p.c.hkv;
+  return units * (p.group + paged_weight_chunks(p)) < (int64_t{1} << 24);   // of 256 threads
+}
+
+void paged_decode_place(PagedDecodeParams &p, int head_dim, void *ws) {
+  const int units = p.c.n_layers * p.c.batch * p.c.hkv;
+  char *at = static_cast<char *>(ws);
+  p.part_o = reinterpret_cast<float *>(at);
+  p.part_ml = p.part_o + static_cast<size_t>(units) * p.splits * p.group * head_dim;
+  at += partial_bytes(units, p.splits, p.group, head_dim);
+  p.len_in = reinterpret_cast<int32_t *>(at);
+  at += aligned(static_cast<size_t>(units) * sizeof(int32_t));
+  p.logits = p.c.weight ? reinterpret_cast<float *>(at) : nullptr;
+  p.logit_pitch = static_cast<int64_t>(logit_pitch(p.c.cap));
+}
+
+}  // namespace reco
