@@ -25,6 +25,8 @@
  *                        decode attention over a paged cache, with an
  *                        optional sliding window, sinks and accumulated
  *                        attention weights                           (Sec. 1)
+ *   reco_paged_evict     keep a budget of rows by accumulated attention
+ *                        weight, compacted within their pages        (Sec. 1)
  *
  * Conventions shared by every call
  * --------------------------------
@@ -88,7 +90,8 @@ enum {
   RECO_DEV_BAD_TOKEN_ID = 4,     /* reflection id or answer token outside [0, vocab) */
   RECO_DEV_BAD_LENGTH = 5,       /* stored len outside [0, capacity] */
   RECO_DEV_BAD_LOGIT = 6,        /* a logit row with no non-NaN value to sample */
-  RECO_DEV_BAD_PAGE = 7          /* a page id of a cached row outside [0, n_pages) */
+  RECO_DEV_BAD_PAGE = 7,         /* a page id of a cached row outside [0, n_pages) */
+  RECO_DEV_BAD_BUDGET = 8        /* an eviction budget below 1 or below sinks + recent */
 };
 
 /* reco_score flags */
@@ -291,6 +294,33 @@ reco_status_t reco_paged_decode_attn(const reco_paged_cache_t *cache, int32_t la
                                      int32_t window, const void *k_new, const void *v_new, void *out,
                                      float *lse, void *ws, size_t ws_bytes, int32_t *dev_err,
                                      hipStream_t stream);
+
+/* ------------------------------------------------------------------------ */
+/* Eviction from a paged cache by accumulated attention weight (the heavy-hitter
+ * policies cited in Section 1).  Per unit with L = len[unit] and
+ * m = budget[lc * budget_layer_stride + seq] (lc = layer - layer0):
+ *   L <= m : everything is kept, nothing is written but kept_idx (0 .. L-1);
+ *   L >  m : the rows [0, sinks), the rows [L - recent, L) and, of those between,
+ *            the m - sinks - recent with the largest cache->weight (ties: lower
+ *            row first) are kept.  They move, in ascending order, to the rows
+ *            0 .. m-1 of the unit (bit-exact copies, weights with them) and len is
+ *            set to m.  Rows and weights at and past m are left as they are; the
+ *            pages past the first ceil(m / page_rows) are the caller's again.
+ *   budget   : int32; [batch] with budget_layer_stride = 0 or [n_layers][batch]
+ *              with stride = batch; 1 or more, and sinks + recent at least
+ *   sinks, recent : >= 0
+ *   kept_idx : nullable [n_layers][batch][n_kv_heads][capacity] int32 output; the
+ *              first entries of each unit receive the kept rows' positions
+ *              (ascending, in numbering before the call), the others are left
+ * cache->weight has to be given; +inf ranks above all, and a negative or NaN weight
+ * among the rows to choose from is RECO_DEV_BAD_SCORE.  A unit whose length, budget,
+ * page ids or weights are bad is left unchanged (kept_idx unspecified) and dev_err
+ * is set.  The workspace is 256-byte aligned. */
+size_t reco_paged_evict_workspace_size(const reco_paged_cache_t *cache, int32_t n_layers);
+reco_status_t reco_paged_evict(const reco_paged_cache_t *cache, int32_t layer0, int32_t n_layers,
+                               const int32_t *budget, int64_t budget_layer_stride, int32_t sinks,
+                               int32_t recent, int32_t *kept_idx, void *ws, size_t ws_bytes,
+                               int32_t *dev_err, hipStream_t stream);
 
 /* ------------------------------------------------------------------------ */
 /* Eq. 3 and Eq. 4 (Section 3.3, reward-banded reflection penalty): for every

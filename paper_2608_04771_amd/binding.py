@@ -30,7 +30,7 @@ RECO_SCORE_CAUSAL = 1
 RECO_POOL_MAX = 0
 RECO_POOL_MEAN = 1
 DEV_ERRORS = {0: "ok", 1: "append overflow", 2: "bad retention", 3: "bad score", 4: "bad token id",
-              5: "bad length", 6: "bad logit row", 7: "bad page"}
+              5: "bad length", 6: "bad logit row", 7: "bad page", 8: "bad budget"}
 
 EXPORTED = [
     "reco_score_workspace_size", "reco_score", "reco_select_compact_workspace_size", "reco_select_compact",
@@ -38,6 +38,7 @@ EXPORTED = [
     "reco_decode_attn_workspace_size", "reco_decode_attn", "reco_decode_attn_noalloc", "reco_logit_penalty",
     "reco_penalty_sample_workspace_size", "reco_penalty_sample",
     "reco_paged_decode_attn_workspace_size", "reco_paged_decode_attn",
+    "reco_paged_evict_workspace_size", "reco_paged_evict",
     "reco_answer_ppl_workspace_size", "reco_answer_ppl", "reco_retention_from_reward", "reco_retention_eq1",
     "reco_kept_count", "reco_status_str", "reco_abi_version",
 ]
@@ -84,6 +85,8 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
         "reco_decode_attn_noalloc": (I32, [C, I32, I32, P, I32, F32, P, P, P, P, P, P, P]),
         "reco_paged_decode_attn_workspace_size": (SZ, [PC, I32, I32]),
         "reco_paged_decode_attn": (I32, [PC, I32, I32, P, I32, F32, I32, I32, P, P, P, P, P, SZ, P, P]),
+        "reco_paged_evict_workspace_size": (SZ, [PC, I32]),
+        "reco_paged_evict": (I32, [PC, I32, I32, P, I64, I32, I32, P, P, SZ, P, P]),
         "reco_logit_penalty": (I32, [P, I32, I32, I64, P, I32, P, F32, F32, F32, F32, F32, P, P]),
         "reco_penalty_sample_workspace_size": (SZ, [I32, I32]),
         "reco_penalty_sample": (I32, [P, I32, I32, I64, P, I32, P, F32, F32, F32, F32, F32, F32, U64, U64, P, P, SZ,
@@ -266,6 +269,11 @@ def paged_decode_attn_workspace_size(cache: PagedKVCache, n_q_heads: int, n_laye
     nl = cache.shape[0] if n_layers is None else n_layers
     with _on(cache.k):
         return int(load_library().reco_paged_decode_attn_workspace_size(cache.ref(), nl, n_q_heads))
+
+
+def paged_evict_workspace_size(cache: PagedKVCache, n_layers: Optional[int] = None) -> int:
+    nl = cache.shape[0] if n_layers is None else n_layers
+    return int(load_library().reco_paged_evict_workspace_size(cache.ref(), nl))
 
 
 def penalty_sample_workspace_size(rows: int, vocab: int) -> int:
@@ -597,6 +605,30 @@ class PreparedPagedDecode:
         if st != RECO_OK:
             _check(st, "reco_paged_decode_attn")
         return self.out, self.lse
+
+
+def reco_paged_evict(cache: PagedKVCache, budget: torch.Tensor, sinks: int = 0, recent: int = 0,
+                     kept_idx: Optional[torch.Tensor] = None, layer0: int = 0, n_layers: Optional[int] = None,
+                     ws: Optional[torch.Tensor] = None, dev_err: Optional[torch.Tensor] = None):
+    """Keep ``budget`` rows of every longer unit, by accumulated weight, the first
+    ``sinks`` and the last ``recent`` always; compact K, V and the weights in
+    their pages (len <- budget).  ``budget`` is int32 [B] or [n_layers][B]."""
+    layer0, nl = _layers(cache, layer0, n_layers)
+    NL, Bsz, H, Cap, D = cache.shape
+    if cache.weight is None:
+        raise ValueError("eviction needs a cache with weights")
+    if budget.dtype != torch.int32 or tuple(budget.shape) not in ((Bsz,), (nl, Bsz)):
+        raise ValueError("budget must be int32 [B] or [n_layers][B]")
+    _expect(kept_idx, "kept_idx", (nl, Bsz, H, Cap), torch.int32)
+    _expect_dev_err(dev_err)
+    _need_cuda(cache.k, budget, kept_idx, ws, dev_err)
+    ws = _ws(lambda: paged_evict_workspace_size(cache, nl), cache.k.device, ws)
+    with _on(cache.k):
+        st = load_library().reco_paged_evict(cache.ref(), layer0, nl, _ptr(budget), 0 if budget.dim() == 1 else Bsz,
+                                             int(sinks), int(recent), _ptr(kept_idx), _ptr(ws), _nbytes(ws),
+                                             _ptr(dev_err), _stream(cache.k.device))
+    _check(st, "reco_paged_evict")
+    return kept_idx
 
 
 def _logit_rows(logits: torch.Tensor):

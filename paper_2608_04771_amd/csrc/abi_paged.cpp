@@ -119,4 +119,36 @@ reco_status_t reco_paged_decode_attn(const reco_paged_cache_t *cache, int32_t la
   return reco::hip_status(reco::launch_paged_decode(p, cache->dtype, cache->head_dim, stream));
 }
 
+// ---------------------------------------------------------------- eviction
+size_t reco_paged_evict_workspace_size(const reco_paged_cache_t *cache, int32_t n_layers) {
+  if (!paged_ok(cache) || paged_supported(cache) != RECO_OK) return 0;
+  const int units = units_of(cache, n_layers);
+  if (units < 1) return 0;
+  return reco::paged_evict_workspace_bytes(units, static_cast<int>(capacity_of(cache)), true);
+}
+
+reco_status_t reco_paged_evict(const reco_paged_cache_t *cache, int32_t layer0, int32_t n_layers,
+                               const int32_t *budget, int64_t budget_layer_stride, int32_t sinks, int32_t recent,
+                               int32_t *kept_idx, void *ws, size_t ws_bytes, int32_t *dev_err, hipStream_t stream) {
+  if (!paged_ok(cache) || !cache->weight || !budget || budget_layer_stride < 0) return RECO_ERR_INVALID_ARG;
+  if (sinks < 0 || recent < 0) return RECO_ERR_INVALID_ARG;
+  if (!paged_layers_ok(cache, layer0, n_layers)) return RECO_ERR_INVALID_ARG;
+  const int units = units_of(cache, n_layers);
+  if (units < 1) return RECO_ERR_INVALID_ARG;
+  const reco_status_t st = paged_supported(cache);
+  if (st != RECO_OK) return st;
+
+  reco::PagedEvictParams p{};
+  p.c = paged_cache(cache, layer0, n_layers, dev_err);
+  const size_t need = reco::paged_evict_workspace_bytes(units, p.c.cap, kept_idx == nullptr);
+  if (!ws || ws_bytes < need || (reinterpret_cast<uintptr_t>(ws) & 255)) return RECO_ERR_WORKSPACE;
+  p.budget = budget;
+  p.budget_stride = budget_layer_stride;
+  p.sinks = sinks;
+  p.recent = recent;
+  p.idx = kept_idx;
+  reco::paged_evict_place(p, ws);
+  return reco::hip_status(reco::launch_paged_evict(p, cache->dtype, cache->head_dim, stream));
+}
+
 }  // extern "C"

@@ -50,4 +50,18 @@ int paged_weight_chunks(const PagedDecodeParams &p);
 bool paged_decode_fits_grid(const PagedDecodeParams &p);
 hipError_t launch_paged_decode(const PagedDecodeParams &p, int dtype, int head_dim, hipStream_t s);
 
+// ---- eviction -----------------------------------------------------------------
+struct PagedEvictParams {
+  PagedCache c;           // with weights
+  const int32_t *budget;  // [batch], or [n_layers][batch] with budget_stride = batch
+  int64_t budget_stride;
+  int32_t *idx;           // [units][cap]  kept rows (the caller's buffer or the workspace)
+  bool idx_wanted;        // the caller's: written for units that keep everything, too
+  int32_t *kept;          // [units]  rows after the call, or -1 where nothing moves
+  int sinks, recent;
+};
+size_t paged_evict_workspace_bytes(int units, int capacity, bool need_idx);
+void paged_evict_place(PagedEvictParams &p, void *ws);
+hipError_t launch_paged_evict(const PagedEvictParams &p, int dtype, int head_dim, hipStream_t s);
+
 }  // namespace reco

@@ -60,4 +60,19 @@ void paged_decode_place(PagedDecodeParams &p, int head_dim, void *ws) {
   p.logit_pitch = static_cast<int64_t>(logit_pitch(p.c.cap));
 }
 
+size_t paged_evict_workspace_bytes(int units, int capacity, bool need_idx) {
+  size_t bytes = aligned(static_cast<size_t>(units) * sizeof(int32_t));
+  if (need_idx) bytes += static_cast<size_t>(units) * capacity * sizeof(int32_t);
+  return bytes;
+}
+
+void paged_evict_place(PagedEvictParams &p, void *ws) {
+  const int units = p.c.n_layers * p.c.batch * p.c.hkv;
+  char *at = static_cast<char *>(ws);
+  p.kept = reinterpret_cast<int32_t *>(at);
+  at += aligned(static_cast<size_t>(units) * sizeof(int32_t));
+  p.idx_wanted = p.idx != nullptr;
+  if (!p.idx) p.idx = reinterpret_cast<int32_t *>(at);
+}
+
 }  // namespace reco
