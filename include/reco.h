@@ -25,6 +25,10 @@
  *                        decode attention over a paged cache, with an
  *                        optional sliding window, sinks and accumulated
  *                        attention weights                           (Sec. 1)
+ *   reco_paged_prefill_attn
+ *                        causal attention of a run of new tokens (a
+ *                        prompt, a chunk of one, an answer probe) over
+ *                        a paged cache, window and sinks optional   (Sec. 3.3)
  *   reco_paged_evict     keep a budget of rows by accumulated attention
  *                        weight, compacted within their pages        (Sec. 1)
  *
@@ -294,6 +298,34 @@ reco_status_t reco_paged_decode_attn(const reco_paged_cache_t *cache, int32_t la
                                      int32_t window, const void *k_new, const void *v_new, void *out,
                                      float *lse, void *ws, size_t ws_bytes, int32_t *dev_err,
                                      hipStream_t stream);
+
+/* ------------------------------------------------------------------------ */
+/* Attention of a run of new tokens over a paged cache: a prompt, a chunk of one, or
+ * the answer probe of Section 3.3 in one call.  Sequence b brings n = n_new[b] tokens
+ * (n_tokens of them where n_new is NULL), the first n of n_tokens places; token t of
+ * a unit with L = len[unit] cached rows stands at row p = L + t and sees the rows
+ * j <= p of the cache and of the run with
+ *   j < sinks  or  j > p - window      (all of them where window = 0).
+ * After the attention the run's K/V rows are written to rows L .. L + n - 1, their
+ * weights (where cache->weight is given) are set to 0, and len becomes L + n.
+ *   q            : [n_layers][batch][n_q_heads][n_tokens][head_dim], cache dtype
+ *   k_new, v_new : [n_layers][batch][n_kv_heads][n_tokens][head_dim]
+ *   n_new        : nullable [batch] int32 in [0, n_tokens]
+ *   out          : like q (output);  lse : nullable, like q without head_dim, fp32
+ * Places past a sequence's tokens are neither read nor written.  A run that does not
+ * fit its unit's capacity (RECO_DEV_APPEND_OVERFLOW), or whose rows' page ids are bad
+ * (RECO_DEV_BAD_PAGE), is attended but not stored; a bad stored length
+ * (RECO_DEV_BAD_LENGTH) is clamped for the attention and nothing is stored; a bad
+ * n_new (RECO_DEV_BAD_LENGTH) counts as 0.  q, k_new, v_new and out are 16-byte
+ * aligned, the workspace 256-byte aligned.  n_tokens >= 1; n_tokens * G <= 2^29 and
+ * fewer than 2^24 workgroups (larger: RECO_ERR_UNSUPPORTED). */
+size_t reco_paged_prefill_attn_workspace_size(const reco_paged_cache_t *cache, int32_t n_layers,
+                                              int32_t n_q_heads, int32_t n_tokens);
+reco_status_t reco_paged_prefill_attn(const reco_paged_cache_t *cache, int32_t layer0, int32_t n_layers,
+                                      const void *q, int32_t n_q_heads, int32_t n_tokens,
+                                      const int32_t *n_new, float scale, int32_t sinks, int32_t window,
+                                      const void *k_new, const void *v_new, void *out, float *lse,
+                                      void *ws, size_t ws_bytes, int32_t *dev_err, hipStream_t stream);
 
 /* ------------------------------------------------------------------------ */
 /* Eviction from a paged cache by accumulated attention weight (the heavy-hitter

@@ -38,6 +38,7 @@ EXPORTED = [
     "reco_decode_attn_workspace_size", "reco_decode_attn", "reco_decode_attn_noalloc", "reco_logit_penalty",
     "reco_penalty_sample_workspace_size", "reco_penalty_sample",
     "reco_paged_decode_attn_workspace_size", "reco_paged_decode_attn",
+    "reco_paged_prefill_attn_workspace_size", "reco_paged_prefill_attn",
     "reco_paged_evict_workspace_size", "reco_paged_evict",
     "reco_answer_ppl_workspace_size", "reco_answer_ppl", "reco_retention_from_reward", "reco_retention_eq1",
     "reco_kept_count", "reco_status_str", "reco_abi_version",
@@ -85,6 +86,8 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
         "reco_decode_attn_noalloc": (I32, [C, I32, I32, P, I32, F32, P, P, P, P, P, P, P]),
         "reco_paged_decode_attn_workspace_size": (SZ, [PC, I32, I32]),
         "reco_paged_decode_attn": (I32, [PC, I32, I32, P, I32, F32, I32, I32, P, P, P, P, P, SZ, P, P]),
+        "reco_paged_prefill_attn_workspace_size": (SZ, [PC, I32, I32, I32]),
+        "reco_paged_prefill_attn": (I32, [PC, I32, I32, P, I32, I32, P, F32, I32, I32, P, P, P, P, P, SZ, P, P]),
         "reco_paged_evict_workspace_size": (SZ, [PC, I32]),
         "reco_paged_evict": (I32, [PC, I32, I32, P, I64, I32, I32, P, P, SZ, P, P]),
         "reco_logit_penalty": (I32, [P, I32, I32, I64, P, I32, P, F32, F32, F32, F32, F32, P, P]),
@@ -269,6 +272,13 @@ def paged_decode_attn_workspace_size(cache: PagedKVCache, n_q_heads: int, n_laye
     nl = cache.shape[0] if n_layers is None else n_layers
     with _on(cache.k):
         return int(load_library().reco_paged_decode_attn_workspace_size(cache.ref(), nl, n_q_heads))
+
+
+def paged_prefill_attn_workspace_size(cache: PagedKVCache, n_q_heads: int, n_tokens: int,
+                                      n_layers: Optional[int] = None) -> int:
+    nl = cache.shape[0] if n_layers is None else n_layers
+    with _on(cache.k):
+        return int(load_library().reco_paged_prefill_attn_workspace_size(cache.ref(), nl, n_q_heads, n_tokens))
 
 
 def paged_evict_workspace_size(cache: PagedKVCache, n_layers: Optional[int] = None) -> int:
@@ -605,6 +615,46 @@ class PreparedPagedDecode:
         if st != RECO_OK:
             _check(st, "reco_paged_decode_attn")
         return self.out, self.lse
+
+
+def reco_paged_prefill_attn(cache: PagedKVCache, q: torch.Tensor, k_new: torch.Tensor, v_new: torch.Tensor,
+                            n_new: Optional[torch.Tensor] = None, sinks: int = 0, window: int = 0,
+                            scale: Optional[float] = None, out: Optional[torch.Tensor] = None,
+                            lse: Optional[torch.Tensor] = None, want_lse: bool = True, layer0: int = 0,
+                            n_layers: Optional[int] = None, ws: Optional[torch.Tensor] = None,
+                            dev_err: Optional[torch.Tensor] = None):
+    """Causal attention of T new tokens per sequence ([n_layers][B][Hq][T][D]) over a
+    paged cache, whose rows they then become; returns (out, lse).  ``n_new`` int32
+    [B]: the real tokens of each sequence (the first ones; places past them are not
+    written).  ``window`` > 0: a token sees its last ``window`` rows (its own among
+    them) and the first ``sinks``."""
+    layer0, nl = _layers(cache, layer0, n_layers)
+    NL, B, H, Cap, D = cache.shape
+    if q.dim() != 5 or q.shape[0] != nl or q.shape[1] != B or q.shape[4] != D or q.dtype != cache.k.dtype:
+        raise ValueError("q must be [n_layers][B][Hq][T][D] in the cache dtype")
+    hq, T = q.shape[2], q.shape[3]
+    if k_new is None or v_new is None:
+        raise ValueError("k_new and v_new must be given")
+    _expect(k_new, "k_new", (nl, B, H, T, D), cache.k.dtype)
+    _expect(v_new, "v_new", (nl, B, H, T, D), cache.k.dtype)
+    _expect(n_new, "n_new", (B,), torch.int32)
+    _expect(out, "out", (nl, B, hq, T, D), cache.k.dtype)
+    _expect(lse, "lse", (nl, B, hq, T), torch.float32)
+    _expect_dev_err(dev_err)
+    _need_cuda(cache.k, q, k_new, v_new, n_new, out, lse, ws, dev_err)
+    if out is None:
+        out = torch.zeros_like(q)
+    if lse is None and want_lse:
+        lse = torch.full((nl, B, hq, T), -math.inf, dtype=torch.float32, device=q.device)
+    ws = _ws(lambda: paged_prefill_attn_workspace_size(cache, hq, T, nl), q.device, ws)
+    scale = 1.0 / math.sqrt(D) if scale is None else float(scale)
+    with _on(q):
+        st = load_library().reco_paged_prefill_attn(cache.ref(), layer0, nl, _ptr(q), hq, T, _ptr(n_new), scale,
+                                                    int(sinks), int(window), _ptr(k_new), _ptr(v_new), _ptr(out),
+                                                    _ptr(lse), _ptr(ws), _nbytes(ws), _ptr(dev_err),
+                                                    _stream(q.device))
+    _check(st, "reco_paged_prefill_attn")
+    return out, lse
 
 
 def reco_paged_evict(cache: PagedKVCache, budget: torch.Tensor, sinks: int = 0, recent: int = 0,

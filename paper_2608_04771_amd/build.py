@@ -20,7 +20,7 @@ LIB = os.path.join(PKG, "libreco.so")
 ARCH = "gfx950"
 
 HIP_SOURCES = ["decode_attn.hip", "score.hip", "select_compact.hip", "pool_scores.hip", "logits.hip", "paged_decode.hip",
-               "paged_evict.hip"]
+               "paged_prefill.hip", "paged_evict.hip"]
 HOST_SOURCES = ["abi.cpp", "abi_paged.cpp", "decode_plan.cpp", "paged_plan.cpp"]
 
 # Packed fp32 instructions are kept out of every kernel (v_pk_* fp32 forms).

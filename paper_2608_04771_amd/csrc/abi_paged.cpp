@@ -14,6 +14,7 @@ namespace {
 
 // Positions rounded up to a tile, and sums of two of them, stay inside int32.
 constexpr int64_t kMaxCapacity = int64_t{1} << 29;
+constexpr int64_t kMaxQueryRows = int64_t{1} << 29;   // of one KV head in a run
 
 bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 
@@ -117,6 +118,55 @@ reco_status_t reco_paged_decode_attn(const reco_paged_cache_t *cache, int32_t la
   if (!reco::paged_decode_fits_grid(p)) return RECO_ERR_UNSUPPORTED;
   reco::paged_decode_place(p, cache->head_dim, ws);
   return reco::hip_status(reco::launch_paged_decode(p, cache->dtype, cache->head_dim, stream));
+}
+
+// ---------------------------------------------------------------- prefill
+size_t reco_paged_prefill_attn_workspace_size(const reco_paged_cache_t *cache, int32_t n_layers, int32_t n_q_heads,
+                                              int32_t n_tokens) {
+  if (!paged_ok(cache) || paged_supported(cache) != RECO_OK) return 0;
+  const int units = units_of(cache, n_layers), G = group_of(cache, n_q_heads);
+  if (units < 1 || G < 1 || G > 16 || n_tokens < 1 || static_cast<int64_t>(n_tokens) * G > kMaxQueryRows) return 0;
+  return reco::prefill_workspace_bytes(units, n_tokens, static_cast<int>(capacity_of(cache)), G, cache->head_dim,
+                                       reco::current_compute_units());
+}
+
+reco_status_t reco_paged_prefill_attn(const reco_paged_cache_t *cache, int32_t layer0, int32_t n_layers,
+                                      const void *q, int32_t n_q_heads, int32_t n_tokens, const int32_t *n_new,
+                                      float scale, int32_t sinks, int32_t window, const void *k_new,
+                                      const void *v_new, void *out, float *lse, void *ws, size_t ws_bytes,
+                                      int32_t *dev_err, hipStream_t stream) {
+  if (!paged_ok(cache) || !q || !k_new || !v_new || !out || sinks < 0 || window < 0 || !isfinite(scale))
+    return RECO_ERR_INVALID_ARG;
+  if (!aligned16(q) || !aligned16(out) || !aligned16(k_new) || !aligned16(v_new)) return RECO_ERR_INVALID_ARG;
+  if (!paged_layers_ok(cache, layer0, n_layers) || n_tokens < 1) return RECO_ERR_INVALID_ARG;
+  const int units = units_of(cache, n_layers), G = group_of(cache, n_q_heads);
+  if (units < 1 || G < 1) return RECO_ERR_INVALID_ARG;
+  const reco_status_t st = paged_supported(cache);
+  if (st != RECO_OK) return st;
+  if (G > 16 || static_cast<int64_t>(n_tokens) * G > kMaxQueryRows) return RECO_ERR_UNSUPPORTED;
+  const int cus = reco::current_compute_units();
+
+  reco::PagedPrefillParams p{};
+  p.c = paged_cache(cache, layer0, n_layers, dev_err);
+  const size_t need = reco::prefill_workspace_bytes(units, n_tokens, p.c.cap, G, cache->head_dim, cus);
+  if (!ws || ws_bytes < need || (reinterpret_cast<uintptr_t>(ws) & 255)) return RECO_ERR_WORKSPACE;
+  p.q = q;
+  p.k_new = k_new;
+  p.v_new = v_new;
+  p.n_new = n_new;
+  p.out = out;
+  p.lse = lse;
+  p.group = G;
+  p.hq = n_q_heads;
+  p.tokens = n_tokens;
+  p.blocks = reco::prefill_blocks(n_tokens, G);
+  p.splits = reco::prefill_splits(units, p.blocks, p.c.cap, sinks, window, cus);
+  p.sinks = sinks;
+  p.window = window;
+  p.scale_log2 = scale * 1.4426950408889634f;
+  if (!reco::prefill_fits_grid(p)) return RECO_ERR_UNSUPPORTED;
+  reco::prefill_place(p, cache->head_dim, ws);
+  return reco::hip_status(reco::launch_paged_prefill(p, cache->dtype, cache->head_dim, stream));
 }
 
 // ---------------------------------------------------------------- eviction

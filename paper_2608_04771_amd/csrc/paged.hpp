@@ -50,6 +50,31 @@ int paged_weight_chunks(const PagedDecodeParams &p);
 bool paged_decode_fits_grid(const PagedDecodeParams &p);
 hipError_t launch_paged_decode(const PagedDecodeParams &p, int dtype, int head_dim, hipStream_t s);
 
+// ---- attention of a run of new tokens -------------------------------------------
+constexpr int kPrefillRows = 128;        // query rows of a workgroup
+constexpr int kPrefillMaxSplits = 64;
+struct PagedPrefillParams {
+  PagedCache c;
+  const void *q;          // [n_layers][batch][hq][tokens][D]
+  const void *k_new;      // [n_layers][batch][hkv][tokens][D]
+  const void *v_new;
+  const int32_t *n_new;   // nullable [batch]: real tokens of each sequence
+  void *out;              // [n_layers][batch][hq][tokens][D]
+  float *lse;             // nullable [n_layers][batch][hq][tokens]
+  int32_t *len_in;        // [units]  lengths before the append
+  float *part_o;          // [units][blocks][splits][kPrefillRows][D]
+  float *part_ml;         // [units][blocks][splits][2][kPrefillRows]
+  int group, hq, tokens, blocks, splits;
+  int sinks, window;
+  float scale_log2;
+};
+int prefill_blocks(int tokens, int group);
+int prefill_splits(int units, int blocks, int capacity, int sinks, int window, int compute_units);
+size_t prefill_workspace_bytes(int units, int tokens, int capacity, int group, int head_dim, int compute_units);
+bool prefill_fits_grid(const PagedPrefillParams &p);
+void prefill_place(PagedPrefillParams &p, int head_dim, void *ws);
+hipError_t launch_paged_prefill(const PagedPrefillParams &p, int dtype, int head_dim, hipStream_t s);
+
 // ---- eviction -----------------------------------------------------------------
 struct PagedEvictParams {
   PagedCache c;           // with weights

@@ -60,6 +60,49 @@ void paged_decode_place(PagedDecodeParams &p, int head_dim, void *ws) {
   p.logit_pitch = static_cast<int64_t>(logit_pitch(p.c.cap));
 }
 
+int prefill_blocks(int tokens, int group) {
+  return static_cast<int>((static_cast<int64_t>(tokens) * group + kPrefillRows - 1) / kPrefillRows);
+}
+
+// Key tiles are split where there are too few blocks of query rows for two workgroups
+// on every compute unit, into pieces of at least four tiles of 64 rows.
+int prefill_splits(int units, int blocks, int capacity, int sinks, int window, int compute_units) {
+  int64_t rows = capacity;
+  if (window > 0) {
+    const int64_t seen = static_cast<int64_t>(sinks) + window + 2 * kPrefillRows;
+    if (seen < rows) rows = seen;
+  }
+  int64_t splits = 2 * static_cast<int64_t>(compute_units) / (static_cast<int64_t>(units) * blocks);
+  if (splits > rows / 256) splits = rows / 256;
+  if (splits > kPrefillMaxSplits) splits = kPrefillMaxSplits;
+  return splits < 1 ? 1 : static_cast<int>(splits);
+}
+
+size_t prefill_workspace_bytes(int units, int tokens, int capacity, int group, int head_dim, int compute_units) {
+  const int blocks = prefill_blocks(tokens, group);
+  const int splits = prefill_splits(units, blocks, capacity, 0, 0, compute_units);   // a window takes no more
+  size_t bytes = aligned(static_cast<size_t>(units) * sizeof(int32_t));
+  if (splits > 1)
+    bytes += static_cast<size_t>(units) * blocks * splits * kPrefillRows * (static_cast<size_t>(head_dim) + 2) * sizeof(float);
+  return bytes;
+}
+
+bool prefill_fits_grid(const PagedPrefillParams &p) {
+  const int64_t units = static_cast<int64_t>(p.c.n_layers) * p.c.batch * p.c.hkv;
+  const int64_t most = int64_t{1} << 24;                 // workgroups of 256 threads
+  return static_cast<int64_t>(p.blocks) * p.splits < most &&
+         units * (p.tokens / 64 + 1 + (p.splits > 1 ? static_cast<int64_t>(p.blocks) * 16 : 0)) < most;
+}
+
+void prefill_place(PagedPrefillParams &p, int head_dim, void *ws) {
+  const size_t units = static_cast<size_t>(p.c.n_layers) * p.c.batch * p.c.hkv;
+  char *at = static_cast<char *>(ws);
+  p.len_in = reinterpret_cast<int32_t *>(at);
+  at += aligned(units * sizeof(int32_t));
+  p.part_o = reinterpret_cast<float *>(at);
+  p.part_ml = p.part_o + units * p.blocks * p.splits * kPrefillRows * head_dim;
+}
+
 size_t paged_evict_workspace_bytes(int units, int capacity, bool need_idx) {
   size_t bytes = aligned(static_cast<size_t>(units) * sizeof(int32_t));
   if (need_idx) bytes += static_cast<size_t>(units) * capacity * sizeof(int32_t);

@@ -1,0 +1,428 @@
+// GQA attention of a run of new tokens over ragged units of a paged KV cache
+// (gfx950): causal, with an optional sliding window and sinks.
+//
+//   token t of a sequence, at row p = L + t, sees the rows j <= p with
+//   j < sinks or j > p - window;   out = softmax(scale <q, k_j>) v_j over them
+//
+// The n tokens' G query heads of one KV head make n * G query rows (row t * G + g),
+// so a group shares its K and V.  A workgroup takes 128 of them, 32 a wave, and walks
+// the key tiles that any of them sees: tiles of the cached rows (in pages), then tiles
+// of the new rows (as the caller gives them; a second kernel puts them into their
+// pages).  Per tile a wave computes
+//   S^T = K_tile . Q^T           (32 keys x 32 rows per block)
+//   O^T += V_tile^T . P^T        (32 columns of the head x 32 rows per block)
+// so that a row's softmax lies in two lanes, the values of S^T are the operand P^T as
+// they are, and rescaling O needs nothing from other lanes.  Statistics and outputs
+// are fp32; P alone is rounded to the cache's type, as its operand has to be.  Where
+// there are few query rows, their key tiles are split over several workgroups and
+// joined by the second kernel.  Long runs are bound by the matrix units.
+#include "paged_device.hpp"
+
+namespace reco {
+
+namespace {
+
+typedef __attribute__((__vector_size__(16 * sizeof(float)))) float f32x16_t;
+typedef short i16x4_t __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) i16x4_t lds_i16x4_t;
+
+constexpr int kRows = kPrefillRows;          // query rows of a workgroup
+constexpr int kWaves = 4;
+constexpr int kThreads = kWaves * kWave;
+
+// 32x32 fragments: lane l has 8 (bf16) or 1 (fp32) consecutive contraction elements of
+// row or column l % 32, group l / 32; the result holds rows 8 (i / 4) + 4 (l / 32) + i % 4
+// of column l % 32.
+template <typename T>
+struct Mma32;
+template <>
+struct Mma32<bf16_t> {
+  static constexpr int kpl = 8;
+  static constexpr int keys = 64;            // of a tile
+  using frag = bf16x8_t;
+  __device__ __forceinline__ static f32x16_t mma(frag a, frag b, f32x16_t c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+  }
+};
+template <>
+struct Mma32<float> {
+  static constexpr int kpl = 1;
+  static constexpr int keys = 32;
+  using frag = float;
+  __device__ __forceinline__ static f32x16_t mma(frag a, frag b, f32x16_t c) {
+    return __builtin_amdgcn_mfma_f32_32x32x2f32(a, b, c, 0, 0, 0);
+  }
+};
+
+template <typename T, int D>
+struct Cfg {
+  using M = Mma32<T>;
+  static constexpr int keys = M::keys;
+  static constexpr int blocks = keys / 32;               // S^T blocks of a tile
+  static constexpr int qk_steps = D / 2 / M::kpl;
+  static constexpr int dtiles = D / 32;
+  static constexpr int pv_steps = 16 / M::kpl;           // per block
+  static constexpr int row_bytes = D * (int)sizeof(T);
+  static constexpr int k_pitch = row_bytes + 16;         // free of bank conflicts
+  static constexpr int v_pitch = row_bytes + 64;
+  static constexpr int stage = keys * (k_pitch + v_pitch);
+  static constexpr int lanes_per_row = row_bytes / 16;
+  static constexpr int wave_rows = kWave / lanes_per_row;   // rows a wave's load takes
+  static constexpr int insts = keys * row_bytes / (kThreads * 16);
+};
+
+// The row of a result element within its 32.
+__device__ __forceinline__ int acc_row(int i, int half) { return 8 * (i / 4) + 4 * half + (i & 3); }
+
+// What one unit's call sees: cached rows in tiles of KT from row 0, new rows in tiles
+// of KT from row L.
+template <int KT>
+struct Run {
+  int L, n, old_tiles;
+
+  __device__ __forceinline__ Run(int len, int tokens) : L(len), n(tokens), old_tiles((len + KT - 1) / KT) {}
+  __device__ __forceinline__ int tile_of(int row) const { return row < L ? row / KT : old_tiles + (row - L) / KT; }
+  __device__ __forceinline__ int start(int tile) const { return tile < old_tiles ? tile * KT : L + (tile - old_tiles) * KT; }
+  __device__ __forceinline__ int end(int tile) const { return min(start(tile) + KT, tile < old_tiles ? L : L + n); }
+};
+
+template <typename T, int D>
+__global__ __launch_bounds__(kThreads, 2) void prefill_kernel(PagedPrefillParams p) {
+  using C = Cfg<T, D>;
+  using M = Mma32<T>;
+  using frag = typename M::frag;
+  constexpr int KT = C::keys;
+  __shared__ __attribute__((aligned(16))) unsigned char smem[2 * C::stage];
+
+  const int lane = threadIdx.x & (kWave - 1);
+  const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) / kWave);
+  const int half = lane >> 5;
+  const int col = lane & 31;
+  const int split = blockIdx.x % p.splits;
+  const int block = p.blocks - 1 - static_cast<int>(blockIdx.x) / p.splits;   // the longest first
+  const int unit = blockIdx.y;
+  const int per_layer = p.c.batch * p.c.hkv;
+  const int lc = unit / per_layer;
+  const int b = (unit % per_layer) / p.c.hkv;
+  const int h = unit % p.c.hkv;
+  const size_t cunit = static_cast<size_t>(p.c.layer0 + lc) * per_layer + unit % per_layer;
+
+  const int len_in = p.c.len[cunit];
+  const int given = p.n_new ? p.n_new[b] : p.tokens;
+  const int n = given < 0 || given > p.tokens ? 0 : given;
+  if (block == 0 && split == 0 && threadIdx.x == 0) {
+    p.len_in[unit] = len_in;                               // for the second kernel, which changes len
+    if (len_in < 0 || len_in > p.c.cap || n != given) report(p.c.dev_err, kDevBadLength);
+  }
+  const int G = p.group;
+  const int r0 = block * kRows;
+  if (r0 >= n * G) return;
+  const Run<KT> run(len_in < 0 ? 0 : min(len_in, p.c.cap), n);
+  const int L = run.L;
+  const int t_lo = r0 / G, t_hi = min(r0 + kRows - 1, n * G - 1) / G;
+
+  // The tiles that any token of the block sees: the sinks', then [first, last].
+  const int lo = p.window > 0 ? max(0, L + t_lo - p.window + 1) : 0;
+  const int s_end = min(p.sinks, lo);
+  const int first = run.tile_of(lo);
+  const int sink_tiles = s_end > 0 ? min(run.tile_of(s_end - 1) + 1, first) : 0;
+  const int skip = first - sink_tiles;
+  const int total = run.tile_of(L + t_hi) + 1 - skip;
+  const int per_split = (total + p.splits - 1) / p.splits;
+  const int i0 = split * per_split;
+  const int i1 = min(total, i0 + per_split);
+  const auto tile_at = [&](int i) { return i < sink_tiles ? i : i + skip; };
+
+  // This lane's query row.
+  const int r = r0 + wave * 32 + col;
+  const bool real = r < n * G;
+  const int t = min(r, n * G - 1) / G;
+  const int pos = L + t;
+  const int low = p.window > 0 ? pos - p.window : -1;     // sees rows above it, and the sinks
+  const size_t qrow = ((static_cast<size_t>(lc) * p.c.batch + b) * p.hq + h * G + (min(r, n * G - 1) - t * G)) *
+                          static_cast<size_t>(p.tokens) + t;
+  frag qf[C::qk_steps];
+  {
+    const T *src = reinterpret_cast<const T *>(p.q) + qrow * D + half * (D / 2);
+#pragma unroll
+    for (int c = 0; c < C::qk_steps; ++c) qf[c] = load_frag(src + c * M::kpl);
+  }
+
+  PagedUnit pages(p.c, cunit);
+  const unsigned char *knew = reinterpret_cast<const unsigned char *>(p.k_new) + static_cast<size_t>(unit) * p.tokens * C::row_bytes;
+  const unsigned char *vnew = reinterpret_cast<const unsigned char *>(p.v_new) + static_cast<size_t>(unit) * p.tokens * C::row_bytes;
+  uint4 kreg[C::insts], vreg[C::insts];
+  // A tile's rows; those past its end are its last one again (finite if that is, and
+  // of no weight).
+  const auto load = [&](int tile) {
+    const int start = run.start(tile), end = run.end(tile);
+#pragma unroll
+    for (int k = 0; k < C::insts; ++k) {
+      const int row0 = start + (k * kWaves + wave) * C::wave_rows;
+      const int from = min(row0, start + ((end - 1 - start) & ~(C::wave_rows - 1)));
+      const int row = min(from + lane / C::lanes_per_row, end - 1) - from;
+      const size_t off = static_cast<size_t>(row * C::row_bytes + (lane % C::lanes_per_row) * 16);
+      if (tile < run.old_tiles) {
+        const size_t at = pages.row_at(from, L) * C::row_bytes;
+        kreg[k] = *reinterpret_cast<const uint4 *>(reinterpret_cast<const unsigned char *>(p.c.k) + at + off);
+        vreg[k] = *reinterpret_cast<const uint4 *>(reinterpret_cast<const unsigned char *>(p.c.v) + at + off);
+      } else {
+        const size_t at = static_cast<size_t>(from - L) * C::row_bytes;
+        kreg[k] = *reinterpret_cast<const uint4 *>(knew + at + off);
+        vreg[k] = *reinterpret_cast<const uint4 *>(vnew + at + off);
+      }
+    }
+  };
+  const auto store = [&](int tile, unsigned char *buf) {
+    const int start = run.start(tile);
+#pragma unroll
+    for (int k = 0; k < C::insts; ++k) {
+      const int row = (k * kWaves + wave) * C::wave_rows + lane / C::lanes_per_row;
+      const int sub = (lane % C::lanes_per_row) * 16;
+      *reinterpret_cast<uint4 *>(buf + row * C::k_pitch + sub) = kreg[k];
+      const int j = min(start + row, run.end(tile) - 1);
+      const unsigned keep = j >= lo || j < s_end ? ~0u : 0u;   // rows that no token here sees count for nothing
+      *reinterpret_cast<uint4 *>(buf + KT * C::k_pitch + row * C::v_pitch + sub) =
+          make_uint4(vreg[k].x & keep, vreg[k].y & keep, vreg[k].z & keep, vreg[k].w & keep);
+    }
+  };
+
+  float m_run = -INFINITY, l_run = 0.f;                  // m in units of the scaled logits
+  f32x16_t o[C::dtiles];
+#pragma unroll
+  for (int dt = 0; dt < C::dtiles; ++dt) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) o[dt][i] = 0.f;
+  }
+
+  if (i0 < i1) {
+    load(tile_at(i0));
+    store(tile_at(i0), smem);
+  }
+  __syncthreads();
+  for (int i = i0; i < i1; ++i) {
+    const unsigned char *kbuf = smem + ((i - i0) & 1) * C::stage;
+    const unsigned char *vbuf = kbuf + KT * C::k_pitch;
+    const int tile = tile_at(i);
+    const int start = run.start(tile), end = run.end(tile);
+    if (i + 1 < i1) load(tile_at(i + 1));
+
+    f32x16_t s[C::blocks];
+#pragma unroll
+    for (int kb = 0; kb < C::blocks; ++kb) {
+#pragma unroll
+      for (int e = 0; e < 16; ++e) s[kb][e] = 0.f;
+      const T *krow = reinterpret_cast<const T *>(kbuf + (kb * 32 + col) * C::k_pitch) + half * (D / 2);
+#pragma unroll
+      for (int c = 0; c < C::qk_steps; ++c) s[kb] = M::mma(load_frag(krow + c * M::kpl), qf[c], s[kb]);
+    }
+
+    // Whether every token of the block sees the whole tile.
+    const bool whole = end - start == KT && end - 1 <= L + t_lo &&
+                       (p.window == 0 || start > L + t_hi - p.window || end <= p.sinks);
+    float x[C::blocks][16];
+    float top = -INFINITY;
+#pragma unroll
+    for (int kb = 0; kb < C::blocks; ++kb) {
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        x[kb][e] = s[kb][e] * p.scale_log2;
+        if (!whole) {
+          const int j = start + kb * 32 + acc_row(e, half);
+          x[kb][e] = j < end && j <= pos && (j > low || j < p.sinks) ? x[kb][e] : -INFINITY;
+        }
+        top = fmaxf(top, x[kb][e]);
+      }
+    }
+    top = fmaxf(top, shfl_xor(top, 32));
+    const float m_new = fmaxf(m_run, top);
+    const float ref = m_new == -INFINITY ? 0.f : m_new;
+    const float alpha = fast_exp2(m_run - ref);
+    float sum = 0.f;
+#pragma unroll
+    for (int kb = 0; kb < C::blocks; ++kb) {
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        x[kb][e] = fast_exp2(x[kb][e] - ref);
+        sum += x[kb][e];
+      }
+    }
+    l_run = l_run * alpha + sum;
+    m_run = m_new;
+#pragma unroll
+    for (int dt = 0; dt < C::dtiles; ++dt) {
+#pragma unroll
+      for (int e = 0; e < 16; ++e) o[dt][e] *= alpha;
+    }
+
+    // Element slot j of step c is result element c * kpl + j: row 8 (e / 4) + 4 half + e % 4.
+#pragma unroll
+    for (int kb = 0; kb < C::blocks; ++kb) {
+#pragma unroll
+      for (int c = 0; c < C::pv_steps; ++c) {
+        frag pf;
+        if constexpr (M::kpl == 1) {
+          pf = x[kb][c];
+        } else {
+#pragma unroll
+          for (int j = 0; j < 8; ++j) pf[j] = static_cast<__bf16>(x[kb][c * 8 + j]);
+        }
+#pragma unroll
+        for (int dt = 0; dt < C::dtiles; ++dt) {
+          frag vf;
+          if constexpr (M::kpl == 1) {
+            vf = *reinterpret_cast<const float *>(vbuf + (kb * 32 + acc_row(c, half)) * C::v_pitch + (dt * 32 + col) * 4);
+          } else {
+            // two transposing reads of four rows each: lane i of 16 gets column i
+            const int row = kb * 32 + c * 16 + 4 * half + (col & 15) / 4;
+            const int at = (dt * 32 + (col & 16) + 4 * (col & 3)) * 2;
+            const i16x4_t a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4_t *)(vbuf + row * C::v_pitch + at));
+            const i16x4_t d = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4_t *)(vbuf + (row + 8) * C::v_pitch + at));
+            const short v[8] = {a[0], a[1], a[2], a[3], d[0], d[1], d[2], d[3]};
+#pragma unroll
+            for (int j = 0; j < 8; ++j) vf[j] = __builtin_bit_cast(__bf16, v[j]);
+          }
+          o[dt] = M::mma(vf, pf, o[dt]);
+        }
+      }
+    }
+    if (i + 1 < i1) store(tile_at(i + 1), smem + ((i + 1 - i0) & 1) * C::stage);
+    __syncthreads();
+  }
+  if (pages.bad && lane == 0) report(p.c.dev_err, kDevBadPage);
+
+  const float l_tot = l_run + shfl_xor(l_run, 32);
+  if (p.splits > 1) {
+    const size_t part = (static_cast<size_t>(unit) * p.blocks + block) * p.splits + split;
+    float *po = p.part_o + (part * kRows + wave * 32 + col) * D;
+    if (half == 0) {
+      p.part_ml[part * 2 * kRows + wave * 32 + col] = m_run;
+      p.part_ml[part * 2 * kRows + kRows + wave * 32 + col] = l_tot;
+    }
+#pragma unroll
+    for (int dt = 0; dt < C::dtiles; ++dt) {
+#pragma unroll
+      for (int e = 0; e < 16; e += 4)
+        *reinterpret_cast<float4 *>(po + dt * 32 + acc_row(e, half)) =
+            make_float4(o[dt][e], o[dt][e + 1], o[dt][e + 2], o[dt][e + 3]);
+    }
+    return;
+  }
+  if (!real) return;
+  const float inv = l_tot == 0.f ? 0.f : 1.f / l_tot;
+  T *dst = reinterpret_cast<T *>(p.out) + qrow * D;
+#pragma unroll
+  for (int dt = 0; dt < C::dtiles; ++dt) {
+#pragma unroll
+    for (int e = 0; e < 16; ++e) dst[dt * 32 + acc_row(e, half)] = from_f32<T>(o[dt][e] * inv);
+  }
+  if (p.lse && half == 0) p.lse[qrow] = l_tot == 0.f ? -INFINITY : (m_run + log2f(l_tot)) * kLn2;
+}
+
+// Joins the splits (workgroups [0, merges)) and puts the new rows into their pages
+// (the others, kAppendRows rows of a unit each).  A unit's rows are appended together or,
+// where they or their pages do not fit, not at all.
+constexpr int kMergeRows = 8;
+constexpr int kAppendRows = 64;
+
+template <typename T, int D>
+__global__ __launch_bounds__(256) void prefill_finish_kernel(PagedPrefillParams p, int merges, int chunks) {
+  const int tid = threadIdx.x;
+  const int per_layer = p.c.batch * p.c.hkv;
+  const int G = p.group;
+  int id = blockIdx.x;
+  if (id < merges) {
+    const int piece = id % (kRows / kMergeRows);
+    id /= kRows / kMergeRows;
+    const int block = id % p.blocks, unit = id / p.blocks;
+    const int lc = unit / per_layer, b = (unit % per_layer) / p.c.hkv, h = unit % p.c.hkv;
+    const int given = p.n_new ? p.n_new[b] : p.tokens;
+    const int n = given < 0 || given > p.tokens ? 0 : given;
+    constexpr int kPer = 256 / kMergeRows;               // threads of a row
+    const int in = piece * kMergeRows + tid / kPer;
+    const int r = block * kRows + in;
+    if (r >= n * G) return;
+    const size_t part = (static_cast<size_t>(unit) * p.blocks + block) * p.splits;
+    float top = -INFINITY;
+    for (int s = 0; s < p.splits; ++s) top = fmaxf(top, p.part_ml[(part + s) * 2 * kRows + in]);
+    const float ref = top == -INFINITY ? 0.f : top;
+    float sum = 0.f;
+    float acc[D / kPer];
+#pragma unroll
+    for (int i = 0; i < D / kPer; ++i) acc[i] = 0.f;
+    for (int s = 0; s < p.splits; ++s) {
+      const float w = fast_exp2(p.part_ml[(part + s) * 2 * kRows + in] - ref);
+      sum += p.part_ml[(part + s) * 2 * kRows + kRows + in] * w;
+      const float *po = p.part_o + ((part + s) * kRows + in) * D + tid % kPer;
+#pragma unroll
+      for (int i = 0; i < D / kPer; ++i) acc[i] += po[i * kPer] * w;
+    }
+    const int t = r / G;
+    const size_t row = ((static_cast<size_t>(lc) * p.c.batch + b) * p.hq + h * G + (r - t * G)) * static_cast<size_t>(p.tokens) + t;
+    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+    T *dst = reinterpret_cast<T *>(p.out) + row * D + tid % kPer;
+#pragma unroll
+    for (int i = 0; i < D / kPer; ++i) dst[i * kPer] = from_f32<T>(acc[i] * inv);
+    if (p.lse && tid % kPer == 0) p.lse[row] = sum == 0.f ? -INFINITY : (ref + log2f(sum)) * kLn2;
+    return;
+  }
+  id -= merges;
+  const int unit = id / chunks, chunk = id % chunks;
+  const int b = (unit % per_layer) / p.c.hkv;
+  const size_t cunit = static_cast<size_t>(p.c.layer0 + unit / per_layer) * per_layer + unit % per_layer;
+  const int given = p.n_new ? p.n_new[b] : p.tokens;
+  const int n = given < 0 || given > p.tokens ? 0 : given;
+  const int L = p.len_in[unit];
+  if (n == 0 || chunk * kAppendRows >= n || L < 0 || L > p.c.cap) return;
+  const bool reporting = chunk == 0 && tid == 0;
+  if (n > p.c.cap - L) {
+    if (reporting) report(p.c.dev_err, kDevAppendOverflow);
+    return;
+  }
+  const int32_t *table = p.c.pages + cunit * static_cast<size_t>(p.c.max_pages);
+  const int shift = p.c.page_shift;
+  bool bad = false;
+  for (int g = (L >> shift) + tid; g <= (L + n - 1) >> shift; g += 256)
+    if (static_cast<unsigned>(table[g]) >= static_cast<unsigned>(p.c.n_pages)) bad = true;
+  if (__syncthreads_or(bad)) {
+    if (reporting) report(p.c.dev_err, kDevBadPage);
+    return;
+  }
+  constexpr int kLanes = D * (int)sizeof(T) / 16;
+  const int rows = min(kAppendRows, n - chunk * kAppendRows);
+  const uint4 *ks = reinterpret_cast<const uint4 *>(p.k_new) + (static_cast<size_t>(unit) * p.tokens + chunk * kAppendRows) * kLanes;
+  const uint4 *vs = reinterpret_cast<const uint4 *>(p.v_new) + (static_cast<size_t>(unit) * p.tokens + chunk * kAppendRows) * kLanes;
+  for (int i = tid; i < rows * kLanes; i += 256) {
+    const int row = L + chunk * kAppendRows + i / kLanes;
+    const size_t at = ((static_cast<size_t>(table[row >> shift]) << shift) + (row & ((1 << shift) - 1))) * kLanes + i % kLanes;
+    reinterpret_cast<uint4 *>(p.c.k)[at] = ks[i];
+    reinterpret_cast<uint4 *>(p.c.v)[at] = vs[i];
+  }
+  if (p.c.weight && tid < rows) p.c.weight[cunit * p.c.cap + L + chunk * kAppendRows + tid] = 0.f;
+  if (reporting) p.c.len[cunit] = L + n;
+}
+
+template <typename T, int D>
+hipError_t launch_typed(const PagedPrefillParams &p, hipStream_t s) {
+  const int units = p.c.n_layers * p.c.batch * p.c.hkv;
+  hipLaunchKernelGGL((prefill_kernel<T, D>), dim3(p.blocks * p.splits, units), dim3(kThreads), 0, s, p);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  const int merges = p.splits > 1 ? units * p.blocks * (kRows / kMergeRows) : 0;
+  const int chunks = (p.tokens + kAppendRows - 1) / kAppendRows;
+  hipLaunchKernelGGL((prefill_finish_kernel<T, D>), dim3(merges + units * chunks), dim3(256), 0, s, p, merges, chunks);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_paged_prefill(const PagedPrefillParams &p, int dtype, int head_dim, hipStream_t s) {
+  if (dtype == 0) {
+    if (head_dim == 64) return launch_typed<float, 64>(p, s);
+    return launch_typed<float, 128>(p, s);
+  }
+  if (head_dim == 64) return launch_typed<bf16_t, 64>(p, s);
+  return launch_typed<bf16_t, 128>(p, s);
+}
+
+}  // namespace reco
