@@ -225,15 +225,15 @@ __global__ __launch_bounds__(kCompThreads) void evict_compact_kernel(PagedEvictP
     return base + ((static_cast<size_t>(table[row >> shift]) << shift) + (row & mask)) * ROWB;
   };
   for (int c0 = 0; c0 < m; c0 += kChunkRows) {
-    uint4 v[kRowsPerThread];
+    u32x4v v[kRowsPerThread];
 #pragma unroll
     for (int i = 0; i < kRowsPerThread; ++i)
-      v[i] = *reinterpret_cast<const uint4 *>(at(idx[min(c0 + i * kRowsPerPass + rrow, m - 1)]));
+      v[i] = *reinterpret_cast<const u32x4v *>(at(idx[min(c0 + i * kRowsPerPass + rrow, m - 1)]));
     __syncthreads();   // every row of this chunk is loaded before any of its places is overwritten
 #pragma unroll
     for (int i = 0; i < kRowsPerThread; ++i) {
       const int d = c0 + i * kRowsPerPass + rrow;
-      if (d < m) *reinterpret_cast<uint4 *>(at(d)) = v[i];
+      if (d < m) *reinterpret_cast<u32x4v *>(at(d)) = v[i];
     }
   }
 }

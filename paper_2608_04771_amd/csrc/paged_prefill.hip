@@ -29,6 +29,7 @@ typedef __attribute__((address_space(3))) i16x4_t lds_i16x4_t;
 constexpr int kRows = kPrefillRows;          // query rows of a workgroup
 constexpr int kWaves = 4;
 constexpr int kThreads = kWaves * kWave;
+constexpr float kSlack = 8.f;                // log2 units that a maximum may grow before O follows
 
 // 32x32 fragments: lane l has 8 (bf16) or 1 (fp32) consecutive contraction elements of
 // row or column l % 32, group l / 32; the result holds rows 8 (i / 4) + 4 (l / 32) + i % 4
@@ -43,6 +44,11 @@ struct Mma32<bf16_t> {
   __device__ __forceinline__ static f32x16_t mma(frag a, frag b, f32x16_t c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
   }
+  __device__ __forceinline__ static frag negated(frag a) {
+    const uint4 u = __builtin_bit_cast(uint4, a);
+    constexpr unsigned k = 0x80008000u;
+    return __builtin_bit_cast(frag, make_uint4(u.x ^ k, u.y ^ k, u.z ^ k, u.w ^ k));
+  }
 };
 template <>
 struct Mma32<float> {
@@ -52,6 +58,7 @@ struct Mma32<float> {
   __device__ __forceinline__ static f32x16_t mma(frag a, frag b, f32x16_t c) {
     return __builtin_amdgcn_mfma_f32_32x32x2f32(a, b, c, 0, 0, 0);
   }
+  __device__ __forceinline__ static frag negated(frag a) { return -a; }
 };
 
 template <typename T, int D>
@@ -145,13 +152,17 @@ __global__ __launch_bounds__(kThreads, 2) void prefill_kernel(PagedPrefillParams
   {
     const T *src = reinterpret_cast<const T *>(p.q) + qrow * D + half * (D / 2);
 #pragma unroll
-    for (int c = 0; c < C::qk_steps; ++c) qf[c] = load_frag(src + c * M::kpl);
+    for (int c = 0; c < C::qk_steps; ++c) {
+      qf[c] = load_frag(src + c * M::kpl);
+      if (p.scale_log2 < 0.f) qf[c] = M::negated(qf[c]);   // so that the largest product is the largest logit
+    }
   }
+  const float scale = fmaxf(fabsf(p.scale_log2), 0x1p-126f);   // times a hidden row's -inf, 0 would be NaN
 
   PagedUnit pages(p.c, cunit);
   const unsigned char *knew = reinterpret_cast<const unsigned char *>(p.k_new) + static_cast<size_t>(unit) * p.tokens * C::row_bytes;
   const unsigned char *vnew = reinterpret_cast<const unsigned char *>(p.v_new) + static_cast<size_t>(unit) * p.tokens * C::row_bytes;
-  uint4 kreg[C::insts], vreg[C::insts];
+  u32x4v kreg[C::insts], vreg[C::insts];
   // A tile's rows; those past its end are its last one again (finite if that is, and
   // of no weight).
   const auto load = [&](int tile) {
@@ -161,16 +172,11 @@ __global__ __launch_bounds__(kThreads, 2) void prefill_kernel(PagedPrefillParams
       const int row0 = start + (k * kWaves + wave) * C::wave_rows;
       const int from = min(row0, start + ((end - 1 - start) & ~(C::wave_rows - 1)));
       const int row = min(from + lane / C::lanes_per_row, end - 1) - from;
-      const size_t off = static_cast<size_t>(row * C::row_bytes + (lane % C::lanes_per_row) * 16);
-      if (tile < run.old_tiles) {
-        const size_t at = pages.row_at(from, L) * C::row_bytes;
-        kreg[k] = *reinterpret_cast<const uint4 *>(reinterpret_cast<const unsigned char *>(p.c.k) + at + off);
-        vreg[k] = *reinterpret_cast<const uint4 *>(reinterpret_cast<const unsigned char *>(p.c.v) + at + off);
-      } else {
-        const size_t at = static_cast<size_t>(from - L) * C::row_bytes;
-        kreg[k] = *reinterpret_cast<const uint4 *>(knew + at + off);
-        vreg[k] = *reinterpret_cast<const uint4 *>(vnew + at + off);
-      }
+      const int off = row * C::row_bytes + (lane % C::lanes_per_row) * 16;
+      const bool old = tile < run.old_tiles;
+      const size_t at = (old ? pages.row_at(from, L) : static_cast<size_t>(from - L)) * C::row_bytes;
+      kreg[k] = *reinterpret_cast<const u32x4v *>((old ? reinterpret_cast<const unsigned char *>(p.c.k) : knew) + at + off);
+      vreg[k] = *reinterpret_cast<const u32x4v *>((old ? reinterpret_cast<const unsigned char *>(p.c.v) : vnew) + at + off);
     }
   };
   const auto store = [&](int tile, unsigned char *buf) {
@@ -179,11 +185,10 @@ __global__ __launch_bounds__(kThreads, 2) void prefill_kernel(PagedPrefillParams
     for (int k = 0; k < C::insts; ++k) {
       const int row = (k * kWaves + wave) * C::wave_rows + lane / C::lanes_per_row;
       const int sub = (lane % C::lanes_per_row) * 16;
-      *reinterpret_cast<uint4 *>(buf + row * C::k_pitch + sub) = kreg[k];
+      *reinterpret_cast<u32x4v *>(buf + row * C::k_pitch + sub) = kreg[k];
       const int j = min(start + row, run.end(tile) - 1);
       const unsigned keep = j >= lo || j < s_end ? ~0u : 0u;   // rows that no token here sees count for nothing
-      *reinterpret_cast<uint4 *>(buf + KT * C::k_pitch + row * C::v_pitch + sub) =
-          make_uint4(vreg[k].x & keep, vreg[k].y & keep, vreg[k].z & keep, vreg[k].w & keep);
+      *reinterpret_cast<u32x4v *>(buf + KT * C::k_pitch + row * C::v_pitch + sub) = vreg[k] & keep;
     }
   };
 
@@ -220,39 +225,46 @@ __global__ __launch_bounds__(kThreads, 2) void prefill_kernel(PagedPrefillParams
     // Whether every token of the block sees the whole tile.
     const bool whole = end - start == KT && end - 1 <= L + t_lo &&
                        (p.window == 0 || start > L + t_hi - p.window || end <= p.sinks);
-    float x[C::blocks][16];
+    if (!whole) {
+#pragma unroll
+      for (int kb = 0; kb < C::blocks; ++kb) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const int j = start + kb * 32 + acc_row(e, half);
+          s[kb][e] = j < end && j <= pos && (j > low || j < p.sinks) ? s[kb][e] : -INFINITY;
+        }
+      }
+    }
     float top = -INFINITY;
 #pragma unroll
     for (int kb = 0; kb < C::blocks; ++kb) {
 #pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        x[kb][e] = s[kb][e] * p.scale_log2;
-        if (!whole) {
-          const int j = start + kb * 32 + acc_row(e, half);
-          x[kb][e] = j < end && j <= pos && (j > low || j < p.sinks) ? x[kb][e] : -INFINITY;
-        }
-        top = fmaxf(top, x[kb][e]);
+      for (int e = 0; e < 16; ++e) top = fmaxf(top, s[kb][e]);
+    }
+    top = fmaxf(top, shfl_xor(top, 32)) * scale;
+    // The reference of the exponentials follows the maximum only where it grew by more
+    // than kSlack (P then stays below 2^kSlack, with the same relative precision), so
+    // that O is seldom rescaled.
+    if (__any(top > m_run + kSlack)) {
+      const float m_new = fmaxf(m_run, top);
+      const float alpha = fast_exp2(m_run - (m_new == -INFINITY ? 0.f : m_new));
+      l_run *= alpha;
+      m_run = m_new;
+#pragma unroll
+      for (int dt = 0; dt < C::dtiles; ++dt) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) o[dt][e] *= alpha;
       }
     }
-    top = fmaxf(top, shfl_xor(top, 32));
-    const float m_new = fmaxf(m_run, top);
-    const float ref = m_new == -INFINITY ? 0.f : m_new;
-    const float alpha = fast_exp2(m_run - ref);
-    float sum = 0.f;
+    const float ref = m_run == -INFINITY ? 0.f : m_run;
+    float x[C::blocks][16];
 #pragma unroll
     for (int kb = 0; kb < C::blocks; ++kb) {
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
-        x[kb][e] = fast_exp2(x[kb][e] - ref);
-        sum += x[kb][e];
+        x[kb][e] = fast_exp2(fmaf(s[kb][e], scale, -ref));
+        l_run += x[kb][e];
       }
-    }
-    l_run = l_run * alpha + sum;
-    m_run = m_new;
-#pragma unroll
-    for (int dt = 0; dt < C::dtiles; ++dt) {
-#pragma unroll
-      for (int e = 0; e < 16; ++e) o[dt][e] *= alpha;
     }
 
     // Element slot j of step c is result element c * kpl + j: row 8 (e / 4) + 4 half + e % 4.
