@@ -127,7 +127,7 @@ size_t reco_paged_prefill_attn_workspace_size(const reco_paged_cache_t *cache, i
   const int units = units_of(cache, n_layers), G = group_of(cache, n_q_heads);
   if (units < 1 || G < 1 || G > 16 || n_tokens < 1 || static_cast<int64_t>(n_tokens) * G > kMaxQueryRows) return 0;
   return reco::prefill_workspace_bytes(units, n_tokens, static_cast<int>(capacity_of(cache)), G, cache->head_dim,
-                                       reco::current_compute_units());
+                                       reco::prefill_tile_rows(cache->dtype), reco::current_compute_units());
 }
 
 reco_status_t reco_paged_prefill_attn(const reco_paged_cache_t *cache, int32_t layer0, int32_t n_layers,
@@ -148,7 +148,8 @@ reco_status_t reco_paged_prefill_attn(const reco_paged_cache_t *cache, int32_t l
 
   reco::PagedPrefillParams p{};
   p.c = paged_cache(cache, layer0, n_layers, dev_err);
-  const size_t need = reco::prefill_workspace_bytes(units, n_tokens, p.c.cap, G, cache->head_dim, cus);
+  const int tile_rows = reco::prefill_tile_rows(cache->dtype);
+  const size_t need = reco::prefill_workspace_bytes(units, n_tokens, p.c.cap, G, cache->head_dim, tile_rows, cus);
   if (!ws || ws_bytes < need || (reinterpret_cast<uintptr_t>(ws) & 255)) return RECO_ERR_WORKSPACE;
   p.q = q;
   p.k_new = k_new;
@@ -160,7 +161,7 @@ reco_status_t reco_paged_prefill_attn(const reco_paged_cache_t *cache, int32_t l
   p.hq = n_q_heads;
   p.tokens = n_tokens;
   p.blocks = reco::prefill_blocks(n_tokens, G);
-  p.splits = reco::prefill_splits(units, p.blocks, p.c.cap, sinks, window, cus);
+  p.splits = reco::prefill_splits(units, p.blocks, p.c.cap, sinks, window, tile_rows, cus);
   p.sinks = sinks;
   p.window = window;
   p.scale_log2 = scale * 1.4426950408889634f;

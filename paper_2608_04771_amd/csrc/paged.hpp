@@ -69,8 +69,10 @@ struct PagedPrefillParams {
   float scale_log2;
 };
 int prefill_blocks(int tokens, int group);
-int prefill_splits(int units, int blocks, int capacity, int sinks, int window, int compute_units);
-size_t prefill_workspace_bytes(int units, int tokens, int capacity, int group, int head_dim, int compute_units);
+constexpr int prefill_tile_rows(int dtype) { return dtype == 0 ? 32 : 64; }   // keys of a tile: fp32, bf16
+int prefill_splits(int units, int blocks, int capacity, int sinks, int window, int tile_rows, int compute_units);
+size_t prefill_workspace_bytes(int units, int tokens, int capacity, int group, int head_dim, int tile_rows,
+                               int compute_units);
 bool prefill_fits_grid(const PagedPrefillParams &p);
 void prefill_place(PagedPrefillParams &p, int head_dim, void *ws);
 hipError_t launch_paged_prefill(const PagedPrefillParams &p, int dtype, int head_dim, hipStream_t s);

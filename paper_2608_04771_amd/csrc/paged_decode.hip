@@ -92,9 +92,9 @@ __device__ __forceinline__ bool append_row(const PagedDecodeParams &p, size_t cu
   if (len_in < 0 || len_in > p.c.cap) code = kDevBadLength;
   else if (p.k_new && len_in == p.c.cap) code = kDevAppendOverflow;
   if (code == 0 && p.k_new) {
-    PagedUnit u(p.c, cunit);
-    *at = u.row_at(len_in, len_in + 1) * D;
-    if (u.bad) code = kDevBadPage;
+    PagedUnit u(p.c, cunit, len_in + 1);
+    *at = u.row_at(u.entry(len_in), len_in) * D;
+    if (u.bad()) code = kDevBadPage;
   }
   if (code && threadIdx.x == 0) report(p.c.dev_err, code);
   return code == 0 && p.k_new;
@@ -146,7 +146,7 @@ __global__ __launch_bounds__(NW * kWave, (Cfg<T, D>::min_wgs)) void paged_split_
   const int n_cache = len_in < 0 ? 0 : (len_in > p.c.cap ? p.c.cap : len_in);
   const bool append = p.k_new != nullptr;
   const SeenTiles seen(n_cache + (append ? 1 : 0), p.sinks, p.window);
-  PagedUnit pages(p.c, cunit);
+  PagedUnit pages(p.c, cunit, n_cache);
   const T *knew = append ? reinterpret_cast<const T *>(p.k_new) + static_cast<size_t>(unit) * D : nullptr;
   const T *vnew = append ? reinterpret_cast<const T *>(p.v_new) + static_cast<size_t>(unit) * D : nullptr;
 
@@ -175,10 +175,11 @@ __global__ __launch_bounds__(NW * kWave, (Cfg<T, D>::min_wgs)) void paged_split_
   };
   const auto find = [&](int i) {
     const int kb = seen.tile(i) * kTile;
-    return Where{{pages.row_at(kb, n_cache), pages.row_at(kb + 16, n_cache)}};
+    const int a = pages.entry(kb), b = pages.entry(kb + 16);
+    return Where{{pages.row_at(a, kb), pages.row_at(b, kb + 16)}};
   };
-  // A tile's rows of K or V.  Rows past the last cached one are the rest of a page
-  // or of page 0 and are masked where they are used; row n_cache is the new one.
+  // A tile's rows of K or V.  Rows past the last cached one are others of the pool and
+  // are masked where they are used; row n_cache is the new one.
   const auto load = [&](Rows<T, D> &reg, const void *pool, const T *fresh, int i, const Where &w) {
     const int kb = seen.tile(i) * kTile;
     const int sub = (lane % C::lanes_per_row) * 16;
@@ -278,7 +279,7 @@ __global__ __launch_bounds__(NW * kWave, (Cfg<T, D>::min_wgs)) void paged_split_
       else attend(i, std::integral_constant<bool, false>{});
     }
   }
-  if (pages.bad && lane == 0) report(p.c.dev_err, kDevBadPage);
+  if (pages.bad() && n_cache > 0 && lane == 0) report(p.c.dev_err, kDevBadPage);
 
   const float l_tot = group4_sum(l_run);
   __threadfence_block();                                  // logits, before other waves read them
@@ -428,9 +429,9 @@ __global__ __launch_bounds__(kMergeThreads) void paged_merge_kernel(PagedDecodeP
     if (k / (kTile / 4) >= seen.total) return;
     bool fresh = false;
     if (p.k_new && len_in >= 0 && len_in < p.c.cap) {
-      PagedUnit u(p.c, cunit);
-      u.row_at(len_in, len_in + 1);
-      fresh = !u.bad;
+      PagedUnit u(p.c, cunit, len_in + 1);
+      u.row_at(u.entry(len_in), len_in);
+      fresh = !u.bad();
     }
     add_weights(p.c.weight + cunit * p.c.cap, p.logits + static_cast<size_t>(unit) * G * p.logit_pitch, p.logit_pitch,
                 G, seen.tile(k / (kTile / 4)) * kTile + k % (kTile / 4) * 4, seen, n, fresh, s_top, s_inv);

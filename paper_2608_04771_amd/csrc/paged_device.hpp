@@ -17,26 +17,26 @@ __device__ __forceinline__ const_i32 *as_const(const int32_t *p) {
   return reinterpret_cast<const_i32 *>(reinterpret_cast<uintptr_t>(p));
 }
 
-// One unit of a paged cache.  Only table entries of pages that hold cached rows
-// are read; an id outside the pool becomes page 0 and is noted.
+// One unit of a paged cache with n cached rows.  Only ids of pages that hold cached
+// rows are used; one outside the pool becomes its last page and is noted.
 struct PagedUnit {
   const_i32 *table;
-  int n_pages, shift;
-  bool bad;
+  int n_pages, shift, last;
+  unsigned worst;
 
-  __device__ __forceinline__ PagedUnit(const PagedCache &c, size_t cunit)
+  __device__ __forceinline__ PagedUnit(const PagedCache &c, size_t cunit, int n)
       : table(as_const(c.pages + cunit * static_cast<size_t>(c.max_pages))), n_pages(c.n_pages), shift(c.page_shift),
-        bad(false) {}
-  // The pool's row of `row`, which has to be the same in all lanes; `n` rows are cached.
-  __device__ __forceinline__ size_t row_at(int row, int n) {
-    int id = 0;
-    if (row < n) id = table[row >> shift];
-    if (static_cast<unsigned>(id) >= static_cast<unsigned>(n_pages)) {
-      id = 0;
-      bad = true;
-    }
+        last(max(n - 1, 0)), worst(0) {}
+  // The table's entry for `row` (the same in all lanes), or for the last cached row
+  // where that comes first.  Without a branch, so that several are on their way at once.
+  __device__ __forceinline__ int entry(int row) const { return table[min(row, last) >> shift]; }
+  // The pool's row of `row`, by its entry.
+  __device__ __forceinline__ size_t row_at(int entry, int row) {
+    worst = max(worst, static_cast<unsigned>(entry));
+    const unsigned id = min(static_cast<unsigned>(entry), static_cast<unsigned>(n_pages - 1));
     return (static_cast<size_t>(id) << shift) + static_cast<size_t>(row & ((1 << shift) - 1));
   }
+  __device__ __forceinline__ bool bad() const { return worst >= static_cast<unsigned>(n_pages); }
 };
 
 // The rows that a token at row n_tot - 1 sees: [0, sink_end) and [lo, n_tot), as

@@ -65,22 +65,23 @@ int prefill_blocks(int tokens, int group) {
 }
 
 // Key tiles are split where there are too few blocks of query rows for two workgroups
-// on every compute unit, into pieces of at least four tiles of 64 rows.
-int prefill_splits(int units, int blocks, int capacity, int sinks, int window, int compute_units) {
+// on every compute unit, into pieces of at least two tiles.
+int prefill_splits(int units, int blocks, int capacity, int sinks, int window, int tile_rows, int compute_units) {
   int64_t rows = capacity;
   if (window > 0) {
     const int64_t seen = static_cast<int64_t>(sinks) + window + 2 * kPrefillRows;
     if (seen < rows) rows = seen;
   }
   int64_t splits = 2 * static_cast<int64_t>(compute_units) / (static_cast<int64_t>(units) * blocks);
-  if (splits > rows / 256) splits = rows / 256;
+  if (splits > rows / (2 * tile_rows)) splits = rows / (2 * tile_rows);
   if (splits > kPrefillMaxSplits) splits = kPrefillMaxSplits;
   return splits < 1 ? 1 : static_cast<int>(splits);
 }
 
-size_t prefill_workspace_bytes(int units, int tokens, int capacity, int group, int head_dim, int compute_units) {
+size_t prefill_workspace_bytes(int units, int tokens, int capacity, int group, int head_dim, int tile_rows,
+                               int compute_units) {
   const int blocks = prefill_blocks(tokens, group);
-  const int splits = prefill_splits(units, blocks, capacity, 0, 0, compute_units);   // a window takes no more
+  const int splits = prefill_splits(units, blocks, capacity, 0, 0, tile_rows, compute_units);   // a window takes no more
   size_t bytes = aligned(static_cast<size_t>(units) * sizeof(int32_t));
   if (splits > 1)
     bytes += static_cast<size_t>(units) * blocks * splits * kPrefillRows * (static_cast<size_t>(head_dim) + 2) * sizeof(float);

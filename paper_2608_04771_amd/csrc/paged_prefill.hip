@@ -143,10 +143,10 @@ __global__ __launch_bounds__(kThreads, 2) void prefill_kernel(PagedPrefillParams
   // This lane's query row.
   const int r = r0 + wave * 32 + col;
   const bool real = r < n * G;
-  const int t = min(r, n * G - 1) / G;
+  const int t = min(r, p.tokens * G - 1) / G;
   const int pos = L + t;
   const int low = p.window > 0 ? pos - p.window : -1;     // sees rows above it, and the sinks
-  const size_t qrow = ((static_cast<size_t>(lc) * p.c.batch + b) * p.hq + h * G + (min(r, n * G - 1) - t * G)) *
+  const size_t qrow = ((static_cast<size_t>(lc) * p.c.batch + b) * p.hq + h * G + (min(r, p.tokens * G - 1) - t * G)) *
                           static_cast<size_t>(p.tokens) + t;
   frag qf[C::qk_steps];
   {
@@ -159,36 +159,67 @@ __global__ __launch_bounds__(kThreads, 2) void prefill_kernel(PagedPrefillParams
   }
   const float scale = fmaxf(fabsf(p.scale_log2), 0x1p-126f);   // times a hidden row's -inf, 0 would be NaN
 
-  PagedUnit pages(p.c, cunit);
+  PagedUnit pages(p.c, cunit, L);
   const unsigned char *knew = reinterpret_cast<const unsigned char *>(p.k_new) + static_cast<size_t>(unit) * p.tokens * C::row_bytes;
   const unsigned char *vnew = reinterpret_cast<const unsigned char *>(p.v_new) + static_cast<size_t>(unit) * p.tokens * C::row_bytes;
-  u32x4v kreg[C::insts], vreg[C::insts];
-  // A tile's rows; those past its end are its last one again (finite if that is, and
-  // of no weight).
-  const auto load = [&](int tile) {
-    const int start = run.start(tile), end = run.end(tile);
+  using Regs = u32x4v[C::insts];
+  Regs kreg, vreg;
+  // A wave's k-th load of a tile takes wave_rows rows from this one on.
+  const auto piece = [&](int k) { return (k * kWaves + wave) * C::wave_rows; };
+  // The table entries of a tile, asked for one tile ahead of its rows.
+  struct Entries {
+    int id[C::insts];
+  };
+  const auto find = [&](int i) {
+    Entries e{};
+    const int tile = tile_at(min(i, i1 - 1));
+    if (tile < run.old_tiles) {
 #pragma unroll
-    for (int k = 0; k < C::insts; ++k) {
-      const int row0 = start + (k * kWaves + wave) * C::wave_rows;
-      const int from = min(row0, start + ((end - 1 - start) & ~(C::wave_rows - 1)));
-      const int row = min(from + lane / C::lanes_per_row, end - 1) - from;
-      const int off = row * C::row_bytes + (lane % C::lanes_per_row) * 16;
-      const bool old = tile < run.old_tiles;
-      const size_t at = (old ? pages.row_at(from, L) : static_cast<size_t>(from - L)) * C::row_bytes;
-      kreg[k] = *reinterpret_cast<const u32x4v *>((old ? reinterpret_cast<const unsigned char *>(p.c.k) : knew) + at + off);
-      vreg[k] = *reinterpret_cast<const u32x4v *>((old ? reinterpret_cast<const unsigned char *>(p.c.v) : vnew) + at + off);
+      for (int k = 0; k < C::insts; ++k) e.id[k] = pages.entry(tile * KT + piece(k));
+    }
+    return e;
+  };
+  // A tile's rows.  Those past its end are other rows of the pool or of the run.
+  const auto load = [&](int i, const Entries &e, Regs &kreg, Regs &vreg) {
+    const int tile = tile_at(min(i, i1 - 1));
+    if (tile < run.old_tiles) {
+#pragma unroll
+      for (int k = 0; k < C::insts; ++k) {
+        const size_t at = pages.row_at(e.id[k], tile * KT + piece(k)) * C::row_bytes;
+        kreg[k] = *reinterpret_cast<const u32x4v *>(reinterpret_cast<const unsigned char *>(p.c.k) + at + lane * 16);
+        vreg[k] = *reinterpret_cast<const u32x4v *>(reinterpret_cast<const unsigned char *>(p.c.v) + at + lane * 16);
+      }
+    } else {
+      const int row0 = (tile - run.old_tiles) * KT;        // of the run
+      const bool all = row0 + KT <= p.tokens;
+#pragma unroll
+      for (int k = 0; k < C::insts; ++k) {
+        const size_t at = static_cast<size_t>(row0 + piece(k)) * C::row_bytes;
+        int off = lane * 16;
+        if (!all) off += min(0, (p.tokens - 1 - row0 - piece(k) - lane / C::lanes_per_row) * C::row_bytes);
+        kreg[k] = *reinterpret_cast<const u32x4v *>(knew + at + off);
+        vreg[k] = *reinterpret_cast<const u32x4v *>(vnew + at + off);
+      }
     }
   };
-  const auto store = [&](int tile, unsigned char *buf) {
-    const int start = run.start(tile);
+  // Rows of V that no token of the block sees count for nothing, whatever they hold.
+  const auto store = [&](int tile, unsigned char *buf, Regs &kreg, Regs &vreg) {
+    const int start = run.start(tile), end = run.end(tile);
+    if (end - start < KT || (start < lo && end > s_end)) {
+#pragma unroll
+      for (int k = 0; k < C::insts; ++k) {
+        const int j = start + piece(k) + lane / C::lanes_per_row;
+        const unsigned keep = j < end && (j >= lo || j < s_end) ? ~0u : 0u;
+        vreg[k] &= keep;
+      }
+    }
+    unsigned char *to = buf + (wave * C::wave_rows + lane / C::lanes_per_row) * C::k_pitch + (lane % C::lanes_per_row) * 16;
+    unsigned char *tv = buf + KT * C::k_pitch + (wave * C::wave_rows + lane / C::lanes_per_row) * C::v_pitch +
+                        (lane % C::lanes_per_row) * 16;
 #pragma unroll
     for (int k = 0; k < C::insts; ++k) {
-      const int row = (k * kWaves + wave) * C::wave_rows + lane / C::lanes_per_row;
-      const int sub = (lane % C::lanes_per_row) * 16;
-      *reinterpret_cast<u32x4v *>(buf + row * C::k_pitch + sub) = kreg[k];
-      const int j = min(start + row, run.end(tile) - 1);
-      const unsigned keep = j >= lo || j < s_end ? ~0u : 0u;   // rows that no token here sees count for nothing
-      *reinterpret_cast<u32x4v *>(buf + KT * C::k_pitch + row * C::v_pitch + sub) = vreg[k] & keep;
+      *reinterpret_cast<u32x4v *>(to + k * kWaves * C::wave_rows * C::k_pitch) = kreg[k];
+      *reinterpret_cast<u32x4v *>(tv + k * kWaves * C::wave_rows * C::v_pitch) = vreg[k];
     }
   };
 
@@ -200,9 +231,14 @@ __global__ __launch_bounds__(kThreads, 2) void prefill_kernel(PagedPrefillParams
     for (int i = 0; i < 16; ++i) o[dt][i] = 0.f;
   }
 
+  Entries next{};
   if (i0 < i1) {
-    load(tile_at(i0));
-    store(tile_at(i0), smem);
+    Regs kfirst, vfirst;                                  // the first two tiles come together
+    const Entries a = find(i0), b = find(i0 + 1);
+    next = find(i0 + 2);
+    load(i0, a, kfirst, vfirst);
+    load(i0 + 1, b, kreg, vreg);
+    store(tile_at(i0), smem, kfirst, vfirst);
   }
   __syncthreads();
   for (int i = i0; i < i1; ++i) {
@@ -210,7 +246,6 @@ __global__ __launch_bounds__(kThreads, 2) void prefill_kernel(PagedPrefillParams
     const unsigned char *vbuf = kbuf + KT * C::k_pitch;
     const int tile = tile_at(i);
     const int start = run.start(tile), end = run.end(tile);
-    if (i + 1 < i1) load(tile_at(i + 1));
 
     f32x16_t s[C::blocks];
 #pragma unroll
@@ -220,6 +255,14 @@ __global__ __launch_bounds__(kThreads, 2) void prefill_kernel(PagedPrefillParams
       const T *krow = reinterpret_cast<const T *>(kbuf + (kb * 32 + col) * C::k_pitch) + half * (D / 2);
 #pragma unroll
       for (int c = 0; c < C::qk_steps; ++c) s[kb] = M::mma(load_frag(krow + c * M::kpl), qf[c], s[kb]);
+    }
+
+    // The next tile's rows to LDS and the one after it asked for, while the vector
+    // units take the softmax.
+    if (i + 1 < i1) {
+      store(tile_at(i + 1), smem + ((i + 1 - i0) & 1) * C::stage, kreg, vreg);
+      load(i + 2, next, kreg, vreg);
+      next = find(i + 3);
     }
 
     // Whether every token of the block sees the whole tile.
@@ -298,43 +341,59 @@ __global__ __launch_bounds__(kThreads, 2) void prefill_kernel(PagedPrefillParams
         }
       }
     }
-    if (i + 1 < i1) store(tile_at(i + 1), smem + ((i + 1 - i0) & 1) * C::stage);
     __syncthreads();
   }
-  if (pages.bad && lane == 0) report(p.c.dev_err, kDevBadPage);
+  if (pages.bad() && lane == 0) report(p.c.dev_err, kDevBadPage);
 
   const float l_tot = l_run + shfl_xor(l_run, 32);
   if (p.splits > 1) {
+    // partials stay in the lanes' order, so that they are written and read whole
     const size_t part = (static_cast<size_t>(unit) * p.blocks + block) * p.splits + split;
-    float *po = p.part_o + (part * kRows + wave * 32 + col) * D;
     if (half == 0) {
       p.part_ml[part * 2 * kRows + wave * 32 + col] = m_run;
       p.part_ml[part * 2 * kRows + kRows + wave * 32 + col] = l_tot;
     }
+    float4 *po = reinterpret_cast<float4 *>(p.part_o + (part * kRows + wave * 32) * D) + lane;
 #pragma unroll
     for (int dt = 0; dt < C::dtiles; ++dt) {
 #pragma unroll
-      for (int e = 0; e < 16; e += 4)
-        *reinterpret_cast<float4 *>(po + dt * 32 + acc_row(e, half)) =
-            make_float4(o[dt][e], o[dt][e + 1], o[dt][e + 2], o[dt][e + 3]);
+      for (int e = 0; e < 4; ++e)
+        po[(dt * 4 + e) * kWave] = make_float4(o[dt][4 * e], o[dt][4 * e + 1], o[dt][4 * e + 2], o[dt][4 * e + 3]);
     }
     return;
   }
-  if (!real) return;
+  // A wave's 32 rows through LDS, so that rows are written whole (the tiles' buffers are
+  // free after the last barrier).
   const float inv = l_tot == 0.f ? 0.f : 1.f / l_tot;
-  T *dst = reinterpret_cast<T *>(p.out) + qrow * D;
+  unsigned char *rows = smem + wave * 32 * C::k_pitch;
 #pragma unroll
   for (int dt = 0; dt < C::dtiles; ++dt) {
 #pragma unroll
-    for (int e = 0; e < 16; ++e) dst[dt * 32 + acc_row(e, half)] = from_f32<T>(o[dt][e] * inv);
+    for (int e = 0; e < 16; e += 4) {
+      T *at = reinterpret_cast<T *>(rows + col * C::k_pitch) + dt * 32 + acc_row(e, half);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) at[j] = from_f32<T>(o[dt][e + j] * inv);
+    }
   }
-  if (p.lse && half == 0) p.lse[qrow] = l_tot == 0.f ? -INFINITY : (m_run + log2f(l_tot)) * kLn2;
+  if (real && p.lse && half == 0) p.lse[qrow] = l_tot == 0.f ? -INFINITY : (m_run + log2f(l_tot)) * kLn2;
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+#pragma unroll
+  for (int k = 0; k < 32 / C::wave_rows; ++k) {
+    const int in = k * C::wave_rows + lane / C::lanes_per_row;
+    const int row = r0 + wave * 32 + in;
+    if (row >= n * G) break;
+    const int tok = row / G;
+    const size_t at = ((static_cast<size_t>(lc) * p.c.batch + b) * p.hq + h * G + (row - tok * G)) *
+                          static_cast<size_t>(p.tokens) + tok;
+    reinterpret_cast<u32x4v *>(p.out)[at * C::lanes_per_row + lane % C::lanes_per_row] =
+        *reinterpret_cast<const u32x4v *>(rows + in * C::k_pitch + (lane % C::lanes_per_row) * 16);
+  }
 }
 
 // Joins the splits (workgroups [0, merges)) and puts the new rows into their pages
 // (the others, kAppendRows rows of a unit each).  A unit's rows are appended together or,
 // where they or their pages do not fit, not at all.
-constexpr int kMergeRows = 8;
+constexpr int kMergeRows = 32;               // a wave's rows, and a quarter of a 32-column block each thread
 constexpr int kAppendRows = 64;
 
 template <typename T, int D>
@@ -344,38 +403,72 @@ __global__ __launch_bounds__(256) void prefill_finish_kernel(PagedPrefillParams 
   const int G = p.group;
   int id = blockIdx.x;
   if (id < merges) {
-    const int piece = id % (kRows / kMergeRows);
-    id /= kRows / kMergeRows;
+    constexpr int kDt = D / 32;
+    const int dt = id % kDt, w32 = id / kDt % (kRows / kMergeRows);
+    id /= kDt * (kRows / kMergeRows);
     const int block = id % p.blocks, unit = id / p.blocks;
     const int lc = unit / per_layer, b = (unit % per_layer) / p.c.hkv, h = unit % p.c.hkv;
     const int given = p.n_new ? p.n_new[b] : p.tokens;
     const int n = given < 0 || given > p.tokens ? 0 : given;
-    constexpr int kPer = 256 / kMergeRows;               // threads of a row
-    const int in = piece * kMergeRows + tid / kPer;
-    const int r = block * kRows + in;
-    if (r >= n * G) return;
+    if (block * kRows + w32 * kMergeRows >= n * G) return;
+    // The splits' weights of the rows: eight threads a row.
+    __shared__ float s_w[kPrefillMaxSplits][kMergeRows];
     const size_t part = (static_cast<size_t>(unit) * p.blocks + block) * p.splits;
-    float top = -INFINITY;
-    for (int s = 0; s < p.splits; ++s) top = fmaxf(top, p.part_ml[(part + s) * 2 * kRows + in]);
-    const float ref = top == -INFINITY ? 0.f : top;
-    float sum = 0.f;
-    float acc[D / kPer];
+    const int lane = tid & (kWave - 1);
+    {
+      constexpr int kPer = 256 / kMergeRows, kEach = kPrefillMaxSplits / kPer;
+      const int row_of = tid / kPer, sub = tid % kPer;
+      const float *ml = p.part_ml + part * 2 * kRows + w32 * kMergeRows + row_of;
+      float m[kEach], l[kEach];
+      float top = -INFINITY, sum = 0.f;
 #pragma unroll
-    for (int i = 0; i < D / kPer; ++i) acc[i] = 0.f;
-    for (int s = 0; s < p.splits; ++s) {
-      const float w = fast_exp2(p.part_ml[(part + s) * 2 * kRows + in] - ref);
-      sum += p.part_ml[(part + s) * 2 * kRows + kRows + in] * w;
-      const float *po = p.part_o + ((part + s) * kRows + in) * D + tid % kPer;
+      for (int i = 0; i < kEach; ++i) {
+        const int s = sub + i * kPer;
+        m[i] = s < p.splits ? ml[static_cast<size_t>(s) * 2 * kRows] : -INFINITY;
+        l[i] = s < p.splits ? ml[static_cast<size_t>(s) * 2 * kRows + kRows] : 0.f;
+        top = fmaxf(top, m[i]);
+      }
 #pragma unroll
-      for (int i = 0; i < D / kPer; ++i) acc[i] += po[i * kPer] * w;
+      for (int d = 1; d < kPer; d <<= 1) top = fmaxf(top, shfl_xor(top, d));
+      const float ref = top == -INFINITY ? 0.f : top;
+#pragma unroll
+      for (int i = 0; i < kEach; ++i) {
+        m[i] = fast_exp2(m[i] - ref);
+        sum += l[i] * m[i];
+      }
+#pragma unroll
+      for (int d = 1; d < kPer; d <<= 1) sum += shfl_xor(sum, d);
+      const float inv = sum == 0.f ? 0.f : 1.f / sum;
+#pragma unroll
+      for (int i = 0; i < kEach; ++i) s_w[sub + i * kPer][row_of] = m[i] * inv;
+      const int r = block * kRows + w32 * kMergeRows + row_of;
+      if (p.lse && dt == 0 && sub == 0 && r < n * G)
+        p.lse[((static_cast<size_t>(lc) * p.c.batch + b) * p.hq + h * G + r % G) * static_cast<size_t>(p.tokens) + r / G] =
+            sum == 0.f ? -INFINITY : (ref + log2f(sum)) * kLn2;
     }
+    __syncthreads();
+    const int row_of = lane & 31, e = tid / kWave;
+    const int r = block * kRows + w32 * kMergeRows + row_of;
+    const float4 *po = reinterpret_cast<const float4 *>(p.part_o + (part * kRows + w32 * kMergeRows) * D) +
+                       (dt * 4 + e) * kWave + lane;
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 8
+    for (int s = 0; s < p.splits; ++s) {
+      const float w = s_w[s][row_of];
+      const float4 x = po[static_cast<size_t>(s) * kRows * (D / 4)];
+      acc.x += x.x * w;
+      acc.y += x.y * w;
+      acc.z += x.z * w;
+      acc.w += x.w * w;
+    }
+    if (r >= n * G) return;
     const int t = r / G;
     const size_t row = ((static_cast<size_t>(lc) * p.c.batch + b) * p.hq + h * G + (r - t * G)) * static_cast<size_t>(p.tokens) + t;
-    const float inv = sum == 0.f ? 0.f : 1.f / sum;
-    T *dst = reinterpret_cast<T *>(p.out) + row * D + tid % kPer;
-#pragma unroll
-    for (int i = 0; i < D / kPer; ++i) dst[i * kPer] = from_f32<T>(acc[i] * inv);
-    if (p.lse && tid % kPer == 0) p.lse[row] = sum == 0.f ? -INFINITY : (ref + log2f(sum)) * kLn2;
+    T *dst = reinterpret_cast<T *>(p.out) + row * D + dt * 32 + acc_row(4 * e, lane >> 5);
+    dst[0] = from_f32<T>(acc.x);
+    dst[1] = from_f32<T>(acc.y);
+    dst[2] = from_f32<T>(acc.z);
+    dst[3] = from_f32<T>(acc.w);
     return;
   }
   id -= merges;
@@ -420,7 +513,7 @@ hipError_t launch_typed(const PagedPrefillParams &p, hipStream_t s) {
   hipLaunchKernelGGL((prefill_kernel<T, D>), dim3(p.blocks * p.splits, units), dim3(kThreads), 0, s, p);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  const int merges = p.splits > 1 ? units * p.blocks * (kRows / kMergeRows) : 0;
+  const int merges = p.splits > 1 ? units * p.blocks * (kRows / kMergeRows) * (D / 32) : 0;
   const int chunks = (p.tokens + kAppendRows - 1) / kAppendRows;
   hipLaunchKernelGGL((prefill_finish_kernel<T, D>), dim3(merges + units * chunks), dim3(256), 0, s, p, merges, chunks);
   return hipGetLastError();
