@@ -60,8 +60,13 @@ void paged_decode_place(PagedDecodeParams &p, int head_dim, void *ws) {
   p.logit_pitch = static_cast<int64_t>(logit_pitch(p.c.cap));
 }
 
-int prefill_blocks(int tokens, int group) {
-  return static_cast<int>((static_cast<int64_t>(tokens) * group + kPrefillRows - 1) / kPrefillRows);
+int prefill_blocks(int tokens, int group, int rows) {
+  return static_cast<int>((static_cast<int64_t>(tokens) * group + rows - 1) / rows);
+}
+
+// Blocks of 256 rows where they give every compute unit two workgroups in turn.
+bool prefill_wide(int units, int tokens, int group, int dtype, int compute_units) {
+  return false && dtype == 1 && static_cast<int64_t>(units) * prefill_blocks(tokens, group, kPrefillWideRows) >= 2 * compute_units;
 }
 
 // Key tiles are split where there are too few blocks of query rows for two workgroups
@@ -80,7 +85,7 @@ int prefill_splits(int units, int blocks, int capacity, int sinks, int window, i
 
 size_t prefill_workspace_bytes(int units, int tokens, int capacity, int group, int head_dim, int tile_rows,
                                int compute_units) {
-  const int blocks = prefill_blocks(tokens, group);
+  const int blocks = prefill_blocks(tokens, group, kPrefillRows);
   const int splits = prefill_splits(units, blocks, capacity, 0, 0, tile_rows, compute_units);   // a window takes no more
   size_t bytes = aligned(static_cast<size_t>(units) * sizeof(int32_t));
   if (splits > 1)

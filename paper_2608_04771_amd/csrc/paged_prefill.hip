@@ -93,6 +93,195 @@ struct Run {
   __device__ __forceinline__ int end(int tile) const { return min(start(tile) + KT, tile < old_tiles ? L : L + n); }
 };
 
+// What a block of query rows sees, as a list of tiles: the sinks', then those of its
+// windows up to its last token.
+template <int KT>
+struct Seen {
+  Run<KT> run;
+  int lo, s_end;                             // rows [0, s_end) and [lo, ...)
+  int sink_tiles, skip, total;
+
+  __device__ __forceinline__ Seen(const Run<KT> &r, int t_lo, int t_hi, int sinks, int window) : run(r) {
+    lo = window > 0 ? max(0, run.L + t_lo - window + 1) : 0;
+    s_end = min(sinks, lo);
+    const int first = run.tile_of(lo);
+    sink_tiles = s_end > 0 ? min(run.tile_of(s_end - 1) + 1, first) : 0;
+    skip = first - sink_tiles;
+    total = run.tile_of(run.L + t_hi) + 1 - skip;
+  }
+  __device__ __forceinline__ int tile(int i) const { return i < sink_tiles ? i : i + skip; }
+};
+
+// Key tiles on their way to LDS: one in registers, and where the next ones lie.  Each
+// lane holds the place of 16 rows of the list's tiles, so 64 / (KT / 16) tiles at a
+// time; the table's entries of the batch after are on their way meanwhile.
+template <typename T, int D>
+struct Stager {
+  using C = Cfg<T, D>;
+  static constexpr int KT = C::keys;
+  static constexpr int kGroups = KT / 16;
+  static constexpr int kBatch = kWave / kGroups;   // tiles
+  using Regs = u32x4v[C::insts];
+  const unsigned char *k, *v, *knew, *vnew;
+  const int32_t *table;
+  const Seen<KT> &seen;
+  int n_pages, shift, tokens, end, wave, lane;
+  unsigned worst;                            // id, of rows that are cached
+  uint64_t place;                            // of this lane's 16 rows: a byte offset
+  int coming;                                // the entry for the same lane of the next batch
+  unsigned off[C::insts];                    // within 16 rows
+  Regs kreg, vreg;
+
+  // Tiles [.., end) of the list.
+  __device__ __forceinline__ Stager(const PagedPrefillParams &p, size_t cunit, int unit, const Seen<KT> &seen_, int end_,
+                                    int wave_, int lane_)
+      : k(static_cast<const unsigned char *>(p.c.k)), v(static_cast<const unsigned char *>(p.c.v)),
+        knew(static_cast<const unsigned char *>(p.k_new) + static_cast<size_t>(unit) * p.tokens * C::row_bytes),
+        vnew(static_cast<const unsigned char *>(p.v_new) + static_cast<size_t>(unit) * p.tokens * C::row_bytes),
+        table(p.c.pages + cunit * static_cast<size_t>(p.c.max_pages)), seen(seen_), n_pages(p.c.n_pages),
+        shift(p.c.page_shift), tokens(p.tokens), end(end_), wave(wave_), lane(lane_), worst(0) {
+#pragma unroll
+    for (int i = 0; i < C::insts; ++i) off[i] = offset(i);
+  }
+
+  // A wave's i-th load of a tile takes wave_rows rows from this one on.
+  __device__ __forceinline__ int piece(int i) const { return (i * kWaves + wave) * C::wave_rows; }
+  __device__ __forceinline__ unsigned offset(int i) const {
+    return (piece(i) % 16 + lane / C::lanes_per_row) * C::row_bytes + (lane % C::lanes_per_row) * 16;
+  }
+  __device__ __forceinline__ int tile(int i) const { return seen.tile(min(i, end - 1)); }
+  // This lane's tile of the batch that starts at tile i, and its rows there.
+  __device__ __forceinline__ int row_of(int i, bool &old) const {
+    const int t = tile(i + lane / kGroups);
+    old = t < seen.run.old_tiles;
+    return (old ? t : t - seen.run.old_tiles) * KT + lane % kGroups * 16;
+  }
+  __device__ __forceinline__ void ask(int i) {
+    bool old;
+    const int row = row_of(i, old);
+    coming = old ? table[min(row, seen.run.L - 1) >> shift] : 0;
+  }
+  // The batch that starts at tile i, whose entries were asked for, and the one after.
+  __device__ __forceinline__ void batch(int i) {
+    bool old;
+    const int row = row_of(i, old);
+    worst = max(worst, static_cast<unsigned>(coming));
+    const unsigned id = min(static_cast<unsigned>(coming), static_cast<unsigned>(n_pages - 1));
+    const unsigned in = old ? row & ((1u << shift) - 1u) : min(row, (tokens - 1) & ~15);
+    place = ((static_cast<uint64_t>(id) << shift) + in) * C::row_bytes;
+    ask(i + kBatch);
+  }
+  // A tile's rows.  Those past its end are other rows of the pool or of the run.
+  struct Place {
+    const unsigned char *k, *v;
+    int lane0;
+  };
+  __device__ __forceinline__ Place find(int i) const {
+    const int at_i = min(i, end - 1);
+    const bool old = seen.tile(at_i) < seen.run.old_tiles;
+    return Place{old ? k : knew, old ? v : vnew, (at_i & (kBatch - 1)) * kGroups};
+  }
+  __device__ __forceinline__ void load(const Place &w, int j, Regs &kr, Regs &vr) const {
+    const int from = w.lane0 + piece(j) / 16;
+    const uint64_t at = static_cast<uint64_t>(static_cast<unsigned>(__builtin_amdgcn_readlane(static_cast<int>(place >> 32), from))) << 32 |
+                        static_cast<unsigned>(__builtin_amdgcn_readlane(static_cast<int>(place), from));
+    kr[j] = *reinterpret_cast<const u32x4v *>(w.k + at + off[j]);
+    vr[j] = *reinterpret_cast<const u32x4v *>(w.v + at + off[j]);
+  }
+  __device__ __forceinline__ void load(int i, Regs &kr, Regs &vr) const {
+    const Place w = find(i);
+#pragma unroll
+    for (int j = 0; j < C::insts; ++j) load(w, j, kr, vr);
+  }
+  // Ahead of load(i): what seldom happens there, the places of a new batch ...
+  __device__ __forceinline__ void turn(int i) {
+    if (i < end && (i & (kBatch - 1)) == 0) batch(i);
+  }
+  // ... and the offsets of a run's last tile, whose rows past the last place must not be
+  // read (no tile of the list comes after it).
+  __device__ __forceinline__ void trim(int i) {
+    const int t = tile(i);
+    const int row0 = (t - seen.run.old_tiles) * KT;
+    if (t < seen.run.old_tiles || row0 + KT <= tokens) return;
+#pragma unroll
+    for (int j = 0; j < C::insts; ++j) {
+      const int base = min((row0 + piece(j)) & ~15, (tokens - 1) & ~15);
+      const int in = min(piece(j) % 16 + lane / C::lanes_per_row, tokens - 1 - base);
+      off[j] = in * C::row_bytes + (lane % C::lanes_per_row) * 16;
+    }
+  }
+  // Rows of V that no token of the block sees count for nothing, whatever they hold.
+  __device__ __forceinline__ void clean(int i, Regs &vr) const {
+    const int t = tile(i);
+    const int from = seen.run.start(t), to = seen.run.end(t);
+    if (to - from == KT && (from >= seen.lo || to <= seen.s_end)) return;
+#pragma unroll
+    for (int j = 0; j < C::insts; ++j) {
+      const int row = from + piece(j) + lane / C::lanes_per_row;
+      const unsigned keep = row < to && (row >= seen.lo || row < seen.s_end) ? ~0u : 0u;
+      vr[j] &= keep;
+    }
+  }
+  __device__ __forceinline__ void store(unsigned char *buf, int j, const Regs &kr, const Regs &vr) const {
+    const int row = j * kWaves * C::wave_rows + wave * C::wave_rows + lane / C::lanes_per_row, sub = (lane % C::lanes_per_row) * 16;
+    *reinterpret_cast<u32x4v *>(buf + row * C::k_pitch + sub) = kr[j];
+    *reinterpret_cast<u32x4v *>(buf + KT * C::k_pitch + row * C::v_pitch + sub) = vr[j];
+  }
+  __device__ __forceinline__ void store(unsigned char *buf, const Regs &kr, const Regs &vr) const {
+#pragma unroll
+    for (int j = 0; j < C::insts; ++j) store(buf, j, kr, vr);
+  }
+};
+
+// V^T operand of 16 keys from `row` on, columns [32 dt, 32 dt + 32): two transposing
+// reads of four rows each, in which lane i of 16 gets column i.
+template <int D>
+__device__ __forceinline__ bf16x8_t v_frag32(const unsigned char *vbuf, int row, int dt, int lane) {
+  using C = Cfg<bf16_t, D>;
+  const unsigned char *at = vbuf + (row + 4 * (lane >> 5) + (lane & 15) / 4) * C::v_pitch + (dt * 32 + (lane & 16) + 4 * (lane & 3)) * 2;
+  const i16x4_t a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4_t *)at);
+  const i16x4_t b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4_t *)(at + 8 * C::v_pitch));
+  const short v[8] = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+  bf16x8_t f;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) f[j] = __builtin_bit_cast(__bf16, v[j]);
+  return f;
+}
+
+// A wave's 32 rows from row0 on, of `rows`, divided by their sums and written whole
+// through LDS (`stage`: 32 rows of its own).  head0: query head 0 of the group.
+template <typename T, int D>
+__device__ __forceinline__ void write_rows(const PagedPrefillParams &p, unsigned char *stage,
+                                           const f32x16_t (&o)[Cfg<T, D>::dtiles], float m, float l, size_t head0,
+                                           int row0, int rows, int lane) {
+  using C = Cfg<T, D>;
+  const int half = lane >> 5, col = lane & 31;
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+  const auto place = [&](int row) {
+    const int t = row / p.group;
+    return (head0 + (row - t * p.group)) * static_cast<size_t>(p.tokens) + t;
+  };
+#pragma unroll
+  for (int dt = 0; dt < C::dtiles; ++dt) {
+#pragma unroll
+    for (int e = 0; e < 16; e += 4) {
+      T *at = reinterpret_cast<T *>(stage + col * C::k_pitch) + dt * 32 + acc_row(e, half);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) at[j] = from_f32<T>(o[dt][e + j] * inv);
+    }
+  }
+  if (p.lse && half == 0 && row0 + col < rows) p.lse[place(row0 + col)] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+#pragma unroll
+  for (int k = 0; k < 32 / C::wave_rows; ++k) {
+    const int in = k * C::wave_rows + lane / C::lanes_per_row;
+    if (row0 + in >= rows) break;
+    reinterpret_cast<u32x4v *>(p.out)[place(row0 + in) * C::lanes_per_row + lane % C::lanes_per_row] =
+        *reinterpret_cast<const u32x4v *>(stage + in * C::k_pitch + (lane % C::lanes_per_row) * 16);
+  }
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+}
+
 template <typename T, int D>
 __global__ __launch_bounds__(kThreads, 2) void prefill_kernel(PagedPrefillParams p) {
   using C = Cfg<T, D>;
@@ -128,21 +317,13 @@ __global__ __launch_bounds__(kThreads, 2) void prefill_kernel(PagedPrefillParams
   const int L = run.L;
   const int t_lo = r0 / G, t_hi = min(r0 + kRows - 1, n * G - 1) / G;
 
-  // The tiles that any token of the block sees: the sinks', then [first, last].
-  const int lo = p.window > 0 ? max(0, L + t_lo - p.window + 1) : 0;
-  const int s_end = min(p.sinks, lo);
-  const int first = run.tile_of(lo);
-  const int sink_tiles = s_end > 0 ? min(run.tile_of(s_end - 1) + 1, first) : 0;
-  const int skip = first - sink_tiles;
-  const int total = run.tile_of(L + t_hi) + 1 - skip;
-  const int per_split = (total + p.splits - 1) / p.splits;
+  const Seen<KT> seen(run, t_lo, t_hi, p.sinks, p.window);
+  const int per_split = (seen.total + p.splits - 1) / p.splits;
   const int i0 = split * per_split;
-  const int i1 = min(total, i0 + per_split);
-  const auto tile_at = [&](int i) { return i < sink_tiles ? i : i + skip; };
+  const int i1 = min(seen.total, i0 + per_split);
 
   // This lane's query row.
   const int r = r0 + wave * 32 + col;
-  const bool real = r < n * G;
   const int t = min(r, p.tokens * G - 1) / G;
   const int pos = L + t;
   const int low = p.window > 0 ? pos - p.window : -1;     // sees rows above it, and the sinks
@@ -159,69 +340,7 @@ __global__ __launch_bounds__(kThreads, 2) void prefill_kernel(PagedPrefillParams
   }
   const float scale = fmaxf(fabsf(p.scale_log2), 0x1p-126f);   // times a hidden row's -inf, 0 would be NaN
 
-  PagedUnit pages(p.c, cunit, L);
-  const unsigned char *knew = reinterpret_cast<const unsigned char *>(p.k_new) + static_cast<size_t>(unit) * p.tokens * C::row_bytes;
-  const unsigned char *vnew = reinterpret_cast<const unsigned char *>(p.v_new) + static_cast<size_t>(unit) * p.tokens * C::row_bytes;
-  using Regs = u32x4v[C::insts];
-  Regs kreg, vreg;
-  // A wave's k-th load of a tile takes wave_rows rows from this one on.
-  const auto piece = [&](int k) { return (k * kWaves + wave) * C::wave_rows; };
-  // The table entries of a tile, asked for one tile ahead of its rows.
-  struct Entries {
-    int id[C::insts];
-  };
-  const auto find = [&](int i) {
-    Entries e{};
-    const int tile = tile_at(min(i, i1 - 1));
-    if (tile < run.old_tiles) {
-#pragma unroll
-      for (int k = 0; k < C::insts; ++k) e.id[k] = pages.entry(tile * KT + piece(k));
-    }
-    return e;
-  };
-  // A tile's rows.  Those past its end are other rows of the pool or of the run.
-  const auto load = [&](int i, const Entries &e, Regs &kreg, Regs &vreg) {
-    const int tile = tile_at(min(i, i1 - 1));
-    if (tile < run.old_tiles) {
-#pragma unroll
-      for (int k = 0; k < C::insts; ++k) {
-        const size_t at = pages.row_at(e.id[k], tile * KT + piece(k)) * C::row_bytes;
-        kreg[k] = *reinterpret_cast<const u32x4v *>(reinterpret_cast<const unsigned char *>(p.c.k) + at + lane * 16);
-        vreg[k] = *reinterpret_cast<const u32x4v *>(reinterpret_cast<const unsigned char *>(p.c.v) + at + lane * 16);
-      }
-    } else {
-      const int row0 = (tile - run.old_tiles) * KT;        // of the run
-      const bool all = row0 + KT <= p.tokens;
-#pragma unroll
-      for (int k = 0; k < C::insts; ++k) {
-        const size_t at = static_cast<size_t>(row0 + piece(k)) * C::row_bytes;
-        int off = lane * 16;
-        if (!all) off += min(0, (p.tokens - 1 - row0 - piece(k) - lane / C::lanes_per_row) * C::row_bytes);
-        kreg[k] = *reinterpret_cast<const u32x4v *>(knew + at + off);
-        vreg[k] = *reinterpret_cast<const u32x4v *>(vnew + at + off);
-      }
-    }
-  };
-  // Rows of V that no token of the block sees count for nothing, whatever they hold.
-  const auto store = [&](int tile, unsigned char *buf, Regs &kreg, Regs &vreg) {
-    const int start = run.start(tile), end = run.end(tile);
-    if (end - start < KT || (start < lo && end > s_end)) {
-#pragma unroll
-      for (int k = 0; k < C::insts; ++k) {
-        const int j = start + piece(k) + lane / C::lanes_per_row;
-        const unsigned keep = j < end && (j >= lo || j < s_end) ? ~0u : 0u;
-        vreg[k] &= keep;
-      }
-    }
-    unsigned char *to = buf + (wave * C::wave_rows + lane / C::lanes_per_row) * C::k_pitch + (lane % C::lanes_per_row) * 16;
-    unsigned char *tv = buf + KT * C::k_pitch + (wave * C::wave_rows + lane / C::lanes_per_row) * C::v_pitch +
-                        (lane % C::lanes_per_row) * 16;
-#pragma unroll
-    for (int k = 0; k < C::insts; ++k) {
-      *reinterpret_cast<u32x4v *>(to + k * kWaves * C::wave_rows * C::k_pitch) = kreg[k];
-      *reinterpret_cast<u32x4v *>(tv + k * kWaves * C::wave_rows * C::v_pitch) = vreg[k];
-    }
-  };
+  Stager<T, D> in(p, cunit, unit, seen, i1, wave, lane);
 
   float m_run = -INFINITY, l_run = 0.f;                  // m in units of the scaled logits
   f32x16_t o[C::dtiles];
@@ -231,39 +350,72 @@ __global__ __launch_bounds__(kThreads, 2) void prefill_kernel(PagedPrefillParams
     for (int i = 0; i < 16; ++i) o[dt][i] = 0.f;
   }
 
-  Entries next{};
   if (i0 < i1) {
-    Regs kfirst, vfirst;                                  // the first two tiles come together
-    const Entries a = find(i0), b = find(i0 + 1);
-    next = find(i0 + 2);
-    load(i0, a, kfirst, vfirst);
-    load(i0 + 1, b, kreg, vreg);
-    store(tile_at(i0), smem, kfirst, vfirst);
+    typename Stager<T, D>::Regs kfirst, vfirst;           // the first two tiles come together
+    in.ask(i0 & -Stager<T, D>::kBatch);
+    in.batch(i0 & -Stager<T, D>::kBatch);
+    in.trim(i0);
+    in.load(i0, kfirst, vfirst);
+    in.turn(i0 + 1);
+    in.trim(i0 + 1);
+    in.load(i0 + 1, in.kreg, in.vreg);
+    in.clean(i0, vfirst);
+    in.store(smem, kfirst, vfirst);
   }
   __syncthreads();
   for (int i = i0; i < i1; ++i) {
     const unsigned char *kbuf = smem + ((i - i0) & 1) * C::stage;
     const unsigned char *vbuf = kbuf + KT * C::k_pitch;
-    const int tile = tile_at(i);
+    const int tile = seen.tile(i);
     const int start = run.start(tile), end = run.end(tile);
 
+    in.clean(i + 1, in.vreg);
+    in.turn(i + 2);
+    in.trim(i + 2);
+    // S^T, with operands read ahead of their products, and between the products the next
+    // tile's rows to LDS and the one after it asked for, piece by piece.
     f32x16_t s[C::blocks];
 #pragma unroll
     for (int kb = 0; kb < C::blocks; ++kb) {
 #pragma unroll
       for (int e = 0; e < 16; ++e) s[kb][e] = 0.f;
-      const T *krow = reinterpret_cast<const T *>(kbuf + (kb * 32 + col) * C::k_pitch) + half * (D / 2);
+    }
+    constexpr int kSteps = C::blocks * C::qk_steps, kAhead = M::kpl == 8 ? 8 : 16, kEach = kSteps / C::insts;
+    unsigned char *to = smem + ((i + 1 - i0) & 1) * C::stage;
+    const typename Stager<T, D>::Place from = in.find(i + 2);
+    frag kf[2][kAhead];
+    const auto read_k = [&](int q) {
 #pragma unroll
-      for (int c = 0; c < C::qk_steps; ++c) s[kb] = M::mma(load_frag(krow + c * M::kpl), qf[c], s[kb]);
+      for (int c = 0; c < kAhead; ++c) {
+        const int z = q * kAhead + c;
+        kf[q & 1][c] = load_frag(reinterpret_cast<const T *>(kbuf + (z / C::qk_steps * 32 + col) * C::k_pitch) + half * (D / 2) +
+                                 z % C::qk_steps * M::kpl);
+      }
+    };
+    read_k(0);
+#pragma unroll
+    for (int z = 0; z < kSteps; ++z) {
+      if (z % kAhead == 0 && z + kAhead < kSteps) read_k(z / kAhead + 1);
+      if (z % kAhead == 0) __builtin_amdgcn_sched_barrier(0);
+      s[z / C::qk_steps] = M::mma(kf[z / kAhead & 1][z % kAhead], qf[z % C::qk_steps], s[z / C::qk_steps]);
+      if (z % kEach == 0) {
+        in.store(to, z / kEach, in.kreg, in.vreg);
+        in.load(from, z / kEach, in.kreg, in.vreg);
+      }
+      __builtin_amdgcn_sched_barrier(0);
     }
-
-    // The next tile's rows to LDS and the one after it asked for, while the vector
-    // units take the softmax.
-    if (i + 1 < i1) {
-      store(tile_at(i + 1), smem + ((i + 1 - i0) & 1) * C::stage, kreg, vreg);
-      load(i + 2, next, kreg, vreg);
-      next = find(i + 3);
-    }
+    constexpr int kParts = C::blocks * C::pv_steps;
+    frag vf[2][C::dtiles];
+    const auto read_v = [&](int q) {
+#pragma unroll
+      for (int dt = 0; dt < C::dtiles; ++dt) {
+        if constexpr (M::kpl == 1)
+          vf[q & 1][dt] = *reinterpret_cast<const float *>(vbuf + acc_row(q, half) * C::v_pitch + (dt * 32 + col) * 4);
+        else
+          vf[q & 1][dt] = v_frag32<D>(vbuf, q * 16, dt, lane);
+      }
+    };
+    read_v(0);
 
     // Whether every token of the block sees the whole tile.
     const bool whole = end - start == KT && end - 1 <= L + t_lo &&
@@ -299,51 +451,40 @@ __global__ __launch_bounds__(kThreads, 2) void prefill_kernel(PagedPrefillParams
         for (int e = 0; e < 16; ++e) o[dt][e] *= alpha;
       }
     }
+    // O^T: part q takes kpl elements of every lane, slot j of which is row
+    // 8 (e / 4) + 4 half + e % 4 of S^T for e = q * kpl + j; the exponentials of a part
+    // lie between the products of the part before.
     const float ref = m_run == -INFINITY ? 0.f : m_run;
-    float x[C::blocks][16];
+    const auto weigh = [&](int q, int j) {
+      const int e = q * M::kpl + j;
+      const float w = fast_exp2(fmaf(s[e / 16][e % 16], scale, -ref));
+      l_run += w;
+      return w;
+    };
+    frag pf[2];
+    const auto put = [&](int q, int j) {
+      if constexpr (M::kpl == 1) pf[q & 1] = weigh(q, j);
+      else pf[q & 1][j] = static_cast<__bf16>(weigh(q, j));
+    };
 #pragma unroll
-    for (int kb = 0; kb < C::blocks; ++kb) {
+    for (int j = 0; j < M::kpl; ++j) put(0, j);
 #pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        x[kb][e] = fast_exp2(fmaf(s[kb][e], scale, -ref));
-        l_run += x[kb][e];
-      }
-    }
-
-    // Element slot j of step c is result element c * kpl + j: row 8 (e / 4) + 4 half + e % 4.
+    for (int q = 0; q < kParts; ++q) {
+      if (q + 1 < kParts) read_v(q + 1);
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-    for (int kb = 0; kb < C::blocks; ++kb) {
+      for (int dt = 0; dt < C::dtiles; ++dt) {
+        o[dt] = M::mma(vf[q & 1][dt], pf[q & 1], o[dt]);
+        if (q + 1 < kParts) {
 #pragma unroll
-      for (int c = 0; c < C::pv_steps; ++c) {
-        frag pf;
-        if constexpr (M::kpl == 1) {
-          pf = x[kb][c];
-        } else {
-#pragma unroll
-          for (int j = 0; j < 8; ++j) pf[j] = static_cast<__bf16>(x[kb][c * 8 + j]);
+          for (int j = dt * M::kpl / C::dtiles; j < (dt + 1) * M::kpl / C::dtiles; ++j) put(q + 1, j);
         }
-#pragma unroll
-        for (int dt = 0; dt < C::dtiles; ++dt) {
-          frag vf;
-          if constexpr (M::kpl == 1) {
-            vf = *reinterpret_cast<const float *>(vbuf + (kb * 32 + acc_row(c, half)) * C::v_pitch + (dt * 32 + col) * 4);
-          } else {
-            // two transposing reads of four rows each: lane i of 16 gets column i
-            const int row = kb * 32 + c * 16 + 4 * half + (col & 15) / 4;
-            const int at = (dt * 32 + (col & 16) + 4 * (col & 3)) * 2;
-            const i16x4_t a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4_t *)(vbuf + row * C::v_pitch + at));
-            const i16x4_t d = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4_t *)(vbuf + (row + 8) * C::v_pitch + at));
-            const short v[8] = {a[0], a[1], a[2], a[3], d[0], d[1], d[2], d[3]};
-#pragma unroll
-            for (int j = 0; j < 8; ++j) vf[j] = __builtin_bit_cast(__bf16, v[j]);
-          }
-          o[dt] = M::mma(vf, pf, o[dt]);
-        }
+        __builtin_amdgcn_sched_barrier(0);
       }
     }
     __syncthreads();
   }
-  if (pages.bad() && lane == 0) report(p.c.dev_err, kDevBadPage);
+  if (in.worst >= static_cast<unsigned>(p.c.n_pages)) report(p.c.dev_err, kDevBadPage);
 
   const float l_tot = l_run + shfl_xor(l_run, 32);
   if (p.splits > 1) {
@@ -362,32 +503,8 @@ __global__ __launch_bounds__(kThreads, 2) void prefill_kernel(PagedPrefillParams
     }
     return;
   }
-  // A wave's 32 rows through LDS, so that rows are written whole (the tiles' buffers are
-  // free after the last barrier).
-  const float inv = l_tot == 0.f ? 0.f : 1.f / l_tot;
-  unsigned char *rows = smem + wave * 32 * C::k_pitch;
-#pragma unroll
-  for (int dt = 0; dt < C::dtiles; ++dt) {
-#pragma unroll
-    for (int e = 0; e < 16; e += 4) {
-      T *at = reinterpret_cast<T *>(rows + col * C::k_pitch) + dt * 32 + acc_row(e, half);
-#pragma unroll
-      for (int j = 0; j < 4; ++j) at[j] = from_f32<T>(o[dt][e + j] * inv);
-    }
-  }
-  if (real && p.lse && half == 0) p.lse[qrow] = l_tot == 0.f ? -INFINITY : (m_run + log2f(l_tot)) * kLn2;
-  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-#pragma unroll
-  for (int k = 0; k < 32 / C::wave_rows; ++k) {
-    const int in = k * C::wave_rows + lane / C::lanes_per_row;
-    const int row = r0 + wave * 32 + in;
-    if (row >= n * G) break;
-    const int tok = row / G;
-    const size_t at = ((static_cast<size_t>(lc) * p.c.batch + b) * p.hq + h * G + (row - tok * G)) *
-                          static_cast<size_t>(p.tokens) + tok;
-    reinterpret_cast<u32x4v *>(p.out)[at * C::lanes_per_row + lane % C::lanes_per_row] =
-        *reinterpret_cast<const u32x4v *>(rows + in * C::k_pitch + (lane % C::lanes_per_row) * 16);
-  }
+  write_rows<T, D>(p, smem + wave * 32 * C::k_pitch, o, m_run, l_tot, (static_cast<size_t>(lc) * p.c.batch + b) * p.hq + h * G,
+                   r0 + wave * 32, n * G, lane);
 }
 
 // Joins the splits (workgroups [0, merges)) and puts the new rows into their pages
