@@ -25,10 +25,13 @@ namespace {
 typedef __attribute__((__vector_size__(16 * sizeof(float)))) float f32x16_t;
 typedef short i16x4_t __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) i16x4_t lds_i16x4_t;
+typedef __attribute__((address_space(3))) unsigned int lds_u32;
+typedef const __attribute__((address_space(1))) unsigned int global_u32;
 
 constexpr int kRows = kPrefillRows;          // query rows of a workgroup
 constexpr int kWaves = 4;
 constexpr int kThreads = kWaves * kWave;
+constexpr int kWaitLoads = 0x0f70;           // vmcnt(0)
 constexpr float kSlack = 8.f;                // log2 units that a maximum may grow before O follows
 
 // 32x32 fragments: lane l has 8 (bf16) or 1 (fp32) consecutive contraction elements of
@@ -70,12 +73,18 @@ struct Cfg {
   static constexpr int dtiles = D / 32;
   static constexpr int pv_steps = 16 / M::kpl;           // per block
   static constexpr int row_bytes = D * (int)sizeof(T);
-  static constexpr int k_pitch = row_bytes + 16;         // free of bank conflicts
-  static constexpr int v_pitch = row_bytes + 64;
-  static constexpr int stage = keys * (k_pitch + v_pitch);
+  static constexpr int stage = keys * row_bytes;         // of K or V, without padding
   static constexpr int lanes_per_row = row_bytes / 16;
   static constexpr int wave_rows = kWave / lanes_per_row;   // rows a wave's load takes
   static constexpr int insts = keys * row_bytes / (kThreads * 16);
+  static constexpr int chunks = lanes_per_row;           // 16-byte pieces of a row
+  // Rows lie in LDS as they are loaded, so their pieces are permuted instead, by what
+  // makes the rows that are read together fall on different banks.
+  __device__ __forceinline__ static int k_swap(int row) { return chunks >= 16 ? row & 15 : (row >> 1) & 7; }
+  __device__ __forceinline__ static int v_swap(int row) {
+    if (sizeof(T) == 4) return ((row >> 2) & 1) << 3;
+    return (chunks >= 16 ? row & 3 : (row >> 1) & 1) << 2;
+  }
 };
 
 // The row of a result element within its 32.
@@ -112,7 +121,7 @@ struct Seen {
   __device__ __forceinline__ int tile(int i) const { return i < sink_tiles ? i : i + skip; }
 };
 
-// Key tiles on their way to LDS: one in registers, and where the next ones lie.  Each
+// Key tiles on their way to LDS, which loads fill without registers between.  Each
 // lane holds the place of 16 rows of the list's tiles, so 64 / (KT / 16) tiles at a
 // time; the table's entries of the batch after are on their way meanwhile.
 template <typename T, int D>
@@ -121,7 +130,6 @@ struct Stager {
   static constexpr int KT = C::keys;
   static constexpr int kGroups = KT / 16;
   static constexpr int kBatch = kWave / kGroups;   // tiles
-  using Regs = u32x4v[C::insts];
   const unsigned char *k, *v, *knew, *vnew;
   const int32_t *table;
   const Seen<KT> &seen;
@@ -129,8 +137,7 @@ struct Stager {
   unsigned worst;                            // id, of rows that are cached
   uint64_t place;                            // of this lane's 16 rows: a byte offset
   int coming;                                // the entry for the same lane of the next batch
-  unsigned off[C::insts];                    // within 16 rows
-  Regs kreg, vreg;
+  unsigned koff[C::insts], voff[C::insts];   // within 16 rows
 
   // Tiles [.., end) of the list.
   __device__ __forceinline__ Stager(const PagedPrefillParams &p, size_t cunit, int unit, const Seen<KT> &seen_, int end_,
@@ -141,13 +148,16 @@ struct Stager {
         table(p.c.pages + cunit * static_cast<size_t>(p.c.max_pages)), seen(seen_), n_pages(p.c.n_pages),
         shift(p.c.page_shift), tokens(p.tokens), end(end_), wave(wave_), lane(lane_), worst(0) {
 #pragma unroll
-    for (int i = 0; i < C::insts; ++i) off[i] = offset(i);
+    for (int i = 0; i < C::insts; ++i) place_in(i, piece(i) % 16 + lane / C::lanes_per_row);
   }
 
   // A wave's i-th load of a tile takes wave_rows rows from this one on.
   __device__ __forceinline__ int piece(int i) const { return (i * kWaves + wave) * C::wave_rows; }
-  __device__ __forceinline__ unsigned offset(int i) const {
-    return (piece(i) % 16 + lane / C::lanes_per_row) * C::row_bytes + (lane % C::lanes_per_row) * 16;
+  // Lane offsets of the i-th load, from row `in` of the 16.
+  __device__ __forceinline__ void place_in(int i, int in) {
+    const int row = piece(i) + lane / C::lanes_per_row, c = lane % C::lanes_per_row;
+    koff[i] = in * C::row_bytes + (c ^ C::k_swap(row)) * 16;
+    voff[i] = in * C::row_bytes + (c ^ C::v_swap(row)) * 16;
   }
   __device__ __forceinline__ int tile(int i) const { return seen.tile(min(i, end - 1)); }
   // This lane's tile of the batch that starts at tile i, and its rows there.
@@ -181,17 +191,17 @@ struct Stager {
     const bool old = seen.tile(at_i) < seen.run.old_tiles;
     return Place{old ? k : knew, old ? v : vnew, (at_i & (kBatch - 1)) * kGroups};
   }
-  __device__ __forceinline__ void load(const Place &w, int j, Regs &kr, Regs &vr) const {
+  __device__ __forceinline__ void load(const Place &w, int j, unsigned char *kbuf, unsigned char *vbuf) const {
     const int from = w.lane0 + piece(j) / 16;
     const uint64_t at = static_cast<uint64_t>(static_cast<unsigned>(__builtin_amdgcn_readlane(static_cast<int>(place >> 32), from))) << 32 |
                         static_cast<unsigned>(__builtin_amdgcn_readlane(static_cast<int>(place), from));
-    kr[j] = *reinterpret_cast<const u32x4v *>(w.k + at + off[j]);
-    vr[j] = *reinterpret_cast<const u32x4v *>(w.v + at + off[j]);
+    __builtin_amdgcn_global_load_lds((global_u32 *)(w.k + at + koff[j]), (lds_u32 *)(kbuf + piece(j) * C::row_bytes), 16, 0, 0);
+    __builtin_amdgcn_global_load_lds((global_u32 *)(w.v + at + voff[j]), (lds_u32 *)(vbuf + piece(j) * C::row_bytes), 16, 0, 0);
   }
-  __device__ __forceinline__ void load(int i, Regs &kr, Regs &vr) const {
+  __device__ __forceinline__ void load(int i, unsigned char *kbuf, unsigned char *vbuf) const {
     const Place w = find(i);
 #pragma unroll
-    for (int j = 0; j < C::insts; ++j) load(w, j, kr, vr);
+    for (int j = 0; j < C::insts; ++j) load(w, j, kbuf, vbuf);
   }
   // Ahead of load(i): what seldom happens there, the places of a new batch ...
   __device__ __forceinline__ void turn(int i) {
@@ -206,46 +216,58 @@ struct Stager {
 #pragma unroll
     for (int j = 0; j < C::insts; ++j) {
       const int base = min((row0 + piece(j)) & ~15, (tokens - 1) & ~15);
-      const int in = min(piece(j) % 16 + lane / C::lanes_per_row, tokens - 1 - base);
-      off[j] = in * C::row_bytes + (lane % C::lanes_per_row) * 16;
+      place_in(j, min(piece(j) % 16 + lane / C::lanes_per_row, tokens - 1 - base));
     }
   }
   // Rows of V that no token of the block sees count for nothing, whatever they hold.
-  __device__ __forceinline__ void clean(int i, Regs &vr) const {
+  __device__ __forceinline__ bool mixed(int i) const {
     const int t = tile(i);
     const int from = seen.run.start(t), to = seen.run.end(t);
-    if (to - from == KT && (from >= seen.lo || to <= seen.s_end)) return;
+    return to - from < KT || (from < seen.lo && to > seen.s_end);
+  }
+  __device__ __forceinline__ void clean(int i, unsigned char *vbuf) const {
+    const int t = tile(i);
+    const int from = seen.run.start(t), to = seen.run.end(t);
 #pragma unroll
     for (int j = 0; j < C::insts; ++j) {
       const int row = from + piece(j) + lane / C::lanes_per_row;
-      const unsigned keep = row < to && (row >= seen.lo || row < seen.s_end) ? ~0u : 0u;
-      vr[j] &= keep;
+      if (!(row < to && (row >= seen.lo || row < seen.s_end)))
+        *reinterpret_cast<u32x4v *>(vbuf + piece(j) * C::row_bytes + lane * 16) = u32x4v{0, 0, 0, 0};
     }
-  }
-  __device__ __forceinline__ void store(unsigned char *buf, int j, const Regs &kr, const Regs &vr) const {
-    const int row = j * kWaves * C::wave_rows + wave * C::wave_rows + lane / C::lanes_per_row, sub = (lane % C::lanes_per_row) * 16;
-    *reinterpret_cast<u32x4v *>(buf + row * C::k_pitch + sub) = kr[j];
-    *reinterpret_cast<u32x4v *>(buf + KT * C::k_pitch + row * C::v_pitch + sub) = vr[j];
-  }
-  __device__ __forceinline__ void store(unsigned char *buf, const Regs &kr, const Regs &vr) const {
-#pragma unroll
-    for (int j = 0; j < C::insts; ++j) store(buf, j, kr, vr);
   }
 };
 
-// V^T operand of 16 keys from `row` on, columns [32 dt, 32 dt + 32): two transposing
-// reads of four rows each, in which lane i of 16 gets column i.
-template <int D>
-__device__ __forceinline__ bf16x8_t v_frag32(const unsigned char *vbuf, int row, int dt, int lane) {
-  using C = Cfg<bf16_t, D>;
-  const unsigned char *at = vbuf + (row + 4 * (lane >> 5) + (lane & 15) / 4) * C::v_pitch + (dt * 32 + (lane & 16) + 4 * (lane & 3)) * 2;
-  const i16x4_t a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4_t *)at);
-  const i16x4_t b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4_t *)(at + 8 * C::v_pitch));
-  const short v[8] = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
-  bf16x8_t f;
+// Where a lane reads operands of K rows [0, 32): step c is at this ^ (c kpl sizeof(T)).
+template <typename T, int D>
+__device__ __forceinline__ int k_base(int lane) {
+  using C = Cfg<T, D>;
+  const int col = lane & 31, half = lane >> 5;
+  return col * C::row_bytes + ((half * (C::chunks / 2)) ^ C::k_swap(col)) * 16;
+}
+// And of V rows [0, 16): columns [32 dt, 32 dt + 32) are at this ^ (32 dt sizeof(T)).
+// bf16 takes them by two transposing reads of four rows each, in which lane i of 16
+// gets column i.
+template <typename T, int D>
+__device__ __forceinline__ int v_base(int lane) {
+  using C = Cfg<T, D>;
+  const int half = lane >> 5;
+  if (sizeof(T) == 4) return 4 * half * C::row_bytes + ((((lane & 31) / 4) ^ C::v_swap(4 * half)) * 16) + (lane & 3) * 4;
+  const int row = 4 * half + (lane & 15) / 4, c = (lane & 16) / 8 + (lane & 3) / 2;
+  return row * C::row_bytes + ((c ^ C::v_swap(row)) * 16) + (lane & 1) * 8;
+}
+template <typename T, int D>
+__device__ __forceinline__ typename Mma32<T>::frag v_frag32(const unsigned char *at) {
+  if constexpr (sizeof(T) == 4) {
+    return *reinterpret_cast<const float *>(at);
+  } else {
+    const i16x4_t a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4_t *)at);
+    const i16x4_t b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4_t *)(at + 8 * Cfg<T, D>::row_bytes));
+    const short v[8] = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+    bf16x8_t f;
 #pragma unroll
-  for (int j = 0; j < 8; ++j) f[j] = __builtin_bit_cast(__bf16, v[j]);
-  return f;
+    for (int j = 0; j < 8; ++j) f[j] = __builtin_bit_cast(__bf16, v[j]);
+    return f;
+  }
 }
 
 // A wave's 32 rows from row0 on, of `rows`, divided by their sums and written whole
@@ -265,7 +287,8 @@ __device__ __forceinline__ void write_rows(const PagedPrefillParams &p, unsigned
   for (int dt = 0; dt < C::dtiles; ++dt) {
 #pragma unroll
     for (int e = 0; e < 16; e += 4) {
-      T *at = reinterpret_cast<T *>(stage + col * C::k_pitch) + dt * 32 + acc_row(e, half);
+      const int byte = (dt * 32 + acc_row(e, half)) * static_cast<int>(sizeof(T));
+      T *at = reinterpret_cast<T *>(stage + col * C::row_bytes + (byte ^ ((col & 7) * 16)));
 #pragma unroll
       for (int j = 0; j < 4; ++j) at[j] = from_f32<T>(o[dt][e + j] * inv);
     }
@@ -277,7 +300,7 @@ __device__ __forceinline__ void write_rows(const PagedPrefillParams &p, unsigned
     const int in = k * C::wave_rows + lane / C::lanes_per_row;
     if (row0 + in >= rows) break;
     reinterpret_cast<u32x4v *>(p.out)[place(row0 + in) * C::lanes_per_row + lane % C::lanes_per_row] =
-        *reinterpret_cast<const u32x4v *>(stage + in * C::k_pitch + (lane % C::lanes_per_row) * 16);
+        *reinterpret_cast<const u32x4v *>(stage + in * C::row_bytes + ((lane % C::lanes_per_row) ^ (in & 7)) * 16);
   }
   asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
 }
@@ -288,7 +311,8 @@ __global__ __launch_bounds__(kThreads, 2) void prefill_kernel(PagedPrefillParams
   using M = Mma32<T>;
   using frag = typename M::frag;
   constexpr int KT = C::keys;
-  __shared__ __attribute__((aligned(16))) unsigned char smem[2 * C::stage];
+  // arrays of their own, so that reads of one need not wait for loads into another
+  __shared__ __attribute__((aligned(1024))) unsigned char k0[C::stage], v0[C::stage], k1[C::stage], v1[C::stage];
 
   const int lane = threadIdx.x & (kWave - 1);
   const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) / kWave);
@@ -350,30 +374,23 @@ __global__ __launch_bounds__(kThreads, 2) void prefill_kernel(PagedPrefillParams
     for (int i = 0; i < 16; ++i) o[dt][i] = 0.f;
   }
 
-  if (i0 < i1) {
-    typename Stager<T, D>::Regs kfirst, vfirst;           // the first two tiles come together
-    in.ask(i0 & -Stager<T, D>::kBatch);
-    in.batch(i0 & -Stager<T, D>::kBatch);
-    in.trim(i0);
-    in.load(i0, kfirst, vfirst);
-    in.turn(i0 + 1);
-    in.trim(i0 + 1);
-    in.load(i0 + 1, in.kreg, in.vreg);
-    in.clean(i0, vfirst);
-    in.store(smem, kfirst, vfirst);
-  }
-  __syncthreads();
-  for (int i = i0; i < i1; ++i) {
-    const unsigned char *kbuf = smem + ((i - i0) & 1) * C::stage;
-    const unsigned char *vbuf = kbuf + KT * C::k_pitch;
+  const int kat = k_base<T, D>(lane), vat = v_base<T, D>(lane);
+
+  // Tile i, in kbuf and vbuf once its loads are done; tile i + 1 goes to kto and vto.
+  const auto step = [&](int i, unsigned char *kbuf, unsigned char *vbuf, unsigned char *kto, unsigned char *vto) {
+    in.turn(i + 1);
+    in.trim(i + 1);
+    __builtin_amdgcn_s_waitcnt(kWaitLoads);
+    __syncthreads();                                      // tile i is there, and no one reads tile i - 1
+    if (in.mixed(i)) {
+      in.clean(i, vbuf);
+      __syncthreads();
+    }
     const int tile = seen.tile(i);
     const int start = run.start(tile), end = run.end(tile);
 
-    in.clean(i + 1, in.vreg);
-    in.turn(i + 2);
-    in.trim(i + 2);
-    // S^T, with operands read ahead of their products, and between the products the next
-    // tile's rows to LDS and the one after it asked for, piece by piece.
+    // S^T, with operands read ahead of their products, and between the products the
+    // next tile asked for, piece by piece.
     f32x16_t s[C::blocks];
 #pragma unroll
     for (int kb = 0; kb < C::blocks; ++kb) {
@@ -381,15 +398,13 @@ __global__ __launch_bounds__(kThreads, 2) void prefill_kernel(PagedPrefillParams
       for (int e = 0; e < 16; ++e) s[kb][e] = 0.f;
     }
     constexpr int kSteps = C::blocks * C::qk_steps, kAhead = M::kpl == 8 ? 8 : 16, kEach = kSteps / C::insts;
-    unsigned char *to = smem + ((i + 1 - i0) & 1) * C::stage;
-    const typename Stager<T, D>::Place from = in.find(i + 2);
+    const typename Stager<T, D>::Place from = in.find(i + 1);
     frag kf[2][kAhead];
     const auto read_k = [&](int q) {
 #pragma unroll
       for (int c = 0; c < kAhead; ++c) {
-        const int z = q * kAhead + c;
-        kf[q & 1][c] = load_frag(reinterpret_cast<const T *>(kbuf + (z / C::qk_steps * 32 + col) * C::k_pitch) + half * (D / 2) +
-                                 z % C::qk_steps * M::kpl);
+        const int z = q * kAhead + c, b = z % C::qk_steps * M::kpl * (int)sizeof(T);
+        kf[q & 1][c] = load_frag(reinterpret_cast<const T *>(kbuf + (kat ^ (b & ~15)) + (b & 15) + z / C::qk_steps * 32 * C::row_bytes));
       }
     };
     read_k(0);
@@ -398,22 +413,16 @@ __global__ __launch_bounds__(kThreads, 2) void prefill_kernel(PagedPrefillParams
       if (z % kAhead == 0 && z + kAhead < kSteps) read_k(z / kAhead + 1);
       if (z % kAhead == 0) __builtin_amdgcn_sched_barrier(0);
       s[z / C::qk_steps] = M::mma(kf[z / kAhead & 1][z % kAhead], qf[z % C::qk_steps], s[z / C::qk_steps]);
-      if (z % kEach == 0) {
-        in.store(to, z / kEach, in.kreg, in.vreg);
-        in.load(from, z / kEach, in.kreg, in.vreg);
-      }
+      if (z % kEach == 0) in.load(from, z / kEach, kto, vto);
       __builtin_amdgcn_sched_barrier(0);
     }
     constexpr int kParts = C::blocks * C::pv_steps;
     frag vf[2][C::dtiles];
     const auto read_v = [&](int q) {
+      const int row = M::kpl == 8 ? 16 * q : 8 * (q / 4) + q % 4;
 #pragma unroll
-      for (int dt = 0; dt < C::dtiles; ++dt) {
-        if constexpr (M::kpl == 1)
-          vf[q & 1][dt] = *reinterpret_cast<const float *>(vbuf + acc_row(q, half) * C::v_pitch + (dt * 32 + col) * 4);
-        else
-          vf[q & 1][dt] = v_frag32<D>(vbuf, q * 16, dt, lane);
-      }
+      for (int dt = 0; dt < C::dtiles; ++dt)
+        vf[q & 1][dt] = v_frag32<T, D>(vbuf + (vat ^ (dt * 32 * (int)sizeof(T))) + row * C::row_bytes);
     };
     read_v(0);
 
@@ -482,8 +491,19 @@ __global__ __launch_bounds__(kThreads, 2) void prefill_kernel(PagedPrefillParams
         __builtin_amdgcn_sched_barrier(0);
       }
     }
-    __syncthreads();
+  };
+  if (i0 < i1) {
+    in.ask(i0 & -Stager<T, D>::kBatch);
+    in.batch(i0 & -Stager<T, D>::kBatch);
+    in.trim(i0);
+    in.load(i0, k0, v0);
+    for (int i = i0; i < i1; i += 2) {
+      step(i, k0, v0, k1, v1);
+      if (i + 1 < i1) step(i + 1, k1, v1, k0, v0);
+    }
   }
+  __builtin_amdgcn_s_waitcnt(kWaitLoads);
+  __syncthreads();
   if (in.worst >= static_cast<unsigned>(p.c.n_pages)) report(p.c.dev_err, kDevBadPage);
 
   const float l_tot = l_run + shfl_xor(l_run, 32);
@@ -503,7 +523,7 @@ __global__ __launch_bounds__(kThreads, 2) void prefill_kernel(PagedPrefillParams
     }
     return;
   }
-  write_rows<T, D>(p, smem + wave * 32 * C::k_pitch, o, m_run, l_tot, (static_cast<size_t>(lc) * p.c.batch + b) * p.hq + h * G,
+  write_rows<T, D>(p, wave < 2 ? (wave == 0 ? k0 : v0) : (wave == 2 ? k1 : v1), o, m_run, l_tot, (static_cast<size_t>(lc) * p.c.batch + b) * p.hq + h * G,
                    r0 + wave * 32, n * G, lane);
 }
 
