@@ -160,9 +160,10 @@ reco_status_t reco_paged_prefill_attn(const reco_paged_cache_t *cache, int32_t l
   p.group = G;
   p.hq = n_q_heads;
   p.tokens = n_tokens;
-  p.wide = reco::prefill_wide(units, n_tokens, G, cache->dtype, cus);
-  p.blocks = reco::prefill_blocks(n_tokens, G, p.wide ? reco::kPrefillWideRows : reco::kPrefillRows);
-  p.splits = p.wide ? 1 : reco::prefill_splits(units, p.blocks, p.c.cap, sinks, window, tile_rows, cus);
+  p.rows = reco::prefill_rows(units, n_tokens, G, cache->dtype, cus);
+  p.blocks = reco::prefill_blocks(n_tokens, G, p.rows);
+  p.splits = p.rows == reco::kPrefillRows
+                 ? reco::prefill_splits(units, p.blocks, p.c.cap, sinks, window, tile_rows, cus) : 1;
   p.sinks = sinks;
   p.window = window;
   p.scale_log2 = scale * 1.4426950408889634f;

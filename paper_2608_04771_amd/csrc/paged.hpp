@@ -52,7 +52,7 @@ hipError_t launch_paged_decode(const PagedDecodeParams &p, int dtype, int head_d
 
 // ---- attention of a run of new tokens -------------------------------------------
 constexpr int kPrefillRows = 128;        // query rows of a workgroup
-constexpr int kPrefillWideRows = 256;    // of one that takes a long bf16 run
+constexpr int kPrefillLongRows = 256;    // of one for long bf16 runs
 constexpr int kPrefillMaxSplits = 64;
 struct PagedPrefillParams {
   PagedCache c;
@@ -66,12 +66,12 @@ struct PagedPrefillParams {
   float *part_o;          // [units][blocks][splits][kPrefillRows][D]
   float *part_ml;         // [units][blocks][splits][2][kPrefillRows]
   int group, hq, tokens, blocks, splits;
-  bool wide;              // blocks of kPrefillWideRows, one split
+  int rows;               // of a block: kPrefillRows, or kPrefillLongRows with one split
   int sinks, window;
   float scale_log2;
 };
 int prefill_blocks(int tokens, int group, int rows);
-bool prefill_wide(int units, int tokens, int group, int dtype, int compute_units);
+int prefill_rows(int units, int tokens, int group, int dtype, int compute_units);
 constexpr int prefill_tile_rows(int dtype) { return dtype == 0 ? 32 : 64; }   // keys of a tile: fp32, bf16
 int prefill_splits(int units, int blocks, int capacity, int sinks, int window, int tile_rows, int compute_units);
 size_t prefill_workspace_bytes(int units, int tokens, int capacity, int group, int head_dim, int tile_rows,

@@ -64,9 +64,10 @@ int prefill_blocks(int tokens, int group, int rows) {
   return static_cast<int>((static_cast<int64_t>(tokens) * group + rows - 1) / rows);
 }
 
-// Blocks of 256 rows where they give every compute unit two workgroups in turn.
-bool prefill_wide(int units, int tokens, int group, int dtype, int compute_units) {
-  return false && dtype == 1 && static_cast<int64_t>(units) * prefill_blocks(tokens, group, kPrefillWideRows) >= 2 * compute_units;
+// Blocks of 256 rows for bf16 where they give every compute unit two workgroups in turn.
+int prefill_rows(int units, int tokens, int group, int dtype, int compute_units) {
+  const int64_t blocks = static_cast<int64_t>(units) * prefill_blocks(tokens, group, kPrefillLongRows);
+  return dtype == 1 && blocks >= 2 * compute_units ? kPrefillLongRows : kPrefillRows;
 }
 
 // Key tiles are split where there are too few blocks of query rows for two workgroups

@@ -30,7 +30,6 @@ typedef const __attribute__((address_space(1))) unsigned int global_u32;
 
 constexpr int kRows = kPrefillRows;          // query rows of a workgroup
 constexpr int kWaves = 4;
-constexpr int kThreads = kWaves * kWave;
 constexpr int kWaitLoads = 0x0f70;           // vmcnt(0)
 constexpr float kSlack = 8.f;                // log2 units that a maximum may grow before O follows
 
@@ -64,7 +63,7 @@ struct Mma32<float> {
   __device__ __forceinline__ static frag negated(frag a) { return -a; }
 };
 
-template <typename T, int D>
+template <typename T, int D, int NW = kWaves>
 struct Cfg {
   using M = Mma32<T>;
   static constexpr int keys = M::keys;
@@ -76,7 +75,7 @@ struct Cfg {
   static constexpr int stage = keys * row_bytes;         // of K or V, without padding
   static constexpr int lanes_per_row = row_bytes / 16;
   static constexpr int wave_rows = kWave / lanes_per_row;   // rows a wave's load takes
-  static constexpr int insts = keys * row_bytes / (kThreads * 16);
+  static constexpr int insts = keys * row_bytes / (NW * kWave * 16);
   static constexpr int chunks = lanes_per_row;           // 16-byte pieces of a row
   // Rows lie in LDS as they are loaded, so their pieces are permuted instead, by what
   // makes the rows that are read together fall on different banks.
@@ -89,6 +88,16 @@ struct Cfg {
 
 // The row of a result element within its 32.
 __device__ __forceinline__ int acc_row(int i, int half) { return 8 * (i / 4) + 4 * half + (i & 3); }
+
+// Which of the rows at and behind `base` the token at row pos does not see.  The bounds
+// are taken relative to base once, so that rows compare as constants.
+struct Hidden {
+  int end, low, sinks;
+
+  __device__ __forceinline__ Hidden(int base, int end_, int pos, int sinks_, int window)
+      : end(min(end_, pos + 1) - base), low(window > 0 ? pos - window - base : -1 - base), sinks(sinks_ - base) {}
+  __device__ __forceinline__ bool at(int c) const { return c >= end || (c <= low && c >= sinks); }
+};
 
 // What one unit's call sees: cached rows in tiles of KT from row 0, new rows in tiles
 // of KT from row L.
@@ -124,9 +133,9 @@ struct Seen {
 // Key tiles on their way to LDS, which loads fill without registers between.  Each
 // lane holds the place of 16 rows of the list's tiles, so 64 / (KT / 16) tiles at a
 // time; the table's entries of the batch after are on their way meanwhile.
-template <typename T, int D>
+template <typename T, int D, int NW = kWaves>
 struct Stager {
-  using C = Cfg<T, D>;
+  using C = Cfg<T, D, NW>;
   static constexpr int KT = C::keys;
   static constexpr int kGroups = KT / 16;
   static constexpr int kBatch = kWave / kGroups;   // tiles
@@ -148,16 +157,16 @@ struct Stager {
         table(p.c.pages + cunit * static_cast<size_t>(p.c.max_pages)), seen(seen_), n_pages(p.c.n_pages),
         shift(p.c.page_shift), tokens(p.tokens), end(end_), wave(wave_), lane(lane_), worst(0) {
 #pragma unroll
-    for (int i = 0; i < C::insts; ++i) place_in(i, piece(i) % 16 + lane / C::lanes_per_row);
+    for (int i = 0; i < C::insts; ++i) place_in(i, piece(i) % 16 + lane / C::lanes_per_row, true, true);
   }
 
   // A wave's i-th load of a tile takes wave_rows rows from this one on.
-  __device__ __forceinline__ int piece(int i) const { return (i * kWaves + wave) * C::wave_rows; }
+  __device__ __forceinline__ int piece(int i) const { return (i * NW + wave) * C::wave_rows; }
   // Lane offsets of the i-th load, from row `in` of the 16.
-  __device__ __forceinline__ void place_in(int i, int in) {
+  __device__ __forceinline__ void place_in(int i, int in, bool k, bool v) {
     const int row = piece(i) + lane / C::lanes_per_row, c = lane % C::lanes_per_row;
-    koff[i] = in * C::row_bytes + (c ^ C::k_swap(row)) * 16;
-    voff[i] = in * C::row_bytes + (c ^ C::v_swap(row)) * 16;
+    if (k) koff[i] = in * C::row_bytes + (c ^ C::k_swap(row)) * 16;
+    if (v) voff[i] = in * C::row_bytes + (c ^ C::v_swap(row)) * 16;
   }
   __device__ __forceinline__ int tile(int i) const { return seen.tile(min(i, end - 1)); }
   // This lane's tile of the batch that starts at tile i, and its rows there.
@@ -184,24 +193,25 @@ struct Stager {
   // A tile's rows.  Those past its end are other rows of the pool or of the run.
   struct Place {
     const unsigned char *k, *v;
-    int lane0;
+    uint64_t at[C::insts];
   };
   __device__ __forceinline__ Place find(int i) const {
     const int at_i = min(i, end - 1);
     const bool old = seen.tile(at_i) < seen.run.old_tiles;
-    return Place{old ? k : knew, old ? v : vnew, (at_i & (kBatch - 1)) * kGroups};
-  }
-  __device__ __forceinline__ void load(const Place &w, int j, unsigned char *kbuf, unsigned char *vbuf) const {
-    const int from = w.lane0 + piece(j) / 16;
-    const uint64_t at = static_cast<uint64_t>(static_cast<unsigned>(__builtin_amdgcn_readlane(static_cast<int>(place >> 32), from))) << 32 |
-                        static_cast<unsigned>(__builtin_amdgcn_readlane(static_cast<int>(place), from));
-    __builtin_amdgcn_global_load_lds((global_u32 *)(w.k + at + koff[j]), (lds_u32 *)(kbuf + piece(j) * C::row_bytes), 16, 0, 0);
-    __builtin_amdgcn_global_load_lds((global_u32 *)(w.v + at + voff[j]), (lds_u32 *)(vbuf + piece(j) * C::row_bytes), 16, 0, 0);
-  }
-  __device__ __forceinline__ void load(int i, unsigned char *kbuf, unsigned char *vbuf) const {
-    const Place w = find(i);
+    Place w{old ? k : knew, old ? v : vnew, {}};
 #pragma unroll
-    for (int j = 0; j < C::insts; ++j) load(w, j, kbuf, vbuf);
+    for (int j = 0; j < C::insts; ++j) {
+      const int from = (at_i & (kBatch - 1)) * kGroups + piece(j) / 16;
+      w.at[j] = static_cast<uint64_t>(static_cast<unsigned>(__builtin_amdgcn_readlane(static_cast<int>(place >> 32), from))) << 32 |
+                static_cast<unsigned>(__builtin_amdgcn_readlane(static_cast<int>(place), from));
+    }
+    return w;
+  }
+  __device__ __forceinline__ void load_k(const Place &w, int j, unsigned char *buf) const {
+    __builtin_amdgcn_global_load_lds((global_u32 *)(w.k + w.at[j] + koff[j]), (lds_u32 *)(buf + piece(j) * C::row_bytes), 16, 0, 0);
+  }
+  __device__ __forceinline__ void load_v(const Place &w, int j, unsigned char *buf) const {
+    __builtin_amdgcn_global_load_lds((global_u32 *)(w.v + w.at[j] + voff[j]), (lds_u32 *)(buf + piece(j) * C::row_bytes), 16, 0, 0);
   }
   // Ahead of load(i): what seldom happens there, the places of a new batch ...
   __device__ __forceinline__ void turn(int i) {
@@ -209,14 +219,14 @@ struct Stager {
   }
   // ... and the offsets of a run's last tile, whose rows past the last place must not be
   // read (no tile of the list comes after it).
-  __device__ __forceinline__ void trim(int i) {
+  __device__ __forceinline__ void trim(int i, bool k = true, bool v = true) {
     const int t = tile(i);
     const int row0 = (t - seen.run.old_tiles) * KT;
     if (t < seen.run.old_tiles || row0 + KT <= tokens) return;
 #pragma unroll
     for (int j = 0; j < C::insts; ++j) {
       const int base = min((row0 + piece(j)) & ~15, (tokens - 1) & ~15);
-      place_in(j, min(piece(j) % 16 + lane / C::lanes_per_row, tokens - 1 - base));
+      place_in(j, min(piece(j) % 16 + lane / C::lanes_per_row, tokens - 1 - base), k, v);
     }
   }
   // Rows of V that no token of the block sees count for nothing, whatever they hold.
@@ -305,9 +315,11 @@ __device__ __forceinline__ void write_rows(const PagedPrefillParams &p, unsigned
   asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
 }
 
-template <typename T, int D>
-__global__ __launch_bounds__(kThreads, 2) void prefill_kernel(PagedPrefillParams p) {
-  using C = Cfg<T, D>;
+template <typename T, int D, int NW>
+__global__ __launch_bounds__(NW * kWave, 2) void prefill_kernel(PagedPrefillParams p) {
+  using C = Cfg<T, D, NW>;
+  using In = Stager<T, D, NW>;
+  constexpr int kRows = 32 * NW;
   using M = Mma32<T>;
   using frag = typename M::frag;
   constexpr int KT = C::keys;
@@ -350,7 +362,6 @@ __global__ __launch_bounds__(kThreads, 2) void prefill_kernel(PagedPrefillParams
   const int r = r0 + wave * 32 + col;
   const int t = min(r, p.tokens * G - 1) / G;
   const int pos = L + t;
-  const int low = p.window > 0 ? pos - p.window : -1;     // sees rows above it, and the sinks
   const size_t qrow = ((static_cast<size_t>(lc) * p.c.batch + b) * p.hq + h * G + (min(r, p.tokens * G - 1) - t * G)) *
                           static_cast<size_t>(p.tokens) + t;
   frag qf[C::qk_steps];
@@ -364,7 +375,7 @@ __global__ __launch_bounds__(kThreads, 2) void prefill_kernel(PagedPrefillParams
   }
   const float scale = fmaxf(fabsf(p.scale_log2), 0x1p-126f);   // times a hidden row's -inf, 0 would be NaN
 
-  Stager<T, D> in(p, cunit, unit, seen, i1, wave, lane);
+  In in(p, cunit, unit, seen, i1, wave, lane);
 
   float m_run = -INFINITY, l_run = 0.f;                  // m in units of the scaled logits
   f32x16_t o[C::dtiles];
@@ -381,11 +392,8 @@ __global__ __launch_bounds__(kThreads, 2) void prefill_kernel(PagedPrefillParams
     in.turn(i + 1);
     in.trim(i + 1);
     __builtin_amdgcn_s_waitcnt(kWaitLoads);
+    if (in.mixed(i)) in.clean(i, vbuf);                   // each wave what it loaded
     __syncthreads();                                      // tile i is there, and no one reads tile i - 1
-    if (in.mixed(i)) {
-      in.clean(i, vbuf);
-      __syncthreads();
-    }
     const int tile = seen.tile(i);
     const int start = run.start(tile), end = run.end(tile);
 
@@ -398,7 +406,7 @@ __global__ __launch_bounds__(kThreads, 2) void prefill_kernel(PagedPrefillParams
       for (int e = 0; e < 16; ++e) s[kb][e] = 0.f;
     }
     constexpr int kSteps = C::blocks * C::qk_steps, kAhead = M::kpl == 8 ? 8 : 16, kEach = kSteps / C::insts;
-    const typename Stager<T, D>::Place from = in.find(i + 1);
+    const typename In::Place from = in.find(i + 1);
     frag kf[2][kAhead];
     const auto read_k = [&](int q) {
 #pragma unroll
@@ -413,7 +421,10 @@ __global__ __launch_bounds__(kThreads, 2) void prefill_kernel(PagedPrefillParams
       if (z % kAhead == 0 && z + kAhead < kSteps) read_k(z / kAhead + 1);
       if (z % kAhead == 0) __builtin_amdgcn_sched_barrier(0);
       s[z / C::qk_steps] = M::mma(kf[z / kAhead & 1][z % kAhead], qf[z % C::qk_steps], s[z / C::qk_steps]);
-      if (z % kEach == 0) in.load(from, z / kEach, kto, vto);
+      if (z % kEach == 0) {
+        in.load_k(from, z / kEach, kto);
+        in.load_v(from, z / kEach, vto);
+      }
       __builtin_amdgcn_sched_barrier(0);
     }
     constexpr int kParts = C::blocks * C::pv_steps;
@@ -430,13 +441,11 @@ __global__ __launch_bounds__(kThreads, 2) void prefill_kernel(PagedPrefillParams
     const bool whole = end - start == KT && end - 1 <= L + t_lo &&
                        (p.window == 0 || start > L + t_hi - p.window || end <= p.sinks);
     if (!whole) {
+      const Hidden hidden(start + 4 * half, end, pos, p.sinks, p.window);
 #pragma unroll
       for (int kb = 0; kb < C::blocks; ++kb) {
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          const int j = start + kb * 32 + acc_row(e, half);
-          s[kb][e] = j < end && j <= pos && (j > low || j < p.sinks) ? s[kb][e] : -INFINITY;
-        }
+        for (int e = 0; e < 16; ++e) s[kb][e] = hidden.at(kb * 32 + acc_row(e, 0)) ? -INFINITY : s[kb][e];
       }
     }
     float top = -INFINITY;
@@ -493,10 +502,15 @@ __global__ __launch_bounds__(kThreads, 2) void prefill_kernel(PagedPrefillParams
     }
   };
   if (i0 < i1) {
-    in.ask(i0 & -Stager<T, D>::kBatch);
-    in.batch(i0 & -Stager<T, D>::kBatch);
+    in.ask(i0 & -In::kBatch);
+    in.batch(i0 & -In::kBatch);
     in.trim(i0);
-    in.load(i0, k0, v0);
+    const typename In::Place from = in.find(i0);
+#pragma unroll
+    for (int j = 0; j < C::insts; ++j) {
+      in.load_k(from, j, k0);
+      in.load_v(from, j, v0);
+    }
     for (int i = i0; i < i1; i += 2) {
       step(i, k0, v0, k1, v1);
       if (i + 1 < i1) step(i + 1, k1, v1, k0, v0);
@@ -523,7 +537,8 @@ __global__ __launch_bounds__(kThreads, 2) void prefill_kernel(PagedPrefillParams
     }
     return;
   }
-  write_rows<T, D>(p, wave < 2 ? (wave == 0 ? k0 : v0) : (wave == 2 ? k1 : v1), o, m_run, l_tot, (static_cast<size_t>(lc) * p.c.batch + b) * p.hq + h * G,
+  unsigned char *mine = wave < NW / 2 ? (wave < NW / 4 ? k0 : v0) : (wave < 3 * NW / 4 ? k1 : v1);
+  write_rows<T, D>(p, mine + wave % (NW / 4) * 32 * C::row_bytes, o, m_run, l_tot, (static_cast<size_t>(lc) * p.c.batch + b) * p.hq + h * G,
                    r0 + wave * 32, n * G, lane);
 }
 
@@ -647,7 +662,12 @@ __global__ __launch_bounds__(256) void prefill_finish_kernel(PagedPrefillParams 
 template <typename T, int D>
 hipError_t launch_typed(const PagedPrefillParams &p, hipStream_t s) {
   const int units = p.c.n_layers * p.c.batch * p.c.hkv;
-  hipLaunchKernelGGL((prefill_kernel<T, D>), dim3(p.blocks * p.splits, units), dim3(kThreads), 0, s, p);
+  if constexpr (sizeof(T) == 2) {
+    if (p.rows == kPrefillLongRows)
+      hipLaunchKernelGGL((prefill_kernel<T, D, 8>), dim3(p.blocks, units), dim3(8 * kWave), 0, s, p);
+  }
+  if (p.rows == kRows)
+    hipLaunchKernelGGL((prefill_kernel<T, D, 4>), dim3(p.blocks * p.splits, units), dim3(4 * kWave), 0, s, p);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   const int merges = p.splits > 1 ? units * p.blocks * (kRows / kMergeRows) * (D / 32) : 0;
