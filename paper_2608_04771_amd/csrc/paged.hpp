@@ -67,6 +67,7 @@ struct PagedPrefillParams {
   float *part_ml;         // [units][blocks][splits][2][kPrefillRows]
   int group, hq, tokens, blocks, splits;
   int rows;               // of a block: kPrefillRows, or kPrefillLongRows with one split
+  int near;               // neighbouring workgroups that share an XCD
   int sinks, window;
   float scale_log2;
 };
@@ -76,6 +77,7 @@ constexpr int prefill_tile_rows(int dtype) { return dtype == 0 ? 32 : 64; }   //
 int prefill_splits(int units, int blocks, int capacity, int sinks, int window, int tile_rows, int compute_units);
 size_t prefill_workspace_bytes(int units, int tokens, int capacity, int group, int head_dim, int tile_rows,
                                int compute_units);
+int prefill_near(int workgroups);
 bool prefill_fits_grid(const PagedPrefillParams &p);
 void prefill_place(PagedPrefillParams &p, int head_dim, void *ws);
 hipError_t launch_paged_prefill(const PagedPrefillParams &p, int dtype, int head_dim, hipStream_t s);

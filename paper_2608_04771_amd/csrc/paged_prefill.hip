@@ -30,6 +30,7 @@ typedef const __attribute__((address_space(1))) unsigned int global_u32;
 
 constexpr int kRows = kPrefillRows;          // query rows of a workgroup
 constexpr int kWaves = 4;
+constexpr int kXcds = 8;
 constexpr int kWaitLoads = 0x0f70;           // vmcnt(0)
 constexpr float kSlack = 8.f;                // log2 units that a maximum may grow before O follows
 
@@ -330,9 +331,18 @@ __global__ __launch_bounds__(NW * kWave, 2) void prefill_kernel(PagedPrefillPara
   const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) / kWave);
   const int half = lane >> 5;
   const int col = lane & 31;
-  const int split = blockIdx.x % p.splits;
-  const int block = p.blocks - 1 - static_cast<int>(blockIdx.x) / p.splits;   // the longest first
-  const int unit = blockIdx.y;
+  const int units = p.c.n_layers * p.c.batch * p.c.hkv;
+  // Workgroups go to the XCDs in turn.  Where there are many, `near` neighbours, which see
+  // mostly the same keys, take turns on one of them and share its L2.
+  int id = blockIdx.x;
+  if (p.near > 1) {
+    const int slot = id / kXcds;
+    id = (slot / p.near * kXcds + id % kXcds) * p.near + slot % p.near;
+    if (id >= units * p.blocks * p.splits) return;
+  }
+  const int split = id % p.splits;
+  const int block = p.blocks - 1 - id / p.splits % p.blocks;   // the longest first
+  const int unit = id / p.splits / p.blocks;
   const int per_layer = p.c.batch * p.c.hkv;
   const int lc = unit / per_layer;
   const int b = (unit % per_layer) / p.c.hkv;
@@ -662,12 +672,14 @@ __global__ __launch_bounds__(256) void prefill_finish_kernel(PagedPrefillParams 
 template <typename T, int D>
 hipError_t launch_typed(const PagedPrefillParams &p, hipStream_t s) {
   const int units = p.c.n_layers * p.c.batch * p.c.hkv;
+  const int all = units * p.blocks * p.splits, turn = kXcds * p.near;
+  const int grid = p.near > 1 ? (all + turn - 1) / turn * turn : all;
   if constexpr (sizeof(T) == 2) {
     if (p.rows == kPrefillLongRows)
-      hipLaunchKernelGGL((prefill_kernel<T, D, 8>), dim3(p.blocks, units), dim3(8 * kWave), 0, s, p);
+      hipLaunchKernelGGL((prefill_kernel<T, D, 8>), dim3(grid), dim3(8 * kWave), 0, s, p);
   }
   if (p.rows == kRows)
-    hipLaunchKernelGGL((prefill_kernel<T, D, 4>), dim3(p.blocks * p.splits, units), dim3(4 * kWave), 0, s, p);
+    hipLaunchKernelGGL((prefill_kernel<T, D, 4>), dim3(grid), dim3(4 * kWave), 0, s, p);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   const int merges = p.splits > 1 ? units * p.blocks * (kRows / kMergeRows) * (D / 32) : 0;
