@@ -312,12 +312,12 @@ reco_status_t reco_paged_decode_attn(const reco_paged_cache_t *cache, int32_t la
  *   k_new, v_new : [n_layers][batch][n_kv_heads][n_tokens][head_dim]
  *   n_new        : nullable [batch] int32 in [0, n_tokens]
  *   out          : like q (output);  lse : nullable, like q without head_dim, fp32
- * Places past a sequence's tokens are neither read nor written.  A run that does not
+ * Places past a sequence's tokens count for nothing and are not written.  A run that does not
  * fit its unit's capacity (RECO_DEV_APPEND_OVERFLOW), or whose rows' page ids are bad
  * (RECO_DEV_BAD_PAGE), is attended but not stored; a bad stored length
  * (RECO_DEV_BAD_LENGTH) is clamped for the attention and nothing is stored; a bad
  * n_new (RECO_DEV_BAD_LENGTH) counts as 0.  q, k_new, v_new and out are 16-byte
- * aligned, the workspace 256-byte aligned.  n_tokens >= 1; n_tokens * G <= 2^29 and
+ * aligned, the workspace 256-byte aligned.  n_tokens >= 1; n_tokens * G <= 2^28 and
  * fewer than 2^24 workgroups (larger: RECO_ERR_UNSUPPORTED). */
 size_t reco_paged_prefill_attn_workspace_size(const reco_paged_cache_t *cache, int32_t n_layers,
                                               int32_t n_q_heads, int32_t n_tokens);

@@ -14,7 +14,7 @@ namespace {
 
 // Positions rounded up to a tile, and sums of two of them, stay inside int32.
 constexpr int64_t kMaxCapacity = int64_t{1} << 29;
-constexpr int64_t kMaxQueryRows = int64_t{1} << 29;   // of one KV head in a run
+constexpr int64_t kMaxQueryRows = int64_t{1} << 28;   // of one KV head in a run
 
 bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 
@@ -64,6 +64,8 @@ reco::PagedCache paged_cache(const reco_paged_cache_t *c, int32_t layer0, int32_
   p.batch = c->batch;
   p.hkv = c->n_kv_heads;
   p.n_pages = c->n_pages;
+  p.by_hkv = reco::FastDiv(c->n_kv_heads);
+  p.by_batch = reco::FastDiv(c->batch);
   p.page_shift = __builtin_ctz(static_cast<unsigned>(c->page_rows));
   p.max_pages = c->max_pages;
   p.cap = static_cast<int>(capacity_of(c));
@@ -109,12 +111,13 @@ reco_status_t reco_paged_decode_attn(const reco_paged_cache_t *cache, int32_t la
   p.out = out;
   p.lse = lse;
   p.group = G;
-  p.hq = n_q_heads;
+  p.by_group = reco::FastDiv(G);
   p.cus = cus;
   p.sinks = sinks;
   p.window = window;
   p.scale_log2 = scale * 1.4426950408889634f;
   p.splits = reco::paged_decode_splits(units, reco::paged_span_tiles(p.c.cap, sinks, window), cus);
+  p.by_splits = reco::FastDiv(p.splits);
   if (!reco::paged_decode_fits_grid(p)) return RECO_ERR_UNSUPPORTED;
   reco::paged_decode_place(p, cache->head_dim, ws);
   return reco::hip_status(reco::launch_paged_decode(p, cache->dtype, cache->head_dim, stream));
@@ -158,7 +161,7 @@ reco_status_t reco_paged_prefill_attn(const reco_paged_cache_t *cache, int32_t l
   p.out = out;
   p.lse = lse;
   p.group = G;
-  p.hq = n_q_heads;
+  p.by_group = reco::FastDiv(G);
   p.tokens = n_tokens;
   p.rows = reco::prefill_rows(units, n_tokens, G, cache->dtype, cus);
   p.blocks = reco::prefill_blocks(n_tokens, G, p.rows);
@@ -167,8 +170,9 @@ reco_status_t reco_paged_prefill_attn(const reco_paged_cache_t *cache, int32_t l
   p.sinks = sinks;
   p.window = window;
   p.scale_log2 = scale * 1.4426950408889634f;
+  p.by_splits = reco::FastDiv(p.splits);
   if (!reco::prefill_fits_grid(p)) return RECO_ERR_UNSUPPORTED;
-  p.near = reco::prefill_near(units * p.blocks * p.splits);
+  p.near = reco::prefill_near(units * p.blocks, p.splits);
   reco::prefill_place(p, cache->head_dim, ws);
   return reco::hip_status(reco::launch_paged_prefill(p, cache->dtype, cache->head_dim, stream));
 }

@@ -8,6 +8,20 @@
 
 namespace reco {
 
+// Division by a number that the host knows: n / d for 0 <= n < 2^28 and n d < 2^36.  The
+// compiler's own takes some 35 instructions in a row, which short kernels wait for.
+struct FastDiv {
+  uint64_t m;
+  int d;
+
+  FastDiv() = default;
+  explicit FastDiv(int divisor) : m(((uint64_t{1} << 36) + divisor - 1) / divisor), d(divisor) {}
+  __host__ __device__ int of(int n) const { return static_cast<int>((static_cast<uint64_t>(static_cast<uint32_t>(n)) * m) >> 36); }
+  __host__ __device__ int rest(int n) const { return n - of(n) * d; }
+};
+
+// A unit is (layer of the call, sequence, KV head) in this order, so that the query heads
+// of unit u start at u * group and its cache unit is layer0 * batch * hkv + u.
 // A page holds 1 << page_shift rows (16 or more) of one unit; cap = max_pages << page_shift.
 struct PagedCache {
   void *k;                // [n_pages][page rows][D]
@@ -16,7 +30,11 @@ struct PagedCache {
   int32_t *len;           // [cache layers][batch][hkv]
   float *weight;          // nullable [cache layers][batch][hkv][cap]
   int32_t *dev_err;
+  FastDiv by_hkv, by_batch;
   int layer0, n_layers, batch, hkv, n_pages, page_shift, max_pages, cap;
+
+  __host__ __device__ size_t unit(int u) const { return static_cast<size_t>(layer0) * batch * hkv + u; }
+  __host__ __device__ int sequence(int u) const { return by_batch.rest(by_hkv.of(u)); }
 };
 
 // ---- attention of one new token ---------------------------------------------
@@ -32,7 +50,8 @@ struct PagedDecodeParams {
   int32_t *len_in;        // [units]  lengths before the append, for the weights
   float *logits;          // [units][group][logit_pitch]  log2-domain logits, where weights are kept
   int64_t logit_pitch;
-  int group, hq, splits, cus;
+  FastDiv by_splits, by_group;
+  int group, splits, cus;
   int sinks, window;      // window 0: every row is visible
   float scale_log2;       // logit scale * log2(e)
 };
@@ -65,7 +84,8 @@ struct PagedPrefillParams {
   int32_t *len_in;        // [units]  lengths before the append
   float *part_o;          // [units][blocks][splits][kPrefillRows][D]
   float *part_ml;         // [units][blocks][splits][2][kPrefillRows]
-  int group, hq, tokens, blocks, splits;
+  FastDiv by_splits, by_group;
+  int group, tokens, blocks, splits;
   int rows;               // of a block: kPrefillRows, or kPrefillLongRows with one split
   int near;               // neighbouring workgroups that share an XCD
   int sinks, window;
@@ -77,7 +97,7 @@ constexpr int prefill_tile_rows(int dtype) { return dtype == 0 ? 32 : 64; }   //
 int prefill_splits(int units, int blocks, int capacity, int sinks, int window, int tile_rows, int compute_units);
 size_t prefill_workspace_bytes(int units, int tokens, int capacity, int group, int head_dim, int tile_rows,
                                int compute_units);
-int prefill_near(int workgroups);
+int prefill_near(int workgroups, int splits);
 bool prefill_fits_grid(const PagedPrefillParams &p);
 void prefill_place(PagedPrefillParams &p, int head_dim, void *ws);
 hipError_t launch_paged_prefill(const PagedPrefillParams &p, int dtype, int head_dim, hipStream_t s);

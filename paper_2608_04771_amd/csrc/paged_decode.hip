@@ -135,12 +135,8 @@ __global__ __launch_bounds__(NW * kWave, (Cfg<T, D>::min_wgs)) void paged_split_
   const int col = lane & 15;
   const int grp = lane >> 4;
   const int split = blockIdx.x, unit = blockIdx.y;
-  const int per_layer = p.c.batch * p.c.hkv;
-  const int lc = unit / per_layer;
-  const int b = (unit % per_layer) / p.c.hkv;
-  const int h = unit % p.c.hkv;
-  const size_t cunit = static_cast<size_t>(p.c.layer0 + lc) * per_layer + static_cast<size_t>(b) * p.c.hkv + h;
-  const size_t oq0 = (static_cast<size_t>(lc) * p.c.batch + b) * p.hq + h * p.group;
+  const size_t cunit = p.c.unit(unit);
+  const size_t oq0 = static_cast<size_t>(unit) * p.group;
 
   const int len_in = p.c.len[cunit];
   const int n_cache = len_in < 0 ? 0 : (len_in > p.c.cap ? p.c.cap : len_in);
@@ -150,7 +146,7 @@ __global__ __launch_bounds__(NW * kWave, (Cfg<T, D>::min_wgs)) void paged_split_
   const T *knew = append ? reinterpret_cast<const T *>(p.k_new) + static_cast<size_t>(unit) * D : nullptr;
   const T *vnew = append ? reinterpret_cast<const T *>(p.v_new) + static_cast<size_t>(unit) * D : nullptr;
 
-  const int per_split = (seen.total + p.splits - 1) / p.splits;
+  const int per_split = p.by_splits.of(seen.total + p.splits - 1);
   const int i0 = split * per_split;
   const int i1 = min(seen.total, i0 + per_split);
 
@@ -398,12 +394,8 @@ __global__ __launch_bounds__(kMergeThreads) void paged_merge_kernel(PagedDecodeP
   const int units = p.c.n_layers * p.c.batch * p.c.hkv;
   const int id = blockIdx.x;
   const bool merging = id < units * G;
-  const int unit = merging ? id / G : (id - units * G) / weight_chunks;
-  const int per_layer = p.c.batch * p.c.hkv;
-  const int lc = unit / per_layer;
-  const int b = (unit % per_layer) / p.c.hkv;
-  const int h = unit % p.c.hkv;
-  const size_t cunit = static_cast<size_t>(p.c.layer0 + lc) * per_layer + static_cast<size_t>(b) * p.c.hkv + h;
+  const int unit = merging ? p.by_group.of(id) : (id - units * G) / weight_chunks;
+  const size_t cunit = p.c.unit(unit);
   const float *pml = p.part_ml + static_cast<size_t>(unit) * S * 2 * G;
 
   if (!merging) {
@@ -438,7 +430,7 @@ __global__ __launch_bounds__(kMergeThreads) void paged_merge_kernel(PagedDecodeP
     return;
   }
 
-  const int qi = id % G;
+  const int qi = id - unit * G;
   const bool append = p.k_new != nullptr && qi == 0;
   const int len_in = qi == 0 ? p.c.len[cunit] : 0;
   T krow = T{}, vrow = T{};
@@ -487,7 +479,7 @@ __global__ __launch_bounds__(kMergeThreads) void paged_merge_kernel(PagedDecodeP
   }
   *reinterpret_cast<float4 *>(&s_acc[sg][dv]) = acc;
   __syncthreads();
-  const size_t oq = (static_cast<size_t>(lc) * p.c.batch + b) * p.hq + h * G + qi;
+  const size_t oq = static_cast<size_t>(unit) * G + qi;
   if (tid < D) {
     float o = 0.f;
 #pragma unroll

@@ -40,10 +40,9 @@ __global__ __launch_bounds__(kSelThreads) void evict_select_kernel(PagedEvictPar
   __shared__ int s_bin, s_krem, s_bad;
 
   const int unit = blockIdx.x;
-  const int per_layer = p.c.batch * p.c.hkv;
-  const int lc = unit / per_layer;
-  const int b = (unit % per_layer) / p.c.hkv;
-  const size_t cunit = static_cast<size_t>(p.c.layer0 + lc) * per_layer + unit % per_layer;
+  const size_t cunit = p.c.unit(unit);
+  const int seq = p.c.by_hkv.of(unit);                 // of all layers
+  const int lc = p.c.by_batch.of(seq), b = p.c.by_batch.rest(seq);
   const int tid = threadIdx.x;
   const int lane = tid & (kWave - 1);
   const int wave = tid / kWave;
@@ -195,7 +194,7 @@ __global__ __launch_bounds__(kCompThreads) void evict_compact_kernel(PagedEvictP
   constexpr int kSlices = ROWB / kSliceBytes;
   const int unit = blockIdx.x;
   const int job = blockIdx.y;                            // K slices, V slices, weights
-  const size_t cunit = static_cast<size_t>(p.c.layer0) * p.c.batch * p.c.hkv + unit;
+  const size_t cunit = p.c.unit(unit);
   const int m = p.kept[unit];
   if (m < 0) return;
   const int32_t *idx = p.idx + static_cast<size_t>(unit) * p.c.cap;

@@ -95,13 +95,13 @@ size_t prefill_workspace_bytes(int units, int tokens, int capacity, int group, i
 }
 
 // A round of an XCD's compute units, where every XCD has four rounds and more.
-int prefill_near(int workgroups) { return workgroups >= 1024 ? 32 : 1; }
+int prefill_near(int workgroups, int splits) { return splits == 1 && workgroups >= 1024 ? 32 : 1; }
 
 bool prefill_fits_grid(const PagedPrefillParams &p) {
   const int64_t units = static_cast<int64_t>(p.c.n_layers) * p.c.batch * p.c.hkv;
   const int64_t most = int64_t{1} << 24;                 // workgroups of 256 threads
   return units * p.blocks * p.splits < most / 2 &&       // of 512, and rounded up
-         units * (p.tokens / 64 + 1 + (p.splits > 1 ? static_cast<int64_t>(p.blocks) * 16 : 0)) < most;
+         p.tokens / 64 + 1 + (p.splits > 1 ? static_cast<int64_t>(p.blocks) * 16 : 0) < most;
 }
 
 void prefill_place(PagedPrefillParams &p, int head_dim, void *ws) {

@@ -291,7 +291,7 @@ __device__ __forceinline__ void write_rows(const PagedPrefillParams &p, unsigned
   const int half = lane >> 5, col = lane & 31;
   const float inv = l == 0.f ? 0.f : 1.f / l;
   const auto place = [&](int row) {
-    const int t = row / p.group;
+    const int t = p.by_group.of(row);
     return (head0 + (row - t * p.group)) * static_cast<size_t>(p.tokens) + t;
   };
 #pragma unroll
@@ -338,19 +338,15 @@ __global__ __launch_bounds__(NW * kWave, 2) void prefill_kernel(PagedPrefillPara
   if (p.near > 1) {
     const int slot = id / kXcds;
     id = (slot / p.near * kXcds + id % kXcds) * p.near + slot % p.near;
-    if (id >= units * p.blocks * p.splits) return;
+    if (id >= units * p.blocks) return;
   }
-  const int split = id % p.splits;
-  const int block = p.blocks - 1 - id / p.splits % p.blocks;   // the longest first
-  const int unit = id / p.splits / p.blocks;
-  const int per_layer = p.c.batch * p.c.hkv;
-  const int lc = unit / per_layer;
-  const int b = (unit % per_layer) / p.c.hkv;
-  const int h = unit % p.c.hkv;
-  const size_t cunit = static_cast<size_t>(p.c.layer0 + lc) * per_layer + unit % per_layer;
+  const int unit = p.near > 1 ? id / p.blocks : blockIdx.y;      // many workgroups take one split
+  const int block = p.blocks - 1 - (p.near > 1 ? id - unit * p.blocks : p.by_splits.of(id));   // the longest first
+  const int split = p.near > 1 ? 0 : p.by_splits.rest(id);
+  const size_t cunit = p.c.unit(unit);
 
   const int len_in = p.c.len[cunit];
-  const int given = p.n_new ? p.n_new[b] : p.tokens;
+  const int given = p.n_new ? p.n_new[p.c.sequence(unit)] : p.tokens;
   const int n = given < 0 || given > p.tokens ? 0 : given;
   if (block == 0 && split == 0 && threadIdx.x == 0) {
     p.len_in[unit] = len_in;                               // for the second kernel, which changes len
@@ -361,19 +357,19 @@ __global__ __launch_bounds__(NW * kWave, 2) void prefill_kernel(PagedPrefillPara
   if (r0 >= n * G) return;
   const Run<KT> run(len_in < 0 ? 0 : min(len_in, p.c.cap), n);
   const int L = run.L;
-  const int t_lo = r0 / G, t_hi = min(r0 + kRows - 1, n * G - 1) / G;
+  const int t_lo = p.by_group.of(r0), t_hi = p.by_group.of(min(r0 + kRows - 1, n * G - 1));
 
   const Seen<KT> seen(run, t_lo, t_hi, p.sinks, p.window);
-  const int per_split = (seen.total + p.splits - 1) / p.splits;
+  const int per_split = p.by_splits.of(seen.total + p.splits - 1);
   const int i0 = split * per_split;
   const int i1 = min(seen.total, i0 + per_split);
 
   // This lane's query row.
   const int r = r0 + wave * 32 + col;
-  const int t = min(r, p.tokens * G - 1) / G;
+  const int t = p.by_group.of(min(r, p.tokens * G - 1));
   const int pos = L + t;
-  const size_t qrow = ((static_cast<size_t>(lc) * p.c.batch + b) * p.hq + h * G + (min(r, p.tokens * G - 1) - t * G)) *
-                          static_cast<size_t>(p.tokens) + t;
+  const size_t head0 = static_cast<size_t>(unit) * G;
+  const size_t qrow = (head0 + (min(r, p.tokens * G - 1) - t * G)) * static_cast<size_t>(p.tokens) + t;
   frag qf[C::qk_steps];
   {
     const T *src = reinterpret_cast<const T *>(p.q) + qrow * D + half * (D / 2);
@@ -548,29 +544,26 @@ __global__ __launch_bounds__(NW * kWave, 2) void prefill_kernel(PagedPrefillPara
     return;
   }
   unsigned char *mine = wave < NW / 2 ? (wave < NW / 4 ? k0 : v0) : (wave < 3 * NW / 4 ? k1 : v1);
-  write_rows<T, D>(p, mine + wave % (NW / 4) * 32 * C::row_bytes, o, m_run, l_tot, (static_cast<size_t>(lc) * p.c.batch + b) * p.hq + h * G,
+  write_rows<T, D>(p, mine + wave % (NW / 4) * 32 * C::row_bytes, o, m_run, l_tot, head0,
                    r0 + wave * 32, n * G, lane);
 }
 
-// Joins the splits (workgroups [0, merges)) and puts the new rows into their pages
-// (the others, kAppendRows rows of a unit each).  A unit's rows are appended together or,
+// Joins the splits (workgroups [0, merges) of a unit) and puts its new rows into their
+// pages (the others, kAppendRows rows each).  A unit's rows are appended together or,
 // where they or their pages do not fit, not at all.
 constexpr int kMergeRows = 32;               // a wave's rows, and a quarter of a 32-column block each thread
 constexpr int kAppendRows = 64;
 
 template <typename T, int D>
-__global__ __launch_bounds__(256) void prefill_finish_kernel(PagedPrefillParams p, int merges, int chunks) {
+__global__ __launch_bounds__(256) void prefill_finish_kernel(PagedPrefillParams p, int merges) {
   const int tid = threadIdx.x;
-  const int per_layer = p.c.batch * p.c.hkv;
   const int G = p.group;
-  int id = blockIdx.x;
-  if (id < merges) {
+  const int unit = blockIdx.y;
+  if (static_cast<int>(blockIdx.x) < merges) {
     constexpr int kDt = D / 32;
-    const int dt = id % kDt, w32 = id / kDt % (kRows / kMergeRows);
-    id /= kDt * (kRows / kMergeRows);
-    const int block = id % p.blocks, unit = id / p.blocks;
-    const int lc = unit / per_layer, b = (unit % per_layer) / p.c.hkv, h = unit % p.c.hkv;
-    const int given = p.n_new ? p.n_new[b] : p.tokens;
+    const int dt = blockIdx.x % kDt, w32 = blockIdx.x / kDt % (kRows / kMergeRows);
+    const int block = blockIdx.x / (kDt * (kRows / kMergeRows));
+    const int given = p.n_new ? p.n_new[p.c.sequence(unit)] : p.tokens;
     const int n = given < 0 || given > p.tokens ? 0 : given;
     if (block * kRows + w32 * kMergeRows >= n * G) return;
     // The splits' weights of the rows: eight threads a row.
@@ -605,7 +598,7 @@ __global__ __launch_bounds__(256) void prefill_finish_kernel(PagedPrefillParams 
       for (int i = 0; i < kEach; ++i) s_w[sub + i * kPer][row_of] = m[i] * inv;
       const int r = block * kRows + w32 * kMergeRows + row_of;
       if (p.lse && dt == 0 && sub == 0 && r < n * G)
-        p.lse[((static_cast<size_t>(lc) * p.c.batch + b) * p.hq + h * G + r % G) * static_cast<size_t>(p.tokens) + r / G] =
+        p.lse[(static_cast<size_t>(unit) * G + p.by_group.rest(r)) * static_cast<size_t>(p.tokens) + p.by_group.of(r)] =
             sum == 0.f ? -INFINITY : (ref + log2f(sum)) * kLn2;
     }
     __syncthreads();
@@ -624,8 +617,8 @@ __global__ __launch_bounds__(256) void prefill_finish_kernel(PagedPrefillParams 
       acc.w += x.w * w;
     }
     if (r >= n * G) return;
-    const int t = r / G;
-    const size_t row = ((static_cast<size_t>(lc) * p.c.batch + b) * p.hq + h * G + (r - t * G)) * static_cast<size_t>(p.tokens) + t;
+    const int t = p.by_group.of(r);
+    const size_t row = (static_cast<size_t>(unit) * G + (r - t * G)) * static_cast<size_t>(p.tokens) + t;
     T *dst = reinterpret_cast<T *>(p.out) + row * D + dt * 32 + acc_row(4 * e, lane >> 5);
     dst[0] = from_f32<T>(acc.x);
     dst[1] = from_f32<T>(acc.y);
@@ -633,21 +626,32 @@ __global__ __launch_bounds__(256) void prefill_finish_kernel(PagedPrefillParams 
     dst[3] = from_f32<T>(acc.w);
     return;
   }
-  id -= merges;
-  const int unit = id / chunks, chunk = id % chunks;
-  const int b = (unit % per_layer) / p.c.hkv;
-  const size_t cunit = static_cast<size_t>(p.c.layer0 + unit / per_layer) * per_layer + unit % per_layer;
-  const int given = p.n_new ? p.n_new[b] : p.tokens;
-  const int n = given < 0 || given > p.tokens ? 0 : given;
+  // The rows come while it is found out where they go.
+  constexpr int kLanes = D * (int)sizeof(T) / 16, kEach = kAppendRows * kLanes / 256;
+  const int first = (blockIdx.x - merges) * kAppendRows;
+  u32x4v k[kEach], v[kEach];
+#pragma unroll
+  for (int i = 0; i < kEach; ++i) {
+    const int row = min(first + (tid + i * 256) / kLanes, p.tokens - 1);
+    const size_t at = (static_cast<size_t>(unit) * p.tokens + row) * kLanes + tid % kLanes;
+    k[i] = reinterpret_cast<const u32x4v *>(p.k_new)[at];
+    v[i] = reinterpret_cast<const u32x4v *>(p.v_new)[at];
+  }
+  const size_t cunit = p.c.unit(unit);
+  const int given = p.n_new ? p.n_new[p.c.sequence(unit)] : p.tokens;
   const int L = p.len_in[unit];
-  if (n == 0 || chunk * kAppendRows >= n || L < 0 || L > p.c.cap) return;
-  const bool reporting = chunk == 0 && tid == 0;
+  const int n = given < 0 || given > p.tokens ? 0 : given;
+  if (first >= n || L < 0 || L > p.c.cap) return;
+  const bool reporting = first == 0 && tid == 0;
   if (n > p.c.cap - L) {
     if (reporting) report(p.c.dev_err, kDevAppendOverflow);
     return;
   }
   const int32_t *table = p.c.pages + cunit * static_cast<size_t>(p.c.max_pages);
   const int shift = p.c.page_shift;
+  int id[kEach];
+#pragma unroll
+  for (int i = 0; i < kEach; ++i) id[i] = table[min(L + first + (tid + i * 256) / kLanes, L + n - 1) >> shift];
   bool bad = false;
   for (int g = (L >> shift) + tid; g <= (L + n - 1) >> shift; g += 256)
     if (static_cast<unsigned>(table[g]) >= static_cast<unsigned>(p.c.n_pages)) bad = true;
@@ -655,36 +659,34 @@ __global__ __launch_bounds__(256) void prefill_finish_kernel(PagedPrefillParams 
     if (reporting) report(p.c.dev_err, kDevBadPage);
     return;
   }
-  constexpr int kLanes = D * (int)sizeof(T) / 16;
-  const int rows = min(kAppendRows, n - chunk * kAppendRows);
-  const uint4 *ks = reinterpret_cast<const uint4 *>(p.k_new) + (static_cast<size_t>(unit) * p.tokens + chunk * kAppendRows) * kLanes;
-  const uint4 *vs = reinterpret_cast<const uint4 *>(p.v_new) + (static_cast<size_t>(unit) * p.tokens + chunk * kAppendRows) * kLanes;
-  for (int i = tid; i < rows * kLanes; i += 256) {
-    const int row = L + chunk * kAppendRows + i / kLanes;
-    const size_t at = ((static_cast<size_t>(table[row >> shift]) << shift) + (row & ((1 << shift) - 1))) * kLanes + i % kLanes;
-    reinterpret_cast<uint4 *>(p.c.k)[at] = ks[i];
-    reinterpret_cast<uint4 *>(p.c.v)[at] = vs[i];
+#pragma unroll
+  for (int i = 0; i < kEach; ++i) {
+    const int t = first + (tid + i * 256) / kLanes;
+    if (t >= n) break;
+    const size_t at = ((static_cast<size_t>(id[i]) << shift) + ((L + t) & ((1 << shift) - 1))) * kLanes + tid % kLanes;
+    reinterpret_cast<u32x4v *>(p.c.k)[at] = k[i];
+    reinterpret_cast<u32x4v *>(p.c.v)[at] = v[i];
   }
-  if (p.c.weight && tid < rows) p.c.weight[cunit * p.c.cap + L + chunk * kAppendRows + tid] = 0.f;
+  if (p.c.weight && tid < kAppendRows && first + tid < n) p.c.weight[cunit * p.c.cap + L + first + tid] = 0.f;
   if (reporting) p.c.len[cunit] = L + n;
 }
 
 template <typename T, int D>
 hipError_t launch_typed(const PagedPrefillParams &p, hipStream_t s) {
   const int units = p.c.n_layers * p.c.batch * p.c.hkv;
-  const int all = units * p.blocks * p.splits, turn = kXcds * p.near;
-  const int grid = p.near > 1 ? (all + turn - 1) / turn * turn : all;
+  const int turn = kXcds * p.near;
+  const dim3 grid = p.near > 1 ? dim3((units * p.blocks + turn - 1) / turn * turn) : dim3(p.blocks * p.splits, units);
   if constexpr (sizeof(T) == 2) {
     if (p.rows == kPrefillLongRows)
-      hipLaunchKernelGGL((prefill_kernel<T, D, 8>), dim3(grid), dim3(8 * kWave), 0, s, p);
+      hipLaunchKernelGGL((prefill_kernel<T, D, 8>), grid, dim3(8 * kWave), 0, s, p);
   }
   if (p.rows == kRows)
-    hipLaunchKernelGGL((prefill_kernel<T, D, 4>), dim3(grid), dim3(4 * kWave), 0, s, p);
+    hipLaunchKernelGGL((prefill_kernel<T, D, 4>), grid, dim3(4 * kWave), 0, s, p);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  const int merges = p.splits > 1 ? units * p.blocks * (kRows / kMergeRows) * (D / 32) : 0;
+  const int merges = p.splits > 1 ? p.blocks * (kRows / kMergeRows) * (D / 32) : 0;
   const int chunks = (p.tokens + kAppendRows - 1) / kAppendRows;
-  hipLaunchKernelGGL((prefill_finish_kernel<T, D>), dim3(merges + units * chunks), dim3(256), 0, s, p, merges, chunks);
+  hipLaunchKernelGGL((prefill_finish_kernel<T, D>), dim3(merges + chunks, units), dim3(256), 0, s, p, merges);
   return hipGetLastError();
 }
 

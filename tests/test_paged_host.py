@@ -63,7 +63,7 @@ def test_attention_arguments_are_refused(call):
 def test_more_refusals():
     c = _cache()
     assert _prefill(c, T=0) == B.RECO_ERR_INVALID_ARG
-    assert _prefill(c, T=1 << 29) == B.RECO_ERR_UNSUPPORTED
+    assert _prefill(c, T=1 << 28) == B.RECO_ERR_UNSUPPORTED
     assert _evict(_cache(weight=0)) == _evict(c, budget=0) == _evict(c, stride=-1) == B.RECO_ERR_INVALID_ARG
     assert _evict(c, sinks=-1) == _evict(c, recent=-1) == B.RECO_ERR_INVALID_ARG
     lib, ref = B.load_library(), ctypes.byref
@@ -80,7 +80,7 @@ def test_more_refusals():
     # a grid of 2^32 threads and more (rows that no device holds) is refused
     huge = _cache(page_rows=4096, max_pages=1 << 17, batch=32000, n_layers=1)
     assert _decode(huge, nl=1, wsb=(1 << 64) - 1) == B.RECO_ERR_UNSUPPORTED
-    assert _prefill(huge, nl=1, T=1 << 27, wsb=(1 << 64) - 1) == B.RECO_ERR_UNSUPPORTED
+    assert _prefill(huge, nl=1, T=1 << 26, wsb=(1 << 64) - 1) == B.RECO_ERR_UNSUPPORTED
 
 
 NL, BS, H, NP, PR, MP, D, HQ = 2, 3, 2, 12, 16, 4, 64, 8
