@@ -52,7 +52,7 @@ struct Cfg {
 };
 
 template <typename T, int D>
-using Rows = uint4[Cfg<T, D>::insts];
+using Rows = u32x4v[Cfg<T, D>::insts];
 
 typedef short i16x4_t __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) i16x4_t lds_i16x4_t;
@@ -102,10 +102,15 @@ __device__ __forceinline__ bool append_row(const PagedDecodeParams &p, size_t cu
 
 // Weights of four rows from `row` on: their probabilities summed over the queries.
 // seen: what the token sees; n: the rows cached before the call; fresh: row n was appended.
+// What the rows had is asked for first, so that it comes with the logits.
 __device__ __forceinline__ void add_weights(float *weight, const float *logits, int64_t pitch, int group, int row,
-                                            const SeenTiles &seen, int n, bool fresh, const float *top,
+                                            const SeenTiles &seen, int n, int cap, bool fresh, const float *top,
                                             const float *inv) {
+  float old[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) old[i] = weight[min(row + i, cap - 1)];
   float w[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
   for (int g = 0; g < group; ++g) {
     const float4 x = *reinterpret_cast<const float4 *>(logits + g * pitch + row);
     w[0] += fast_exp2(x.x - top[g]) * inv[g];
@@ -116,14 +121,12 @@ __device__ __forceinline__ void add_weights(float *weight, const float *logits, 
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const int j = row + i;
-    if (!seen.sees(j)) continue;
-    if (j < n) weight[j] += w[i];
-    else if (fresh) weight[j] = w[i];
+    if (seen.sees(j) && (j < n || fresh)) weight[j] = j < n ? old[i] + w[i] : w[i];
   }
 }
 
 template <typename T, int D, int NW>
-__global__ __launch_bounds__(NW * kWave, (Cfg<T, D>::min_wgs)) void paged_split_kernel(PagedDecodeParams p) {
+__global__ __launch_bounds__(NW * kWave, NW == 8 ? 1 : (Cfg<T, D>::min_wgs)) void paged_split_kernel(PagedDecodeParams p) {
   using C = Cfg<T, D>;
   using MF = Mfma<T>;
   using frag = typename MF::frag;
@@ -142,7 +145,6 @@ __global__ __launch_bounds__(NW * kWave, (Cfg<T, D>::min_wgs)) void paged_split_
   const int n_cache = len_in < 0 ? 0 : (len_in > p.c.cap ? p.c.cap : len_in);
   const bool append = p.k_new != nullptr;
   const SeenTiles seen(n_cache + (append ? 1 : 0), p.sinks, p.window);
-  PagedUnit pages(p.c, cunit, n_cache);
   const T *knew = append ? reinterpret_cast<const T *>(p.k_new) + static_cast<size_t>(unit) * D : nullptr;
   const T *vnew = append ? reinterpret_cast<const T *>(p.v_new) + static_cast<size_t>(unit) * D : nullptr;
 
@@ -165,44 +167,66 @@ __global__ __launch_bounds__(NW * kWave, (Cfg<T, D>::min_wgs)) void paged_split_
   unsigned char *stage = smem + wave * C::wave_stage;
   float *logits = p.logits ? p.logits + (static_cast<size_t>(unit) * p.group + col) * p.logit_pitch + 4 * grp : nullptr;
 
-  // The pool rows of a tile's two halves, which may lie in two pages.
+  // Where the wave's tiles lie: each lane holds the place of 16 rows, so 32 tiles at a
+  // time; the table's entries of the batch after are on their way meanwhile.
+  constexpr int kBatch = kWave / 2;
+  const int mine = i1 - i0 - wave > 0 ? (i1 - i0 - wave + NW - 1) / NW : 0;   // tiles of the wave
+  const int32_t *table = p.c.pages + cunit * static_cast<size_t>(p.c.max_pages);
+  const auto tile_of = [&](int k) { return seen.tile(i0 + wave + NW * min(k, mine - 1)); };
+  const auto row_of = [&](int batch) { return tile_of(batch * kBatch + lane / 2) * kTile + lane % 2 * 16; };
+  unsigned worst = 0;
+  int coming = 0;
+  uint64_t place = 0;
+  const auto ask = [&](int batch) { coming = table[max(min(row_of(batch), n_cache - 1), 0) >> p.c.page_shift]; };
+  const auto turn = [&](int batch) {
+    const unsigned id = min(static_cast<unsigned>(coming), static_cast<unsigned>(p.c.n_pages - 1));
+    worst = max(worst, static_cast<unsigned>(coming));
+    place = ((static_cast<uint64_t>(id) << p.c.page_shift) + (row_of(batch) & ((1 << p.c.page_shift) - 1))) * C::row_bytes;
+    ask(batch + 1);
+  };
   struct Where {
-    size_t at[2];
+    uint64_t at[2];
   };
-  const auto find = [&](int i) {
-    const int kb = seen.tile(i) * kTile;
-    const int a = pages.entry(kb), b = pages.entry(kb + 16);
-    return Where{{pages.row_at(a, kb), pages.row_at(b, kb + 16)}};
-  };
-  // A tile's rows of K or V.  Rows past the last cached one are others of the pool and
-  // are masked where they are used; row n_cache is the new one.
-  const auto load = [&](Rows<T, D> &reg, const void *pool, const T *fresh, int i, const Where &w) {
-    const int kb = seen.tile(i) * kTile;
-    const int sub = (lane % C::lanes_per_row) * 16;
+  const auto find = [&](int k) {
+    Where w;
 #pragma unroll
-    for (int k = 0; k < C::insts; ++k) {
-      const int half = k / (C::insts / 2);
-      const int r = k * C::rows_per_inst + lane / C::lanes_per_row;
-      const unsigned char *src = reinterpret_cast<const unsigned char *>(pool) +
-                                 (w.at[half] + (k % (C::insts / 2)) * C::rows_per_inst) * C::row_bytes + lane * 16;
-      if (append && kb + r == n_cache) src = reinterpret_cast<const unsigned char *>(fresh) + sub;
-      reg[k] = nt_load_u4(src);
+    for (int hf = 0; hf < 2; ++hf) {
+      const int from = (k & (kBatch - 1)) * 2 + hf;
+      w.at[hf] = static_cast<uint64_t>(static_cast<unsigned>(__builtin_amdgcn_readlane(static_cast<int>(place >> 32), from))) << 32 |
+                 static_cast<unsigned>(__builtin_amdgcn_readlane(static_cast<int>(place), from));
     }
+    return w;
   };
+  // Rows of K or V of a tile.  Rows past the last cached one are others of the pool and
+  // are masked where they are used; the new row is put where it belongs in LDS.
+  const auto load = [&](Rows<T, D> &reg, const void *pool, const Where &w) {
+#pragma unroll
+    for (int j = 0; j < C::insts; ++j)
+      reg[j] = __builtin_nontemporal_load(reinterpret_cast<const u32x4v *>(
+          static_cast<const unsigned char *>(pool) + w.at[j / (C::insts / 2)] + j % (C::insts / 2) * (kWave * 16) + lane * 16));
+  };
+  const auto fresh_row = [&](const T *row) {
+    return append ? *reinterpret_cast<const uint4 *>(reinterpret_cast<const unsigned char *>(row) + lane % C::lanes_per_row * 16)
+                  : make_uint4(0, 0, 0, 0);
+  };
+  const uint4 kfresh = fresh_row(knew), vfresh = fresh_row(vnew);
 
   Rows<T, D> kreg, vreg;
-  const auto attend = [&](int i, auto whole) {
-    constexpr bool kWhole = decltype(whole)::value;
-    const int kb = seen.tile(i) * kTile;
-    const bool more = i + NW < i1;
-    Where next{};
-    if (more) next = find(i + NW);
+  const auto attend = [&](int k) {
+    const int kb = tile_of(k) * kTile;
+    const bool whole = seen.whole(kb, n_cache);
+    const bool holds_new = append && kb <= n_cache && n_cache < kb + kTile;
+    const bool more = k + 1 < mine;
+    if (((k + 1) & (kBatch - 1)) == 0) turn((k + 1) / kBatch);
+    const Where next = find(k + 1);
 #pragma unroll
-    for (int k = 0; k < C::insts; ++k) {
-      const int r = k * C::rows_per_inst + lane / C::lanes_per_row;
-      *reinterpret_cast<uint4 *>(stage + r * C::k_stride + (lane % C::lanes_per_row) * 16) = kreg[k];
+    for (int j = 0; j < C::insts; ++j) {
+      const int r = j * C::rows_per_inst + lane / C::lanes_per_row;
+      *reinterpret_cast<u32x4v *>(stage + r * C::k_stride + (lane % C::lanes_per_row) * 16) = kreg[j];
     }
-    if (more) load(kreg, p.c.k, knew, i + NW, next);
+    if (more) load(kreg, p.c.k, next);
+    if (holds_new && lane < C::lanes_per_row)
+      *reinterpret_cast<uint4 *>(stage + (n_cache - kb) * C::k_stride + lane * 16) = kfresh;
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     f32x4_t s[2];
 #pragma unroll
@@ -214,14 +238,15 @@ __global__ __launch_bounds__(NW * kWave, (Cfg<T, D>::min_wgs)) void paged_split_
     }
 
     float x[8];
-    float top = -INFINITY;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const int row = kb + (e >> 2) * 16 + 4 * grp + (e & 3);
-      x[e] = s[e >> 2][e & 3] * p.scale_log2;
-      if constexpr (!kWhole) x[e] = seen.sees(row) ? x[e] : -INFINITY;
-      top = fmaxf(top, x[e]);
+    for (int e = 0; e < 8; ++e) x[e] = s[e >> 2][e & 3] * p.scale_log2;
+    if (!whole) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[e] = seen.sees(kb + (e >> 2) * 16 + 4 * grp + (e & 3)) ? x[e] : -INFINITY;
     }
+    float top = x[0];
+#pragma unroll
+    for (int e = 1; e < 8; ++e) top = fmaxf(top, x[e]);
     if (logits && col < p.group) {
       *reinterpret_cast<float4 *>(logits + kb) = make_float4(x[0], x[1], x[2], x[3]);
       *reinterpret_cast<float4 *>(logits + kb + 16) = make_float4(x[4], x[5], x[6], x[7]);
@@ -241,22 +266,29 @@ __global__ __launch_bounds__(NW * kWave, (Cfg<T, D>::min_wgs)) void paged_split_
 #pragma unroll
     for (int dt = 0; dt < C::dtiles; ++dt) {
 #pragma unroll
-      for (int j = 0; j < 4; ++j) o[dt][j] *= alpha;
+      for (int e = 0; e < 4; ++e) o[dt][e] *= alpha;
     }
 
+    if (!whole) {                                         // a NaN that is not seen, times 0, would be NaN
 #pragma unroll
-    for (int k = 0; k < C::insts; ++k) {
-      const int r = k * C::rows_per_inst + lane / C::lanes_per_row;
-      uint2 *dst = reinterpret_cast<uint2 *>(stage + r * C::v_stride + (lane % C::lanes_per_row) * 16);
-      uint4 v = vreg[k];
-      if constexpr (!kWhole) {                            // a NaN that is not seen, times 0, would be NaN
-        const unsigned keep = seen.sees(kb + r) ? ~0u : 0u;
-        v = make_uint4(v.x & keep, v.y & keep, v.z & keep, v.w & keep);
+      for (int j = 0; j < C::insts; ++j) {
+        const unsigned keep = seen.sees(kb + j * C::rows_per_inst + lane / C::lanes_per_row) ? ~0u : 0u;
+        vreg[j] &= u32x4v{keep, keep, keep, keep};
       }
-      dst[0] = make_uint2(v.x, v.y);
-      dst[1] = make_uint2(v.z, v.w);
     }
-    if (more) load(vreg, p.c.v, vnew, i + NW, next);
+#pragma unroll
+    for (int j = 0; j < C::insts; ++j) {
+      const int r = j * C::rows_per_inst + lane / C::lanes_per_row;
+      uint2 *dst = reinterpret_cast<uint2 *>(stage + r * C::v_stride + (lane % C::lanes_per_row) * 16);
+      dst[0] = make_uint2(vreg[j][0], vreg[j][1]);
+      dst[1] = make_uint2(vreg[j][2], vreg[j][3]);
+    }
+    if (more) load(vreg, p.c.v, next);
+    if (holds_new && lane < C::lanes_per_row) {
+      uint2 *dst = reinterpret_cast<uint2 *>(stage + (n_cache - kb) * C::v_stride + lane * 16);
+      dst[0] = make_uint2(vfresh.x, vfresh.y);
+      dst[1] = make_uint2(vfresh.z, vfresh.w);
+    }
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
 #pragma unroll
     for (int dt = 0; dt < C::dtiles; ++dt) {
@@ -266,16 +298,15 @@ __global__ __launch_bounds__(NW * kWave, (Cfg<T, D>::min_wgs)) void paged_split_
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
   };
 
-  if (i0 + wave < i1) {
-    const Where first = find(i0 + wave);
-    load(kreg, p.c.k, knew, i0 + wave, first);
-    load(vreg, p.c.v, vnew, i0 + wave, first);
-    for (int i = i0 + wave; i < i1; i += NW) {
-      if (seen.whole(seen.tile(i) * kTile, n_cache)) attend(i, std::integral_constant<bool, true>{});
-      else attend(i, std::integral_constant<bool, false>{});
-    }
+  if (mine > 0) {
+    ask(0);
+    turn(0);
+    const Where first = find(0);
+    load(kreg, p.c.k, first);
+    load(vreg, p.c.v, first);
+    for (int k = 0; k < mine; ++k) attend(k);
   }
-  if (pages.bad() && n_cache > 0 && lane == 0) report(p.c.dev_err, kDevBadPage);
+  if (worst >= static_cast<unsigned>(p.c.n_pages) && n_cache > 0) report(p.c.dev_err, kDevBadPage);
 
   const float l_tot = group4_sum(l_run);
   __threadfence_block();                                  // logits, before other waves read them
@@ -366,7 +397,7 @@ __global__ __launch_bounds__(NW * kWave, (Cfg<T, D>::min_wgs)) void paged_split_
   float *weight = p.c.weight + cunit * p.c.cap;
   for (int k = threadIdx.x; k < seen.total * (kTile / 4); k += kThreads)
     add_weights(weight, lg, p.logit_pitch, p.group, seen.tile(k / (kTile / 4)) * kTile + k % (kTile / 4) * 4, seen,
-                n_cache, put, s_top, s_inv);
+                n_cache, p.c.cap, put, s_top, s_inv);
 }
 
 // Joins the splits.  Workgroups [0, units * group) take one query head of one unit
@@ -426,7 +457,8 @@ __global__ __launch_bounds__(kMergeThreads) void paged_merge_kernel(PagedDecodeP
       fresh = !u.bad();
     }
     add_weights(p.c.weight + cunit * p.c.cap, p.logits + static_cast<size_t>(unit) * G * p.logit_pitch, p.logit_pitch,
-                G, seen.tile(k / (kTile / 4)) * kTile + k % (kTile / 4) * 4, seen, n, fresh, s_top, s_inv);
+                G, seen.tile(k / (kTile / 4)) * kTile + k % (kTile / 4) * 4, seen, n, p.c.cap,
+                fresh, s_top, s_inv);
     return;
   }
 
