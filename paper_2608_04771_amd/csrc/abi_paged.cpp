@@ -20,6 +20,8 @@ bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 
 
 int64_t capacity_of(const reco_paged_cache_t *c) { return static_cast<int64_t>(c->max_pages) * c->page_rows; }
 
+int row_bytes_of(const reco_paged_cache_t *c) { return c->head_dim * (c->dtype == RECO_F32 ? 4 : 2); }
+
 bool paged_ok(const reco_paged_cache_t *c) {
   return c && c->k && c->v && c->pages && c->len && c->n_layers >= 1 && c->batch >= 1 && c->n_kv_heads >= 1 &&
          c->n_pages >= 1 && c->page_rows >= 1 && c->max_pages >= 1 && aligned16(c->k) && aligned16(c->v) &&
@@ -182,7 +184,7 @@ size_t reco_paged_evict_workspace_size(const reco_paged_cache_t *cache, int32_t 
   if (!paged_ok(cache) || paged_supported(cache) != RECO_OK) return 0;
   const int units = units_of(cache, n_layers);
   if (units < 1) return 0;
-  return reco::paged_evict_workspace_bytes(units, static_cast<int>(capacity_of(cache)), true);
+  return reco::paged_evict_workspace_bytes(units, static_cast<int>(capacity_of(cache)), row_bytes_of(cache), true);
 }
 
 reco_status_t reco_paged_evict(const reco_paged_cache_t *cache, int32_t layer0, int32_t n_layers,
@@ -198,14 +200,14 @@ reco_status_t reco_paged_evict(const reco_paged_cache_t *cache, int32_t layer0, 
 
   reco::PagedEvictParams p{};
   p.c = paged_cache(cache, layer0, n_layers, dev_err);
-  const size_t need = reco::paged_evict_workspace_bytes(units, p.c.cap, kept_idx == nullptr);
+  const size_t need = reco::paged_evict_workspace_bytes(units, p.c.cap, row_bytes_of(cache), kept_idx == nullptr);
   if (!ws || ws_bytes < need || (reinterpret_cast<uintptr_t>(ws) & 255)) return RECO_ERR_WORKSPACE;
   p.budget = budget;
   p.budget_stride = budget_layer_stride;
   p.sinks = sinks;
   p.recent = recent;
   p.idx = kept_idx;
-  reco::paged_evict_place(p, ws);
+  reco::paged_evict_place(p, units, row_bytes_of(cache), ws);
   return reco::hip_status(reco::launch_paged_evict(p, cache->dtype, cache->head_dim, stream));
 }
 

@@ -110,10 +110,17 @@ struct PagedEvictParams {
   int32_t *idx;           // [units][cap]  kept rows (the caller's buffer or the workspace)
   bool idx_wanted;        // the caller's: written for units that keep everything, too
   int32_t *kept;          // [units]  rows after the call, or -1 where nothing moves
+  int32_t *state;         // [units][state_pitch]  chunks taken, loaded in order, and loaded (one flag each)
+  int64_t state_pitch;
   int sinks, recent;
+  int chunk_rows;         // rows of a chunk of the compaction
+  int workers;            // its workgroups for a unit
 };
-size_t paged_evict_workspace_bytes(int units, int capacity, bool need_idx);
-void paged_evict_place(PagedEvictParams &p, void *ws);
+constexpr int kEvictState = 2;
+constexpr int kEvictWorkers = 32;
+constexpr int evict_chunk_rows(int row_bytes) { return 32768 / row_bytes; }
+size_t paged_evict_workspace_bytes(int units, int capacity, int row_bytes, bool need_idx);
+void paged_evict_place(PagedEvictParams &p, int units, int row_bytes, void *ws);
 hipError_t launch_paged_evict(const PagedEvictParams &p, int dtype, int head_dim, hipStream_t s);
 
 }  // namespace reco

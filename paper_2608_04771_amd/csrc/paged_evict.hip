@@ -8,10 +8,14 @@
 //   wave owns a stretch of rows, 64 at a time, so ballots and one sum over the
 //   waves' counts give every kept row its place.  Up to kHeld weights a thread stay
 //   in registers.
-// compact: one workgroup per unit and 128-byte column of K or V, or per unit's
-//   weights, moves row idx[p] to row p in ascending chunks.  idx[p] >= p, so a
-//   chunk's rows, once all are loaded, can be stored over anything that earlier
-//   chunks held, and rows that later chunks read lie behind.
+// compact: moves row idx[p] to row p, K, V and weight, in chunks of 32 KB of K and of V
+//   that a unit's workgroups take in ascending order.  idx[p] >= p, so a chunk's places
+//   hold rows that it or an earlier chunk moves: a workgroup loads its chunk into
+//   registers, says so, waits until all earlier chunks of the unit are loaded, and
+//   stores.  Loading waits for nothing and chunks are taken in order by workgroups that
+//   run, so the wait ends whatever the order of dispatch.  It is bound by the rows'
+//   bytes (112 units, 9,516 of 16,384 rows of 2 x 256 bytes: 225 us, 4.9 TB/s; with
+//   chunks of 16 KB 248); a chunk of rows that stay where they are is not read.
 #include "paged_device.hpp"
 
 namespace reco {
@@ -179,61 +183,94 @@ __global__ __launch_bounds__(kSelThreads) void evict_select_kernel(PagedEvictPar
     pos += __popcll(keep_mask);
     eq += __popcll(eq_mask);
   });
+  int32_t *state = p.state + static_cast<size_t>(unit) * p.state_pitch;
+  for (int i = tid; i < kEvictState + (m + p.chunk_rows - 1) / p.chunk_rows; i += kSelThreads) state[i] = 0;
   if (tid == 0) p.kept[unit] = m;
 }
 
 constexpr int kCompThreads = 256;
-constexpr int kSliceBytes = 128;
-constexpr int kLanesPerRow = kSliceBytes / 16;
-constexpr int kRowsPerPass = kCompThreads / kLanesPerRow;
-constexpr int kRowsPerThread = 8;
-constexpr int kChunkRows = kRowsPerPass * kRowsPerThread;
+// LDS that no one uses keeps three workgroups on a compute unit: more of them in flight
+// cost rate (all 28 layers of a 7B shape, per call: 257 us with 2.6 of them, 268 with 1.3).
+constexpr int kCompLds = 48 * 1024;
+constexpr int kMaxSpins = 1 << 20;           // of a microsecond or so
+
+__device__ __forceinline__ int relaxed_load(const int32_t *p) {
+  return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
 
 template <int ROWB>
 __global__ __launch_bounds__(kCompThreads) void evict_compact_kernel(PagedEvictParams p) {
-  constexpr int kSlices = ROWB / kSliceBytes;
+  constexpr int kLanesPerRow = ROWB / 16;
+  constexpr int kRowsPerPass = kCompThreads / kLanesPerRow;
+  constexpr int kPasses = evict_chunk_rows(ROWB) / kRowsPerPass;
+  constexpr int kRows = kPasses * kRowsPerPass;
+  static_assert(kRows <= kCompThreads, "a weight a thread");
+  __shared__ int s_ticket;
+
   const int unit = blockIdx.x;
-  const int job = blockIdx.y;                            // K slices, V slices, weights
+  const int tid = threadIdx.x;
   const size_t cunit = p.c.unit(unit);
   const int m = p.kept[unit];
   if (m < 0) return;
   const int32_t *idx = p.idx + static_cast<size_t>(unit) * p.c.cap;
   const int32_t *table = p.c.pages + cunit * static_cast<size_t>(p.c.max_pages);
   const int shift = p.c.page_shift, mask = (1 << shift) - 1;
+  int32_t *ticket = p.state + static_cast<size_t>(unit) * p.state_pitch;
+  int32_t *prefix = ticket + 1;                          // chunks before this one are known to be loaded
+  int32_t *loaded = ticket + kEvictState;
+  unsigned char *k = reinterpret_cast<unsigned char *>(p.c.k) + tid % kLanesPerRow * 16;
+  unsigned char *v = reinterpret_cast<unsigned char *>(p.c.v) + tid % kLanesPerRow * 16;
+  float *weight = p.c.weight + cunit * p.c.cap;
+  const auto at = [&](int row) { return ((static_cast<size_t>(table[row >> shift]) << shift) + (row & mask)) * ROWB; };
 
-  if (job == 2 * kSlices) {
-    float *weight = p.c.weight + cunit * p.c.cap;
-    for (int c0 = 0; c0 < m; c0 += kCompThreads * 8) {
-      float x[8];
+  if (tid == 0) s_ticket = atomicAdd(ticket, 1);
+  __syncthreads();
+  for (;;) {
+    const int c = s_ticket;
+    const int r0 = c * kRows;
+    if (r0 >= m) break;                                  // the same for the workgroup
+    const int last = min(r0 + kRows, m) - 1;
+    const bool moves = idx[last] != last;
+    int from[kPasses], wfrom = 0;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) x[i] = weight[idx[min(c0 + i * kCompThreads + (int)threadIdx.x, m - 1)]];
-      __syncthreads();
+    for (int i = 0; i < kPasses; ++i) from[i] = idx[min(r0 + i * kRowsPerPass + tid / kLanesPerRow, last)];
+    if (tid < kRows) wfrom = idx[min(r0 + tid, last)];
+    const int known = relaxed_load(prefix);
+    u32x4v kr[kPasses], vr[kPasses];
+    float w = 0.f;
+    if (moves) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const int d = c0 + i * kCompThreads + threadIdx.x;
-        if (d < m) weight[d] = x[i];
+      for (int i = 0; i < kPasses; ++i) {
+        const size_t o = at(from[i]);
+        kr[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4v *>(k + o));
+        vr[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4v *>(v + o));
       }
+      if (tid < kRows) w = weight[wfrom];
     }
-    if (threadIdx.x == 0) p.c.len[cunit] = m;
-    return;
-  }
-  unsigned char *base = reinterpret_cast<unsigned char *>(job < kSlices ? p.c.k : p.c.v) +
-                        (job % kSlices) * kSliceBytes + (threadIdx.x % kLanesPerRow) * 16;
-  const int rrow = threadIdx.x / kLanesPerRow;
-  const auto at = [&](int row) {
-    return base + ((static_cast<size_t>(table[row >> shift]) << shift) + (row & mask)) * ROWB;
-  };
-  for (int c0 = 0; c0 < m; c0 += kChunkRows) {
-    u32x4v v[kRowsPerThread];
-#pragma unroll
-    for (int i = 0; i < kRowsPerThread; ++i)
-      v[i] = *reinterpret_cast<const u32x4v *>(at(idx[min(c0 + i * kRowsPerPass + rrow, m - 1)]));
-    __syncthreads();   // every row of this chunk is loaded before any of its places is overwritten
-#pragma unroll
-    for (int i = 0; i < kRowsPerThread; ++i) {
-      const int d = c0 + i * kRowsPerPass + rrow;
-      if (d < m) *reinterpret_cast<u32x4v *>(at(d)) = v[i];
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");     // the rows are in registers
+    __syncthreads();
+    if (tid == 0) {
+      __hip_atomic_store(&loaded[c], 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      s_ticket = atomicAdd(ticket, 1);
     }
+    // Bounded, so that a workspace that another call writes meanwhile cannot hang the device.
+    for (int f = known + tid, spins = 0; f < c; f += kCompThreads)
+      while (!relaxed_load(&loaded[f]) && ++spins < kMaxSpins) __builtin_amdgcn_s_sleep(1);
+    __syncthreads();
+    if (tid == 0) atomicMax(prefix, c);
+    if (moves) {
+#pragma unroll
+      for (int i = 0; i < kPasses; ++i) {
+        const int row = r0 + i * kRowsPerPass + tid / kLanesPerRow;
+        if (row <= last) {
+          const size_t o = at(row);
+          __builtin_nontemporal_store(kr[i], reinterpret_cast<u32x4v *>(k + o));
+          __builtin_nontemporal_store(vr[i], reinterpret_cast<u32x4v *>(v + o));
+        }
+      }
+      if (r0 + tid <= last && tid < kRows) weight[r0 + tid] = w;
+    }
+    if (c == 0 && tid == 0) p.c.len[cunit] = m;
   }
 }
 
@@ -245,10 +282,10 @@ hipError_t launch_paged_evict(const PagedEvictParams &p, int dtype, int head_dim
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   const int rowb = head_dim * (dtype == 0 ? 4 : 2);
-  const dim3 grid(units, 2 * (rowb / kSliceBytes) + 1);
-  if (rowb == 128) hipLaunchKernelGGL(evict_compact_kernel<128>, grid, dim3(kCompThreads), 0, s, p);
-  else if (rowb == 256) hipLaunchKernelGGL(evict_compact_kernel<256>, grid, dim3(kCompThreads), 0, s, p);
-  else hipLaunchKernelGGL(evict_compact_kernel<512>, grid, dim3(kCompThreads), 0, s, p);
+  const dim3 grid(units, p.workers);
+  if (rowb == 128) hipLaunchKernelGGL(evict_compact_kernel<128>, grid, dim3(kCompThreads), kCompLds, s, p);
+  else if (rowb == 256) hipLaunchKernelGGL(evict_compact_kernel<256>, grid, dim3(kCompThreads), kCompLds, s, p);
+  else hipLaunchKernelGGL(evict_compact_kernel<512>, grid, dim3(kCompThreads), kCompLds, s, p);
   return hipGetLastError();
 }
 

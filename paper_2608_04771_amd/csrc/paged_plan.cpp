@@ -118,19 +118,32 @@ void prefill_place(PagedPrefillParams &p, int head_dim, void *ws) {
   p.part_ml = p.part_o + units * p.blocks * p.splits * kPrefillRows * head_dim;
 }
 
-size_t paged_evict_workspace_bytes(int units, int capacity, bool need_idx) {
-  size_t bytes = aligned(static_cast<size_t>(units) * sizeof(int32_t));
-  if (need_idx) bytes += static_cast<size_t>(units) * capacity * sizeof(int32_t);
+static int64_t evict_state_pitch(int capacity, int row_bytes) {
+  const int rows = evict_chunk_rows(row_bytes);
+  return kEvictState + (static_cast<int64_t>(capacity) + rows - 1) / rows;
+}
+
+size_t paged_evict_workspace_bytes(int units, int capacity, int row_bytes, bool need_idx) {
+  const size_t n = static_cast<size_t>(units);
+  size_t bytes = aligned(n * sizeof(int32_t)) + aligned(n * evict_state_pitch(capacity, row_bytes) * sizeof(int32_t));
+  if (need_idx) bytes += n * capacity * sizeof(int32_t);
   return bytes;
 }
 
-void paged_evict_place(PagedEvictParams &p, void *ws) {
-  const int units = p.c.n_layers * p.c.batch * p.c.hkv;
+void paged_evict_place(PagedEvictParams &p, int units, int row_bytes, void *ws) {
   char *at = static_cast<char *>(ws);
   p.kept = reinterpret_cast<int32_t *>(at);
   at += aligned(static_cast<size_t>(units) * sizeof(int32_t));
+  p.state = reinterpret_cast<int32_t *>(at);
+  p.state_pitch = evict_state_pitch(p.c.cap, row_bytes);
+  at += aligned(static_cast<size_t>(units) * p.state_pitch * sizeof(int32_t));
   p.idx_wanted = p.idx != nullptr;
   if (!p.idx) p.idx = reinterpret_cast<int32_t *>(at);
+  p.chunk_rows = evict_chunk_rows(row_bytes);
+  // A workgroup for each chunk, up to where a few units alone fill the device; those of
+  // units that keep everything, or fewer rows, end at once.
+  const int64_t chunks = p.state_pitch - kEvictState;
+  p.workers = static_cast<int>(chunks < kEvictWorkers ? chunks : kEvictWorkers);
 }
 
 }  // namespace reco
