@@ -238,3 +238,52 @@ def test_graph_replays_match_eager():
         torch.cuda.synchronize()
         assert torch.equal(out, o) and torch.equal(lse, z), rep
         assert torch.equal(cap.k.view(torch.int16), ref.k.view(torch.int16)), rep
+
+
+@pytest.mark.parametrize("dtype,D,G,L,T,sinks,window", [
+    (BF, 128, 4, 0, 100, 0, 0), (BF, 128, 7, 70, 100, 3, 40), (F32, 64, 1, 33, 70, 0, 0), (F32, 128, 3, 64, 40, 2, 16),
+    (BF, 64, 1, 200, 90, 0, 33), (BF, 64, 16, 5, 20, 0, 0)])
+def test_values_that_only_some_tokens_see(dtype, D, G, L, T, sinks, window):
+    # infinities and NaN in V reach the tokens that see them, and their columns, alone
+    p = Paged(np.full((1, 1, 2), L), 16, D, dtype, spare=T, seed=D + T)
+    q, kn, vn = _inputs(p, G, T, 11)
+    inf, nan = float("inf"), float("nan")
+    for u in np.ndindex(1, 1, 2):
+        for r, c, x in ((1, 0, nan), (L + T // 2, 3, inf), (L + T // 2, 5, nan), (L + T // 3, 40, -inf), (L + T - 1, 17, nan),
+                        (L + T // 2 + 1, 3, -inf), (L // 2, 60, inf), (L + 2, D - 1, inf)):
+            if r >= L:
+                vn[u][r - L, c] = x
+            else:
+                page, row = p.where(u, [r])
+                p.v[page, row, c] = x
+    cache = p.upload()
+    out, lse = B.reco_paged_prefill_attn(cache, q.cuda(), kn.cuda(), vn.cuda(), None, sinks, window)
+    out, lse = out.cpu().double(), lse.cpu()
+    s = 1 / math.sqrt(D)
+    for u in np.ndindex(1, 1, 2):
+        k, v = p.rows(u)
+        k, v = torch.cat([k, kn[u]]), torch.cat([v, vn[u]])
+        for t in range(T):
+            ref, rl, _ = attend(k, v, q[u[:2]][u[2] * G:(u[2] + 1) * G, t], L + t, s, sinks, window)
+            got, fin = out[u[:2]][u[2] * G:(u[2] + 1) * G, t], torch.isfinite(ref)
+            what = f"unit {u} token {t}"
+            for same in (torch.isnan, torch.isposinf, torch.isneginf):
+                assert torch.equal(same(got), same(ref)), what
+            close_out(got[fin], ref[fin], v, dtype, what)
+            close_lse(lse[u[:2]][u[2] * G:(u[2] + 1) * G, t], rl, dtype, what)
+
+
+@pytest.mark.parametrize("dtype,D,G", [(BF, 128, 4), (F32, 64, 2)])
+def test_earlier_tokens_do_not_depend_on_later_rows(dtype, D, G):
+    # the run's last rows hold NaN in K and V: all tokens before them get the bits they
+    # would get if they were ordinary
+    T = 90
+    p = Paged(np.full((1, 1, 2), 50), 16, D, dtype, spare=T, seed=4)
+    q, kn, vn = _inputs(p, G, T, 12)
+    a = B.reco_paged_prefill_attn(p.upload(), q.cuda(), kn.cuda(), vn.cuda())
+    for x in (kn, vn):
+        x[..., T - 20:, :] = float("nan")
+    b = B.reco_paged_prefill_attn(p.upload(), q.cuda(), kn.cuda(), vn.cuda())
+    for x, y in zip(a, b):
+        assert torch.equal(x[:, :, :, :T - 20], y[:, :, :, :T - 20])
+        assert torch.isnan(y[:, :, :, T - 20:]).all()
