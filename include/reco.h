@@ -119,8 +119,8 @@ typedef struct reco_kv_cache {
  * of page pages[unit][j / page_rows], so a unit can hold
  * capacity = max_pages * page_rows rows, and pages that its rows do not reach
  * need not exist: only the first ceil(len / page_rows) ids of a unit (and the
- * ids of rows that a call appends) are ever read.  Ids outside [0, n_pages) among
- * these set RECO_DEV_BAD_PAGE.  Several units may share pages that no call
+ * ids of rows that a call appends) count.  Ids outside [0, n_pages) among these set
+ * RECO_DEV_BAD_PAGE.  Several units may share pages that no call
  * writes to; what a call writes (appended rows, evicted units) has to lie in
  * pages of one unit, each once in its list. */
 typedef struct reco_paged_cache {
@@ -286,7 +286,7 @@ reco_status_t reco_decode_attn_noalloc(const reco_kv_cache_t *cache, int32_t lay
  * and an appended row's weight is set to its own (nothing has to be cleared for
  * it); weights of rows that are not seen are left as they are.
  * A unit with no rows to see gets out = 0 and lse = -inf.  Rows whose page id is bad
- * are taken from page 0; an append whose own page id is bad is not performed (the
+ * are taken from the pool's last page; an append whose own page id is bad is not performed (the
  * token still takes part in the attention).  Tensors are 16-byte aligned; the
  * workspace, whose size depends on the current device and on whether weights are
  * kept, 256-byte aligned.  Sizes whose grid would pass 2^32 threads (far beyond any
@@ -312,8 +312,9 @@ reco_status_t reco_paged_decode_attn(const reco_paged_cache_t *cache, int32_t la
  *   k_new, v_new : [n_layers][batch][n_kv_heads][n_tokens][head_dim]
  *   n_new        : nullable [batch] int32 in [0, n_tokens]
  *   out          : like q (output);  lse : nullable, like q without head_dim, fp32
- * Places past a sequence's tokens count for nothing and are not written.  A run that does not
- * fit its unit's capacity (RECO_DEV_APPEND_OVERFLOW), or whose rows' page ids are bad
+ * Places past a sequence's tokens count for nothing and are not written; infinities
+ * and NaN in rows reach the tokens that see them alone.  A run that does not fit
+ * its unit's capacity (RECO_DEV_APPEND_OVERFLOW), or whose rows' page ids are bad
  * (RECO_DEV_BAD_PAGE), is attended but not stored; a bad stored length
  * (RECO_DEV_BAD_LENGTH) is clamped for the attention and nothing is stored; a bad
  * n_new (RECO_DEV_BAD_LENGTH) counts as 0.  q, k_new, v_new and out are 16-byte
@@ -347,7 +348,7 @@ reco_status_t reco_paged_prefill_attn(const reco_paged_cache_t *cache, int32_t l
  * cache->weight has to be given; +inf ranks above all, and a negative or NaN weight
  * among the rows to choose from is RECO_DEV_BAD_SCORE.  A unit whose length, budget,
  * page ids or weights are bad is left unchanged (kept_idx unspecified) and dev_err
- * is set.  The workspace is 256-byte aligned. */
+ * is set.  The workspace is 256-byte aligned and serves one call at a time. */
 size_t reco_paged_evict_workspace_size(const reco_paged_cache_t *cache, int32_t n_layers);
 reco_status_t reco_paged_evict(const reco_paged_cache_t *cache, int32_t layer0, int32_t n_layers,
                                const int32_t *budget, int64_t budget_layer_stride, int32_t sinks,
