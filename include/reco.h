@@ -319,7 +319,7 @@ reco_status_t reco_paged_decode_attn(const reco_paged_cache_t *cache, int32_t la
  * (RECO_DEV_BAD_LENGTH) is clamped for the attention and nothing is stored; a bad
  * n_new (RECO_DEV_BAD_LENGTH) counts as 0.  q, k_new, v_new and out are 16-byte
  * aligned, the workspace 256-byte aligned.  n_tokens >= 1; n_tokens * G <= 2^28 and
- * fewer than 2^24 workgroups (larger: RECO_ERR_UNSUPPORTED). */
+ * fewer than 2^22 workgroups (larger: RECO_ERR_UNSUPPORTED). */
 size_t reco_paged_prefill_attn_workspace_size(const reco_paged_cache_t *cache, int32_t n_layers,
                                               int32_t n_q_heads, int32_t n_tokens);
 reco_status_t reco_paged_prefill_attn(const reco_paged_cache_t *cache, int32_t layer0, int32_t n_layers,

@@ -165,7 +165,7 @@ reco_status_t reco_paged_prefill_attn(const reco_paged_cache_t *cache, int32_t l
   p.group = G;
   p.by_group = reco::FastDiv(G);
   p.tokens = n_tokens;
-  p.rows = reco::prefill_rows(units, n_tokens, G, cache->dtype, cus);
+  p.rows = reco::prefill_rows(units, n_tokens, G, p.c.cap, window, cache->dtype, cus);
   p.blocks = reco::prefill_blocks(n_tokens, G, p.rows);
   p.splits = p.rows == reco::kPrefillRows
                  ? reco::prefill_splits(units, p.blocks, p.c.cap, sinks, window, tile_rows, cus) : 1;
@@ -174,7 +174,7 @@ reco_status_t reco_paged_prefill_attn(const reco_paged_cache_t *cache, int32_t l
   p.scale_log2 = scale * 1.4426950408889634f;
   p.by_splits = reco::FastDiv(p.splits);
   if (!reco::prefill_fits_grid(p)) return RECO_ERR_UNSUPPORTED;
-  p.near = reco::prefill_near(units * p.blocks, p.splits);
+  reco::prefill_pieces(p, units);
   reco::prefill_place(p, cache->head_dim, ws);
   return reco::hip_status(reco::launch_paged_prefill(p, cache->dtype, cache->head_dim, stream));
 }

@@ -73,6 +73,7 @@ hipError_t launch_paged_decode(const PagedDecodeParams &p, int dtype, int head_d
 constexpr int kPrefillRows = 128;        // query rows of a workgroup
 constexpr int kPrefillLongRows = 256;    // of one for long bf16 runs
 constexpr int kPrefillMaxSplits = 64;
+constexpr int kXcds = 8;
 struct PagedPrefillParams {
   PagedCache c;
   const void *q;          // [n_layers][batch][hq][tokens][D]
@@ -84,20 +85,22 @@ struct PagedPrefillParams {
   int32_t *len_in;        // [units]  lengths before the append
   float *part_o;          // [units][blocks][splits][kPrefillRows][D]
   float *part_ml;         // [units][blocks][splits][2][kPrefillRows]
-  FastDiv by_splits, by_group;
+  FastDiv by_splits, by_group, by_near;
   int group, tokens, blocks, splits;
   int rows;               // of a block: kPrefillRows, or kPrefillLongRows with one split
-  int near;               // neighbouring workgroups that share an XCD
+  int pieces;             // of a unit's blocks, each for one XCD, where there are many; else 0
+  int near;               // blocks of a piece
+  bool spread;            // a piece's blocks are every pieces-th, not neighbours
   int sinks, window;
   float scale_log2;
 };
 int prefill_blocks(int tokens, int group, int rows);
-int prefill_rows(int units, int tokens, int group, int dtype, int compute_units);
+int prefill_rows(int units, int tokens, int group, int capacity, int window, int dtype, int compute_units);
 constexpr int prefill_tile_rows(int dtype) { return dtype == 0 ? 32 : 64; }   // keys of a tile: fp32, bf16
 int prefill_splits(int units, int blocks, int capacity, int sinks, int window, int tile_rows, int compute_units);
 size_t prefill_workspace_bytes(int units, int tokens, int capacity, int group, int head_dim, int tile_rows,
                                int compute_units);
-int prefill_near(int workgroups, int splits);
+void prefill_pieces(PagedPrefillParams &p, int units);
 bool prefill_fits_grid(const PagedPrefillParams &p);
 void prefill_place(PagedPrefillParams &p, int head_dim, void *ws);
 hipError_t launch_paged_prefill(const PagedPrefillParams &p, int dtype, int head_dim, hipStream_t s);

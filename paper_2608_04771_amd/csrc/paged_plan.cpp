@@ -69,10 +69,20 @@ int prefill_blocks(int tokens, int group, int rows) {
   return static_cast<int>((static_cast<int64_t>(tokens) * group + rows - 1) / rows);
 }
 
-// Blocks of 256 rows for bf16 where they give every compute unit two workgroups in turn.
-int prefill_rows(int units, int tokens, int group, int dtype, int compute_units) {
+// Blocks of 256 rows for bf16, whose eight waves share a tile, where a block sees many
+// keys (1,024 by what the call can know: 2,048 tokens of 32 units of 4 heads 204 -> 191 us
+// against blocks of 128; prompts of 200 to 512 tokens 40 -> 45) and the blocks fill the
+// last round of two workgroups on every compute unit, or it is one of many (at 1.5 rounds,
+// 2,452 tokens of 16 units of 5 heads, 181 -> 213 us; at 4, 8,192 of 16 of 4, 1,178 -> 1,066).
+int prefill_rows(int units, int tokens, int group, int capacity, int window, int dtype, int compute_units) {
+  if (dtype != 1) return kPrefillRows;
   const int64_t blocks = static_cast<int64_t>(units) * prefill_blocks(tokens, group, kPrefillLongRows);
-  return dtype == 1 && blocks >= 2 * compute_units ? kPrefillLongRows : kPrefillRows;
+  const int64_t round = 2 * static_cast<int64_t>(compute_units), rounds = (blocks + round - 1) / round;
+  const int own = tokens < capacity ? tokens : capacity;
+  int keys = capacity - own / 2;
+  if (window > 0 && window < keys) keys = window;
+  const bool even = blocks >= 3 * round || 8 * blocks >= 7 * rounds * round;
+  return keys >= 1024 && even ? kPrefillLongRows : kPrefillRows;
 }
 
 // Key tiles are split where there are too few blocks of query rows for two workgroups
@@ -99,13 +109,35 @@ size_t prefill_workspace_bytes(int units, int tokens, int capacity, int group, i
   return bytes;
 }
 
-// A round of an XCD's compute units, where every XCD has four rounds and more.
-int prefill_near(int workgroups, int splits) { return splits == 1 && workgroups >= 1024 ? 32 : 1; }
+// Where every XCD has four rounds of its compute units and more, a piece is up to one
+// round's blocks of a unit: as many as leave the XCDs with the same number of pieces, or
+// nearly.  Without a window a block's work grows with its place, so a piece takes blocks
+// from everywhere (its XCD's others wait for none: 8,192 tokens of 16 units of 4 heads
+// 1,601 -> 1,031 us); with one, neighbours see the same keys.
+void prefill_pieces(PagedPrefillParams &p, int units) {
+  const int64_t all = static_cast<int64_t>(units) * p.blocks;
+  p.pieces = p.near = 0;
+  p.spread = p.window == 0 || p.window >= p.tokens;
+  p.by_near = FastDiv(1);
+  if (p.splits > 1 || all < 1024) return;
+  double least = 1e30;
+  for (int near = 32; near >= 8; --near) {
+    const int pieces = (p.blocks + near - 1) / near;
+    const int size = (p.blocks + pieces - 1) / pieces;
+    const int64_t turns = (static_cast<int64_t>(units) * pieces + kXcds - 1) / kXcds;
+    const double cost = static_cast<double>(turns * kXcds * size) / static_cast<double>(all);
+    if (cost > 0.97 * least) continue;                   // smaller pieces have to be worth it
+    least = cost;
+    p.pieces = pieces;
+    p.near = size;
+  }
+  p.by_near = FastDiv(p.near);
+}
 
 bool prefill_fits_grid(const PagedPrefillParams &p) {
   const int64_t units = static_cast<int64_t>(p.c.n_layers) * p.c.batch * p.c.hkv;
   const int64_t most = int64_t{1} << 24;                 // workgroups of 256 threads
-  return units * p.blocks * p.splits < most / 2 &&       // of 512, and rounded up
+  return units * p.blocks * p.splits < most / 4 &&       // of 512, and pieces rounded up
          p.tokens / 64 + 1 + (p.splits > 1 ? static_cast<int64_t>(p.blocks) * 16 : 0) < most;
 }
 

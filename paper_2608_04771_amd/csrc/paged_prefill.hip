@@ -32,7 +32,6 @@ typedef const __attribute__((address_space(1))) unsigned int global_u32;
 
 constexpr int kRows = kPrefillRows;          // query rows of a workgroup
 constexpr int kWaves = 4;
-constexpr int kXcds = 8;
 constexpr int kWaitLoads = 0x0f70;           // vmcnt(0)
 constexpr float kSlack = 8.f;                // log2 units that a maximum may grow before O follows
 
@@ -356,17 +355,21 @@ __global__ __launch_bounds__(NW * kWave, 2) void prefill_kernel(PagedPrefillPara
   const int half = lane >> 5;
   const int col = lane & 31;
   const int units = p.c.n_layers * p.c.batch * p.c.hkv;
-  // Workgroups go to the XCDs in turn.  Where there are many, `near` neighbours, which see
-  // mostly the same keys, take turns on one of them and share its L2.
-  int id = blockIdx.x;
-  if (p.near > 1) {
-    const int slot = id / kXcds;
-    id = (slot / p.near * kXcds + id % kXcds) * p.near + slot % p.near;
-    if (id >= units * p.blocks) return;
+  // Workgroups go to the XCDs in turn.  Where there are many, a piece of a unit's blocks,
+  // which see mostly the same keys, takes its turn on one XCD and shares its L2.
+  int unit = blockIdx.y, block, split = 0;
+  if (p.pieces > 0) {
+    const int slot = blockIdx.x / kXcds;
+    const int turn = p.by_near.of(slot), pos = p.by_near.rest(slot);
+    const int piece = turn * kXcds + blockIdx.x % kXcds;
+    unit = piece / p.pieces;
+    block = p.spread ? piece % p.pieces + p.pieces * pos : piece % p.pieces * p.near + pos;
+    if (unit >= units || block >= p.blocks) return;
+  } else {
+    block = p.by_splits.of(blockIdx.x);
+    split = p.by_splits.rest(blockIdx.x);
   }
-  const int unit = p.near > 1 ? id / p.blocks : blockIdx.y;      // many workgroups take one split
-  const int block = p.blocks - 1 - (p.near > 1 ? id - unit * p.blocks : p.by_splits.of(id));   // the longest first
-  const int split = p.near > 1 ? 0 : p.by_splits.rest(id);
+  block = p.blocks - 1 - block;                          // the longest first
   const size_t cunit = p.c.unit(unit);
 
   const int len_in = p.c.len[cunit];
@@ -771,8 +774,8 @@ __global__ __launch_bounds__(256) void prefill_finish_kernel(PagedPrefillParams 
 template <typename T, int D>
 hipError_t launch_typed(const PagedPrefillParams &p, hipStream_t s) {
   const int units = p.c.n_layers * p.c.batch * p.c.hkv;
-  const int turn = kXcds * p.near;
-  const dim3 grid = p.near > 1 ? dim3((units * p.blocks + turn - 1) / turn * turn) : dim3(p.blocks * p.splits, units);
+  const dim3 grid = p.pieces > 0 ? dim3((units * p.pieces + kXcds - 1) / kXcds * kXcds * p.near)
+                                 : dim3(p.blocks * p.splits, units);
   if constexpr (sizeof(T) == 2) {
     if (p.rows == kPrefillLongRows)
       hipLaunchKernelGGL((prefill_kernel<T, D, 8>), grid, dim3(8 * kWave), 0, s, p);

@@ -287,3 +287,35 @@ def test_earlier_tokens_do_not_depend_on_later_rows(dtype, D, G):
     for x, y in zip(a, b):
         assert torch.equal(x[:, :, :, :T - 20], y[:, :, :, :T - 20])
         assert torch.isnan(y[:, :, :, T - 20:]).all()
+
+
+@pytest.mark.parametrize("D,sinks,window", [(128, 0, 0), (128, 5, 1090), (64, 0, 0), (64, 70, 1024)])
+@pytest.mark.parametrize("page", [16, 128])
+def test_blocks_of_256_rows(D, sinks, window, page):
+    # runs that fill two rounds of such blocks, over caches with room for many keys
+    rng = np.random.RandomState(D + window)
+    lens = rng.randint(0, 400, (1, 40, 2))
+    lens[0, :8, 0] = [0, 1, 64, 63, 128, 65, 1000, 1300]
+    news = rng.randint(1, 241, 40)
+    news[:7] = [240, 0, 1, 64, 129, 240, 200]
+    p = Paged(lens, page, D, BF, spare=240, seed=D, weights=window == 1090, extra_pages=1024 // page)
+    _check(p, 12, 240, [int(x) for x in news], sinks, window, every=7)
+
+
+@pytest.mark.parametrize("window", [0, 1100])
+def test_long_prompts_in_blocks_of_256_rows(window):
+    _check(Paged([[[0, 700] * 4]], 64, 64, BF, spare=2400, seed=9), 12, 2400, None, 4, window, every=3)
+
+
+def test_values_that_only_some_tokens_see_in_blocks_of_256_rows():
+    # the run's second half holds NaN in K and V: the first half gets the bits it gets
+    # from ordinary rows
+    p = Paged(np.full((1, 40, 2), 30), 16, 128, BF, spare=240, seed=8, extra_pages=64)
+    q, kn, vn = (x.cuda() for x in _inputs(p, 12, 240, 13))
+    a = B.reco_paged_prefill_attn(p.upload(), q, kn, vn)
+    for x in (kn, vn):
+        x[..., 117:, :] = float("nan")
+    b = B.reco_paged_prefill_attn(p.upload(), q, kn, vn)
+    for x, y in zip(a, b):
+        assert torch.equal(x[:, :, :, :117], y[:, :, :, :117])
+        assert torch.isnan(y[:, :, :, 117:]).all()
