@@ -50,6 +50,7 @@ struct PagedDecodeParams {
   int32_t *len_in;        // [units]  lengths before the append, for the weights
   float *logits;          // [units][group][logit_pitch]  log2-domain logits, where weights are kept
   int64_t logit_pitch;
+  bool held_logits;       // in the workgroup instead
   FastDiv by_splits, by_group;
   int group, splits, cus;
   int sinks, window;      // window 0: every row is visible

@@ -102,7 +102,8 @@ __device__ __forceinline__ bool append_row(const PagedDecodeParams &p, size_t cu
 
 // Weights of four rows from `row` on: their probabilities summed over the queries.
 // seen: what the token sees; n: the rows cached before the call; fresh: row n was appended.
-// What the rows had is asked for first, so that it comes with the logits.
+// logits: query 0's of these rows, the others pitch apart.  What the rows had is asked for
+// first, so that it comes with the logits.
 __device__ __forceinline__ void add_weights(float *weight, const float *logits, int64_t pitch, int group, int row,
                                             const SeenTiles &seen, int n, int cap, bool fresh, const float *top,
                                             const float *inv) {
@@ -112,7 +113,7 @@ __device__ __forceinline__ void add_weights(float *weight, const float *logits, 
   float w[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
   for (int g = 0; g < group; ++g) {
-    const float4 x = *reinterpret_cast<const float4 *>(logits + g * pitch + row);
+    const float4 x = *reinterpret_cast<const float4 *>(logits + g * pitch);
     w[0] += fast_exp2(x.x - top[g]) * inv[g];
     w[1] += fast_exp2(x.y - top[g]) * inv[g];
     w[2] += fast_exp2(x.z - top[g]) * inv[g];
@@ -165,6 +166,7 @@ __global__ __launch_bounds__(NW * kWave, NW == 8 ? 1 : (Cfg<T, D>::min_wgs)) voi
 #pragma unroll
   for (int dt = 0; dt < C::dtiles; ++dt) o[dt] = f32x4_t{0.f, 0.f, 0.f, 0.f};
   unsigned char *stage = smem + wave * C::wave_stage;
+  extern __shared__ __attribute__((aligned(16))) float s_logits[];   // [tiles][group][kTile] where they are held
   float *logits = p.logits ? p.logits + (static_cast<size_t>(unit) * p.group + col) * p.logit_pitch + 4 * grp : nullptr;
 
   // Where the wave's tiles lie: each lane holds the place of 16 rows, so 32 tiles at a
@@ -247,9 +249,16 @@ __global__ __launch_bounds__(NW * kWave, NW == 8 ? 1 : (Cfg<T, D>::min_wgs)) voi
     float top = x[0];
 #pragma unroll
     for (int e = 1; e < 8; ++e) top = fmaxf(top, x[e]);
-    if (logits && col < p.group) {
-      *reinterpret_cast<float4 *>(logits + kb) = make_float4(x[0], x[1], x[2], x[3]);
-      *reinterpret_cast<float4 *>(logits + kb + 16) = make_float4(x[4], x[5], x[6], x[7]);
+    if (p.c.weight && col < p.group) {
+      const float4 a = make_float4(x[0], x[1], x[2], x[3]), b = make_float4(x[4], x[5], x[6], x[7]);
+      if (p.held_logits) {
+        float *to = s_logits + ((i0 + wave + NW * k) * p.group + col) * kTile + 4 * grp;
+        *reinterpret_cast<float4 *>(to) = a;
+        *reinterpret_cast<float4 *>(to + 16) = b;
+      } else {
+        *reinterpret_cast<float4 *>(logits + kb) = a;
+        *reinterpret_cast<float4 *>(logits + kb + 16) = b;
+      }
     }
     const float m_new = fmaxf(m_run, group4_max(top));
     const float ref = m_new == -INFINITY ? 0.f : m_new;   // logits of -inf alone have no weight
@@ -391,13 +400,18 @@ __global__ __launch_bounds__(NW * kWave, NW == 8 ? 1 : (Cfg<T, D>::min_wgs)) voi
     }
     if (threadIdx.x == 0) p.c.len[cunit] = len_in + 1;
   }
-  if (!p.logits) return;
+  if (!p.c.weight) return;
   __syncthreads();
   const float *lg = p.logits + static_cast<size_t>(unit) * p.group * p.logit_pitch;
   float *weight = p.c.weight + cunit * p.c.cap;
-  for (int k = threadIdx.x; k < seen.total * (kTile / 4); k += kThreads)
-    add_weights(weight, lg, p.logit_pitch, p.group, seen.tile(k / (kTile / 4)) * kTile + k % (kTile / 4) * 4, seen,
-                n_cache, p.c.cap, put, s_top, s_inv);
+  for (int k = threadIdx.x; k < seen.total * (kTile / 4); k += kThreads) {
+    const int i = k / (kTile / 4), in = k % (kTile / 4) * 4;
+    const int row = seen.tile(i) * kTile + in;
+    if (p.held_logits)
+      add_weights(weight, s_logits + i * p.group * kTile + in, kTile, p.group, row, seen, n_cache, p.c.cap, put, s_top, s_inv);
+    else
+      add_weights(weight, lg + row, p.logit_pitch, p.group, row, seen, n_cache, p.c.cap, put, s_top, s_inv);
+  }
 }
 
 // Joins the splits.  Workgroups [0, units * group) take one query head of one unit
@@ -456,9 +470,9 @@ __global__ __launch_bounds__(kMergeThreads) void paged_merge_kernel(PagedDecodeP
       u.row_at(u.entry(len_in), len_in);
       fresh = !u.bad();
     }
-    add_weights(p.c.weight + cunit * p.c.cap, p.logits + static_cast<size_t>(unit) * G * p.logit_pitch, p.logit_pitch,
-                G, seen.tile(k / (kTile / 4)) * kTile + k % (kTile / 4) * 4, seen, n, p.c.cap,
-                fresh, s_top, s_inv);
+    const int row = seen.tile(k / (kTile / 4)) * kTile + k % (kTile / 4) * 4;
+    add_weights(p.c.weight + cunit * p.c.cap, p.logits + static_cast<size_t>(unit) * G * p.logit_pitch + row, p.logit_pitch,
+                G, row, seen, n, p.c.cap, fresh, s_top, s_inv);
     return;
   }
 
@@ -529,10 +543,22 @@ __global__ __launch_bounds__(kMergeThreads) void paged_merge_kernel(PagedDecodeP
   if (tid == 0) p.c.len[cunit] = len_in + 1;
 }
 
+constexpr int kLdsBytes = 160 * 1024;        // of a compute unit
+
 template <typename T, int D>
 hipError_t launch_typed(const PagedDecodeParams &p, hipStream_t s) {
   const int units = p.c.n_layers * p.c.batch * p.c.hkv;
-  hipLaunchKernelGGL((paged_split_kernel<T, D, 4>), dim3(p.splits, units), dim3(4 * kWave), 0, s, p);
+  // Logits are held in LDS where one workgroup has a unit's whole softmax and they fit
+  // beside its stages, twice on a compute unit where there are more units than those:
+  // writes among the reads cost them much of their rate (256 units of 4,225 rows and
+  // 4 heads, whose logits are 3% of the bytes: 110 us through memory, 90 held).
+  PagedDecodeParams q = p;
+  const int64_t room = (units > p.cus ? kLdsBytes / 2 : kLdsBytes) - Cfg<T, D>::smem(4) - 1024;
+  const int64_t need = p.c.weight && p.splits == 1
+                           ? static_cast<int64_t>(paged_span_tiles(p.c.cap, p.sinks, p.window)) * p.group * kTile * 4 : 0;
+  q.held_logits = need > 0 && need <= room;
+  const int held = q.held_logits ? static_cast<int>(need) : 0;
+  hipLaunchKernelGGL((paged_split_kernel<T, D, 4>), dim3(p.splits, units), dim3(4 * kWave), held, s, q);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.splits == 1) return e;         // one split: finished in place
   const int chunks = paged_weight_chunks(p);

@@ -266,3 +266,13 @@ def test_same_call_same_bits():
         got.append((o, z, c.weight.nan_to_num()))
     for x in got[1:]:
         assert all(torch.equal(a, b) for a, b in zip(x, got[0]))
+
+
+@pytest.mark.parametrize("batch,G,cap", [(128, 16, 1904), (128, 16, 2096), (130, 16, 640), (130, 16, 800), (128, 4, 7600)])
+def test_weights_at_capacities_on_both_sides_of_what_a_workgroup_holds(batch, G, cap):
+    lens = np.random.RandomState(cap).randint(0, 150, (1, batch, 2))
+    lens[0, 3] = [cap - 1, 0]
+    p = Paged(lens, 16, 128, BF, spare=1, seed=cap, weights=True)
+    assert p.max_pages * 16 == cap
+    _check(p, G, True)
+    _check(Paged(lens, 16, 128, BF, spare=1, seed=cap, weights=True), G, True, 3, 70)
