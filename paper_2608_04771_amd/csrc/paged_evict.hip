@@ -28,17 +28,20 @@ constexpr int kHeld = 16;                    // weights a thread keeps in regist
 constexpr int kCopies = 4;                   // copies of each histogram bin
 constexpr int kMaxBins = 2048;
 
-__device__ __forceinline__ int wave_incl_scan(int v, int lane) {
-#pragma unroll
-  for (int d = 1; d < kWave; d <<= 1) {
-    const int o = __shfl_up(v, d, kWave);
-    if (lane >= d) v += o;
-  }
+// Sum of the lanes up to this one: within rows of 16 lanes, then rows 1 and 3 take the
+// last lane of the row before, and the upper half the last of the lower.
+__device__ __forceinline__ int wave_incl_scan(int v) {
+  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, false);   // row_shr 1, 2, 4, 8
+  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false);   // row_bcast 15
+  v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);   // row_bcast 31
   return v;
 }
 
 __global__ __launch_bounds__(kSelThreads) void evict_select_kernel(PagedEvictParams p) {
-  __shared__ __attribute__((aligned(16))) int hist[kMaxBins * kCopies];
+  __shared__ __attribute__((aligned(16))) int hists[2][kMaxBins * kCopies];   // in turn
   __shared__ int wsum[kSelWaves];
   __shared__ int2 wcount[kSelWaves];
   __shared__ int s_bin, s_krem, s_bad;
@@ -67,7 +70,7 @@ __global__ __launch_bounds__(kSelThreads) void evict_select_kernel(PagedEvictPar
     return;
   }
   if (tid == 0) s_bad = 0;
-  __syncthreads();
+  for (int i = tid; i < 2 * kMaxBins * kCopies / 4; i += kSelThreads) reinterpret_cast<int4 *>(hists)[i] = make_int4(0, 0, 0, 0);
 
   const int lo = p.sinks, hi = L - p.recent;           // the rows to choose from
   const int k = m - p.sinks - p.recent;                // of them
@@ -98,6 +101,7 @@ __global__ __launch_bounds__(kSelThreads) void evict_select_kernel(PagedEvictPar
       for (int i = 0; i < turns; ++i) f(bits(j0 + i * kWave), j0 + i * kWave);
     }
   };
+  __syncthreads();                                     // the histograms are clear, and s_bad
   // The unit's pages, which the compaction then trusts.
   int page_bad = 0;
   const int32_t *table = p.c.pages + cunit * static_cast<size_t>(p.c.max_pages);
@@ -112,8 +116,9 @@ __global__ __launch_bounds__(kSelThreads) void evict_select_kernel(PagedEvictPar
   for (int pass = 0; pass < 3; ++pass) {
     const int sh = shifts[pass];
     const int nb = 1 << nbits[pass];
-    for (int i = tid; i < nb * kCopies / 4; i += kSelThreads) reinterpret_cast<int4 *>(hist)[i] = make_int4(0, 0, 0, 0);
-    __syncthreads();
+    int *hist = hists[pass & 1];
+    if (pass == 1)                                       // for the last pass
+      for (int i = tid; i < (1 << 10) * kCopies / 4; i += kSelThreads) reinterpret_cast<int4 *>(hists[0])[i] = make_int4(0, 0, 0, 0);
     for_each([&](uint32_t u, int j) {
       if (j >= lo && j < hi && (u & pmask) == prefix) atomicAdd(&hist[((u >> sh) & (nb - 1)) * kCopies + lane % kCopies], 1);
     });
@@ -129,10 +134,10 @@ __global__ __launch_bounds__(kSelThreads) void evict_select_kernel(PagedEvictPar
     const bool two = nb == kMaxBins;
     const int first = two ? count(2 * tid) : count(tid);
     const int second = two ? count(2 * tid + 1) : 0;
-    const int incl = wave_incl_scan(first + second, lane);
+    const int incl = wave_incl_scan(first + second);
     if (lane == kWave - 1) wsum[wave] = incl;
     __syncthreads();
-    const int wincl = wave_incl_scan(lane < kSelWaves ? wsum[lane] : 0, lane);
+    const int wincl = wave_incl_scan(lane < kSelWaves ? wsum[lane] : 0);
     const int total = __shfl(wincl, kSelWaves - 1, kWave);
     const int before = wave == 0 ? 0 : __shfl(wincl, wave - 1, kWave);
     const int above = total - before - incl;           // rows in the bins of later threads
