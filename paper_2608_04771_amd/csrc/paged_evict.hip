@@ -194,8 +194,9 @@ __global__ __launch_bounds__(kSelThreads) void evict_select_kernel(PagedEvictPar
 }
 
 constexpr int kCompThreads = 256;
-// LDS that no one uses keeps three workgroups on a compute unit: more of them in flight
-// cost rate (all 28 layers of a 7B shape, per call: 257 us with 2.6 of them, 268 with 1.3).
+// LDS that no one uses keeps three workgroups on a compute unit: fewer or more of them
+// cost rate (all 28 layers of a 7B shape, per call: 257 us with 2.6 on a compute unit, 268
+// with 1.3; in chunks of 16 KB 280 with 2.6, 308 with 7.9).
 constexpr int kCompLds = 48 * 1024;
 constexpr int kMaxSpins = 1 << 20;           // of a microsecond or so
 

@@ -115,7 +115,7 @@ size_t prefill_workspace_bytes(int units, int tokens, int capacity, int group, i
 // round's blocks of a unit: as many as leave the XCDs with the same number of pieces, or
 // nearly.  Without a window a block's work grows with its place, so a piece takes blocks
 // from everywhere (its XCD's others wait for none: 8,192 tokens of 16 units of 4 heads
-// 1,601 -> 1,031 us); with one, neighbours see the same keys.
+// 1,601 -> 1,066 us); with one, neighbours see the same keys.
 void prefill_pieces(PagedPrefillParams &p, int units) {
   const int64_t all = static_cast<int64_t>(units) * p.blocks;
   p.pieces = p.near = 0;

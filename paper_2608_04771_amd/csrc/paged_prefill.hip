@@ -5,7 +5,7 @@
 //   j < sinks or j > p - window;   out = softmax(scale <q, k_j>) v_j over them
 //
 // The n tokens' G query heads of one KV head make n * G query rows (row t * G + g),
-// so a group shares its K and V.  A workgroup takes 128 of them, 32 a wave, and walks
+// so a group shares its K and V.  A workgroup takes 128 of them, or 256, 32 a wave, and walks
 // the key tiles that any of them sees: tiles of the cached rows (in pages), then tiles
 // of the new rows (as the caller gives them; a second kernel puts them into their
 // pages).  Per tile a wave computes
@@ -15,7 +15,14 @@
 // they are, and rescaling O needs nothing from other lanes.  Statistics and outputs
 // are fp32; P alone is rounded to the cache's type, as its operand has to be.  Where
 // there are few query rows, their key tiles are split over several workgroups and
-// joined by the second kernel.  Long runs are bound by the matrix units.
+// joined by the second kernel.
+//
+// Long runs are bound by the matrix units and what feeds them: 16,384 tokens of a 7B
+// layer in a window of 4,096 take 835-870 us, 970-1,010 TFLOP/s, where a large library
+// product reaches 1,190 on the same card.  No one part is the rest: without the loads to
+// LDS it takes 18% less, without the reads of K 18%, of V 6%, without the exponentials
+// 6%.  64 rows a wave (half the LDS reads) need more registers than a wave has and copy
+// (1,110 us on chunks that take 786); two tiles in flight by halves of a workgroup, 985.
 #include "paged_device.hpp"
 
 #include <type_traits>
