@@ -225,10 +225,15 @@ class PagedKVCache:
         _expect(weight, "weight", (NL, B, H, max_pages * page_rows), torch.float32)
         _need_cuda(k, v, pages, length, weight)
         self.k, self.v, self.pages, self.length, self.weight = k, v, pages, length, weight
-        self.shape = (NL, B, H, max_pages * page_rows, D)   # the capacity of a unit among them
         self.struct = RecoPagedCache(k.data_ptr(), v.data_ptr(), pages.data_ptr(), length.data_ptr(),
                                      None if weight is None else weight.data_ptr(), NL, B, H, n_pages, page_rows,
                                      max_pages, D, RECO_F32 if k.dtype == torch.float32 else RECO_BF16)
+
+    @property
+    def shape(self):
+        """(NL, B, H, capacity of a unit, D)"""
+        (NL, B, H, max_pages), (_, page_rows, D) = self.pages.shape, self.k.shape
+        return NL, B, H, max_pages * page_rows, D
 
     def ref(self):
         return ctypes.byref(self.struct)
