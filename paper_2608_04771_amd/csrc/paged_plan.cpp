@@ -86,8 +86,10 @@ int prefill_rows(int units, int tokens, int group, int capacity, int window, int
 }
 
 // Key tiles are split where there are too few blocks of query rows for two workgroups
-// on every compute unit, into pieces of at least two tiles of bf16 or one of fp32, whose
-// products take sixteen times as long (90 tokens of 2 units of 4 heads: 28 -> 22 us per call).
+// on every compute unit, into pieces of at least six tiles of bf16 (32 tokens over 9,645
+// rows of 4 units of 7 heads: 30.0 us per call by twos, 31.3 by fours, 27.1 by sixes, 30.3 by
+// eights) or one of fp32, whose products take sixteen times as long (90 tokens of 2 units of
+// 4 heads: 28 us by twos, 22 by ones).
 int prefill_splits(int units, int blocks, int capacity, int sinks, int window, int tile_rows, int compute_units) {
   int64_t rows = capacity;
   if (window > 0) {
@@ -95,7 +97,7 @@ int prefill_splits(int units, int blocks, int capacity, int sinks, int window, i
     if (seen < rows) rows = seen;
   }
   int64_t splits = 2 * static_cast<int64_t>(compute_units) / (static_cast<int64_t>(units) * blocks);
-  const int64_t pieces = rows / (tile_rows == prefill_tile_rows(0) ? tile_rows : 2 * tile_rows);
+  const int64_t pieces = rows / (tile_rows == prefill_tile_rows(0) ? tile_rows : 6 * tile_rows);
   if (splits > pieces) splits = pieces;
   if (splits > kPrefillMaxSplits) splits = kPrefillMaxSplits;
   return splits < 1 ? 1 : static_cast<int>(splits);
