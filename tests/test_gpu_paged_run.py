@@ -217,3 +217,29 @@ def test_streams_and_graphs_of_a_step():
             for x, y in zip((a.k, a.v, a.weight, a.length) + bufs[0][:2], (b.k, b.v, b.weight, b.length) + bufs[1][:2]):
                 assert torch.equal(x.view(torch.int8), y.view(torch.int8)), f"replay {i}"
     torch.cuda.synchronize()
+
+
+def test_rows_past_4_gib_of_a_pool():
+    # the same rows at a large pool's end and in a small one give the same bits
+    D, page, far, cap = 128, 4096, 4150, 8192
+    g = torch.Generator().manual_seed(6)
+    kv = [torch.randn((4, page, D), generator=g).to(BF).cuda() for _ in "kv"]
+    length = torch.tensor([[[5000, 4095]]], dtype=torch.int32)
+    weight = torch.rand((1, 1, 2, cap), generator=g)
+    small = B.PagedKVCache(*(x.clone() for x in kv), torch.tensor([[[[2, 0], [3, 1]]]], dtype=torch.int32).cuda(),
+                           length.cuda(), weight.cuda())
+    pool = [torch.empty((far + 4, page, D), dtype=BF, device="cuda") for _ in "kv"]      # 4.05 GiB each
+    for x, y in zip(pool, kv):
+        x[far:] = y
+    large = B.PagedKVCache(*pool, small.pages + far, length.cuda(), weight.cuda())
+    q, kn, vn = (torch.randn((1, 1, n, 70, D), generator=g).to(BF).cuda() for n in (8, 2, 2))
+    budget = torch.tensor([3000], dtype=torch.int32).cuda()
+    got = []
+    for c in (small, large):
+        r = list(B.reco_paged_prefill_attn(c, q, kn, vn))
+        r += B.reco_paged_decode_attn(c, *(x[:, :, :, 0].contiguous() for x in (q, kn, vn)))
+        B.reco_paged_evict(c, budget, 4, 32)
+        r += B.reco_paged_decode_attn(c, *(x[:, :, :, 1].contiguous() for x in (q, kn, vn)))
+        got.append(r + [c.k[-4:], c.v[-4:], c.weight, c.length])
+    for i, (x, y) in enumerate(zip(*got)):
+        assert torch.equal(x.contiguous().view(torch.int8), y.contiguous().view(torch.int8)), i
