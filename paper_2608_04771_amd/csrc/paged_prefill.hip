@@ -365,7 +365,9 @@ __global__ __launch_bounds__(NW * kWave, 2) void prefill_kernel(PagedPrefillPara
   // Workgroups go to the XCDs in turn.  Where there are many, a piece of a unit's blocks,
   // which see mostly the same keys, takes its turn on one XCD and shares its L2.
   // Where there are few, all units' longest blocks come first (768 fp32 blocks, 1.5 rounds
-  // of two on a compute unit: 330 -> 230 us), or, split, all run at once.
+  // of two on a compute unit: 330 -> 230 us; 256 in two splits each, all at once: 54 -> 47),
+  // unless a unit is rather splits than blocks, which then lie together (48 uneven units of
+  // 2 blocks in 5 splits: 61 us, 68 the other way).
   int unit = blockIdx.y, block = blockIdx.x, split = 0;
   if (p.pieces > 0) {
     const int slot = blockIdx.x / kXcds;
@@ -374,12 +376,13 @@ __global__ __launch_bounds__(NW * kWave, 2) void prefill_kernel(PagedPrefillPara
     unit = piece / p.pieces;
     block = p.spread ? piece % p.pieces + p.pieces * pos : piece % p.pieces * p.near + pos;
     if (unit >= units || block >= p.blocks) return;
-  } else if (p.splits > 1) {
-    block = p.by_splits.of(blockIdx.x);
+  } else if (p.blocks > p.splits) {
+    unit = p.by_splits.of(blockIdx.x);
+    block = blockIdx.y;
     split = p.by_splits.rest(blockIdx.x);
   } else {
-    unit = blockIdx.x;
-    block = blockIdx.y;
+    block = p.by_splits.of(blockIdx.x);
+    split = p.by_splits.rest(blockIdx.x);
   }
   block = p.blocks - 1 - block;                          // the longest first
   const size_t cunit = p.c.unit(unit);
@@ -787,7 +790,7 @@ template <typename T, int D>
 hipError_t launch_typed(const PagedPrefillParams &p, hipStream_t s) {
   const int units = p.c.n_layers * p.c.batch * p.c.hkv;
   const dim3 grid = p.pieces > 0 ? dim3((units * p.pieces + kXcds - 1) / kXcds * kXcds * p.near)
-                    : p.splits > 1 ? dim3(p.blocks * p.splits, units) : dim3(units, p.blocks);
+                    : p.blocks > p.splits ? dim3(units * p.splits, p.blocks) : dim3(p.blocks * p.splits, units);
   if constexpr (sizeof(T) == 2) {
     if (p.rows == kPrefillLongRows)
       hipLaunchKernelGGL((prefill_kernel<T, D, 8>), grid, dim3(8 * kWave), 0, s, p);
