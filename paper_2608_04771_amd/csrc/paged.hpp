@@ -74,6 +74,7 @@ hipError_t launch_paged_decode(const PagedDecodeParams &p, int dtype, int head_d
 constexpr int kPrefillRows = 128;        // query rows of a workgroup
 constexpr int kPrefillLongRows = 256;    // of one for long bf16 runs
 constexpr int kPrefillMaxSplits = 64;
+constexpr int kPrefillAppendRows = 128;  // of a workgroup that appends
 constexpr int kXcds = 8;
 struct PagedPrefillParams {
   PagedCache c;

@@ -141,8 +141,9 @@ void prefill_pieces(PagedPrefillParams &p, int units) {
 bool prefill_fits_grid(const PagedPrefillParams &p) {
   const int64_t units = static_cast<int64_t>(p.c.n_layers) * p.c.batch * p.c.hkv;
   const int64_t most = int64_t{1} << 24;                 // workgroups of 256 threads
-  return units * p.blocks * p.splits < most / 4 &&       // of 512, and pieces rounded up
-         p.tokens / 64 + 1 + (p.splits > 1 ? static_cast<int64_t>(p.blocks) * 16 : 0) < most;
+  const int64_t chunks = p.tokens / kPrefillAppendRows + 1;
+  return units * (static_cast<int64_t>(p.blocks) * p.splits + chunks) < most / 4 &&   // of 512, and pieces rounded up
+         chunks + (p.splits > 1 ? static_cast<int64_t>(p.blocks) * 16 : 0) < most;
 }
 
 void prefill_place(PagedPrefillParams &p, int head_dim, void *ws) {

@@ -7,7 +7,7 @@
 // The n tokens' G query heads of one KV head make n * G query rows (row t * G + g),
 // so a group shares its K and V.  A workgroup takes 128 of them, or 256, 32 a wave, and walks
 // the key tiles that any of them sees: tiles of the cached rows (in pages), then tiles
-// of the new rows (as the caller gives them; a second kernel puts them into their
+// of the new rows (as the caller gives them; other workgroups put them into their
 // pages).  Per tile a wave computes
 //   S^T = K_tile . Q^T           (32 keys x 32 rows per block)
 //   O^T += V_tile^T . P^T        (32 columns of the head x 32 rows per block)
@@ -346,6 +346,59 @@ __device__ __forceinline__ void write_rows(const PagedPrefillParams &p, unsigned
   asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
 }
 
+// Puts rows [first, first + kAppendRows) of a unit's run into their pages; a unit's rows are
+// appended together or, where they or their pages do not fit, not at all.  The rows come
+// while it is found out where they go.  Attention may go on meanwhile: it has no use for
+// rows of the cache past L (prompts of 200 to 512 tokens 42.5 -> 38.5 us per call against a
+// kernel after the attention, 16,384 tokens 850 -> 856).  Returns whether the unit's rows
+// are stored.
+constexpr int kAppendRows = kPrefillAppendRows;
+
+template <typename T, int D, int NT>
+__device__ __forceinline__ bool append_run(const PagedPrefillParams &p, int unit, int first, int L) {
+  const int tid = threadIdx.x;
+  constexpr int kLanes = D * (int)sizeof(T) / 16, kEach = kAppendRows * kLanes / NT;
+  u32x4v k[kEach], v[kEach];
+#pragma unroll
+  for (int i = 0; i < kEach; ++i) {
+    const int row = min(first + (tid + i * NT) / kLanes, p.tokens - 1);
+    const size_t at = (static_cast<size_t>(unit) * p.tokens + row) * kLanes + tid % kLanes;
+    k[i] = reinterpret_cast<const u32x4v *>(p.k_new)[at];
+    v[i] = reinterpret_cast<const u32x4v *>(p.v_new)[at];
+  }
+  const size_t cunit = p.c.unit(unit);
+  const int given = p.n_new ? p.n_new[p.c.sequence(unit)] : p.tokens;
+  const int n = given < 0 || given > p.tokens ? 0 : given;
+  if (first >= n || L < 0 || L > p.c.cap) return false;
+  const bool reporting = first == 0 && tid == 0;
+  if (n > p.c.cap - L) {
+    if (reporting) report(p.c.dev_err, kDevAppendOverflow);
+    return false;
+  }
+  const int32_t *table = p.c.pages + cunit * static_cast<size_t>(p.c.max_pages);
+  const int shift = p.c.page_shift;
+  int id[kEach];
+#pragma unroll
+  for (int i = 0; i < kEach; ++i) id[i] = table[min(L + first + (tid + i * NT) / kLanes, L + n - 1) >> shift];
+  bool bad = false;
+  for (int g = (L >> shift) + tid; g <= (L + n - 1) >> shift; g += NT)
+    if (static_cast<unsigned>(table[g]) >= static_cast<unsigned>(p.c.n_pages)) bad = true;
+  if (__syncthreads_or(bad)) {
+    if (reporting) report(p.c.dev_err, kDevBadPage);
+    return false;
+  }
+#pragma unroll
+  for (int i = 0; i < kEach; ++i) {
+    const int t = first + (tid + i * NT) / kLanes;
+    if (t >= n) break;
+    const size_t at = ((static_cast<size_t>(id[i]) << shift) + ((L + t) & ((1 << shift) - 1))) * kLanes + tid % kLanes;
+    reinterpret_cast<u32x4v *>(p.c.k)[at] = k[i];
+    reinterpret_cast<u32x4v *>(p.c.v)[at] = v[i];
+  }
+  if (p.c.weight && tid < kAppendRows && first + tid < n) p.c.weight[cunit * p.c.cap + L + first + tid] = 0.f;
+  return true;
+}
+
 template <typename T, int D, int NW>
 __global__ __launch_bounds__(NW * kWave, 2) void prefill_kernel(PagedPrefillParams p) {
   using C = Cfg<T, D, NW>;
@@ -369,20 +422,33 @@ __global__ __launch_bounds__(NW * kWave, 2) void prefill_kernel(PagedPrefillPara
   // unless a unit is rather splits than blocks, which then lie together (48 uneven units of
   // 2 blocks in 5 splits: 61 us, 68 the other way).
   int unit = blockIdx.y, block = blockIdx.x, split = 0;
+  int chunk = -1;                                        // of the rows to append, after all blocks
   if (p.pieces > 0) {
+    const int attending = (units * p.pieces + kXcds - 1) / kXcds * kXcds * p.near;
     const int slot = blockIdx.x / kXcds;
     const int turn = p.by_near.of(slot), pos = p.by_near.rest(slot);
     const int piece = turn * kXcds + blockIdx.x % kXcds;
     unit = piece / p.pieces;
     block = p.spread ? piece % p.pieces + p.pieces * pos : piece % p.pieces * p.near + pos;
-    if (unit >= units || block >= p.blocks) return;
-  } else if (p.blocks > p.splits) {
+    const int more = static_cast<int>(blockIdx.x) - attending;
+    if (more >= 0) {
+      unit = more % units;
+      chunk = more / units;
+    } else if (unit >= units || block >= p.blocks) {
+      return;
+    }
+  } else if (p.splits == 1 || p.blocks > p.splits) {
     unit = p.by_splits.of(blockIdx.x);
     block = blockIdx.y;
     split = p.by_splits.rest(blockIdx.x);
+    if (block >= p.blocks) chunk = block - p.blocks;
   } else {
     block = p.by_splits.of(blockIdx.x);
     split = p.by_splits.rest(blockIdx.x);
+  }
+  if (chunk >= 0) {
+    append_run<T, D, NW * kWave>(p, unit, chunk * kAppendRows, p.c.len[p.c.unit(unit)]);
+    return;
   }
   block = p.blocks - 1 - block;                          // the longest first
   const size_t cunit = p.c.unit(unit);
@@ -663,11 +729,9 @@ __global__ __launch_bounds__(NW * kWave, 2) void prefill_kernel(PagedPrefillPara
                    r0 + wave * 32, n * G, lane);
 }
 
-// Joins the splits (workgroups [0, merges) of a unit) and puts its new rows into their
-// pages (the others, kAppendRows rows each).  A unit's rows are appended together or,
-// where they or their pages do not fit, not at all.
+// Where there are splits: joins them (workgroups [0, merges) of a unit) and puts the new
+// rows into their pages (the others).
 constexpr int kMergeRows = 32;               // a wave's rows, and a quarter of a 32-column block each thread
-constexpr int kAppendRows = 64;
 
 template <typename T, int D>
 __global__ __launch_bounds__(256) void prefill_finish_kernel(PagedPrefillParams p, int merges) {
@@ -741,55 +805,32 @@ __global__ __launch_bounds__(256) void prefill_finish_kernel(PagedPrefillParams 
     dst[3] = from_f32<T>(acc.w);
     return;
   }
-  // The rows come while it is found out where they go.
-  constexpr int kLanes = D * (int)sizeof(T) / 16, kEach = kAppendRows * kLanes / 256;
-  const int first = (blockIdx.x - merges) * kAppendRows;
-  u32x4v k[kEach], v[kEach];
-#pragma unroll
-  for (int i = 0; i < kEach; ++i) {
-    const int row = min(first + (tid + i * 256) / kLanes, p.tokens - 1);
-    const size_t at = (static_cast<size_t>(unit) * p.tokens + row) * kLanes + tid % kLanes;
-    k[i] = reinterpret_cast<const u32x4v *>(p.k_new)[at];
-    v[i] = reinterpret_cast<const u32x4v *>(p.v_new)[at];
-  }
+  const int first = (blockIdx.x - merges) * kAppendRows, L = p.len_in[unit];
+  if (append_run<T, D, 256>(p, unit, first, L) && first == 0 && tid == 0)
+    p.c.len[p.c.unit(unit)] = L + (p.n_new ? p.n_new[p.c.sequence(unit)] : p.tokens);
+}
+
+// Where there are none, the first kernel's last workgroups have put the rows, and what
+// is left are the lengths, which no one reads any more.
+__global__ __launch_bounds__(kWave) void prefill_len_kernel(PagedPrefillParams p) {
+  const int unit = blockIdx.x;
   const size_t cunit = p.c.unit(unit);
-  const int given = p.n_new ? p.n_new[p.c.sequence(unit)] : p.tokens;
-  const int L = p.len_in[unit];
-  const int n = given < 0 || given > p.tokens ? 0 : given;
-  if (first >= n || L < 0 || L > p.c.cap) return;
-  const bool reporting = first == 0 && tid == 0;
-  if (n > p.c.cap - L) {
-    if (reporting) report(p.c.dev_err, kDevAppendOverflow);
-    return;
-  }
+  const int L = p.c.len[cunit];
+  const int n = p.n_new ? p.n_new[p.c.sequence(unit)] : p.tokens;
+  if (n < 1 || n > p.tokens || L < 0 || L > p.c.cap || n > p.c.cap - L) return;
   const int32_t *table = p.c.pages + cunit * static_cast<size_t>(p.c.max_pages);
-  const int shift = p.c.page_shift;
-  int id[kEach];
-#pragma unroll
-  for (int i = 0; i < kEach; ++i) id[i] = table[min(L + first + (tid + i * 256) / kLanes, L + n - 1) >> shift];
   bool bad = false;
-  for (int g = (L >> shift) + tid; g <= (L + n - 1) >> shift; g += 256)
-    if (static_cast<unsigned>(table[g]) >= static_cast<unsigned>(p.c.n_pages)) bad = true;
-  if (__syncthreads_or(bad)) {
-    if (reporting) report(p.c.dev_err, kDevBadPage);
-    return;
-  }
-#pragma unroll
-  for (int i = 0; i < kEach; ++i) {
-    const int t = first + (tid + i * 256) / kLanes;
-    if (t >= n) break;
-    const size_t at = ((static_cast<size_t>(id[i]) << shift) + ((L + t) & ((1 << shift) - 1))) * kLanes + tid % kLanes;
-    reinterpret_cast<u32x4v *>(p.c.k)[at] = k[i];
-    reinterpret_cast<u32x4v *>(p.c.v)[at] = v[i];
-  }
-  if (p.c.weight && tid < kAppendRows && first + tid < n) p.c.weight[cunit * p.c.cap + L + first + tid] = 0.f;
-  if (reporting) p.c.len[cunit] = L + n;
+  for (int g = (L >> p.c.page_shift) + threadIdx.x; g <= (L + n - 1) >> p.c.page_shift; g += kWave)
+    bad |= static_cast<unsigned>(table[g]) >= static_cast<unsigned>(p.c.n_pages);
+  if (!__any(bad) && threadIdx.x == 0) p.c.len[cunit] = L + n;
 }
 
 template <typename T, int D>
 hipError_t launch_typed(const PagedPrefillParams &p, hipStream_t s) {
   const int units = p.c.n_layers * p.c.batch * p.c.hkv;
-  const dim3 grid = p.pieces > 0 ? dim3((units * p.pieces + kXcds - 1) / kXcds * kXcds * p.near)
+  const int chunks = (p.tokens + kAppendRows - 1) / kAppendRows;
+  const dim3 grid = p.pieces > 0 ? dim3((units * p.pieces + kXcds - 1) / kXcds * kXcds * p.near + units * chunks)
+                    : p.splits == 1 ? dim3(units, p.blocks + chunks)
                     : p.blocks > p.splits ? dim3(units * p.splits, p.blocks) : dim3(p.blocks * p.splits, units);
   if constexpr (sizeof(T) == 2) {
     if (p.rows == kPrefillLongRows)
@@ -799,9 +840,12 @@ hipError_t launch_typed(const PagedPrefillParams &p, hipStream_t s) {
     hipLaunchKernelGGL((prefill_kernel<T, D, 4>), grid, dim3(4 * kWave), 0, s, p);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  const int merges = p.splits > 1 ? p.blocks * (kRows / kMergeRows) * (D / 32) : 0;
-  const int chunks = (p.tokens + kAppendRows - 1) / kAppendRows;
-  hipLaunchKernelGGL((prefill_finish_kernel<T, D>), dim3(merges + chunks, units), dim3(256), 0, s, p, merges);
+  if (p.splits > 1) {
+    const int merges = p.blocks * (kRows / kMergeRows) * (D / 32);
+    hipLaunchKernelGGL((prefill_finish_kernel<T, D>), dim3(merges + chunks, units), dim3(256), 0, s, p, merges);
+  } else {
+    hipLaunchKernelGGL(prefill_len_kernel, dim3(units), dim3(kWave), 0, s, p);
+  }
   return hipGetLastError();
 }
 
