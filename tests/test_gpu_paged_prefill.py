@@ -319,3 +319,43 @@ def test_values_that_only_some_tokens_see_in_blocks_of_256_rows():
     for x, y in zip(a, b):
         assert torch.equal(x[:, :, :, :117], y[:, :, :, :117])
         assert torch.isnan(y[:, :, :, 117:]).all()
+
+
+@pytest.mark.parametrize("batch,code", [(300, 1), (300, 7), (300, 5), (700, 1), (700, 7), (700, 5)])
+def test_units_that_do_not_fit_among_many(batch, code):
+    # enough units that none is split: rows are stored beside the attention, and those
+    # of units 3 (bad) and 7 (a bad count) are not
+    T, page, D = 150, 16, 64
+    lens = np.random.RandomState(batch + code).randint(0, 40, (1, batch, 1))
+    lens[0, 3, 0] = 37
+    p = Paged(lens, page, D, BF, spare=T, seed=code, weights=True)
+    q, kn, vn = _inputs(p, 2, T, 5)
+    news = np.random.RandomState(1).randint(0, T + 1, batch)
+    news[[3, 7]] = T, T + 1
+    if code == 1:
+        p.length[0, 3, 0] = p.max_pages * page - T + 1
+        p.pages[0, 3, 0] = p.pages[0, 3, 0, 0]              # rows past the 37 are whatever lies there
+    elif code == 7:
+        p.pages[0, 3, 0, 37 // page + 3] = -5
+    else:
+        p.length[0, 3, 0] = p.max_pages * page + 1
+        p.pages[0, 3, 0] = p.pages[0, 3, 0, 0]
+    news[7] = T + 1 if code == 5 else 0
+    cache = p.upload()
+    err = torch.zeros(1, dtype=torch.int32, device="cuda")
+    B.reco_paged_prefill_attn(cache, q.cuda(), kn.cuda(), vn.cuda(), torch.tensor(news, dtype=torch.int32).cuda(),
+                              dev_err=err)
+    assert err.item() == code
+    k0, v0, n0, w0 = p.k.clone(), p.v.clone(), p.length.clone(), p.weight.clone()
+    for b in range(batch):
+        if b in (3, 7):
+            continue
+        L, n = int(lens[0, b, 0]), int(news[b])
+        at = p.where((0, b, 0), torch.arange(L, L + n))
+        k0[at], v0[at] = kn[0, b, 0, :n], vn[0, b, 0, :n]
+        n0[0, b, 0] += n
+        w0[0, b, 0, L:L + n] = 0.0
+    assert torch.equal(cache.k.cpu().view(torch.int16), k0.view(torch.int16))
+    assert torch.equal(cache.v.cpu().view(torch.int16), v0.view(torch.int16))
+    assert torch.equal(cache.length.cpu(), n0)
+    assert torch.equal(cache.weight.cpu().view(torch.int32), w0.view(torch.int32))
