@@ -95,7 +95,8 @@ enum {
   RECO_DEV_BAD_LENGTH = 5,       /* stored len outside [0, capacity] */
   RECO_DEV_BAD_LOGIT = 6,        /* a logit row with no non-NaN value to sample */
   RECO_DEV_BAD_PAGE = 7,         /* a page id of a cached row outside [0, n_pages) */
-  RECO_DEV_BAD_BUDGET = 8        /* an eviction budget below 1 or below sinks + recent */
+  RECO_DEV_BAD_BUDGET = 8,       /* an eviction budget below 1 or below sinks + recent */
+  RECO_DEV_STALLED = 9           /* an eviction's rows were not read in time to be replaced */
 };
 
 /* reco_score flags */
@@ -348,7 +349,10 @@ reco_status_t reco_paged_prefill_attn(const reco_paged_cache_t *cache, int32_t l
  * cache->weight has to be given; +inf ranks above all, and a negative or NaN weight
  * among the rows to choose from is RECO_DEV_BAD_SCORE.  A unit whose length, budget,
  * page ids or weights are bad is left unchanged (kept_idx unspecified) and dev_err
- * is set.  The workspace is 256-byte aligned and serves one call at a time. */
+ * is set.  The workspace is 256-byte aligned and serves one call at a time.  A unit
+ * whose rows are not read in time to be replaced (another call has written the
+ * workspace meanwhile) is given up: RECO_DEV_STALLED, its len stays L, and what its
+ * rows and weights hold then is unspecified. */
 size_t reco_paged_evict_workspace_size(const reco_paged_cache_t *cache, int32_t n_layers);
 reco_status_t reco_paged_evict(const reco_paged_cache_t *cache, int32_t layer0, int32_t n_layers,
                                const int32_t *budget, int64_t budget_layer_stride, int32_t sinks,

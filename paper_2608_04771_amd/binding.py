@@ -30,7 +30,7 @@ RECO_SCORE_CAUSAL = 1
 RECO_POOL_MAX = 0
 RECO_POOL_MEAN = 1
 DEV_ERRORS = {0: "ok", 1: "append overflow", 2: "bad retention", 3: "bad score", 4: "bad token id",
-              5: "bad length", 6: "bad logit row", 7: "bad page", 8: "bad budget"}
+              5: "bad length", 6: "bad logit row", 7: "bad page", 8: "bad budget", 9: "stalled eviction"}
 
 EXPORTED = [
     "reco_score_workspace_size", "reco_score", "reco_select_compact_workspace_size", "reco_select_compact",

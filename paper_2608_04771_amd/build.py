@@ -3,7 +3,9 @@
 Usage: ``python -m paper_2608_04771_amd.build`` or ``build_library()``.
 Always recompiles; the objects go to ``paper_2608_04771_amd/_build/`` and the
 library to ``paper_2608_04771_amd/libreco.so``.  ``build_c_driver()`` then
-compiles ``tests/c_abi/reco_c_driver``, a plain C client of the ABI."""
+compiles ``tests/c_abi/reco_c_driver``, a plain C client of the ABI, and
+``build_compact_client()`` ``tests/c_abi/libcompact_client.so``, through which a
+GPU test calls the eviction's compaction alone."""
 from __future__ import annotations
 
 import concurrent.futures as cf
@@ -89,7 +91,27 @@ def build_c_driver() -> str:
     return C_DRIVER
 
 
+COMPACT_CLIENT_SRC = os.path.join(ROOT, "tests", "c_abi", "compact_client.cpp")
+COMPACT_CLIENT = os.path.join(ROOT, "tests", "c_abi", "libcompact_client.so")
+
+
+def build_compact_client() -> str:
+    """Compile the client of the eviction's compaction kernel (host code only)
+    against the built libreco.so."""
+    rocm = os.environ.get("ROCM_PATH", "/opt/rocm")
+    cxx = shutil.which("g++") or shutil.which("c++")
+    if cxx is None:
+        raise RuntimeError("no C++ compiler found for the compaction's client")
+    tmp = COMPACT_CLIENT + ".tmp"
+    _run([cxx, "-std=c++17", "-O2", "-Wall", "-Werror", "-shared", "-fPIC", "-D__HIP_PLATFORM_AMD__",
+          f"-I{os.path.join(rocm, 'include')}", f"-I{CSRC}", f"-I{os.path.join(ROOT, 'include')}", COMPACT_CLIENT_SRC,
+          "-o", tmp, f"-L{PKG}", "-lreco", "-Wl,-rpath,$ORIGIN/../../paper_2608_04771_amd"])
+    os.replace(tmp, COMPACT_CLIENT)
+    return COMPACT_CLIENT
+
+
 if __name__ == "__main__":
     path = build_library(verbose="-v" in sys.argv)
     print(path)
     print(build_c_driver())
+    print(build_compact_client())

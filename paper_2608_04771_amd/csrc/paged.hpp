@@ -115,17 +115,21 @@ struct PagedEvictParams {
   int32_t *idx;           // [units][cap]  kept rows (the caller's buffer or the workspace)
   bool idx_wanted;        // the caller's: written for units that keep everything, too
   int32_t *kept;          // [units]  rows after the call, or -1 where nothing moves
-  int32_t *state;         // [units][state_pitch]  chunks taken, loaded in order, and loaded (one flag each)
+  int32_t *state;         // [units][state_pitch]  chunks taken, loaded in order, stored, and loaded (one flag each)
   int64_t state_pitch;
   int sinks, recent;
   int chunk_rows;         // rows of a chunk of the compaction
   int workers;            // its workgroups for a unit
+  int max_spins;          // of a workgroup that waits for earlier chunks
 };
-constexpr int kEvictState = 2;
+constexpr int kEvictState = 3;
+constexpr int kEvictSpins = 1 << 20;         // of a microsecond or so
 constexpr int kEvictWorkers = 32;
 constexpr int evict_chunk_rows(int row_bytes) { return 32768 / row_bytes; }
 size_t paged_evict_workspace_bytes(int units, int capacity, int row_bytes, bool need_idx);
 void paged_evict_place(PagedEvictParams &p, int units, int row_bytes, void *ws);
 hipError_t launch_paged_evict(const PagedEvictParams &p, int dtype, int head_dim, hipStream_t s);
+// The compaction alone, of units whose kept rows, counts and state are set.
+hipError_t launch_evict_compact(const PagedEvictParams &p, int row_bytes, hipStream_t s);
 
 }  // namespace reco

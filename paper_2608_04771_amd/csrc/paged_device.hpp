@@ -8,7 +8,8 @@
 
 namespace reco {
 
-constexpr int kDevAppendOverflow = 1, kDevBadScore = 3, kDevBadLength = 5, kDevBadPage = 7, kDevBadBudget = 8;
+constexpr int kDevAppendOverflow = 1, kDevBadScore = 3, kDevBadLength = 5, kDevBadPage = 7, kDevBadBudget = 8,
+              kDevStalled = 9;
 
 // Table entries are read through the scalar unit where their index is the same
 // in all lanes: no kernel writes the table.

@@ -13,7 +13,9 @@
 //   hold rows that it or an earlier chunk moves: a workgroup loads its chunk into
 //   registers, says so, waits until all earlier chunks of the unit are loaded, and
 //   stores.  Loading waits for nothing and chunks are taken in order by workgroups that
-//   run, so the wait ends whatever the order of dispatch.  It is bound by the rows'
+//   run, so the wait ends whatever the order of dispatch.  It is bounded all the same:
+//   a workgroup that waits in vain (its workspace is another call's, too) stores nothing
+//   and reports it, and len changes only once all chunks are stored.  It is bound by the rows'
 //   bytes (112 units, 9,516 of 16,384 rows of 2 x 256 bytes: 225 us, 4.9 TB/s; with
 //   chunks of 16 KB 248); a chunk of rows that stay where they are is not read.
 #include "paged_device.hpp"
@@ -198,7 +200,6 @@ constexpr int kCompThreads = 256;
 // cost rate (all 28 layers of a 7B shape, per call: 257 us with 2.6 on a compute unit, 268
 // with 1.3; in chunks of 16 KB 280 with 2.6, 308 with 7.9).
 constexpr int kCompLds = 48 * 1024;
-constexpr int kMaxSpins = 1 << 20;           // of a microsecond or so
 
 __device__ __forceinline__ int relaxed_load(const int32_t *p) {
   return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
@@ -223,6 +224,7 @@ __global__ __launch_bounds__(kCompThreads) void evict_compact_kernel(PagedEvictP
   const int shift = p.c.page_shift, mask = (1 << shift) - 1;
   int32_t *ticket = p.state + static_cast<size_t>(unit) * p.state_pitch;
   int32_t *prefix = ticket + 1;                          // chunks before this one are known to be loaded
+  int32_t *stored = ticket + 2;                          // chunks whose rows are in their places
   int32_t *loaded = ticket + kEvictState;
   unsigned char *k = reinterpret_cast<unsigned char *>(p.c.k) + tid % kLanesPerRow * 16;
   unsigned char *v = reinterpret_cast<unsigned char *>(p.c.v) + tid % kLanesPerRow * 16;
@@ -231,6 +233,7 @@ __global__ __launch_bounds__(kCompThreads) void evict_compact_kernel(PagedEvictP
 
   if (tid == 0) s_ticket = atomicAdd(ticket, 1);
   __syncthreads();
+  int mine = 0;                                          // chunks that this workgroup has stored
   for (;;) {
     const int c = s_ticket;
     const int r0 = c * kRows;
@@ -260,9 +263,13 @@ __global__ __launch_bounds__(kCompThreads) void evict_compact_kernel(PagedEvictP
       s_ticket = atomicAdd(ticket, 1);
     }
     // Bounded, so that a workspace that another call writes meanwhile cannot hang the device.
-    for (int f = known + tid, spins = 0; f < c; f += kCompThreads)
-      while (!relaxed_load(&loaded[f]) && ++spins < kMaxSpins) __builtin_amdgcn_s_sleep(1);
-    __syncthreads();
+    int spins = 0;
+    for (int f = known + tid; f < c && spins <= p.max_spins; f += kCompThreads)
+      while (!relaxed_load(&loaded[f]) && ++spins <= p.max_spins) __builtin_amdgcn_s_sleep(1);
+    if (__syncthreads_or(spins > p.max_spins)) {         // rows that this chunk's would replace may still be wanted
+      if (tid == 0) report(p.c.dev_err, kDevStalled);
+      break;
+    }
     if (tid == 0) atomicMax(prefix, c);
     if (moves) {
 #pragma unroll
@@ -276,8 +283,10 @@ __global__ __launch_bounds__(kCompThreads) void evict_compact_kernel(PagedEvictP
       }
       if (r0 + tid <= last && tid < kRows) weight[r0 + tid] = w;
     }
-    if (c == 0 && tid == 0) p.c.len[cunit] = m;
+    ++mine;
   }
+  // Whoever stores the unit's last chunk sets its length.
+  if (mine > 0 && tid == 0 && atomicAdd(stored, mine) + mine == (m + kRows - 1) / kRows) p.c.len[cunit] = m;
 }
 
 }  // namespace
@@ -286,9 +295,11 @@ hipError_t launch_paged_evict(const PagedEvictParams &p, int dtype, int head_dim
   const int units = p.c.n_layers * p.c.batch * p.c.hkv;
   hipLaunchKernelGGL(evict_select_kernel, dim3(units), dim3(kSelThreads), 0, s, p);
   hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return e;
-  const int rowb = head_dim * (dtype == 0 ? 4 : 2);
-  const dim3 grid(units, p.workers);
+  return e != hipSuccess ? e : launch_evict_compact(p, head_dim * (dtype == 0 ? 4 : 2), s);
+}
+
+hipError_t launch_evict_compact(const PagedEvictParams &p, int rowb, hipStream_t s) {
+  const dim3 grid(p.c.n_layers * p.c.batch * p.c.hkv, p.workers);
   if (rowb == 128) hipLaunchKernelGGL(evict_compact_kernel<128>, grid, dim3(kCompThreads), kCompLds, s, p);
   else if (rowb == 256) hipLaunchKernelGGL(evict_compact_kernel<256>, grid, dim3(kCompThreads), kCompLds, s, p);
   else hipLaunchKernelGGL(evict_compact_kernel<512>, grid, dim3(kCompThreads), kCompLds, s, p);

@@ -181,6 +181,7 @@ void paged_evict_place(PagedEvictParams &p, int units, int row_bytes, void *ws) 
   // units that keep everything, or fewer rows, end at once.
   const int64_t chunks = p.state_pitch - kEvictState;
   p.workers = static_cast<int>(chunks < kEvictWorkers ? chunks : kEvictWorkers);
+  p.max_spins = kEvictSpins;
 }
 
 }  // namespace reco
