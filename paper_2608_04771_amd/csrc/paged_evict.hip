@@ -212,7 +212,7 @@ __global__ __launch_bounds__(kCompThreads) void evict_compact_kernel(PagedEvictP
   constexpr int kPasses = evict_chunk_rows(ROWB) / kRowsPerPass;
   constexpr int kRows = kPasses * kRowsPerPass;
   static_assert(kRows <= kCompThreads, "a weight a thread");
-  __shared__ int s_ticket;
+  __shared__ int s_ticket, s_known;
 
   const int unit = blockIdx.x;
   const int tid = threadIdx.x;
@@ -231,11 +231,18 @@ __global__ __launch_bounds__(kCompThreads) void evict_compact_kernel(PagedEvictP
   float *weight = p.c.weight + cunit * p.c.cap;
   const auto at = [&](int row) { return ((static_cast<size_t>(table[row >> shift]) << shift) + (row & mask)) * ROWB; };
 
-  if (tid == 0) s_ticket = atomicAdd(ticket, 1);
+  // A chunk, and before which one all are known to be loaded: the same for the whole
+  // workgroup, so that its waves together wait for every chunk between the two.
+  const auto take = [&] {
+    const int chunk = atomicAdd(ticket, 1), before = relaxed_load(prefix);
+    s_ticket = chunk;
+    s_known = before;
+  };
+  if (tid == 0) take();
   __syncthreads();
   int mine = 0;                                          // chunks that this workgroup has stored
   for (;;) {
-    const int c = s_ticket;
+    const int c = s_ticket, known = s_known;
     const int r0 = c * kRows;
     if (r0 >= m) break;                                  // the same for the workgroup
     const int last = min(r0 + kRows, m) - 1;
@@ -244,7 +251,6 @@ __global__ __launch_bounds__(kCompThreads) void evict_compact_kernel(PagedEvictP
 #pragma unroll
     for (int i = 0; i < kPasses; ++i) from[i] = idx[min(r0 + i * kRowsPerPass + tid / kLanesPerRow, last)];
     if (tid < kRows) wfrom = idx[min(r0 + tid, last)];
-    const int known = relaxed_load(prefix);
     u32x4v kr[kPasses], vr[kPasses];
     float w = 0.f;
     if (moves) {
@@ -260,7 +266,7 @@ __global__ __launch_bounds__(kCompThreads) void evict_compact_kernel(PagedEvictP
     __syncthreads();
     if (tid == 0) {
       __hip_atomic_store(&loaded[c], 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-      s_ticket = atomicAdd(ticket, 1);
+      take();
     }
     // Bounded, so that a workspace that another call writes meanwhile cannot hang the device.
     int spins = 0;
