@@ -239,6 +239,9 @@ __global__ __launch_bounds__(NW * kWave, NW == 8 ? 1 : (Cfg<T, D>::min_wgs)) voi
 #pragma unroll
       for (int c = 0; c < C::qk_steps; ++c) s[hf] = MF::mma(load_frag(krow + c * C::kpl), qf[c], s[hf]);
     }
+    // V's rows take the place of K's, which other lanes read: the compiler must not put
+    // the writes first (a wave's LDS accesses are done in order, so nothing waits).
+    asm volatile("" ::: "memory");
 
     float x[8];
 #pragma unroll
