@@ -527,6 +527,15 @@ class PreparedDecode:
         return self.out, self.lse
 
 
+def _row_counts(**counts):
+    """Counts of rows as the C ABI takes them; a larger one would lose its upper bits on
+    the way (2**32 + 5 rows of window would be five)."""
+    for what, n in counts.items():
+        if not -2 ** 31 <= int(n) < 2 ** 31:
+            raise ValueError(f"{what} must fit 32 bits, got {n}")
+    return tuple(int(n) for n in counts.values())
+
+
 def _paged_decode_shapes(cache: PagedKVCache, nl: int, q: torch.Tensor, k_new, v_new, out, lse):
     NL, B, H, Cap, D = cache.shape
     if q.dim() != 4 or q.shape[0] != nl or q.shape[1] != B or q.shape[3] != D or q.dtype != cache.k.dtype:
@@ -552,6 +561,7 @@ def reco_paged_decode_attn(cache: PagedKVCache, q: torch.Tensor, k_new: Optional
     ``window`` rows (its own among them) and the first ``sinks``.  A cache with
     weights accumulates them."""
     layer0, nl = _layers(cache, layer0, n_layers)
+    sinks, window = _row_counts(sinks=sinks, window=window)
     hq = _paged_decode_shapes(cache, nl, q, k_new, v_new, out, lse)
     _expect_dev_err(dev_err)
     _need_cuda(cache.k, q, k_new, v_new, out, lse, ws, dev_err)
@@ -563,8 +573,8 @@ def reco_paged_decode_attn(cache: PagedKVCache, q: torch.Tensor, k_new: Optional
     ws = _ws(lambda: paged_decode_attn_workspace_size(cache, hq, nl), q.device, ws)
     scale = 1.0 / math.sqrt(D) if scale is None else float(scale)
     with _on(q):
-        st = load_library().reco_paged_decode_attn(cache.ref(), layer0, nl, _ptr(q), hq, scale, int(sinks),
-                                                   int(window), _ptr(k_new), _ptr(v_new), _ptr(out), _ptr(lse),
+        st = load_library().reco_paged_decode_attn(cache.ref(), layer0, nl, _ptr(q), hq, scale, sinks,
+                                                   window, _ptr(k_new), _ptr(v_new), _ptr(out), _ptr(lse),
                                                    _ptr(ws), _nbytes(ws), _ptr(dev_err), _stream(q.device))
     _check(st, "reco_paged_decode_attn")
     return out, lse
@@ -581,6 +591,7 @@ class PreparedPagedDecode:
                  scale: Optional[float] = None, layer0: int = 0, n_layers: Optional[int] = None):
         layer0, nl = _layers(cache, layer0, n_layers)
         NL, Bsz, H, Cap, D = cache.shape
+        sinks, window = _row_counts(sinks=sinks, window=window)
         hq = int(n_q_heads)
         if out is None or ws is None:
             raise ValueError("out and ws must be given")
@@ -597,7 +608,7 @@ class PreparedPagedDecode:
         self._q_shape, self._kv_shape = (nl, Bsz, hq, D), (nl, Bsz, H, D)
         scale = 1.0 / math.sqrt(D) if scale is None else float(scale)
         self._head = (cache.ref(), layer0, nl)
-        self._mid = (hq, scale, int(sinks), int(window))
+        self._mid = (hq, scale, sinks, window)
         self._tail = (_ptr(out), _ptr(lse), _ptr(ws), _nbytes(ws), _ptr(dev_err))
 
     def _check_t(self, t: torch.Tensor, what: str, shape):
@@ -630,6 +641,7 @@ def reco_paged_prefill_attn(cache: PagedKVCache, q: torch.Tensor, k_new: torch.T
     written).  ``window`` > 0: a token sees its last ``window`` rows (its own among
     them) and the first ``sinks``."""
     layer0, nl = _layers(cache, layer0, n_layers)
+    sinks, window = _row_counts(sinks=sinks, window=window)
     NL, B, H, Cap, D = cache.shape
     if q.dim() != 5 or q.shape[0] != nl or q.shape[1] != B or q.shape[4] != D or q.dtype != cache.k.dtype:
         raise ValueError("q must be [n_layers][B][Hq][T][D] in the cache dtype")
@@ -651,7 +663,7 @@ def reco_paged_prefill_attn(cache: PagedKVCache, q: torch.Tensor, k_new: torch.T
     scale = 1.0 / math.sqrt(D) if scale is None else float(scale)
     with _on(q):
         st = load_library().reco_paged_prefill_attn(cache.ref(), layer0, nl, _ptr(q), hq, T, _ptr(n_new), scale,
-                                                    int(sinks), int(window), _ptr(k_new), _ptr(v_new), _ptr(out),
+                                                    sinks, window, _ptr(k_new), _ptr(v_new), _ptr(out),
                                                     _ptr(lse), _ptr(ws), _nbytes(ws), _ptr(dev_err),
                                                     _stream(q.device))
     _check(st, "reco_paged_prefill_attn")
@@ -665,6 +677,7 @@ def reco_paged_evict(cache: PagedKVCache, budget: torch.Tensor, sinks: int = 0, 
     ``sinks`` and the last ``recent`` always; compact K, V and the weights in
     their pages (len <- budget).  ``budget`` is int32 [B] or [n_layers][B]."""
     layer0, nl = _layers(cache, layer0, n_layers)
+    sinks, recent = _row_counts(sinks=sinks, recent=recent)
     NL, Bsz, H, Cap, D = cache.shape
     if cache.weight is None:
         raise ValueError("eviction needs a cache with weights")
@@ -676,7 +689,7 @@ def reco_paged_evict(cache: PagedKVCache, budget: torch.Tensor, sinks: int = 0, 
     ws = _ws(lambda: paged_evict_workspace_size(cache, nl), cache.k.device, ws)
     with _on(cache.k):
         st = load_library().reco_paged_evict(cache.ref(), layer0, nl, _ptr(budget), 0 if budget.dim() == 1 else Bsz,
-                                             int(sinks), int(recent), _ptr(kept_idx), _ptr(ws), _nbytes(ws),
+                                             sinks, recent, _ptr(kept_idx), _ptr(ws), _nbytes(ws),
                                              _ptr(dev_err), _stream(cache.k.device))
     _check(st, "reco_paged_evict")
     return kept_idx
