@@ -174,7 +174,7 @@ reco_status_t reco_paged_prefill_attn(const reco_paged_cache_t *cache, int32_t l
   p.scale_log2 = scale * 1.4426950408889634f;
   p.by_splits = reco::FastDiv(p.splits);
   if (!reco::prefill_fits_grid(p)) return RECO_ERR_UNSUPPORTED;
-  reco::prefill_pieces(p, units);
+  reco::prefill_pieces(p, units, cus);
   reco::prefill_place(p, cache->head_dim, ws);
   return reco::hip_status(reco::launch_paged_prefill(p, cache->dtype, cache->head_dim, stream));
 }

@@ -102,7 +102,8 @@ constexpr int prefill_tile_rows(int dtype) { return dtype == 0 ? 32 : 64; }   //
 int prefill_splits(int units, int blocks, int capacity, int sinks, int window, int tile_rows, int compute_units);
 size_t prefill_workspace_bytes(int units, int tokens, int capacity, int group, int head_dim, int tile_rows,
                                int compute_units);
-void prefill_pieces(PagedPrefillParams &p, int units);
+constexpr int kDeviceUnits = 256;        // compute units of a whole MI355X
+void prefill_pieces(PagedPrefillParams &p, int units, int compute_units = kDeviceUnits);
 bool prefill_fits_grid(const PagedPrefillParams &p);
 void prefill_place(PagedPrefillParams &p, int head_dim, void *ws);
 hipError_t launch_paged_prefill(const PagedPrefillParams &p, int dtype, int head_dim, hipStream_t s);

@@ -114,18 +114,20 @@ size_t prefill_workspace_bytes(int units, int tokens, int capacity, int group, i
 }
 
 // Where every XCD has four rounds of its compute units and more, a piece is up to one
-// round's blocks of a unit: as many as leave the XCDs with the same number of pieces, or
-// nearly.  Without a window a block's work grows with its place, so a piece takes blocks
+// round's blocks of a unit, and a quarter of that at least: as many as leave the XCDs with
+// the same number of pieces, or nearly.  A partition of the device has fewer compute units,
+// and its workgroups take eight turns all the same.  Without a window a block's work grows with its place, so a piece takes blocks
 // from everywhere (its XCD's others wait for none: 8,192 tokens of 16 units of 4 heads
 // 1,601 -> 1,066 us); with one, neighbours see the same keys.
-void prefill_pieces(PagedPrefillParams &p, int units) {
+void prefill_pieces(PagedPrefillParams &p, int units, int compute_units) {
   const int64_t all = static_cast<int64_t>(units) * p.blocks;
   p.pieces = p.near = 0;
   p.spread = p.window == 0 || p.window >= p.tokens;
   p.by_near = FastDiv(1);
-  if (p.splits > 1 || all < 1024) return;
+  if (p.splits > 1 || all < 4 * static_cast<int64_t>(compute_units)) return;
+  const int round = compute_units < kXcds ? 1 : compute_units / kXcds;
   double least = 1e30;
-  for (int near = 32; near >= 8; --near) {
+  for (int near = round; near >= (round + 3) / 4; --near) {
     const int pieces = (p.blocks + near - 1) / near;
     const int size = (p.blocks + pieces - 1) / pieces;
     const int64_t turns = (static_cast<int64_t>(units) * pieces + kXcds - 1) / kXcds;
