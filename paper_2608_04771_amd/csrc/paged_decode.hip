@@ -28,6 +28,7 @@ namespace reco {
 namespace {
 
 constexpr int kTile = kPagedTile;
+constexpr int kSplitWaves = 4;                        // waves of a workgroup
 
 template <typename T, int D>
 struct Cfg {
@@ -46,8 +47,8 @@ struct Cfg {
   static constexpr int rows_per_inst = kWave / lanes_per_row;
   static constexpr int insts = kTile / rows_per_inst;   // 1 KB loads per tile of K or V
   static constexpr int min_wgs = sizeof(T) == 4 && D == 128 ? 1 : 2;
-  static constexpr int smem(int nw) {
-    const int a = nw * wave_stage, b = nw * 16 * (2 + merge_pitch) * 4;
+  static constexpr int smem() {
+    const int a = kSplitWaves * wave_stage, b = kSplitWaves * 16 * (2 + merge_pitch) * 4;
     return a > b ? a : b;
   }
 };
@@ -127,13 +128,13 @@ __device__ __forceinline__ void add_weights(float *weight, const float *logits, 
   }
 }
 
-template <typename T, int D, int NW>
-__global__ __launch_bounds__(NW * kWave, NW == 8 ? 1 : (Cfg<T, D>::min_wgs)) void paged_split_kernel(PagedDecodeParams p) {
+template <typename T, int D>
+__global__ __launch_bounds__(kSplitWaves * kWave, (Cfg<T, D>::min_wgs)) void paged_split_kernel(PagedDecodeParams p) {
   using C = Cfg<T, D>;
   using MF = Mfma<T>;
   using frag = typename MF::frag;
-  constexpr int kThreads = NW * kWave;
-  __shared__ __attribute__((aligned(16))) unsigned char smem[C::smem(NW)];
+  constexpr int kThreads = kSplitWaves * kWave;
+  __shared__ __attribute__((aligned(16))) unsigned char smem[C::smem()];
 
   const int lane = threadIdx.x & (kWave - 1);
   const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) / kWave);
@@ -173,9 +174,9 @@ __global__ __launch_bounds__(NW * kWave, NW == 8 ? 1 : (Cfg<T, D>::min_wgs)) voi
   // Where the wave's tiles lie: each lane holds the place of 16 rows, so 32 tiles at a
   // time; the table's entries of the batch after are on their way meanwhile.
   constexpr int kBatch = kWave / 2;
-  const int mine = i1 - i0 - wave > 0 ? (i1 - i0 - wave + NW - 1) / NW : 0;   // tiles of the wave
+  const int mine = i1 - i0 - wave > 0 ? (i1 - i0 - wave + kSplitWaves - 1) / kSplitWaves : 0;   // tiles of the wave
   const int32_t *table = p.c.pages + cunit * static_cast<size_t>(p.c.max_pages);
-  const auto tile_of = [&](int k) { return seen.tile(i0 + wave + NW * min(k, mine - 1)); };
+  const auto tile_of = [&](int k) { return seen.tile(i0 + wave + kSplitWaves * min(k, mine - 1)); };
   const auto row_of = [&](int batch) { return tile_of(batch * kBatch + lane / 2) * kTile + lane % 2 * 16; };
   unsigned worst = 0;
   int coming = 0;
@@ -256,7 +257,7 @@ __global__ __launch_bounds__(NW * kWave, NW == 8 ? 1 : (Cfg<T, D>::min_wgs)) voi
     if (p.c.weight && col < p.group) {
       const float4 a = make_float4(x[0], x[1], x[2], x[3]), b = make_float4(x[4], x[5], x[6], x[7]);
       if (p.held_logits) {
-        float *to = s_logits + ((i0 + wave + NW * k) * p.group + col) * kTile + 4 * grp;
+        float *to = s_logits + ((i0 + wave + kSplitWaves * k) * p.group + col) * kTile + 4 * grp;
         *reinterpret_cast<float4 *>(to) = a;
         *reinterpret_cast<float4 *>(to + 16) = b;
       } else {
@@ -324,9 +325,9 @@ __global__ __launch_bounds__(NW * kWave, NW == 8 ? 1 : (Cfg<T, D>::min_wgs)) voi
   const float l_tot = group4_sum(l_run);
   __threadfence_block();                                  // logits, before other waves read them
   __syncthreads();
-  float *mw = reinterpret_cast<float *>(smem);            // [NW][16]
-  float *lw = mw + NW * 16;                               // [NW][16]
-  float *ow = lw + NW * 16;                               // [NW][16][merge_pitch]
+  float *mw = reinterpret_cast<float *>(smem);            // [kSplitWaves][16]
+  float *lw = mw + kSplitWaves * 16;                               // [kSplitWaves][16]
+  float *ow = lw + kSplitWaves * 16;                               // [kSplitWaves][16][merge_pitch]
   if (grp == 0) {
     mw[wave * 16 + col] = m_run;
     lw[wave * 16 + col] = l_tot;
@@ -339,12 +340,12 @@ __global__ __launch_bounds__(NW * kWave, NW == 8 ? 1 : (Cfg<T, D>::min_wgs)) voi
   const auto merged = [&](int qi, int d, float &M, float &L) {
     M = -INFINITY;
 #pragma unroll
-    for (int w = 0; w < NW; ++w) M = fmaxf(M, mw[w * 16 + qi]);
+    for (int w = 0; w < kSplitWaves; ++w) M = fmaxf(M, mw[w * 16 + qi]);
     L = 0.f;
     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
     const float ref = M == -INFINITY ? 0.f : M;
 #pragma unroll
-    for (int w = 0; w < NW; ++w) {
+    for (int w = 0; w < kSplitWaves; ++w) {
       const float e = fast_exp2(mw[w * 16 + qi] - ref);
       const float4 v = *reinterpret_cast<const float4 *>(ow + (w * 16 + qi) * C::merge_pitch + d);
       acc.x += v.x * e;
@@ -557,12 +558,12 @@ hipError_t launch_typed(const PagedDecodeParams &p, hipStream_t s) {
   // writes among the reads cost them much of their rate (256 units of 4,225 rows and
   // 4 heads, whose logits are 3% of the bytes: 110 us through memory, 90 held).
   PagedDecodeParams q = p;
-  const int64_t room = (units > p.cus ? kLdsBytes / 2 : kLdsBytes) - Cfg<T, D>::smem(4) - 1024;
+  const int64_t room = (units > p.cus ? kLdsBytes / 2 : kLdsBytes) - Cfg<T, D>::smem() - 1024;
   const int64_t need = p.c.weight && p.splits == 1
                            ? static_cast<int64_t>(paged_span_tiles(p.c.cap, p.sinks, p.window)) * p.group * kTile * 4 : 0;
   q.held_logits = need > 0 && need <= room;
   const int held = q.held_logits ? static_cast<int>(need) : 0;
-  hipLaunchKernelGGL((paged_split_kernel<T, D, 4>), dim3(p.splits, units), dim3(4 * kWave), held, s, q);
+  hipLaunchKernelGGL((paged_split_kernel<T, D>), dim3(p.splits, units), dim3(kSplitWaves * kWave), held, s, q);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.splits == 1) return e;         // one split: finished in place
   const int chunks = paged_weight_chunks(p);

@@ -170,16 +170,16 @@ struct Stager {
   // Before the list's first tile.
   __device__ __forceinline__ void start() {
 #pragma unroll
-    for (int i = 0; i < C::insts; ++i) place_in(i, piece(i) % 16 + lane / C::lanes_per_row, true, true);
+    for (int i = 0; i < C::insts; ++i) place_in(i, piece(i) % 16 + lane / C::lanes_per_row);
   }
 
   // A wave's i-th load of a tile takes wave_rows rows from this one on.
   __device__ __forceinline__ int piece(int i) const { return (i * NW + wave) * C::wave_rows; }
   // Lane offsets of the i-th load, from row `in` of the 16.
-  __device__ __forceinline__ void place_in(int i, int in, bool k, bool v) {
+  __device__ __forceinline__ void place_in(int i, int in) {
     const int row = piece(i) + lane / C::lanes_per_row, c = lane % C::lanes_per_row;
-    if (k) koff[i] = in * C::row_bytes + (c ^ C::k_swap(row)) * 16;
-    if (v) voff[i] = in * C::row_bytes + (c ^ C::v_swap(row)) * 16;
+    koff[i] = in * C::row_bytes + (c ^ C::k_swap(row)) * 16;
+    voff[i] = in * C::row_bytes + (c ^ C::v_swap(row)) * 16;
   }
   __device__ __forceinline__ int tile(int i) const { return seen.tile(min(i, end - 1)); }
   // This lane's tile of the batch that starts at tile i, and its rows there.
@@ -232,14 +232,14 @@ struct Stager {
   }
   // ... and the offsets of a run's last tile, whose rows past the last place must not be
   // read (no tile of the list comes after it).
-  __device__ __forceinline__ void trim(int i, bool k = true, bool v = true) {
+  __device__ __forceinline__ void trim(int i) {
     const int t = tile(i);
     const int row0 = (t - seen.run.old_tiles) * KT;
     if (t < seen.run.old_tiles || row0 + KT <= tokens) return;
 #pragma unroll
     for (int j = 0; j < C::insts; ++j) {
       const int base = min((row0 + piece(j)) & ~15, (tokens - 1) & ~15);
-      place_in(j, min(piece(j) % 16 + lane / C::lanes_per_row, tokens - 1 - base), k, v);
+      place_in(j, min(piece(j) % 16 + lane / C::lanes_per_row, tokens - 1 - base));
     }
   }
   // Rows of V that no token of the block sees count for nothing, whatever they hold.
