@@ -212,7 +212,7 @@ __global__ __launch_bounds__(kCompThreads) void evict_compact_kernel(PagedEvictP
   constexpr int kPasses = evict_chunk_rows(ROWB) / kRowsPerPass;
   constexpr int kRows = kPasses * kRowsPerPass;
   static_assert(kRows <= kCompThreads, "a weight a thread");
-  __shared__ int s_ticket, s_known;
+  __shared__ int s_ticket, s_known, s_stalled;
 
   const int unit = blockIdx.x;
   const int tid = threadIdx.x;
@@ -224,7 +224,7 @@ __global__ __launch_bounds__(kCompThreads) void evict_compact_kernel(PagedEvictP
   const int shift = p.c.page_shift, mask = (1 << shift) - 1;
   int32_t *ticket = p.state + static_cast<size_t>(unit) * p.state_pitch;
   int32_t *prefix = ticket + 1;                          // chunks before this one are known to be loaded
-  int32_t *stored = ticket + 2;                          // chunks whose rows are in their places
+  int32_t *stored = ticket + 2;                          // chunks that are, or are being, stored
   int32_t *loaded = ticket + kEvictState;
   unsigned char *k = reinterpret_cast<unsigned char *>(p.c.k) + tid % kLanesPerRow * 16;
   unsigned char *v = reinterpret_cast<unsigned char *>(p.c.v) + tid % kLanesPerRow * 16;
@@ -238,9 +238,12 @@ __global__ __launch_bounds__(kCompThreads) void evict_compact_kernel(PagedEvictP
     s_ticket = chunk;
     s_known = before;
   };
-  if (tid == 0) take();
+  if (tid == 0) {
+    s_stalled = 0;
+    take();
+  }
   __syncthreads();
-  int mine = 0;                                          // chunks that this workgroup has stored
+  int mine = 0;                                          // chunks that this workgroup stores
   for (;;) {
     const int c = s_ticket, known = s_known;
     const int r0 = c * kRows;
@@ -272,11 +275,20 @@ __global__ __launch_bounds__(kCompThreads) void evict_compact_kernel(PagedEvictP
     int spins = 0;
     for (int f = known + tid; f < c && spins <= p.max_spins; f += kCompThreads)
       while (!relaxed_load(&loaded[f]) && ++spins <= p.max_spins) __builtin_amdgcn_s_sleep(1);
-    if (__syncthreads_or(spins > p.max_spins)) {         // rows that this chunk's would replace may still be wanted
+    if (spins > p.max_spins) s_stalled = 1;
+    __syncthreads();
+    if (s_stalled) {                                     // rows that this chunk's would replace may still be wanted
       if (tid == 0) report(p.c.dev_err, kDevStalled);
-      break;
+      return;
     }
-    if (tid == 0) atomicMax(prefix, c);
+    // Nothing keeps the chunk from being stored now: whoever counts the unit's last one
+    // sets its length, beside the stores.
+    ++mine;
+    int count = 0;
+    if (tid == 0) {
+      atomicMax(prefix, c);
+      if (s_ticket * kRows >= m) count = atomicAdd(stored, mine) + mine;
+    }
     if (moves) {
 #pragma unroll
       for (int i = 0; i < kPasses; ++i) {
@@ -289,10 +301,8 @@ __global__ __launch_bounds__(kCompThreads) void evict_compact_kernel(PagedEvictP
       }
       if (r0 + tid <= last && tid < kRows) weight[r0 + tid] = w;
     }
-    ++mine;
+    if (tid == 0 && count == (m + kRows - 1) / kRows) p.c.len[cunit] = m;
   }
-  // Whoever stores the unit's last chunk sets its length.
-  if (mine > 0 && tid == 0 && atomicAdd(stored, mine) + mine == (m + kRows - 1) / kRows) p.c.len[cunit] = m;
 }
 
 }  // namespace
