@@ -527,13 +527,13 @@ class PreparedDecode:
         return self.out, self.lse
 
 
-def _row_counts(**counts):
-    """Counts of rows as the C ABI takes them; a larger one would lose its upper bits on
+def _row_count(n, what: str) -> int:
+    """A count of rows as the C ABI takes it; a larger one would lose its upper bits on
     the way (2**32 + 5 rows of window would be five)."""
-    for what, n in counts.items():
-        if not -2 ** 31 <= int(n) < 2 ** 31:
-            raise ValueError(f"{what} must fit 32 bits, got {n}")
-    return tuple(int(n) for n in counts.values())
+    n = int(n)
+    if not -0x80000000 <= n <= 0x7fffffff:
+        raise ValueError(f"{what} must fit 32 bits, got {n}")
+    return n
 
 
 def _paged_decode_shapes(cache: PagedKVCache, nl: int, q: torch.Tensor, k_new, v_new, out, lse):
@@ -561,7 +561,7 @@ def reco_paged_decode_attn(cache: PagedKVCache, q: torch.Tensor, k_new: Optional
     ``window`` rows (its own among them) and the first ``sinks``.  A cache with
     weights accumulates them."""
     layer0, nl = _layers(cache, layer0, n_layers)
-    sinks, window = _row_counts(sinks=sinks, window=window)
+    sinks, window = _row_count(sinks, "sinks"), _row_count(window, "window")
     hq = _paged_decode_shapes(cache, nl, q, k_new, v_new, out, lse)
     _expect_dev_err(dev_err)
     _need_cuda(cache.k, q, k_new, v_new, out, lse, ws, dev_err)
@@ -591,7 +591,7 @@ class PreparedPagedDecode:
                  scale: Optional[float] = None, layer0: int = 0, n_layers: Optional[int] = None):
         layer0, nl = _layers(cache, layer0, n_layers)
         NL, Bsz, H, Cap, D = cache.shape
-        sinks, window = _row_counts(sinks=sinks, window=window)
+        sinks, window = _row_count(sinks, "sinks"), _row_count(window, "window")
         hq = int(n_q_heads)
         if out is None or ws is None:
             raise ValueError("out and ws must be given")
@@ -641,7 +641,7 @@ def reco_paged_prefill_attn(cache: PagedKVCache, q: torch.Tensor, k_new: torch.T
     written).  ``window`` > 0: a token sees its last ``window`` rows (its own among
     them) and the first ``sinks``."""
     layer0, nl = _layers(cache, layer0, n_layers)
-    sinks, window = _row_counts(sinks=sinks, window=window)
+    sinks, window = _row_count(sinks, "sinks"), _row_count(window, "window")
     NL, B, H, Cap, D = cache.shape
     if q.dim() != 5 or q.shape[0] != nl or q.shape[1] != B or q.shape[4] != D or q.dtype != cache.k.dtype:
         raise ValueError("q must be [n_layers][B][Hq][T][D] in the cache dtype")
@@ -677,7 +677,7 @@ def reco_paged_evict(cache: PagedKVCache, budget: torch.Tensor, sinks: int = 0, 
     ``sinks`` and the last ``recent`` always; compact K, V and the weights in
     their pages (len <- budget).  ``budget`` is int32 [B] or [n_layers][B]."""
     layer0, nl = _layers(cache, layer0, n_layers)
-    sinks, recent = _row_counts(sinks=sinks, recent=recent)
+    sinks, recent = _row_count(sinks, "sinks"), _row_count(recent, "recent")
     NL, Bsz, H, Cap, D = cache.shape
     if cache.weight is None:
         raise ValueError("eviction needs a cache with weights")
