@@ -58,6 +58,11 @@
  *   each unit; rows at or beyond len are never read as keys.
  * - GQA: query head hq (0 <= hq < n_q_heads) attends through KV head
  *   hq / G with G = n_q_heads / n_kv_heads (1 <= G <= 16).
+ * - Attention's logits, softmax statistics, partial results and accumulated
+ *   weights are fp32.  Over a bf16 cache (dense or paged) each probability is
+ *   rounded to bf16, by 2^-8 of it at most, where it is multiplied with V, and
+ *   the result once more; log-sum-exps, statistics and weights come from the
+ *   unrounded ones.  Over an fp32 cache nothing is rounded to fewer bits.
  * - A call covers layers [layer0, layer0 + n_layers) of the cache; per-layer
  *   inputs and outputs (queries, scores, outputs) are laid out with a
  *   leading [n_layers] dimension for exactly those layers.

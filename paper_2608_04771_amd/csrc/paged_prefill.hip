@@ -18,11 +18,15 @@
 // joined by the second kernel.
 //
 // Long runs are bound by the matrix units and what feeds them: 16,384 tokens of a 7B
-// layer in a window of 4,096 take 835-870 us, 970-1,010 TFLOP/s, where a large library
-// product reaches 1,190 on the same card.  No one part is the rest: without the loads to
+// layer in a window of 4,096 take 860 us (the median; 838 at best), 980 TFLOP/s, where a
+// large library product reaches 1,190 on the same card.  No one part is the rest: without the loads to
 // LDS it takes 18% less, without the reads of K 18%, of V 6%, without the exponentials
 // 6%.  64 rows a wave (half the LDS reads) need more registers than a wave has and copy
-// (1,110 us on chunks that take 786); two tiles in flight by halves of a workgroup, 985.
+// (1,110 us on chunks that took 786 then); two tiles in flight by halves of a workgroup, 985.
+// The careful pass over blocks with infinities or NaN (below) is compiled into the same
+// kernel and costs every call registers: at head_dim 128 bf16 245 vector registers, 233
+// without it, fp32 256 and 106 more in memory, 245 without; at 64 bf16 237 and 147, fp32 219
+// and 169.
 #include "paged_device.hpp"
 
 #include <type_traits>
@@ -349,8 +353,8 @@ __device__ __forceinline__ void write_rows(const PagedPrefillParams &p, unsigned
 // Puts rows [first, first + kAppendRows) of a unit's run into their pages; a unit's rows are
 // appended together or, where they or their pages do not fit, not at all.  The rows come
 // while it is found out where they go.  Attention may go on meanwhile: it has no use for
-// rows of the cache past L (prompts of 200 to 512 tokens 42.5 -> 38.5 us per call against a
-// kernel after the attention, 16,384 tokens 850 -> 856).  Returns whether the unit's rows
+// rows of the cache past L (against a kernel after the attention, prompts of 200 to 512
+// tokens take 4 us less of 39 per call, 16,384 tokens 6 us more of 850).  Returns whether the unit's rows
 // are stored.
 constexpr int kAppendRows = kPrefillAppendRows;
 
