@@ -31,6 +31,10 @@
  *                        a paged cache, window and sinks optional   (Sec. 3.3)
  *   reco_paged_evict     keep a budget of rows by accumulated attention
  *                        weight, compacted within their pages        (Sec. 1)
+ *   reco_rope            rotation of query or key rows by their
+ *                        positions, on one to four axes              (Sec. 1)
+ *   reco_paged_append    rows appended to a paged cache, keys rotated
+ *                        on the way                                  (Sec. 1)
  *
  * Conventions shared by every call
  * --------------------------------
@@ -363,6 +367,68 @@ reco_status_t reco_paged_evict(const reco_paged_cache_t *cache, int32_t layer0, 
                                const int32_t *budget, int64_t budget_layer_stride, int32_t sinks,
                                int32_t recent, int32_t *kept_idx, void *ws, size_t ws_bytes,
                                int32_t *dev_err, hipStream_t stream);
+
+/* ------------------------------------------------------------------------ */
+/* [host] Rows of head_dim elements each, one for every (layer, sequence, head, token)
+ * of a call; read during the call, not retained.  A row's elements are contiguous; row
+ * (l, b, h, t) starts at data + l * layer + b * seq + h * head + t * token elements, so
+ * that a projection's output is taken as it lies.  data and all strides are multiples
+ * of 16 bytes.  Rows that a call writes must not overlap. */
+typedef struct reco_rows {
+  void *data;
+  int64_t layer, seq, head, token;   /* in elements */
+} reco_rows_t;
+
+/* [host] A rotation by positions; read during the call, not retained.  Pair i of a row
+ * is turned by the angle pos[axis[i]][b][t] * inv_freq[i] (radians):
+ *   (x, y) <- (x cos a - y sin a, x sin a + y cos a).
+ * Text has one axis; images and video have several (time, height, width, ...), each
+ * with pairs of its own.  Positions may be negative: the rotation by -p undoes that by
+ * p, and is its gradient.  Angles are formed in 64 bits and reduced to a turn there, so
+ * that far positions keep fp32's precision; products are fp32, and each result is
+ * rounded to the rows' type once. */
+typedef struct reco_rope {
+  const float *inv_freq;  /* [rot_dim / 2] */
+  const int32_t *pos;     /* [n_axes][batch][n_tokens] */
+  const int32_t *axis;    /* [host] nullable [rot_dim / 2], each in [0, n_axes); NULL: all 0 */
+  int32_t n_axes;         /* 1 to 4 */
+  int32_t rot_dim;        /* rotated elements, the first ones of a row: a multiple of 16, at
+                             most head_dim; the others pass unchanged, bit for bit */
+  int32_t interleaved;    /* 0: pair i is elements (i, i + rot_dim / 2); 1: (2 i, 2 i + 1) */
+} reco_rope_t;
+
+/* Rotates rows of n_heads heads (queries, keys, or both where they lie behind each
+ * other) from x to out, which may be the same rows (in place).
+ *   n_new    : nullable [batch] int32 in [0, n_tokens]: the real tokens of each sequence,
+ *              the first ones; places past them are neither read nor written.  A bad one
+ *              counts as 0 (RECO_DEV_BAD_LENGTH)
+ *   head_dim : 64 or 128;  dtype : reco_dtype_t
+ * At most 1,024 heads, 65,535 sequences and layers, and 2^24 tokens
+ * (larger: RECO_ERR_UNSUPPORTED). */
+reco_status_t reco_rope(const reco_rope_t *rope, const reco_rows_t *x, const reco_rows_t *out,
+                        int32_t n_layers, int32_t batch, int32_t n_heads, int32_t n_tokens,
+                        int32_t head_dim, int32_t dtype, const int32_t *n_new, int32_t *dev_err,
+                        hipStream_t stream);
+
+/* Appends n = n_new[b] tokens (n_tokens of them where n_new is NULL) to every unit of a
+ * paged cache, without attention: row L + t of a unit with L = len[unit] becomes k_new's
+ * row, rotated where rope is given, and v_new's as it is; weights of the new rows (where
+ * cache->weight is given) become 0, and len L + n.  Queries that go with them are
+ * rotated in the same pass.
+ *   rope         : nullable: rows are taken as they are
+ *   k_new, v_new : rows of n_kv_heads heads, cache dtype
+ *   q, q_out     : both NULL or rows of n_q_heads heads, cache dtype; q_out may be q
+ * Decode attention without an append (k_new = NULL) then sees the rows.  A unit whose
+ * length is bad (RECO_DEV_BAD_LENGTH), whose run does not fit its capacity
+ * (RECO_DEV_APPEND_OVERFLOW) or whose rows' page ids are bad (RECO_DEV_BAD_PAGE) keeps
+ * its len; what its pages hold past that is then unspecified.  A bad n_new counts as 0
+ * (RECO_DEV_BAD_LENGTH).  q_out is written in all these cases.  At most 1,024 heads and
+ * 2^24 tokens (larger: RECO_ERR_UNSUPPORTED). */
+reco_status_t reco_paged_append(const reco_paged_cache_t *cache, int32_t layer0, int32_t n_layers,
+                                const reco_rope_t *rope, int32_t n_tokens, const int32_t *n_new,
+                                const reco_rows_t *k_new, const reco_rows_t *v_new,
+                                const reco_rows_t *q, const reco_rows_t *q_out, int32_t n_q_heads,
+                                int32_t *dev_err, hipStream_t stream);
 
 /* ------------------------------------------------------------------------ */
 /* Eq. 3 and Eq. 4 (Section 3.3, reward-banded reflection penalty): for every

@@ -39,7 +39,7 @@ EXPORTED = [
     "reco_penalty_sample_workspace_size", "reco_penalty_sample",
     "reco_paged_decode_attn_workspace_size", "reco_paged_decode_attn",
     "reco_paged_prefill_attn_workspace_size", "reco_paged_prefill_attn",
-    "reco_paged_evict_workspace_size", "reco_paged_evict",
+    "reco_paged_evict_workspace_size", "reco_paged_evict", "reco_rope", "reco_paged_append",
     "reco_answer_ppl_workspace_size", "reco_answer_ppl", "reco_retention_from_reward", "reco_retention_eq1",
     "reco_kept_count", "reco_status_str", "reco_abi_version",
 ]
@@ -59,6 +59,16 @@ class RecoPagedCache(ctypes.Structure):
                 ("head_dim", ctypes.c_int32), ("dtype", ctypes.c_int32)]
 
 
+class RecoRows(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("layer", ctypes.c_int64), ("seq", ctypes.c_int64),
+                ("head", ctypes.c_int64), ("token", ctypes.c_int64)]
+
+
+class RecoRope(ctypes.Structure):
+    _fields_ = [("inv_freq", ctypes.c_void_p), ("pos", ctypes.c_void_p), ("axis", ctypes.POINTER(ctypes.c_int32)),
+                ("n_axes", ctypes.c_int32), ("rot_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32)]
+
+
 _lib = None
 
 
@@ -74,6 +84,8 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
                                            ctypes.c_double, ctypes.c_size_t, ctypes.c_uint32, ctypes.c_uint64)
     C = ctypes.POINTER(RecoKVCache)
     PC = ctypes.POINTER(RecoPagedCache)
+    RR = ctypes.POINTER(RecoRows)
+    RP = ctypes.POINTER(RecoRope)
     sig = {
         "reco_score_workspace_size": (SZ, [C, I32, I32, I32]),
         "reco_score": (I32, [C, I32, I32, P, I32, I32, F32, U32, P, P, P, SZ, P, P]),
@@ -90,6 +102,8 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
         "reco_paged_prefill_attn": (I32, [PC, I32, I32, P, I32, I32, P, F32, I32, I32, P, P, P, P, P, SZ, P, P]),
         "reco_paged_evict_workspace_size": (SZ, [PC, I32]),
         "reco_paged_evict": (I32, [PC, I32, I32, P, I64, I32, I32, P, P, SZ, P, P]),
+        "reco_rope": (I32, [RP, RR, RR, I32, I32, I32, I32, I32, I32, P, P, P]),
+        "reco_paged_append": (I32, [PC, I32, I32, RP, I32, P, RR, RR, RR, RR, I32, P, P]),
         "reco_logit_penalty": (I32, [P, I32, I32, I64, P, I32, P, F32, F32, F32, F32, F32, P, P]),
         "reco_penalty_sample_workspace_size": (SZ, [I32, I32]),
         "reco_penalty_sample": (I32, [P, I32, I32, I64, P, I32, P, F32, F32, F32, F32, F32, F32, U64, U64, P, P, SZ,
@@ -693,6 +707,222 @@ def reco_paged_evict(cache: PagedKVCache, budget: torch.Tensor, sinks: int = 0, 
                                              _ptr(dev_err), _stream(cache.k.device))
     _check(st, "reco_paged_evict")
     return kept_idx
+
+
+class Rope:
+    """A rotation by positions: ``inv_freq`` fp32 [rot_dim / 2] on the GPU, radians per
+    position of each pair, and the axis of each pair (``axes``, of 0 to 3; none: all
+    pairs turn by axis 0).  Pair i is the elements (i, i + rot_dim / 2) of a row, or
+    (2 i, 2 i + 1) where ``interleaved``."""
+
+    def __init__(self, inv_freq: torch.Tensor, axes: Optional[Sequence[int]] = None, interleaved: bool = False):
+        if inv_freq.dtype != torch.float32 or inv_freq.dim() != 1 or inv_freq.numel() < 1:
+            raise ValueError("inv_freq must be float32 [rot_dim / 2]")
+        _need_cuda(inv_freq)
+        n = inv_freq.numel()
+        axes = None if axes is None else [int(a) for a in axes]
+        if axes is not None and (len(axes) != n or min(axes) < 0 or max(axes) > 3):
+            raise ValueError(f"axes must give each of the {n} pairs an axis of 0 to 3")
+        self.inv_freq, self.rot_dim, self.interleaved = inv_freq, 2 * n, bool(interleaved)
+        self.n_axes = 1 if axes is None else max(axes) + 1
+        self._axes = None if axes is None else (ctypes.c_int32 * n)(*axes)
+
+    def _struct(self, pos: torch.Tensor) -> RecoRope:
+        return RecoRope(self.inv_freq.data_ptr(), pos.data_ptr(), self._axes, self.n_axes, self.rot_dim,
+                        int(self.interleaved))
+
+    def _check_pos(self, pos: torch.Tensor, batch: int, T: int):
+        shapes = [(self.n_axes, batch, T)] + ([(batch, T)] if self.n_axes == 1 else [])
+        if T == 1:
+            shapes += [x[:-1] for x in shapes]
+        if pos is None or pos.dtype != torch.int32 or tuple(pos.shape) not in shapes:
+            raise ValueError(f"pos must be int32 [{self.n_axes}][B={batch}][T={T}]")
+        _need_cuda(pos, self.inv_freq)
+
+
+class _Rows:
+    """A tensor's rows as the C ABI takes them: [n_layers][B][heads][T][D], or without T
+    for one token, in any order of memory whose rows are contiguous and 16-byte aligned."""
+
+    __slots__ = ("shape", "dtype", "device", "what", "struct", "_strides", "_piece", "_token", "_write")
+
+    def __init__(self, what: str, shape, dtype: torch.dtype, device, write: bool = False):
+        self.what, self.shape, self.dtype, self.device, self._write = what, tuple(shape), dtype, device, write
+        self._token = len(self.shape) == 4
+        self._piece = 4 if dtype == torch.float32 else 8
+        self._strides = None
+        self.struct = RecoRows()
+
+    def take(self, t: torch.Tensor):
+        if tuple(t.shape) != self.shape or t.dtype != self.dtype or t.device != self.device:
+            raise ValueError(f"{self.what} must be {_DT.get(self.dtype, self.dtype)} {list(self.shape)} on {self.device}, "
+                             f"got {_DT.get(t.dtype, t.dtype)} {list(t.shape)} on {t.device}")
+        st = t.stride()
+        if st != self._strides:
+            if st[-1] != 1 or any(n > 1 and x % self._piece for n, x in zip(self.shape[:-1], st[:-1])):
+                raise ValueError(f"{self.what}: rows must be contiguous and multiples of 16 bytes apart")
+            st4 = [x if n > 1 else 0 for n, x in zip(self.shape[:-1], st[:-1])]      # those of one are not used
+            if self._write:
+                end = self.shape[-1]
+                for x, n in sorted((x, n) for n, x in zip(self.shape[:-1], st4) if n > 1):
+                    if x < end:
+                        raise ValueError(f"{self.what}: rows must not overlap")
+                    end = x * (n - 1) + end
+            s = self.struct
+            s.layer, s.seq, s.head = st4[:3]
+            s.token = 0 if self._token else st4[3]
+            self._strides = st
+        p = t.data_ptr()
+        if p & 15:
+            raise ValueError(f"{self.what} must be 16-byte aligned")
+        self.struct.data = p
+        return ctypes.byref(self.struct)
+
+
+def _no_partial_overlap(x: torch.Tensor, out: torch.Tensor, what: str):
+    """``out`` is x itself, or none of its rows meet x's."""
+    def span(t):
+        return t.data_ptr(), t.data_ptr() + t.element_size() * (1 + sum((n - 1) * s for n, s in zip(t.shape, t.stride())))
+    (a, a1), (b, b1) = span(x), span(out)
+    if a1 <= b or b1 <= a or (a == b and x.stride() == out.stride()):
+        return
+    d, e = abs(a - b), x.element_size()
+    heads = x.shape[2] * x.stride(2) * e
+    others = [s * e for i, (n, s) in enumerate(zip(x.shape, x.stride())) if i not in (2, x.dim() - 1) and n > 1]
+    if x.stride() == out.stride() and heads <= d and all(d + heads <= s for s in others):
+        return                                             # other heads of the same tokens
+    raise ValueError(f"{what} must be the same rows as its input or meet none of them")
+
+
+class PreparedRope:
+    """reco_rope for a loop that calls it again and again with the same positions
+    tensor, output and counts (whose contents may change): those are checked once
+    here, each call checks its input."""
+
+    def __init__(self, rope: Rope, pos: torch.Tensor, out: torch.Tensor, n_new: Optional[torch.Tensor] = None,
+                 dev_err: Optional[torch.Tensor] = None):
+        if out.dim() not in (4, 5) or out.dtype not in (torch.float32, torch.bfloat16) or out.numel() == 0:
+            raise ValueError("rows must be float32 or bfloat16 [NL][B][H][T][D], or without T for one token")
+        NL, Bsz, H, *T, D = out.shape
+        T = T[0] if T else 1
+        if rope.rot_dim > D:
+            raise ValueError(f"rot_dim {rope.rot_dim} is larger than a row of {D}")
+        rope._check_pos(pos, Bsz, T)
+        _expect(n_new, "n_new", (Bsz,), torch.int32)
+        _expect_dev_err(dev_err)
+        _need_cuda(pos, n_new, dev_err)
+        _same_gpu(out, pos)
+        self.out = out
+        self._keep = (rope, pos, n_new, dev_err)
+        self._fn = load_library().reco_rope
+        self._dev = out.device
+        self._struct = rope._struct(pos)
+        self._in = _Rows("x", out.shape, out.dtype, out.device)
+        self._head = ctypes.byref(self._struct)
+        self._out = _Rows("out", out.shape, out.dtype, out.device, write=True).take(out)
+        self._tail = (NL, Bsz, H, T, D, RECO_F32 if out.dtype == torch.float32 else RECO_BF16, _ptr(n_new),
+                      _ptr(dev_err))
+
+    def __call__(self, x: torch.Tensor) -> torch.Tensor:
+        xr = self._in.take(x)
+        _no_partial_overlap(x, self.out, "out")
+        with _on(x):
+            st = self._fn(self._head, xr, self._out, *self._tail, _stream(self._dev))
+        if st != RECO_OK:
+            _check(st, "reco_rope")
+        return self.out
+
+
+def reco_rope(rope: Rope, x: torch.Tensor, pos: torch.Tensor, n_new: Optional[torch.Tensor] = None,
+              out: Optional[torch.Tensor] = None, dev_err: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Rows x ([NL][B][H][T][D], or [NL][B][H][D] for one token, of any strides whose rows
+    are contiguous) rotated by ``pos`` (int32 [B][T], or [n_axes][B][T]); returns ``out``
+    (contiguous where none is given; x itself rotates in place).  ``n_new`` int32 [B]: the
+    real tokens of each sequence, the first ones; places past them are not written."""
+    if out is None:
+        out = torch.empty(x.shape, dtype=x.dtype, device=x.device) if n_new is None else \
+            torch.zeros(x.shape, dtype=x.dtype, device=x.device)
+    return PreparedRope(rope, pos, out, n_new, dev_err)(x)
+
+
+class PreparedPagedAppend:
+    """reco_paged_append for a loop that calls it again and again with the same cache,
+    positions tensor, rotated queries and counts (whose contents may change): those are
+    checked once here, each call checks the new rows.  ``n_tokens`` None: rows without
+    the dimension T, one token each."""
+
+    def __init__(self, cache: PagedKVCache, n_tokens: Optional[int] = None, rope: Optional[Rope] = None,
+                 pos: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None,
+                 n_new: Optional[torch.Tensor] = None, layer0: int = 0, n_layers: Optional[int] = None,
+                 dev_err: Optional[torch.Tensor] = None):
+        layer0, nl = _layers(cache, layer0, n_layers)
+        NL, Bsz, H, Cap, D = cache.shape
+        run = () if n_tokens is None else (_row_count(n_tokens, "n_tokens"),)
+        T = run[0] if run else 1
+        if T < 1:
+            raise ValueError("n_tokens must be 1 or more")
+        if (rope is None) != (pos is None):
+            raise ValueError("rope and pos must be given together")
+        if rope is not None:
+            if rope.rot_dim > D:
+                raise ValueError(f"rot_dim {rope.rot_dim} is larger than a row of {D}")
+            rope._check_pos(pos, Bsz, T)
+        dt, dev = cache.k.dtype, cache.k.device
+        hq = 0
+        if q_out is not None:
+            if q_out.dim() != 4 + len(run):
+                raise ValueError("q_out must be [n_layers][B][Hq][T][D] (without T for one token)")
+            hq = q_out.shape[2]
+        _expect(n_new, "n_new", (Bsz,), torch.int32)
+        _expect_dev_err(dev_err)
+        _need_cuda(cache.k, pos, n_new, dev_err)
+        self.cache, self.q_out = cache, q_out
+        self._keep = (rope, pos, n_new, dev_err)
+        self._fn = load_library().reco_paged_append
+        self._dev = dev
+        self._k, self._v = (_Rows(what, (nl, Bsz, H, *run, D), dt, dev) for what in ("k_new", "v_new"))
+        self._q = self._qo = None
+        if q_out is not None:
+            shape = (nl, Bsz, hq, *run, D)
+            self._q = _Rows("q", shape, dt, dev)
+            self._qo = _Rows("q_out", shape, dt, dev, write=True).take(q_out)
+        self._struct = None if rope is None else rope._struct(pos)
+        self._head = (cache.ref(), layer0, nl, None if rope is None else ctypes.byref(self._struct), T, _ptr(n_new))
+        self._tail = (hq, _ptr(dev_err))
+
+    def __call__(self, k_new: torch.Tensor, v_new: torch.Tensor, q: Optional[torch.Tensor] = None):
+        if (q is None) != (self._q is None):
+            raise ValueError("q and q_out must be given together")
+        k, v = self._k.take(k_new), self._v.take(v_new)
+        qr = None
+        if q is not None:
+            qr = self._q.take(q)
+            _no_partial_overlap(q, self.q_out, "q_out")
+        with _on(k_new):
+            st = self._fn(*self._head, k, v, qr, self._qo, *self._tail, _stream(self._dev))
+        if st != RECO_OK:
+            _check(st, "reco_paged_append")
+        return self.q_out
+
+
+def reco_paged_append(cache: PagedKVCache, k_new: torch.Tensor, v_new: torch.Tensor, rope: Optional[Rope] = None,
+                      pos: Optional[torch.Tensor] = None, q: Optional[torch.Tensor] = None,
+                      n_new: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None, layer0: int = 0,
+                      n_layers: Optional[int] = None, dev_err: Optional[torch.Tensor] = None):
+    """Append rows k_new, v_new ([n_layers][B][H][T][D], or [n_layers][B][H][D] for one
+    token, of any strides whose rows are contiguous) to every unit, keys rotated by
+    ``rope`` at ``pos`` (int32 [B][T], or [n_axes][B][T]); returns the queries q
+    ([n_layers][B][Hq][T][D]) rotated with them (``q_out``, contiguous where none is
+    given), or None.  ``n_new`` int32 [B]: the real tokens of each sequence, the first
+    ones.  Decode attention without k_new then sees the rows."""
+    if k_new.dim() not in (4, 5):
+        raise ValueError("k_new must be [n_layers][B][H][T][D] (without T for one token)")
+    if q is not None and q_out is None:
+        q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device) if n_new is None else \
+            torch.zeros(q.shape, dtype=q.dtype, device=q.device)
+    call = PreparedPagedAppend(cache, k_new.shape[3] if k_new.dim() == 5 else None, rope, pos, q_out, n_new, layer0,
+                               n_layers, dev_err)
+    return call(k_new, v_new, q)
 
 
 def _logit_rows(logits: torch.Tensor):

@@ -1,5 +1,5 @@
-// C ABI of the operators over a paged KV cache: host-side argument validation,
-// workspace sizing and launches, in the manner of abi.cpp.
+// C ABI of the operators over a paged KV cache, and of the rotation by positions:
+// host-side argument validation, workspace sizing and launches, in the manner of abi.cpp.
 #include "reco.h"
 
 #include <hip/hip_runtime.h>
@@ -9,12 +9,15 @@
 
 #include "abi_common.hpp"
 #include "paged.hpp"
+#include "rope.hpp"
 
 namespace {
 
 // Positions rounded up to a tile, and sums of two of them, stay inside int32.
 constexpr int64_t kMaxCapacity = int64_t{1} << 29;
 constexpr int64_t kMaxQueryRows = int64_t{1} << 28;   // of one KV head in a run
+constexpr int kMaxRowTokens = 1 << 24;
+constexpr int kMaxRowHeads = 1024;                    // of a rotated or appended token (their places lie in LDS)
 
 bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 
@@ -74,9 +77,99 @@ reco::PagedCache paged_cache(const reco_paged_cache_t *c, int32_t layer0, int32_
   return p;
 }
 
+// Rows that a kernel can address: strides and base are whole 16-byte pieces.
+bool rows_ok(const reco_rows_t *r, int elem) {
+  if (!r || !r->data || !aligned16(r->data)) return false;
+  const int64_t piece = 16 / elem;
+  return r->layer % piece == 0 && r->seq % piece == 0 && r->head % piece == 0 && r->token % piece == 0;
+}
+
+reco::RowsOf rows_of(const reco_rows_t *r) { return reco::RowsOf{r->data, r->layer, r->seq, r->head, r->token}; }
+
+// Rotation, sizes and types that both calls have; layers is the call's.
+reco_status_t rope_params(reco::RopeParams &p, const reco_rope_t *rope, int32_t n_layers, int32_t batch,
+                          int32_t n_tokens, int32_t head_dim, int32_t dtype, const int32_t *n_new, int32_t *dev_err) {
+  if (n_layers < 1 || batch < 1 || n_tokens < 1) return RECO_ERR_INVALID_ARG;
+  if (rope) {
+    if (!rope->inv_freq || !rope->pos || rope->n_axes < 1 || rope->rot_dim < 2 || rope->rot_dim % 2 ||
+        rope->rot_dim > head_dim || rope->interleaved < 0 || rope->interleaved > 1)
+      return RECO_ERR_INVALID_ARG;
+    if (rope->axis) {
+      for (int i = 0; i < rope->rot_dim / 2; ++i)
+        if (rope->axis[i] < 0 || rope->axis[i] >= rope->n_axes) return RECO_ERR_INVALID_ARG;
+    }
+  }
+  if (head_dim != 64 && head_dim != 128) return RECO_ERR_UNSUPPORTED;
+  if (dtype != RECO_F32 && dtype != RECO_BF16) return RECO_ERR_UNSUPPORTED;
+  if (batch > 65535 || n_layers > 65535) return RECO_ERR_UNSUPPORTED;
+  if (n_tokens > kMaxRowTokens) return RECO_ERR_UNSUPPORTED;
+  if (rope) {
+    if (rope->n_axes > reco::kRopeMaxAxes || rope->rot_dim % 16) return RECO_ERR_UNSUPPORTED;
+    p.freq = rope->inv_freq;
+    p.pos = rope->pos;
+    p.rot = rope->rot_dim;
+    p.pairs = rope->interleaved != 0;
+    for (int i = 0; rope->axis && i < rope->rot_dim / 2; ++i)
+      p.axis[i / 32] |= static_cast<uint64_t>(rope->axis[i]) << (2 * (i % 32));
+  }
+  p.block = reco::rope_block(n_tokens);
+  p.n_new = n_new;
+  p.dev_err = dev_err;
+  p.layers = n_layers;
+  p.batch = batch;
+  p.tokens = n_tokens;
+  return RECO_OK;
+}
+
 }  // namespace
 
 extern "C" {
+
+// ---------------------------------------------------------------- rotation
+reco_status_t reco_rope(const reco_rope_t *rope, const reco_rows_t *x, const reco_rows_t *out, int32_t n_layers,
+                        int32_t batch, int32_t n_heads, int32_t n_tokens, int32_t head_dim, int32_t dtype,
+                        const int32_t *n_new, int32_t *dev_err, hipStream_t stream) {
+  const int elem = dtype == RECO_F32 ? 4 : 2;
+  if (!rope || !rows_ok(x, elem) || !rows_ok(out, elem) || n_heads < 1) return RECO_ERR_INVALID_ARG;
+  reco::RopeParams p{};
+  const reco_status_t st = rope_params(p, rope, n_layers, batch, n_tokens, head_dim, dtype, n_new, dev_err);
+  if (st != RECO_OK) return st;
+  if (n_heads > kMaxRowHeads) return RECO_ERR_UNSUPPORTED;
+  p.q = rows_of(x);
+  p.q_out = rows_of(out);
+  p.heads = n_heads;
+  return reco::hip_status(reco::launch_rope(p, dtype, head_dim, stream));
+}
+
+// ---------------------------------------------------------------- append
+reco_status_t reco_paged_append(const reco_paged_cache_t *cache, int32_t layer0, int32_t n_layers,
+                                const reco_rope_t *rope, int32_t n_tokens, const int32_t *n_new,
+                                const reco_rows_t *k_new, const reco_rows_t *v_new, const reco_rows_t *q,
+                                const reco_rows_t *q_out, int32_t n_q_heads, int32_t *dev_err, hipStream_t stream) {
+  if (!paged_ok(cache)) return RECO_ERR_INVALID_ARG;
+  const int elem = cache->dtype == RECO_F32 ? 4 : 2;
+  if (!rows_ok(k_new, elem) || !rows_ok(v_new, elem) || (q == nullptr) != (q_out == nullptr))
+    return RECO_ERR_INVALID_ARG;
+  if (q && (!rows_ok(q, elem) || !rows_ok(q_out, elem) || n_q_heads < 1)) return RECO_ERR_INVALID_ARG;
+  if (!paged_layers_ok(cache, layer0, n_layers)) return RECO_ERR_INVALID_ARG;
+  const int units = units_of(cache, n_layers);
+  if (units < 1) return RECO_ERR_INVALID_ARG;
+  reco_status_t st = paged_supported(cache);
+  if (st != RECO_OK) return st;
+  reco::RopeParams p{};
+  st = rope_params(p, rope, n_layers, cache->batch, n_tokens, cache->head_dim, cache->dtype, n_new, dev_err);
+  if (st != RECO_OK) return st;
+  if ((q && n_q_heads > kMaxRowHeads) || cache->n_kv_heads > kMaxRowHeads) return RECO_ERR_UNSUPPORTED;
+  p.c = paged_cache(cache, layer0, n_layers, dev_err);
+  p.k = rows_of(k_new);
+  p.v = rows_of(v_new);
+  if (q) {
+    p.q = rows_of(q);
+    p.q_out = rows_of(q_out);
+    p.heads = n_q_heads;
+  }
+  return reco::hip_status(reco::launch_rope(p, cache->dtype, cache->head_dim, stream));
+}
 
 // ---------------------------------------------------------------- decode
 size_t reco_paged_decode_attn_workspace_size(const reco_paged_cache_t *cache, int32_t n_layers, int32_t n_q_heads) {

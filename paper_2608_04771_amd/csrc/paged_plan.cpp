@@ -3,6 +3,7 @@
 #include "paged.hpp"
 
 #include "decode_plan.hpp"
+#include "rope.hpp"
 
 namespace reco {
 
@@ -155,6 +156,13 @@ void prefill_place(PagedPrefillParams &p, int head_dim, void *ws) {
   at += aligned(units * sizeof(int32_t));
   p.part_o = reinterpret_cast<float *>(at);
   p.part_ml = p.part_o + units * p.blocks * p.splits * kPrefillRows * head_dim;
+}
+
+// A run of up to eight tokens is one workgroup's, which then sets the lengths itself.
+int rope_block(int tokens) {
+  int block = 1;
+  while (block < tokens && block < kRopeMaxBlock) block *= 2;
+  return block;
 }
 
 static int64_t evict_state_pitch(int capacity, int row_bytes) {
