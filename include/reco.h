@@ -31,6 +31,9 @@
  *                        a paged cache, window and sinks optional   (Sec. 3.3)
  *   reco_paged_evict     keep a budget of rows by accumulated attention
  *                        weight, compacted within their pages        (Sec. 1)
+ *   reco_paged_shared_decode_attn
+ *                        decode attention of sequences whose first rows
+ *                        are the same ones, read once for all        (Sec. 1)
  *   reco_rope            rotation of query or key rows by their
  *                        positions, on one to four axes              (Sec. 1)
  *   reco_paged_append    rows appended to a paged cache, keys rotated
@@ -105,7 +108,8 @@ enum {
   RECO_DEV_BAD_LOGIT = 6,        /* a logit row with no non-NaN value to sample */
   RECO_DEV_BAD_PAGE = 7,         /* a page id of a cached row outside [0, n_pages) */
   RECO_DEV_BAD_BUDGET = 8,       /* an eviction budget below 1 or below sinks + recent */
-  RECO_DEV_STALLED = 9           /* an eviction's rows were not read in time to be replaced */
+  RECO_DEV_STALLED = 9,          /* an eviction's rows were not read in time to be replaced */
+  RECO_DEV_BAD_GROUP = 10        /* groups of sequences that do not ascend from 0 to the batch */
 };
 
 /* reco_score flags */
@@ -337,6 +341,35 @@ reco_status_t reco_paged_prefill_attn(const reco_paged_cache_t *cache, int32_t l
                                       const int32_t *n_new, float scale, int32_t sinks, int32_t window,
                                       const void *k_new, const void *v_new, void *out, float *lse,
                                       void *ws, size_t ws_bytes, int32_t *dev_err, hipStream_t stream);
+
+/* ------------------------------------------------------------------------ */
+/* Decode attention of sequences that share their first rows, as samples of one prompt
+ * do: reco_paged_decode_attn's computation, append and errors, with the shared rows read
+ * once for all sequences of a group.  Group g is the sequences [first[g], first[g + 1]);
+ * the rows j < shared[lc * shared_layer_stride + g] (lc = layer - layer0) of each of its
+ * units are those of the group's first sequence, whose list of pages gives them: entries of the
+ * others' lists for pages that hold no row past them are not used.
+ *   q, k_new, v_new, sinks, window, out, lse, ws, scale : as for reco_paged_decode_attn;
+ *              a window counts each sequence's rows, shared and own
+ *   first    : [n_groups + 1] int32, from 0 to batch, ascending (a group may be empty);
+ *              1 <= n_groups <= batch
+ *   shared   : int32; [n_groups] with shared_layer_stride = 0 or [n_layers][n_groups]
+ *              with stride = n_groups; at most the shortest len of a group's units
+ * A shared count outside that is clamped (RECO_DEV_BAD_LENGTH); a list of groups that does
+ * not ascend from 0 to batch counts as none, each unit's rows then being all its own
+ * (RECO_DEV_BAD_GROUP).  Appended rows go to each unit's own pages, so a page that shared
+ * rows fill in part is a unit's own from there on.  cache->weight must be NULL
+ * (RECO_ERR_UNSUPPORTED otherwise): a row that several sequences see cannot be evicted from one. */
+size_t reco_paged_shared_decode_attn_workspace_size(const reco_paged_cache_t *cache, int32_t n_layers,
+                                                    int32_t n_q_heads, int32_t n_groups);
+reco_status_t reco_paged_shared_decode_attn(const reco_paged_cache_t *cache, int32_t layer0,
+                                            int32_t n_layers, const void *q, int32_t n_q_heads,
+                                            float scale, int32_t sinks, int32_t window,
+                                            const int32_t *first, int32_t n_groups,
+                                            const int32_t *shared, int64_t shared_layer_stride,
+                                            const void *k_new, const void *v_new, void *out, float *lse,
+                                            void *ws, size_t ws_bytes, int32_t *dev_err,
+                                            hipStream_t stream);
 
 /* ------------------------------------------------------------------------ */
 /* Eviction from a paged cache by accumulated attention weight (the heavy-hitter

@@ -30,7 +30,7 @@ RECO_SCORE_CAUSAL = 1
 RECO_POOL_MAX = 0
 RECO_POOL_MEAN = 1
 DEV_ERRORS = {0: "ok", 1: "append overflow", 2: "bad retention", 3: "bad score", 4: "bad token id",
-              5: "bad length", 6: "bad logit row", 7: "bad page", 8: "bad budget", 9: "stalled eviction"}
+              5: "bad length", 6: "bad logit row", 7: "bad page", 8: "bad budget", 9: "stalled eviction", 10: "bad group"}
 
 EXPORTED = [
     "reco_score_workspace_size", "reco_score", "reco_select_compact_workspace_size", "reco_select_compact",
@@ -40,6 +40,7 @@ EXPORTED = [
     "reco_paged_decode_attn_workspace_size", "reco_paged_decode_attn",
     "reco_paged_prefill_attn_workspace_size", "reco_paged_prefill_attn",
     "reco_paged_evict_workspace_size", "reco_paged_evict", "reco_rope", "reco_paged_append",
+    "reco_paged_shared_decode_attn_workspace_size", "reco_paged_shared_decode_attn",
     "reco_answer_ppl_workspace_size", "reco_answer_ppl", "reco_retention_from_reward", "reco_retention_eq1",
     "reco_kept_count", "reco_status_str", "reco_abi_version",
 ]
@@ -102,6 +103,9 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
         "reco_paged_prefill_attn": (I32, [PC, I32, I32, P, I32, I32, P, F32, I32, I32, P, P, P, P, P, SZ, P, P]),
         "reco_paged_evict_workspace_size": (SZ, [PC, I32]),
         "reco_paged_evict": (I32, [PC, I32, I32, P, I64, I32, I32, P, P, SZ, P, P]),
+        "reco_paged_shared_decode_attn_workspace_size": (SZ, [PC, I32, I32, I32]),
+        "reco_paged_shared_decode_attn": (I32, [PC, I32, I32, P, I32, F32, I32, I32, P, I32, P, I64, P, P, P, P, P, SZ,
+                                                P, P]),
         "reco_rope": (I32, [RP, RR, RR, I32, I32, I32, I32, I32, I32, P, P, P]),
         "reco_paged_append": (I32, [PC, I32, I32, RP, I32, P, RR, RR, RR, RR, I32, P, P]),
         "reco_logit_penalty": (I32, [P, I32, I32, I64, P, I32, P, F32, F32, F32, F32, F32, P, P]),
@@ -296,6 +300,13 @@ def paged_prefill_attn_workspace_size(cache: PagedKVCache, n_q_heads: int, n_tok
         return int(load_library().reco_paged_prefill_attn_workspace_size(cache.ref(), nl, n_q_heads, n_tokens))
 
 
+def paged_shared_decode_attn_workspace_size(cache: PagedKVCache, n_q_heads: int, n_groups: int,
+                                            n_layers: Optional[int] = None) -> int:
+    nl = cache.shape[0] if n_layers is None else n_layers
+    with _on(cache.k):
+        return int(load_library().reco_paged_shared_decode_attn_workspace_size(cache.ref(), nl, n_q_heads, n_groups))
+
+
 def paged_evict_workspace_size(cache: PagedKVCache, n_layers: Optional[int] = None) -> int:
     nl = cache.shape[0] if n_layers is None else n_layers
     return int(load_library().reco_paged_evict_workspace_size(cache.ref(), nl))
@@ -327,6 +338,13 @@ def paged_decode_workspace(cache: PagedKVCache, n_q_heads: int, n_layers: Option
     """A workspace for reco_paged_decode_attn (contents need not be initialised).
     Do not share one between overlapping calls."""
     return _ws(lambda: paged_decode_attn_workspace_size(cache, n_q_heads, n_layers), cache.k.device, None)
+
+
+def paged_shared_decode_workspace(cache: PagedKVCache, n_q_heads: int, n_groups: int,
+                                  n_layers: Optional[int] = None) -> torch.Tensor:
+    """A workspace for reco_paged_shared_decode_attn (contents need not be
+    initialised).  Do not share one between overlapping calls."""
+    return _ws(lambda: paged_shared_decode_attn_workspace_size(cache, n_q_heads, n_groups, n_layers), cache.k.device, None)
 
 
 def _score_shapes(cache: KVCache, nl: int, q_win: torch.Tensor, w: int, scores, row_stats):
@@ -641,6 +659,85 @@ class PreparedPagedDecode:
         if st != RECO_OK:
             _check(st, "reco_paged_decode_attn")
         return self.out, self.lse
+
+
+class PreparedPagedSharedDecode:
+    """reco_paged_shared_decode_attn for a loop that calls it again and again with the same
+    cache, groups, outputs, workspace and error word (whose contents may change): those are
+    checked once here, each call checks the tensors that change from token to token."""
+
+    def __init__(self, cache: PagedKVCache, n_q_heads: int, first: torch.Tensor, shared: torch.Tensor,
+                 out: torch.Tensor, lse: Optional[torch.Tensor], ws: torch.Tensor,
+                 dev_err: Optional[torch.Tensor] = None, sinks: int = 0, window: int = 0,
+                 scale: Optional[float] = None, layer0: int = 0, n_layers: Optional[int] = None):
+        layer0, nl = _layers(cache, layer0, n_layers)
+        NL, Bsz, H, Cap, D = cache.shape
+        sinks, window = _row_count(sinks, "sinks"), _row_count(window, "window")
+        hq = int(n_q_heads)
+        if out is None or ws is None:
+            raise ValueError("out and ws must be given")
+        if cache.weight is not None:
+            raise ValueError("rows that sequences share have no weight of one: the cache must be without weights")
+        if first.dtype != torch.int32 or first.dim() != 1 or not 2 <= first.numel() <= Bsz + 1:
+            raise ValueError(f"first must be int32 [n_groups + 1], of 1 to {Bsz} groups")
+        groups = first.numel() - 1
+        if shared.dtype != torch.int32 or tuple(shared.shape) not in ((groups,), (nl, groups)):
+            raise ValueError("shared must be int32 [n_groups] or [n_layers][n_groups]")
+        _expect(out, "out", (nl, Bsz, hq, D), cache.k.dtype)
+        _expect(lse, "lse", (nl, Bsz, hq), torch.float32)
+        _expect_dev_err(dev_err)
+        _need_cuda(cache.k, first, shared, out, lse, ws, dev_err)
+        if _nbytes(ws) < paged_shared_decode_attn_workspace_size(cache, hq, groups, nl):
+            raise ValueError("ws is smaller than reco_paged_shared_decode_attn_workspace_size")
+        self.cache, self.out, self.lse = cache, out, lse
+        self._keep = (first, shared, ws, dev_err)
+        self._fn = load_library().reco_paged_shared_decode_attn
+        self._dev, self._dt = cache.k.device, cache.k.dtype
+        self._q_shape, self._kv_shape = (nl, Bsz, hq, D), (nl, Bsz, H, D)
+        scale = 1.0 / math.sqrt(D) if scale is None else float(scale)
+        self._head = (cache.ref(), layer0, nl)
+        self._mid = (hq, scale, sinks, window, _ptr(first), groups, _ptr(shared), 0 if shared.dim() == 1 else groups)
+        self._tail = (_ptr(out), _ptr(lse), _ptr(ws), _nbytes(ws), _ptr(dev_err))
+
+    def _check_t(self, t: torch.Tensor, what: str, shape):
+        if tuple(t.shape) != shape or t.dtype != self._dt or t.device != self._dev or not t.is_contiguous():
+            raise ValueError(f"{what} must be a contiguous {_DT[self._dt]} {list(shape)} tensor on {self._dev}")
+
+    def __call__(self, q: torch.Tensor, k_new: Optional[torch.Tensor] = None, v_new: Optional[torch.Tensor] = None):
+        self._check_t(q, "q", self._q_shape)
+        if (k_new is None) != (v_new is None):
+            raise ValueError("k_new and v_new must be given together")
+        if k_new is not None:
+            self._check_t(k_new, "k_new", self._kv_shape)
+            self._check_t(v_new, "v_new", self._kv_shape)
+        with _on(q):
+            st = self._fn(*self._head, _ptr(q), *self._mid, _ptr(k_new), _ptr(v_new), *self._tail, _stream(self._dev))
+        if st != RECO_OK:
+            _check(st, "reco_paged_shared_decode_attn")
+        return self.out, self.lse
+
+
+def reco_paged_shared_decode_attn(cache: PagedKVCache, q: torch.Tensor, first: torch.Tensor, shared: torch.Tensor,
+                                  k_new: Optional[torch.Tensor] = None, v_new: Optional[torch.Tensor] = None,
+                                  sinks: int = 0, window: int = 0, scale: Optional[float] = None,
+                                  out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None,
+                                  want_lse: bool = True, layer0: int = 0, n_layers: Optional[int] = None,
+                                  ws: Optional[torch.Tensor] = None, dev_err: Optional[torch.Tensor] = None):
+    """reco_paged_decode_attn for groups of sequences whose first rows are the same ones,
+    which are read once for all; returns (out, lse).  ``first`` int32 [n_groups + 1]: group
+    g is the sequences first[g] to first[g + 1] - 1, ``shared`` int32 [n_groups] or
+    [n_layers][n_groups] its shared rows, taken from its first sequence's pages."""
+    _, nl = _layers(cache, layer0, n_layers)
+    if q.dim() != 4:
+        raise ValueError("q must be [n_layers][B][Hq][D] in the cache dtype")
+    hq = q.shape[2]
+    if out is None:
+        out = torch.empty_like(q)
+    if lse is None and want_lse:
+        lse = torch.empty((nl, cache.shape[1], hq), dtype=torch.float32, device=q.device)
+    ws = _ws(lambda: paged_shared_decode_attn_workspace_size(cache, hq, first.numel() - 1, nl), q.device, ws)
+    call = PreparedPagedSharedDecode(cache, hq, first, shared, out, lse, ws, dev_err, sinks, window, scale, layer0, nl)
+    return call(q, k_new, v_new)
 
 
 def reco_paged_prefill_attn(cache: PagedKVCache, q: torch.Tensor, k_new: torch.Tensor, v_new: torch.Tensor,

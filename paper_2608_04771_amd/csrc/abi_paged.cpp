@@ -272,6 +272,67 @@ reco_status_t reco_paged_prefill_attn(const reco_paged_cache_t *cache, int32_t l
   return reco::hip_status(reco::launch_paged_prefill(p, cache->dtype, cache->head_dim, stream));
 }
 
+// ---------------------------------------------------------------- shared prefixes
+size_t reco_paged_shared_decode_attn_workspace_size(const reco_paged_cache_t *cache, int32_t n_layers,
+                                                    int32_t n_q_heads, int32_t n_groups) {
+  if (!paged_ok(cache) || paged_supported(cache) != RECO_OK) return 0;
+  const int units = units_of(cache, n_layers), G = group_of(cache, n_q_heads);
+  if (units < 1 || G < 1 || G > 16 || n_groups < 1 || n_groups > cache->batch) return 0;
+  return reco::paged_shared_workspace_bytes(units / cache->batch, cache->batch, G, n_groups,
+                                            static_cast<int>(capacity_of(cache)), cache->head_dim,
+                                            reco::current_compute_units());
+}
+
+reco_status_t reco_paged_shared_decode_attn(const reco_paged_cache_t *cache, int32_t layer0, int32_t n_layers,
+                                            const void *q, int32_t n_q_heads, float scale, int32_t sinks,
+                                            int32_t window, const int32_t *first, int32_t n_groups,
+                                            const int32_t *shared, int64_t shared_layer_stride, const void *k_new,
+                                            const void *v_new, void *out, float *lse, void *ws, size_t ws_bytes,
+                                            int32_t *dev_err, hipStream_t stream) {
+  if (!paged_ok(cache) || !q || !out || !first || !shared || sinks < 0 || window < 0 || !isfinite(scale))
+    return RECO_ERR_INVALID_ARG;
+  if ((k_new == nullptr) != (v_new == nullptr) || shared_layer_stride < 0) return RECO_ERR_INVALID_ARG;
+  if (!aligned16(q) || !aligned16(out) || !aligned16(k_new) || !aligned16(v_new)) return RECO_ERR_INVALID_ARG;
+  if (!paged_layers_ok(cache, layer0, n_layers) || n_groups < 1 || n_groups > cache->batch) return RECO_ERR_INVALID_ARG;
+  const int units = units_of(cache, n_layers), G = group_of(cache, n_q_heads);
+  if (units < 1 || G < 1) return RECO_ERR_INVALID_ARG;
+  const reco_status_t st = paged_supported(cache);
+  if (st != RECO_OK) return st;
+  if (G > 16 || cache->weight) return RECO_ERR_UNSUPPORTED;   // a shared row has no weight of one sequence
+  const int cus = reco::current_compute_units(), jobs = units / cache->batch;
+
+  reco::PagedSharedParams p{};
+  p.c = paged_cache(cache, layer0, n_layers, dev_err);
+  const size_t need =
+      reco::paged_shared_workspace_bytes(jobs, cache->batch, G, n_groups, p.c.cap, cache->head_dim, cus);
+  if (!ws || ws_bytes < need || (reinterpret_cast<uintptr_t>(ws) & 255)) return RECO_ERR_WORKSPACE;
+  p.q = q;
+  p.k_new = k_new;
+  p.v_new = v_new;
+  p.out = out;
+  p.lse = lse;
+  p.first = first;
+  p.shared = shared;
+  p.shared_stride = shared_layer_stride;
+  p.group = G;
+  p.groups = n_groups;
+  p.rows = units * G;
+  p.sinks = sinks;
+  p.window = window;
+  p.scale_log2 = scale * 1.4426950408889634f;
+  const int span = reco::shared_span_rows(p.c.cap, sinks, window);
+  p.blocks = reco::shared_blocks(cache->batch, G, n_groups);
+  p.splits = reco::shared_splits(jobs, p.blocks, span, cus);
+  p.own_splits = reco::shared_own_splits(units, span, cus);
+  p.by_splits = reco::FastDiv(p.splits);
+  p.by_own = reco::FastDiv(p.own_splits);
+  p.by_blocks = reco::FastDiv(p.blocks);
+  p.by_group = reco::FastDiv(G);
+  if (!reco::paged_shared_fits_grid(p)) return RECO_ERR_UNSUPPORTED;
+  reco::paged_shared_place(p, cache->head_dim, ws);
+  return reco::hip_status(reco::launch_paged_shared(p, cache->dtype, cache->head_dim, stream));
+}
+
 // ---------------------------------------------------------------- eviction
 size_t reco_paged_evict_workspace_size(const reco_paged_cache_t *cache, int32_t n_layers) {
   if (!paged_ok(cache) || paged_supported(cache) != RECO_OK) return 0;

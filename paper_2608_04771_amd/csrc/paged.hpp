@@ -108,6 +108,41 @@ bool prefill_fits_grid(const PagedPrefillParams &p);
 void prefill_place(PagedPrefillParams &p, int head_dim, void *ws);
 hipError_t launch_paged_prefill(const PagedPrefillParams &p, int dtype, int head_dim, hipStream_t s);
 
+// ---- attention of one new token over shared first rows -----------------------------
+constexpr int kSharedRows = 128;         // query rows of a workgroup
+constexpr int kSharedMaxSplits = 64;     // of the shared rows, and of a unit's own ones
+constexpr int kSharedMaxParts = 2 * kSharedMaxSplits;
+struct PagedSharedParams {
+  PagedCache c;
+  const void *q;          // [n_layers][batch][hq][D]
+  const void *k_new;      // nullable [n_layers][batch][hkv][D]
+  const void *v_new;
+  void *out;              // [n_layers][batch][hq][D]
+  float *lse;             // nullable [n_layers][batch][hq]
+  const int32_t *first;   // [groups + 1]  first sequence of each group, and the batch
+  const int32_t *shared;  // [groups], or [n_layers][groups] with shared_stride = groups
+  int64_t shared_stride;
+  float *part_o;          // [splits, own_splits][rows][D], rows (layer, KV head, sequence, query head)
+  float *part_ml;         // [splits, own_splits][rows][2]  (maximum, sum)
+  FastDiv by_splits, by_own, by_blocks, by_group;
+  int group, groups, rows;
+  int blocks;             // most blocks of kSharedRows query rows that all groups have
+  int splits, own_splits;
+  int common_wgs;         // workgroups of the shared rows
+  int sinks, window;
+  float scale_log2;
+};
+int shared_blocks(int batch, int group, int groups);
+int shared_splits(int jobs, int blocks, int span_rows, int compute_units);
+int shared_own_splits(int units, int span_rows, int compute_units);
+int shared_span_rows(int capacity, int sinks, int window);
+size_t paged_shared_workspace_bytes(int jobs, int batch, int group, int groups, int capacity, int head_dim,
+                                    int compute_units);
+// Places the parts of a call's workspace and sets its workgroups; the sizes and splits are set.
+void paged_shared_place(PagedSharedParams &p, int head_dim, void *ws);
+bool paged_shared_fits_grid(const PagedSharedParams &p);
+hipError_t launch_paged_shared(const PagedSharedParams &p, int dtype, int head_dim, hipStream_t s);
+
 // ---- eviction -----------------------------------------------------------------
 struct PagedEvictParams {
   PagedCache c;           // with weights

@@ -20,6 +20,7 @@
 // and V), and that workgroup, or the merge kernel's later ones, turn them into weights,
 // row by row in the order of the queries, so sums do not depend on scheduling.
 #include "paged_device.hpp"
+#include "paged_tiles.hpp"
 
 #include <type_traits>
 
@@ -27,65 +28,7 @@ namespace reco {
 
 namespace {
 
-constexpr int kTile = kPagedTile;
-constexpr int kSplitWaves = 4;                        // waves of a workgroup
-
-template <typename T, int D>
-struct Cfg {
-  using MF = Mfma<T>;
-  static constexpr int kpl = MF::kPerLane;
-  static constexpr int dq = D / 4;                  // head-dim elements per lane group for Q.K
-  static constexpr int qk_steps = dq / kpl;
-  static constexpr int dtiles = D / 16;
-  static constexpr int pv_ops = kTile / MF::kPerOp;
-  static constexpr int row_bytes = D * (int)sizeof(T);
-  static constexpr int k_stride = row_bytes + 16;   // LDS pitches, free of bank conflicts
-  static constexpr int v_stride = row_bytes + 8;
-  static constexpr int wave_stage = kTile * k_stride;
-  static constexpr int merge_pitch = D + 4;
-  static constexpr int lanes_per_row = row_bytes / 16;
-  static constexpr int rows_per_inst = kWave / lanes_per_row;
-  static constexpr int insts = kTile / rows_per_inst;   // 1 KB loads per tile of K or V
-  static constexpr int min_wgs = sizeof(T) == 4 && D == 128 ? 1 : 2;
-  static constexpr int smem() {
-    const int a = kSplitWaves * wave_stage, b = kSplitWaves * 16 * (2 + merge_pitch) * 4;
-    return a > b ? a : b;
-  }
-};
-
-template <typename T, int D>
-using Rows = u32x4v[Cfg<T, D>::insts];
-
-typedef short i16x4_t __attribute__((ext_vector_type(4)));
-typedef __attribute__((address_space(3))) i16x4_t lds_i16x4_t;
-
-// V^T operand of instruction c: lane (col, grp) holds column dt * 16 + col of the
-// rows of elements e = c * kpl + j, row (e / 4) * 16 + 4 * grp + e % 4.  bf16 takes
-// them with two transposing LDS reads of four rows each.
-template <typename T, int D>
-__device__ __forceinline__ typename Mfma<T>::frag v_frag(const unsigned char *stage, int c, int grp, int dt, int col) {
-  using C = Cfg<T, D>;
-  typename Mfma<T>::frag a;
-  if constexpr (C::kpl == 1) {
-    const int row = (c >> 2) * 16 + 4 * grp + (c & 3);
-    a = *reinterpret_cast<const float *>(stage + row * C::v_stride + (dt * 16 + col) * 4);
-  } else {
-    const int row = 32 * c + 4 * grp + col / 4;
-    const int at = (dt * 16 + 4 * (col % 4)) * 2;
-    const i16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4_t *)(stage + row * C::v_stride + at));
-    const i16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4_t *)(stage + (row + 16) * C::v_stride + at));
-    const short v[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
-#pragma unroll
-    for (int j = 0; j < 8; ++j) a[j] = __builtin_bit_cast(__bf16, v[j]);
-  }
-  return a;
-}
-
-template <typename T>
-__device__ __forceinline__ typename Mfma<T>::frag p_frag(const float (&pv)[8], int c) {
-  if constexpr (Mfma<T>::kPerLane == 1) return pv[c];
-  else return pack_frag8(pv);
-}
+using namespace tiles16;
 
 // Where a unit's new row goes, or that it goes nowhere (the first such code is reported).
 template <typename T, int D>

@@ -158,6 +158,54 @@ void prefill_place(PagedPrefillParams &p, int head_dim, void *ws) {
   p.part_ml = p.part_o + units * p.blocks * p.splits * kPrefillRows * head_dim;
 }
 
+int shared_blocks(int batch, int group, int groups) {
+  const int64_t rows = static_cast<int64_t>(batch) * group + static_cast<int64_t>(groups) * (kSharedRows - 1);
+  return static_cast<int>(rows / kSharedRows);            // each group's last block may not be whole
+}
+
+int shared_span_rows(int capacity, int sinks, int window) {
+  const int64_t seen = window == 0 ? capacity : static_cast<int64_t>(sinks) + window;
+  return static_cast<int>(seen < capacity ? seen : capacity);
+}
+
+// Two workgroups on every compute unit share the common rows of `jobs` (layers and KV heads);
+// a split keeps 256 rows of what a call may see.
+int shared_splits(int jobs, int blocks, int span_rows, int compute_units) {
+  int64_t splits = 2 * static_cast<int64_t>(compute_units) / (static_cast<int64_t>(jobs) * blocks);
+  if (splits > span_rows / 256) splits = span_rows / 256;
+  if (splits > kSharedMaxSplits) splits = kSharedMaxSplits;
+  return splits < 1 ? 1 : static_cast<int>(splits);
+}
+
+int shared_own_splits(int units, int span_rows, int compute_units) {
+  int splits = compute_units / units;
+  if (splits > span_rows / 256) splits = span_rows / 256;
+  if (splits > kSharedMaxSplits) splits = kSharedMaxSplits;
+  return splits < 1 ? 1 : splits;
+}
+
+size_t paged_shared_workspace_bytes(int jobs, int batch, int group, int groups, int capacity, int head_dim,
+                                    int compute_units) {
+  // a window takes no more splits than the whole cache does
+  const size_t parts = static_cast<size_t>(shared_splits(jobs, shared_blocks(batch, group, groups), capacity, compute_units)) +
+                       shared_own_splits(jobs * batch, capacity, compute_units);
+  return parts * jobs * batch * group * (static_cast<size_t>(head_dim) + 2) * sizeof(float);
+}
+
+void paged_shared_place(PagedSharedParams &p, int head_dim, void *ws) {
+  const int64_t jobs = static_cast<int64_t>(p.c.n_layers) * p.c.hkv * p.splits;
+  p.common_wgs = static_cast<int>((jobs + kXcds - 1) / kXcds * kXcds * p.blocks);
+  p.part_o = static_cast<float *>(ws);
+  p.part_ml = p.part_o + static_cast<size_t>(p.splits + p.own_splits) * p.rows * head_dim;
+}
+
+// Workgroups of 256 threads, and what FastDiv divides.
+bool paged_shared_fits_grid(const PagedSharedParams &p) {
+  const int64_t most = int64_t{1} << 24, units = static_cast<int64_t>(p.c.n_layers) * p.c.batch * p.c.hkv;
+  const int64_t jobs = static_cast<int64_t>(p.c.n_layers) * p.c.hkv * p.splits + kXcds;
+  return jobs * p.blocks + units * p.own_splits < most && units * p.group < most;
+}
+
 // A run of up to eight tokens is one workgroup's, which then sets the lengths itself.
 int rope_block(int tokens) {
   int block = 1;

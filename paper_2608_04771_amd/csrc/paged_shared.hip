@@ -1,0 +1,863 @@
+// GQA attention of one new token of every sequence over a paged KV cache (gfx950), where
+// sequences come in groups whose first rows are the same ones:
+//
+//   out = softmax(scale <q, k_j>) v_j over the rows j that the token sees,
+//   rows j < shared[group] being those of the group's first sequence.
+//
+// Softmax over two sets of rows is joined from each set's (max, sum, output), so a group's
+// query rows (sequence * G + head, of one layer and KV head) take the rows that all of
+// them see together, once, and each unit its other rows alone:
+//   common  [0, min(sinks, c)) and [c, shared), c the largest window start of the group
+//   own     [max(lo, sinks), c) of the shared rows, the rows from `shared` on, the new one
+// One launch has both kinds of workgroups, so that neither kind's last ones leave the
+// device idle; the second joins their parts and commits the append.
+//
+// The common part is the prefill kernel's: 128 query rows a workgroup, 32 a wave, key tiles
+// that the waves share through LDS,
+//   S^T = K_tile . Q^T (32 keys x 32 rows),   O^T += V_tile^T . P^T.
+// The own part is the decode kernel's: 16 padded query heads, tiles of 32 keys that are a
+// wave's own.  Statistics and outputs are fp32; P alone is rounded to the cache's type, as
+// its operand has to be.
+#include "paged_device.hpp"
+#include "paged_tiles.hpp"
+
+namespace reco {
+
+namespace {
+
+constexpr int kNW = 4;                       // waves of a workgroup
+constexpr int kRows = kSharedRows;           // query rows of one
+static_assert(kRows == 32 * kNW, "32 rows a wave");
+constexpr int kWaitLoads = 0x0f70;           // vmcnt(0)
+constexpr float kSlack = 8.f;                // log2 units that a maximum may grow before O follows
+
+__device__ __forceinline__ int wave_all_min(int v) {
+#pragma unroll
+  for (int m = 1; m < kWave; m <<= 1) v = min(v, __shfl_xor(v, m, kWave));
+  return v;
+}
+__device__ __forceinline__ int wave_all_max(int v) {
+#pragma unroll
+  for (int m = 1; m < kWave; m <<= 1) v = max(v, __shfl_xor(v, m, kWave));
+  return v;
+}
+
+// One group of sequences [from, to), and its place in the list.
+struct Group {
+  int id, from, to;
+  int row0;             // of the block that was looked for
+  bool ok;              // the list ascends from 0 to the batch
+};
+
+// The group of block `block` (of kRows query rows each, groups in order), or with
+// block < 0 that of sequence b.  id is -1 where there is none.
+__device__ __forceinline__ Group find_group(const PagedSharedParams &p, int block, int b, int lane) {
+  Group g{-1, 0, 0, 0, true};
+  int before = 0;
+  for (int g0 = 0; g0 < p.groups; g0 += kWave) {
+    const int i = g0 + lane;
+    const int from = p.first[min(i, p.groups)], to = p.first[min(i + 1, p.groups)];
+    const bool in = i < p.groups;
+    const bool ok = !in || (from <= to && from >= 0 && to <= p.c.batch && (i > 0 || from == 0) &&
+                            (i + 1 < p.groups || to == p.c.batch));
+    g.ok = g.ok && __all(ok);
+    int mine = 0, until = 0;
+    if (block >= 0) {
+      mine = in && ok ? ((to - from) * p.group + kRows - 1) / kRows : 0;
+      until = mine;
+#pragma unroll
+      for (int m = 1; m < kWave; m <<= 1) {
+        const int other = __shfl_up(until, m, kWave);
+        until += lane >= m ? other : 0;
+      }
+      until += before;
+      before = __shfl(until, kWave - 1, kWave);
+    }
+    const bool hit = block >= 0 ? block < until && block >= until - mine : in && b >= from && b < to;
+    const unsigned long long who = __ballot(hit);
+    if (who && g.id < 0) {
+      const int at = __builtin_ctzll(who);
+      g.id = g0 + at;
+      g.from = __builtin_amdgcn_readlane(from, at);
+      g.to = __builtin_amdgcn_readlane(to, at);
+      g.row0 = block >= 0 ? (block - __builtin_amdgcn_readlane(until - mine, at)) * kRows : 0;
+    }
+  }
+  return g;
+}
+
+// What the sequences of a group see together of one layer and KV head.
+struct Common {
+  int rows;             // shared ones
+  int sinks, start;     // [0, sinks) and [start, rows)
+};
+
+__device__ __forceinline__ Common common_rows(const PagedSharedParams &p, const Group &g, int layer, int head, int lane,
+                                              bool reporting) {
+  const int extra = p.k_new ? 1 : 0;
+  int least = p.c.cap, start = 0;
+  for (int b = g.from + lane; b < g.to; b += kWave) {
+    const int len = p.c.len[p.c.unit((layer * p.c.batch + b) * p.c.hkv + head)];
+    const int n = max(0, min(len, p.c.cap));
+    least = min(least, n);
+    if (p.window > 0) start = max(start, n + extra - p.window);
+  }
+  least = wave_all_min(least);
+  const int given = p.shared[layer * p.shared_stride + g.id];
+  Common c;
+  c.rows = max(0, min(given, least));
+  if (reporting && c.rows != given) report(p.c.dev_err, kDevBadLength);
+  c.start = min(wave_all_max(start), c.rows);
+  c.sinks = min(p.sinks, c.start);
+  return c;
+}
+
+// A list of tiles of KT rows that covers ranges of rows one after the other.
+template <int KT, int N>
+struct Tiles {
+  int from[N], to[N], until[N];              // until: tiles of the ranges up to this one
+  int total;
+
+  __device__ __forceinline__ void set(int i, int a, int b) {
+    from[i] = a;
+    to[i] = b;
+    const int n = b > a ? (b + KT - 1) / KT - a / KT : 0;
+    until[i] = (i > 0 ? until[i > 0 ? i - 1 : 0] : 0) + n;
+    total = until[i];
+  }
+  struct At {
+    int row, from, to, range;                // the tile's first row, its range's rows
+  };
+  __device__ __forceinline__ At at(int i) const {
+    At a{(from[0] / KT + i) * KT, from[0], to[0], 0};
+#pragma unroll
+    for (int r = 1; r < N; ++r) {
+      if (i >= until[r - 1]) a = At{(from[r] / KT + i - until[r - 1]) * KT, from[r], to[r], r};
+    }
+    return a;
+  }
+};
+
+// ------------------------------------------------------------------ common rows
+// Key tiles on their way to LDS, which loads fill without registers between.  Each lane
+// holds the place of 16 rows of the list's tiles; the table's entries of the batch after
+// are on their way meanwhile.
+template <typename T, int D>
+struct Feed {
+  using C = tiles32::Cfg<T, D, kNW>;
+  static constexpr int KT = C::keys;
+  static constexpr int kGroups = KT / 16;
+  static constexpr int kBatch = kWave / kGroups;         // tiles
+  using List = Tiles<KT, 2>;
+  const unsigned char *k, *v;
+  const int32_t *table;
+  const List &list;
+  int n_pages, shift, end, wave, lane;
+  unsigned worst;                            // id, of rows that are seen
+  uint64_t place;                            // of this lane's 16 rows: a byte offset
+  int coming;                                // the entry for the same lane of the next batch
+  unsigned koff[C::insts], voff[C::insts];   // within 16 rows
+
+  // Tiles [.., end) of the list.
+  __device__ __forceinline__ Feed(const PagedSharedParams &p, size_t cunit, const List &list_, int end_, int wave_, int lane_)
+      : k(static_cast<const unsigned char *>(p.c.k)), v(static_cast<const unsigned char *>(p.c.v)),
+        table(p.c.pages + cunit * static_cast<size_t>(p.c.max_pages)), list(list_), n_pages(p.c.n_pages),
+        shift(p.c.page_shift), end(end_), wave(wave_), lane(lane_), worst(0) {
+#pragma unroll
+    for (int i = 0; i < C::insts; ++i) {
+      const int row = piece(i) + lane / C::lanes_per_row, c = lane % C::lanes_per_row;
+      koff[i] = row % 16 * C::row_bytes + (c ^ C::k_swap(row)) * 16;
+      voff[i] = row % 16 * C::row_bytes + (c ^ C::v_swap(row)) * 16;
+    }
+  }
+  // A wave's i-th load of a tile takes wave_rows rows from this one on.
+  __device__ __forceinline__ int piece(int i) const { return (i * kNW + wave) * C::wave_rows; }
+  // The first of this lane's 16 rows in the batch that starts at tile i, and whether any is seen.
+  __device__ __forceinline__ int row_of(int i, bool &seen) const {
+    const typename List::At a = list.at(min(i + lane / kGroups, end - 1));
+    const int row = a.row + lane % kGroups * 16;
+    seen = row < a.to && row + 16 > a.from;
+    return row;
+  }
+  __device__ __forceinline__ void ask(int i) {
+    bool seen;
+    const int row = row_of(i, seen);
+    coming = seen ? table[row >> shift] : 0;
+  }
+  // The batch that starts at tile i, whose entries were asked for, and the one after.
+  __device__ __forceinline__ void batch(int i) {
+    bool seen;
+    const int row = row_of(i, seen);
+    worst = max(worst, static_cast<unsigned>(coming));
+    const unsigned id = min(static_cast<unsigned>(coming), static_cast<unsigned>(n_pages - 1));
+    place = ((static_cast<uint64_t>(id) << shift) + (row & ((1u << shift) - 1u))) * C::row_bytes;
+    ask(i + kBatch);
+  }
+  struct Place {
+    uint64_t at[C::insts];
+  };
+  __device__ __forceinline__ Place find(int i) const {
+    const int at_i = min(i, end - 1);
+    Place w;
+#pragma unroll
+    for (int j = 0; j < C::insts; ++j) {
+      const int from = (at_i & (kBatch - 1)) * kGroups + piece(j) / 16;
+      w.at[j] = static_cast<uint64_t>(static_cast<unsigned>(__builtin_amdgcn_readlane(static_cast<int>(place >> 32), from))) << 32 |
+                static_cast<unsigned>(__builtin_amdgcn_readlane(static_cast<int>(place), from));
+    }
+    return w;
+  }
+  __device__ __forceinline__ void load_k(const Place &w, int j, unsigned char *buf) const {
+    __builtin_amdgcn_global_load_lds((tiles32::global_u32 *)(k + w.at[j] + koff[j]), (tiles32::lds_u32 *)(buf + piece(j) * C::row_bytes), 16, 0, 0);
+  }
+  __device__ __forceinline__ void load_v(const Place &w, int j, unsigned char *buf) const {
+    __builtin_amdgcn_global_load_lds((tiles32::global_u32 *)(v + w.at[j] + voff[j]), (tiles32::lds_u32 *)(buf + piece(j) * C::row_bytes), 16, 0, 0);
+  }
+  __device__ __forceinline__ void turn(int i) {
+    if (i < end && (i & (kBatch - 1)) == 0) batch(i);
+  }
+  // Rows of V outside the range count for nothing, whatever they hold.
+  __device__ __forceinline__ void clean(const typename List::At &a, unsigned char *vbuf) const {
+#pragma unroll
+    for (int j = 0; j < C::insts; ++j) {
+      const int row = a.row + piece(j) + lane / C::lanes_per_row;
+      if (row < a.from || row >= a.to)
+        *reinterpret_cast<u32x4v *>(vbuf + piece(j) * C::row_bytes + lane * 16) = u32x4v{0, 0, 0, 0};
+    }
+  }
+};
+
+// LDS of a workgroup: four buffers, of the common part's K and V of two tiles, or of a
+// wave's tile each.
+template <typename T, int D>
+constexpr int area_bytes() {
+  const int a = tiles32::Cfg<T, D, kNW>::stage, b = tiles16::Cfg<T, D>::wave_stage,
+            c = 16 * (2 + tiles16::Cfg<T, D>::merge_pitch) * 4;
+  return a > b ? (a > c ? a : c) : (b > c ? b : c);
+}
+
+template <typename T, int D>
+__device__ __forceinline__ void attend_common(const PagedSharedParams &p, int id, unsigned char *k0, unsigned char *v0,
+                                              unsigned char *k1, unsigned char *v1) {
+  using namespace tiles32;
+  using C = tiles32::Cfg<T, D, kNW>;
+  using In = Feed<T, D>;
+  using M = Mma32<T>;
+  using frag = typename M::frag;
+  constexpr int KT = C::keys;
+  const int lane = threadIdx.x & (kWave - 1);
+  const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) / kWave);
+  const int half = lane >> 5;
+  const int col = lane & 31;
+
+  // The blocks of a layer, KV head and split take their turn on one XCD, beside each other,
+  // so that those of a group share the keys' way through its L2.
+  const int slot = id / kXcds;
+  const int turn = p.by_blocks.of(slot), block = p.by_blocks.rest(slot);
+  const int job = turn * kXcds + id % kXcds;
+  const int lh = p.by_splits.of(job), split = p.by_splits.rest(job);
+  const int layer = p.c.by_hkv.of(lh), head = p.c.by_hkv.rest(lh);
+  if (layer >= p.c.n_layers) return;
+  const Group g = find_group(p, block, 0, lane);
+  if (!g.ok || g.id < 0) return;
+  const int rows = (g.to - g.from) * p.group;
+  const Common seen = common_rows(p, g, layer, head, lane, threadIdx.x == 0 && split == 0 && g.row0 == 0);
+  typename In::List list;
+  list.set(0, 0, seen.sinks);
+  list.set(1, seen.start, seen.rows);
+  const int per_split = p.by_splits.of(list.total + p.splits - 1);
+  const int i0 = split * per_split;
+  const int i1 = min(list.total, i0 + per_split);
+
+  // This lane's query row.
+  const int wave_row = g.row0 + wave * 32;
+  const bool active = wave_row < rows;
+  const int r = min(wave_row + col, rows - 1);
+  const int b = g.from + p.by_group.of(r);
+  const size_t qrow = (static_cast<size_t>(layer * p.c.batch + b) * p.c.hkv + head) * p.group + p.by_group.rest(r);
+  frag qf[C::qk_steps];
+  {
+    const T *src = reinterpret_cast<const T *>(p.q) + qrow * D + half * (D / 2);
+#pragma unroll
+    for (int c = 0; c < C::qk_steps; ++c) {
+      qf[c] = load_frag(src + c * M::kpl);
+      if (p.scale_log2 < 0.f) qf[c] = M::negated(qf[c]);   // so that the largest product is the largest logit
+    }
+  }
+  const float scale = fmaxf(fabsf(p.scale_log2), 0x1p-126f);   // times a hidden row's -inf, 0 would be NaN
+
+  In in(p, p.c.unit((layer * p.c.batch + g.from) * p.c.hkv + head), list, i1, wave, lane);
+  float m_run = -INFINITY, l_run = 0.f;                  // m in units of the scaled logits
+  f32x16_t o[C::dtiles];
+#pragma unroll
+  for (int dt = 0; dt < C::dtiles; ++dt) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) o[dt][i] = 0.f;
+  }
+  const int kat = k_base<T, D>(lane), vat = v_base<T, D>(lane);
+
+  // Tile i, in kbuf and vbuf once its loads are done; tile i + 1 goes to kto and vto.
+  const auto step = [&](int i, unsigned char *kbuf, unsigned char *vbuf, unsigned char *kto, unsigned char *vto)
+                        __attribute__((always_inline)) {
+    in.turn(i + 1);
+    const typename In::List::At tile = list.at(i);
+    const bool whole = tile.row >= tile.from && tile.row + KT <= tile.to;
+    __builtin_amdgcn_s_waitcnt(kWaitLoads);
+    if (!whole) in.clean(tile, vbuf);                     // each wave looks after what it loaded
+    __syncthreads();                                      // tile i is there, and no one reads tile i - 1
+    const typename In::Place from = in.find(i + 1);
+    if (!active) {
+#pragma unroll
+      for (int j = 0; j < C::insts; ++j) {
+        in.load_k(from, j, kto);
+        in.load_v(from, j, vto);
+      }
+      return;
+    }
+
+    // S^T, with operands read ahead of their products, and between the products the
+    // next tile asked for, piece by piece.
+    f32x16_t s[C::blocks];
+#pragma unroll
+    for (int kb = 0; kb < C::blocks; ++kb) {
+#pragma unroll
+      for (int e = 0; e < 16; ++e) s[kb][e] = 0.f;
+    }
+    constexpr int kSteps = C::blocks * C::qk_steps, kAhead = M::kpl == 8 ? 8 : 16, kEach = kSteps / C::insts;
+    frag kf[2][kAhead];
+    const auto read_k = [&](int q) {
+#pragma unroll
+      for (int c = 0; c < kAhead; ++c) {
+        const int z = q * kAhead + c, byte = z % C::qk_steps * M::kpl * (int)sizeof(T);
+        kf[q & 1][c] = load_frag(reinterpret_cast<const T *>(kbuf + (kat ^ (byte & ~15)) + (byte & 15) + z / C::qk_steps * 32 * C::row_bytes));
+      }
+    };
+    read_k(0);
+#pragma unroll
+    for (int z = 0; z < kSteps; ++z) {
+      if (z % kAhead == 0 && z + kAhead < kSteps) read_k(z / kAhead + 1);
+      if (z % kAhead == 0) __builtin_amdgcn_sched_barrier(0);
+      s[z / C::qk_steps] = M::mma(kf[z / kAhead & 1][z % kAhead], qf[z % C::qk_steps], s[z / C::qk_steps]);
+      if (z % kEach == 0) {
+        in.load_k(from, z / kEach, kto);
+        in.load_v(from, z / kEach, vto);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    constexpr int kParts = C::blocks * C::pv_steps;
+    frag vf[2][C::dtiles];
+    const auto read_v = [&](int q) {
+      const int row = M::kpl == 8 ? 16 * q : 8 * (q / 4) + q % 4;
+#pragma unroll
+      for (int dt = 0; dt < C::dtiles; ++dt)
+        vf[q & 1][dt] = v_frag32<T, D>(vbuf + (vat ^ (dt * 32 * (int)sizeof(T))) + row * C::row_bytes);
+    };
+    read_v(0);
+
+    if (!whole) {
+      const int low = tile.from - tile.row - 4 * half, high = tile.to - tile.row - 4 * half;
+#pragma unroll
+      for (int kb = 0; kb < C::blocks; ++kb) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const int c = kb * 32 + acc_row(e, 0);
+          s[kb][e] = c < low || c >= high ? -INFINITY : s[kb][e];
+        }
+      }
+    }
+    float top = -INFINITY;
+#pragma unroll
+    for (int kb = 0; kb < C::blocks; ++kb) {
+#pragma unroll
+      for (int e = 0; e < 16; ++e) top = fmaxf(top, s[kb][e]);
+    }
+    top = fmaxf(top, shfl_xor(top, 32)) * scale;
+    // The reference of the exponentials follows the maximum only where it grew by more
+    // than kSlack (P then stays below 2^kSlack, with the same relative precision), so
+    // that O is seldom rescaled.
+    if (__any(top > m_run + kSlack)) {
+      const float m_new = fmaxf(m_run, top);
+      const float alpha = fast_exp2(m_run - (m_new == -INFINITY ? 0.f : m_new));
+      l_run *= alpha;
+      m_run = m_new;
+#pragma unroll
+      for (int dt = 0; dt < C::dtiles; ++dt) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) o[dt][e] *= alpha;
+      }
+    }
+    // O^T: part q takes kpl elements of every lane, slot j of which is row
+    // 8 (e / 4) + 4 half + e % 4 of S^T for e = q * kpl + j; the exponentials of a part
+    // lie between the products of the part before.
+    const float ref = m_run == -INFINITY ? 0.f : m_run;
+    const auto weigh = [&](int q, int j) {
+      const int e = q * M::kpl + j;
+      const float w = fast_exp2(fmaf(s[e / 16][e % 16], scale, -ref));
+      l_run += w;
+      return w;
+    };
+    frag pf[2];
+    const auto put = [&](int q, int j) {
+      if constexpr (M::kpl == 1) pf[q & 1] = weigh(q, j);
+      else pf[q & 1][j] = static_cast<__bf16>(weigh(q, j));
+    };
+#pragma unroll
+    for (int j = 0; j < M::kpl; ++j) put(0, j);
+#pragma unroll
+    for (int q = 0; q < kParts; ++q) {
+      if (q + 1 < kParts) read_v(q + 1);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int dt = 0; dt < C::dtiles; ++dt) {
+        o[dt] = M::mma(vf[q & 1][dt], pf[q & 1], o[dt]);
+        if (q + 1 < kParts) {
+#pragma unroll
+          for (int j = dt * M::kpl / C::dtiles; j < (dt + 1) * M::kpl / C::dtiles; ++j) put(q + 1, j);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    }
+  };
+  if (i0 < i1) {
+    in.ask(i0 & -In::kBatch);
+    in.batch(i0 & -In::kBatch);
+    const typename In::Place from = in.find(i0);
+#pragma unroll
+    for (int j = 0; j < C::insts; ++j) {
+      in.load_k(from, j, k0);
+      in.load_v(from, j, v0);
+    }
+    for (int i = i0; i < i1; i += 2) {
+      step(i, k0, v0, k1, v1);
+      if (i + 1 < i1) step(i + 1, k1, v1, k0, v0);
+    }
+  }
+  __builtin_amdgcn_s_waitcnt(kWaitLoads);
+  if (in.worst >= static_cast<unsigned>(p.c.n_pages)) report(p.c.dev_err, kDevBadPage);
+
+  const float l_tot = l_run + shfl_xor(l_run, 32);
+  if (wave_row + col >= rows) return;
+  const size_t part = static_cast<size_t>(split) * p.rows +
+                      (static_cast<size_t>(lh) * p.c.batch + g.from) * p.group + wave_row + col;
+  if (half == 0) {
+    p.part_ml[2 * part] = m_run;
+    p.part_ml[2 * part + 1] = l_tot;
+  }
+  if (i0 >= i1) return;                                   // without tiles, sum 0: not read
+  float4 *po = reinterpret_cast<float4 *>(p.part_o + part * D) + half;
+#pragma unroll
+  for (int dt = 0; dt < C::dtiles; ++dt) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      po[dt * 8 + 2 * e] = make_float4(o[dt][4 * e], o[dt][4 * e + 1], o[dt][4 * e + 2], o[dt][4 * e + 3]);
+  }
+}
+
+// ------------------------------------------------------------------ a unit's own rows
+template <typename T, int D>
+__device__ __forceinline__ void attend_own(const PagedSharedParams &p, int id, unsigned char *a0, unsigned char *a1,
+                                           unsigned char *a2, unsigned char *a3) {
+  using namespace tiles16;
+  using C = tiles16::Cfg<T, D>;
+  using MF = Mfma<T>;
+  using frag = typename MF::frag;
+  constexpr int kThreads = kNW * kWave;
+  const int lane = threadIdx.x & (kWave - 1);
+  const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) / kWave);
+  const int col = lane & 15;
+  const int grp = lane >> 4;
+  const int unit = p.by_own.of(id), split = p.by_own.rest(id);
+  const int lb = p.c.by_hkv.of(unit), head = p.c.by_hkv.rest(unit);
+  const int layer = p.c.by_batch.of(lb), b = p.c.by_batch.rest(lb);
+  const size_t cunit = p.c.unit(unit);
+  const size_t part0 = ((static_cast<size_t>(layer) * p.c.hkv + head) * p.c.batch + b) * p.group;
+
+  const int len_in = p.c.len[cunit];
+  const int n_cache = max(0, min(len_in, p.c.cap));
+  const bool append = p.k_new != nullptr;
+  const int n = n_cache + (append ? 1 : 0);
+  const int lo = p.window > 0 && n > p.window ? n - p.window : 0;
+  const Group g = find_group(p, -1, b, lane);
+  Common seen{0, 0, 0};
+  if (g.ok) seen = common_rows(p, g, layer, head, lane, false);
+  const bool alone = !g.ok;                               // no sharing at all
+  const size_t lead = alone ? cunit : p.c.unit((layer * p.c.batch + g.from) * p.c.hkv + head);
+  if (alone && split == 0) {
+    if (threadIdx.x == 0) report(p.c.dev_err, kDevBadGroup);
+    for (int i = threadIdx.x; i < p.splits * p.group; i += kThreads) {
+      const size_t part = static_cast<size_t>(i / p.group) * p.rows + part0 + i % p.group;
+      p.part_ml[2 * part] = -INFINITY;
+      p.part_ml[2 * part + 1] = 0.f;
+    }
+  }
+
+  using List = Tiles<kTile, 3>;
+  List list;
+  list.set(0, max(lo, seen.sinks), seen.start);           // shared rows that not all see
+  list.set(1, seen.rows, min(p.sinks, lo));               // sinks behind them
+  list.set(2, max(seen.rows, lo), n);
+  const int per_split = p.by_own.of(list.total + p.own_splits - 1);
+  const int i0 = split * per_split;
+  const int i1 = min(list.total, i0 + per_split);
+
+  frag qf[C::qk_steps];
+  {
+    const T *qrow = reinterpret_cast<const T *>(p.q) + (static_cast<size_t>(unit) * p.group + col) * D + grp * C::dq;
+#pragma unroll
+    for (int c = 0; c < C::qk_steps; ++c) qf[c] = col < p.group ? load_frag(qrow + c * C::kpl) : zero_frag(frag{});
+  }
+  float m_run = -INFINITY, l_run = 0.f;
+  f32x4_t o[C::dtiles];
+#pragma unroll
+  for (int dt = 0; dt < C::dtiles; ++dt) o[dt] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  unsigned char *stage = wave < 2 ? (wave == 0 ? a0 : a1) : (wave == 2 ? a2 : a3);
+
+  // Where the wave's tiles lie: each lane holds the place of 16 rows, so 32 tiles at a
+  // time; the table's entries of the batch after are on their way meanwhile.
+  constexpr int kBatch = kWave / 2;
+  const int mine = i1 - i0 - wave > 0 ? (i1 - i0 - wave + kNW - 1) / kNW : 0;   // tiles of the wave
+  const int32_t *own_table = p.c.pages + cunit * static_cast<size_t>(p.c.max_pages);
+  const int32_t *lead_table = p.c.pages + lead * static_cast<size_t>(p.c.max_pages);
+  const auto tile_of = [&](int k) { return list.at(i0 + wave + kNW * min(k, mine - 1)); };
+  unsigned worst = 0;
+  int coming = 0;
+  uint64_t place = 0;
+  const auto ask = [&](int batch) {
+    const typename List::At a = tile_of(batch * kBatch + lane / 2);
+    const int row = a.row + lane % 2 * 16;
+    const bool cached = row < min(a.to, n_cache) && row + 16 > a.from;
+    coming = cached ? (a.range == 0 ? lead_table : own_table)[row >> p.c.page_shift] : 0;
+  };
+  const auto turn = [&](int batch) {
+    const typename List::At a = tile_of(batch * kBatch + lane / 2);
+    const int row = a.row + lane % 2 * 16;
+    const unsigned page = min(static_cast<unsigned>(coming), static_cast<unsigned>(p.c.n_pages - 1));
+    worst = max(worst, static_cast<unsigned>(coming));
+    place = ((static_cast<uint64_t>(page) << p.c.page_shift) + (row & ((1 << p.c.page_shift) - 1))) * C::row_bytes;
+    ask(batch + 1);
+  };
+  struct Where {
+    uint64_t at[2];
+  };
+  const auto find = [&](int k) {
+    Where w;
+#pragma unroll
+    for (int hf = 0; hf < 2; ++hf) {
+      const int from = (k & (kBatch - 1)) * 2 + hf;
+      w.at[hf] = static_cast<uint64_t>(static_cast<unsigned>(__builtin_amdgcn_readlane(static_cast<int>(place >> 32), from))) << 32 |
+                 static_cast<unsigned>(__builtin_amdgcn_readlane(static_cast<int>(place), from));
+    }
+    return w;
+  };
+  // Rows outside the range are others of the pool and are masked where they are used; the
+  // new row is put where it belongs in LDS.
+  const auto load = [&](Rows<T, D> &reg, const void *pool, const Where &w) {
+#pragma unroll
+    for (int j = 0; j < C::insts; ++j)
+      reg[j] = __builtin_nontemporal_load(reinterpret_cast<const u32x4v *>(
+          static_cast<const unsigned char *>(pool) + w.at[j / (C::insts / 2)] + j % (C::insts / 2) * (kWave * 16) + lane * 16));
+  };
+  const auto fresh_row = [&](const void *rows) {
+    return append ? *reinterpret_cast<const uint4 *>(static_cast<const unsigned char *>(rows) +
+                                                     static_cast<size_t>(unit) * C::row_bytes + lane % C::lanes_per_row * 16)
+                  : make_uint4(0, 0, 0, 0);
+  };
+  const uint4 kfresh = fresh_row(p.k_new), vfresh = fresh_row(p.v_new);
+
+  Rows<T, D> kreg, vreg;
+  const auto attend = [&](int k) {
+    const typename List::At tile = tile_of(k);
+    const int kb = tile.row;
+    const bool holds_new = append && tile.range == 2 && kb <= n_cache && n_cache < kb + kTile;
+    const bool whole = kb >= tile.from && kb + kTile <= tile.to && !holds_new;
+    const bool more = k + 1 < mine;
+    if (((k + 1) & (kBatch - 1)) == 0) turn((k + 1) / kBatch);
+    const Where next = find(k + 1);
+#pragma unroll
+    for (int j = 0; j < C::insts; ++j) {
+      const int r = j * C::rows_per_inst + lane / C::lanes_per_row;
+      *reinterpret_cast<u32x4v *>(stage + r * C::k_stride + (lane % C::lanes_per_row) * 16) = kreg[j];
+    }
+    if (more) load(kreg, p.c.k, next);
+    if (holds_new && lane < C::lanes_per_row)
+      *reinterpret_cast<uint4 *>(stage + (n_cache - kb) * C::k_stride + lane * 16) = kfresh;
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    f32x4_t s[2];
+#pragma unroll
+    for (int hf = 0; hf < 2; ++hf) {
+      const T *krow = reinterpret_cast<const T *>(stage + (hf * 16 + col) * C::k_stride) + grp * C::dq;
+      s[hf] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int c = 0; c < C::qk_steps; ++c) s[hf] = MF::mma(load_frag(krow + c * C::kpl), qf[c], s[hf]);
+    }
+    // V's rows take the place of K's, which other lanes read: the compiler must not put
+    // the writes first (a wave's LDS accesses are done in order, so nothing waits).
+    asm volatile("" ::: "memory");
+
+    float x[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = s[e >> 2][e & 3] * p.scale_log2;
+    if (!whole) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const int row = kb + (e >> 2) * 16 + 4 * grp + (e & 3);
+        x[e] = row >= tile.from && row < tile.to ? x[e] : -INFINITY;
+      }
+    }
+    float top = x[0];
+#pragma unroll
+    for (int e = 1; e < 8; ++e) top = fmaxf(top, x[e]);
+    const float m_new = fmaxf(m_run, group4_max(top));
+    const float ref = m_new == -INFINITY ? 0.f : m_new;   // logits of -inf alone have no weight
+    const float alpha = fast_exp2(m_run - ref);
+    float pv[8];
+    float sum = 0.f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      pv[e] = fast_exp2(x[e] - ref);
+      sum += pv[e];
+    }
+    l_run = l_run * alpha + sum;
+    m_run = m_new;
+#pragma unroll
+    for (int dt = 0; dt < C::dtiles; ++dt) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[dt][e] *= alpha;
+    }
+    if (!whole) {                                         // a NaN that is not seen, times 0, would be NaN
+#pragma unroll
+      for (int j = 0; j < C::insts; ++j) {
+        const int row = kb + j * C::rows_per_inst + lane / C::lanes_per_row;
+        const unsigned keep = row >= tile.from && row < tile.to ? ~0u : 0u;
+        vreg[j] &= u32x4v{keep, keep, keep, keep};
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < C::insts; ++j) {
+      const int r = j * C::rows_per_inst + lane / C::lanes_per_row;
+      uint2 *dst = reinterpret_cast<uint2 *>(stage + r * C::v_stride + (lane % C::lanes_per_row) * 16);
+      dst[0] = make_uint2(vreg[j][0], vreg[j][1]);
+      dst[1] = make_uint2(vreg[j][2], vreg[j][3]);
+    }
+    if (more) load(vreg, p.c.v, next);
+    if (holds_new && lane < C::lanes_per_row) {
+      uint2 *dst = reinterpret_cast<uint2 *>(stage + (n_cache - kb) * C::v_stride + lane * 16);
+      dst[0] = make_uint2(vfresh.x, vfresh.y);
+      dst[1] = make_uint2(vfresh.z, vfresh.w);
+    }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+#pragma unroll
+    for (int dt = 0; dt < C::dtiles; ++dt) {
+#pragma unroll
+      for (int c = 0; c < C::pv_ops; ++c) o[dt] = MF::mma(v_frag<T, D>(stage, c, grp, dt, col), p_frag<T>(pv, c), o[dt]);
+    }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+  };
+  if (mine > 0) {
+    ask(0);
+    turn(0);
+    const Where first = find(0);
+    load(kreg, p.c.k, first);
+    load(vreg, p.c.v, first);
+    for (int k = 0; k < mine; ++k) attend(k);
+  }
+  if (worst >= static_cast<unsigned>(p.c.n_pages)) report(p.c.dev_err, kDevBadPage);
+
+  // The waves' parts meet in LDS: outputs [16][merge_pitch], maxima, sums.
+  const float l_tot = group4_sum(l_run);
+  float *ow = reinterpret_cast<float *>(stage);
+  if (grp == 0) {
+    ow[16 * C::merge_pitch + col] = m_run;
+    ow[16 * C::merge_pitch + 16 + col] = l_tot;
+  }
+#pragma unroll
+  for (int dt = 0; dt < C::dtiles; ++dt)
+    *reinterpret_cast<float4 *>(ow + col * C::merge_pitch + dt * 16 + 4 * grp) =
+        make_float4(o[dt][0], o[dt][1], o[dt][2], o[dt][3]);
+  __syncthreads();
+  const float *area[kNW] = {reinterpret_cast<const float *>(a0), reinterpret_cast<const float *>(a1),
+                            reinterpret_cast<const float *>(a2), reinterpret_cast<const float *>(a3)};
+  const size_t part = static_cast<size_t>(p.splits + split) * p.rows + part0;
+  for (int idx = threadIdx.x; idx < p.group * (D / 4); idx += kThreads) {
+    const int qi = idx / (D / 4);
+    const int d = (idx - qi * (D / 4)) * 4;
+    float M = -INFINITY, L = 0.f;
+#pragma unroll
+    for (int w = 0; w < kNW; ++w) M = fmaxf(M, area[w][16 * C::merge_pitch + qi]);
+    const float ref = M == -INFINITY ? 0.f : M;
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+    for (int w = 0; w < kNW; ++w) {
+      const float e = fast_exp2(area[w][16 * C::merge_pitch + qi] - ref);
+      const float4 x = *reinterpret_cast<const float4 *>(area[w] + qi * C::merge_pitch + d);
+      acc.x += x.x * e;
+      acc.y += x.y * e;
+      acc.z += x.z * e;
+      acc.w += x.w * e;
+      L += area[w][16 * C::merge_pitch + 16 + qi] * e;
+    }
+    *reinterpret_cast<float4 *>(p.part_o + (part + qi) * D + d) = acc;
+    if (d == 0) {
+      p.part_ml[2 * (part + qi)] = M;
+      p.part_ml[2 * (part + qi) + 1] = L;
+    }
+  }
+}
+
+template <typename T, int D>
+__global__ __launch_bounds__(kNW * kWave, 2) void shared_attn_kernel(PagedSharedParams p) {
+  // arrays of their own, so that reads of one need not wait for loads into another
+  __shared__ __attribute__((aligned(1024))) unsigned char a0[area_bytes<T, D>()], a1[area_bytes<T, D>()],
+      a2[area_bytes<T, D>()], a3[area_bytes<T, D>()];
+  const int id = blockIdx.x;
+  if (id < p.common_wgs) attend_common<T, D>(p, id, a0, a1, a2, a3);
+  else attend_own<T, D>(p, id - p.common_wgs, a0, a1, a2, a3);
+}
+
+// ------------------------------------------------------------------ the join
+// D / 4 threads have a row, kSub times where there are many parts.  Query head 0 of a unit
+// commits the append.
+constexpr int kJoinThreads = 256;
+
+template <typename T, int D, int kSub>
+__global__ __launch_bounds__(kJoinThreads) void shared_join_kernel(PagedSharedParams p) {
+  constexpr int kLanes = D / 4, kEach = kLanes * kSub, kPer = kJoinThreads / kEach;   // rows of a workgroup
+  constexpr int kMost = kSharedMaxParts / kSub;                                       // parts of a thread
+  __shared__ __attribute__((aligned(16))) float s_acc[kSub > 1 ? kSub : 1][kSub > 1 ? D : 1];
+  __shared__ float s_w[kPer][kSharedMaxParts];
+  const int tid = threadIdx.x;
+  const int lane = tid % kLanes, sub = tid / kLanes % kSub, in = tid / kEach;
+  const size_t row = static_cast<size_t>(blockIdx.x) * kPer + in;
+  const bool real = row < p.rows;
+  const int S = p.splits + p.own_splits;
+
+  // the parts are asked for together with their statistics
+  float4 x[kMost < 8 ? kMost : 8];
+  constexpr int kAhead = kMost < 8 ? kMost : 8;
+  const float *po = p.part_o + row * D + lane * 4;
+#pragma unroll
+  for (int i = 0; i < kAhead; ++i) {
+    const int s = sub + i * kSub;
+    x[i] = real && s < S ? *reinterpret_cast<const float4 *>(po + static_cast<size_t>(s) * p.rows * D) : make_float4(0.f, 0.f, 0.f, 0.f);
+  }
+  float M = -INFINITY, L = 0.f;
+  {
+    constexpr int kTurns = (kSharedMaxParts + kLanes - 1) / kLanes;
+    float m[kTurns], l[kTurns];
+#pragma unroll
+    for (int i = 0; i < kTurns; ++i) {
+      const int s = lane + i * kLanes;
+      const bool there = real && s < S;
+      const float2 ml = there ? reinterpret_cast<const float2 *>(p.part_ml)[static_cast<size_t>(s) * p.rows + row] : make_float2(-INFINITY, 0.f);
+      m[i] = ml.x;
+      l[i] = ml.y;
+      M = fmaxf(M, m[i]);
+    }
+#pragma unroll
+    for (int d = 1; d < kLanes; d <<= 1) M = fmaxf(M, shfl_xor(M, d));
+    const float ref = M == -INFINITY ? 0.f : M;
+#pragma unroll
+    for (int i = 0; i < kTurns; ++i) {
+      m[i] = fast_exp2(m[i] - ref);
+      L += l[i] * m[i];
+      // a part without rows has no output
+      if (sub == 0 && lane + i * kLanes < kSharedMaxParts) s_w[in][lane + i * kLanes] = l[i] == 0.f ? 0.f : m[i];
+    }
+#pragma unroll
+    for (int d = 1; d < kLanes; d <<= 1) L += shfl_xor(L, d);
+  }
+  __syncthreads();
+  const float inv = L == 0.f ? 0.f : 1.f / L;
+  float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+  const auto add = [&](int s, const float4 &y) {
+    const float w = s_w[in][s] * inv;
+    acc.x += w == 0.f ? 0.f : w * y.x;
+    acc.y += w == 0.f ? 0.f : w * y.y;
+    acc.z += w == 0.f ? 0.f : w * y.z;
+    acc.w += w == 0.f ? 0.f : w * y.w;
+  };
+#pragma unroll
+  for (int i = 0; i < kAhead; ++i) {
+    if (sub + i * kSub < S) add(sub + i * kSub, x[i]);
+  }
+#pragma unroll 4
+  for (int s = sub + kAhead * kSub; s < S; s += kSub)
+    if (real) add(s, *reinterpret_cast<const float4 *>(po + static_cast<size_t>(s) * p.rows * D));
+  if constexpr (kSub > 1) {
+    *reinterpret_cast<float4 *>(&s_acc[sub][lane * 4]) = acc;
+    __syncthreads();
+    if (sub > 0) return;
+#pragma unroll
+    for (int i = 1; i < kSub; ++i) {
+      const float4 y = *reinterpret_cast<const float4 *>(&s_acc[i][lane * 4]);
+      acc.x += y.x;
+      acc.y += y.y;
+      acc.z += y.z;
+      acc.w += y.w;
+    }
+  }
+  if (!real) return;
+  // rows are (layer, KV head, sequence, query head); units (layer, sequence, KV head)
+  const int flat = static_cast<int>(row);
+  const int lhb = p.by_group.of(flat), qi = p.by_group.rest(flat);
+  const int lh = p.c.by_batch.of(lhb), b = p.c.by_batch.rest(lhb);
+  const int layer = p.c.by_hkv.of(lh), head = p.c.by_hkv.rest(lh);
+  const int unit = (layer * p.c.batch + b) * p.c.hkv + head;
+  const size_t oq = static_cast<size_t>(unit) * p.group + qi;
+  T *dst = reinterpret_cast<T *>(p.out) + oq * D + lane * 4;
+  dst[0] = from_f32<T>(acc.x);
+  dst[1] = from_f32<T>(acc.y);
+  dst[2] = from_f32<T>(acc.z);
+  dst[3] = from_f32<T>(acc.w);
+  if (p.lse && lane == 0) p.lse[oq] = L == 0.f ? -INFINITY : (M + log2f(L)) * kLn2;
+  if (qi != 0) return;
+  const size_t cunit = p.c.unit(unit);
+  const int len_in = p.c.len[cunit];
+  int code = 0, page = 0;
+  if (len_in < 0 || len_in > p.c.cap) code = kDevBadLength;
+  else if (p.k_new && len_in == p.c.cap) code = kDevAppendOverflow;
+  if (code == 0 && p.k_new) {
+    page = p.c.pages[cunit * static_cast<size_t>(p.c.max_pages) + (len_in >> p.c.page_shift)];
+    if (static_cast<unsigned>(page) >= static_cast<unsigned>(p.c.n_pages)) code = kDevBadPage;
+  }
+  if (code && lane == 0) report(p.c.dev_err, code);
+  if (code || !p.k_new) return;
+  const size_t at = ((static_cast<size_t>(page) << p.c.page_shift) + (len_in & ((1 << p.c.page_shift) - 1))) * D + lane * 4;
+  const size_t from = static_cast<size_t>(unit) * D + lane * 4;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    reinterpret_cast<T *>(p.c.k)[at + i] = reinterpret_cast<const T *>(p.k_new)[from + i];
+    reinterpret_cast<T *>(p.c.v)[at + i] = reinterpret_cast<const T *>(p.v_new)[from + i];
+  }
+  if (lane == 0) p.c.len[cunit] = len_in + 1;
+}
+
+template <typename T, int D, int kSub>
+hipError_t launch_join(const PagedSharedParams &p, hipStream_t s) {
+  constexpr int kPer = kJoinThreads / (D / 4 * kSub);
+  hipLaunchKernelGGL((shared_join_kernel<T, D, kSub>), dim3((p.rows + kPer - 1) / kPer), dim3(kJoinThreads), 0, s, p);
+  return hipGetLastError();
+}
+
+template <typename T, int D>
+hipError_t launch_typed(const PagedSharedParams &p, hipStream_t s) {
+  const int units = p.c.n_layers * p.c.batch * p.c.hkv;
+  hipLaunchKernelGGL((shared_attn_kernel<T, D>), dim3(p.common_wgs + units * p.own_splits), dim3(kNW * kWave), 0, s, p);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  if (p.splits + p.own_splits > 8) return launch_join<T, D, kJoinThreads / (D / 4)>(p, s);
+  return launch_join<T, D, 1>(p, s);
+}
+
+}  // namespace
+
+hipError_t launch_paged_shared(const PagedSharedParams &p, int dtype, int head_dim, hipStream_t s) {
+  if (dtype == 0) {
+    if (head_dim == 64) return launch_typed<float, 64>(p, s);
+    return launch_typed<float, 128>(p, s);
+  }
+  if (head_dim == 64) return launch_typed<bf16_t, 64>(p, s);
+  return launch_typed<bf16_t, 128>(p, s);
+}
+
+}  // namespace reco
