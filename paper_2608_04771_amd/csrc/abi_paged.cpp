@@ -279,7 +279,7 @@ size_t reco_paged_shared_decode_attn_workspace_size(const reco_paged_cache_t *ca
   const int units = units_of(cache, n_layers), G = group_of(cache, n_q_heads);
   if (units < 1 || G < 1 || G > 16 || n_groups < 1 || n_groups > cache->batch) return 0;
   return reco::paged_shared_workspace_bytes(units / cache->batch, cache->batch, G, n_groups,
-                                            static_cast<int>(capacity_of(cache)), cache->head_dim,
+                                            static_cast<int>(capacity_of(cache)), cache->head_dim, cache->dtype,
                                             reco::current_compute_units());
 }
 
@@ -304,7 +304,7 @@ reco_status_t reco_paged_shared_decode_attn(const reco_paged_cache_t *cache, int
   reco::PagedSharedParams p{};
   p.c = paged_cache(cache, layer0, n_layers, dev_err);
   const size_t need =
-      reco::paged_shared_workspace_bytes(jobs, cache->batch, G, n_groups, p.c.cap, cache->head_dim, cus);
+      reco::paged_shared_workspace_bytes(jobs, cache->batch, G, n_groups, p.c.cap, cache->head_dim, cache->dtype, cus);
   if (!ws || ws_bytes < need || (reinterpret_cast<uintptr_t>(ws) & 255)) return RECO_ERR_WORKSPACE;
   p.q = q;
   p.k_new = k_new;
@@ -322,7 +322,7 @@ reco_status_t reco_paged_shared_decode_attn(const reco_paged_cache_t *cache, int
   p.scale_log2 = scale * 1.4426950408889634f;
   const int span = reco::shared_span_rows(p.c.cap, sinks, window);
   p.blocks = reco::shared_blocks(cache->batch, G, n_groups);
-  p.splits = reco::shared_splits(jobs, p.blocks, span, cus);
+  p.splits = reco::shared_splits(jobs, p.blocks, units, span, cache->dtype, cus);
   p.own_splits = reco::shared_own_splits(units, span, cus);
   p.by_splits = reco::FastDiv(p.splits);
   p.by_own = reco::FastDiv(p.own_splits);

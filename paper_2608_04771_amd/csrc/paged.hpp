@@ -128,15 +128,15 @@ struct PagedSharedParams {
   int group, groups, rows;
   int blocks;             // most blocks of kSharedRows query rows that all groups have
   int splits, own_splits;
-  int common_wgs;         // workgroups of the shared rows
+  int common_wgs, own_wgs;   // workgroups of the rows that groups see together (whole eights), and of the others
   int sinks, window;
   float scale_log2;
 };
 int shared_blocks(int batch, int group, int groups);
-int shared_splits(int jobs, int blocks, int span_rows, int compute_units);
+int shared_splits(int jobs, int blocks, int units, int span_rows, int dtype, int compute_units);
 int shared_own_splits(int units, int span_rows, int compute_units);
 int shared_span_rows(int capacity, int sinks, int window);
-size_t paged_shared_workspace_bytes(int jobs, int batch, int group, int groups, int capacity, int head_dim,
+size_t paged_shared_workspace_bytes(int jobs, int batch, int group, int groups, int capacity, int head_dim, int dtype,
                                     int compute_units);
 // Places the parts of a call's workspace and sets its workgroups; the sizes and splits are set.
 void paged_shared_place(PagedSharedParams &p, int head_dim, void *ws);

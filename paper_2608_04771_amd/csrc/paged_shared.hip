@@ -29,6 +29,7 @@ constexpr int kNW = 4;                       // waves of a workgroup
 constexpr int kRows = kSharedRows;           // query rows of one
 static_assert(kRows == 32 * kNW, "32 rows a wave");
 constexpr int kWaitLoads = 0x0f70;           // vmcnt(0)
+constexpr int kMix = 32;                     // compute units of an XCD
 constexpr float kSlack = 8.f;                // log2 units that a maximum may grow before O follows
 
 __device__ __forceinline__ int wave_all_min(int v) {
@@ -42,6 +43,23 @@ __device__ __forceinline__ int wave_all_max(int v) {
   return v;
 }
 
+// What a workgroup needs first, asked for at once where it fits a wave: the list of groups,
+// their counts of shared rows and the lengths of a layer's and KV head's units.
+struct Asked {
+  int from, to, shared, len;
+};
+__device__ __forceinline__ int ask_len(const PagedSharedParams &p, int layer, int head, int b) {
+  return p.c.len[p.c.unit((layer * p.c.batch + b) * p.c.hkv + head)];
+}
+__device__ __forceinline__ Asked ask_first(const PagedSharedParams &p, int layer, int head, int lane) {
+  Asked a;
+  a.from = p.first[min(lane, p.groups)];
+  a.to = p.first[min(lane + 1, p.groups)];
+  a.shared = p.shared[layer * p.shared_stride + min(lane, p.groups - 1)];
+  a.len = ask_len(p, layer, head, min(lane, p.c.batch - 1));
+  return a;
+}
+
 // One group of sequences [from, to), and its place in the list.
 struct Group {
   int id, from, to;
@@ -51,12 +69,13 @@ struct Group {
 
 // The group of block `block` (of kRows query rows each, groups in order), or with
 // block < 0 that of sequence b.  id is -1 where there is none.
-__device__ __forceinline__ Group find_group(const PagedSharedParams &p, int block, int b, int lane) {
+__device__ __forceinline__ Group find_group(const PagedSharedParams &p, const Asked &asked, int block, int b, int lane) {
   Group g{-1, 0, 0, 0, true};
   int before = 0;
   for (int g0 = 0; g0 < p.groups; g0 += kWave) {
     const int i = g0 + lane;
-    const int from = p.first[min(i, p.groups)], to = p.first[min(i + 1, p.groups)];
+    const int from = g0 == 0 ? asked.from : p.first[min(i, p.groups)];
+    const int to = g0 == 0 ? asked.to : p.first[min(i + 1, p.groups)];
     const bool in = i < p.groups;
     const bool ok = !in || (from <= to && from >= 0 && to <= p.c.batch && (i > 0 || from == 0) &&
                             (i + 1 < p.groups || to == p.c.batch));
@@ -92,22 +111,23 @@ struct Common {
   int sinks, start;     // [0, sinks) and [start, rows)
 };
 
-__device__ __forceinline__ Common common_rows(const PagedSharedParams &p, const Group &g, int layer, int head, int lane,
-                                              bool reporting) {
+__device__ __forceinline__ Common common_rows(const PagedSharedParams &p, const Asked &asked, const Group &g, int layer,
+                                              int head, int lane, bool reporting) {
   const int extra = p.k_new ? 1 : 0;
   int least = p.c.cap, start = 0;
-  for (int b = g.from + lane; b < g.to; b += kWave) {
-    const int len = p.c.len[p.c.unit((layer * p.c.batch + b) * p.c.hkv + head)];
+  const auto count = [&](int len) {
     const int n = max(0, min(len, p.c.cap));
     least = min(least, n);
     if (p.window > 0) start = max(start, n + extra - p.window);
-  }
+  };
+  if (lane >= g.from && lane < g.to) count(asked.len);
+  for (int b = max(g.from, kWave) + lane; b < g.to; b += kWave) count(ask_len(p, layer, head, b));
   least = wave_all_min(least);
-  const int given = p.shared[layer * p.shared_stride + g.id];
+  const int given = g.id < kWave ? __builtin_amdgcn_readlane(asked.shared, g.id) : p.shared[layer * p.shared_stride + g.id];
   Common c;
   c.rows = max(0, min(given, least));
   if (reporting && c.rows != given) report(p.c.dev_err, kDevBadLength);
-  c.start = min(wave_all_max(start), c.rows);
+  c.start = p.window > 0 ? min(wave_all_max(start), c.rows) : 0;
   c.sinks = min(p.sinks, c.start);
   return c;
 }
@@ -258,10 +278,11 @@ __device__ __forceinline__ void attend_common(const PagedSharedParams &p, int id
   const int lh = p.by_splits.of(job), split = p.by_splits.rest(job);
   const int layer = p.c.by_hkv.of(lh), head = p.c.by_hkv.rest(lh);
   if (layer >= p.c.n_layers) return;
-  const Group g = find_group(p, block, 0, lane);
+  const Asked asked = ask_first(p, layer, head, lane);
+  const Group g = find_group(p, asked, block, 0, lane);
   if (!g.ok || g.id < 0) return;
   const int rows = (g.to - g.from) * p.group;
-  const Common seen = common_rows(p, g, layer, head, lane, threadIdx.x == 0 && split == 0 && g.row0 == 0);
+  const Common seen = common_rows(p, asked, g, layer, head, lane, threadIdx.x == 0 && split == 0 && g.row0 == 0);
   typename In::List list;
   list.set(0, 0, seen.sinks);
   list.set(1, seen.start, seen.rows);
@@ -472,14 +493,15 @@ __device__ __forceinline__ void attend_own(const PagedSharedParams &p, int id, u
   const size_t cunit = p.c.unit(unit);
   const size_t part0 = ((static_cast<size_t>(layer) * p.c.hkv + head) * p.c.batch + b) * p.group;
 
+  const Asked asked = ask_first(p, layer, head, lane);
   const int len_in = p.c.len[cunit];
   const int n_cache = max(0, min(len_in, p.c.cap));
   const bool append = p.k_new != nullptr;
   const int n = n_cache + (append ? 1 : 0);
   const int lo = p.window > 0 && n > p.window ? n - p.window : 0;
-  const Group g = find_group(p, -1, b, lane);
+  const Group g = find_group(p, asked, -1, b, lane);
   Common seen{0, 0, 0};
-  if (g.ok) seen = common_rows(p, g, layer, head, lane, false);
+  if (g.ok) seen = common_rows(p, asked, g, layer, head, lane, false);
   const bool alone = !g.ok;                               // no sharing at all
   const size_t lead = alone ? cunit : p.c.unit((layer * p.c.batch + g.from) * p.c.hkv + head);
   if (alone && split == 0) {
@@ -675,26 +697,25 @@ __device__ __forceinline__ void attend_own(const PagedSharedParams &p, int id, u
     *reinterpret_cast<float4 *>(ow + col * C::merge_pitch + dt * 16 + 4 * grp) =
         make_float4(o[dt][0], o[dt][1], o[dt][2], o[dt][3]);
   __syncthreads();
-  const float *area[kNW] = {reinterpret_cast<const float *>(a0), reinterpret_cast<const float *>(a1),
-                            reinterpret_cast<const float *>(a2), reinterpret_cast<const float *>(a3)};
+  const auto area = [&](int w) { return reinterpret_cast<const float *>(w < 2 ? (w == 0 ? a0 : a1) : (w == 2 ? a2 : a3)); };
   const size_t part = static_cast<size_t>(p.splits + split) * p.rows + part0;
   for (int idx = threadIdx.x; idx < p.group * (D / 4); idx += kThreads) {
     const int qi = idx / (D / 4);
     const int d = (idx - qi * (D / 4)) * 4;
     float M = -INFINITY, L = 0.f;
 #pragma unroll
-    for (int w = 0; w < kNW; ++w) M = fmaxf(M, area[w][16 * C::merge_pitch + qi]);
+    for (int w = 0; w < kNW; ++w) M = fmaxf(M, area(w)[16 * C::merge_pitch + qi]);
     const float ref = M == -INFINITY ? 0.f : M;
     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
     for (int w = 0; w < kNW; ++w) {
-      const float e = fast_exp2(area[w][16 * C::merge_pitch + qi] - ref);
-      const float4 x = *reinterpret_cast<const float4 *>(area[w] + qi * C::merge_pitch + d);
+      const float e = fast_exp2(area(w)[16 * C::merge_pitch + qi] - ref);
+      const float4 x = *reinterpret_cast<const float4 *>(area(w) + qi * C::merge_pitch + d);
       acc.x += x.x * e;
       acc.y += x.y * e;
       acc.z += x.z * e;
       acc.w += x.w * e;
-      L += area[w][16 * C::merge_pitch + 16 + qi] * e;
+      L += area(w)[16 * C::merge_pitch + 16 + qi] * e;
     }
     *reinterpret_cast<float4 *>(p.part_o + (part + qi) * D + d) = acc;
     if (d == 0) {
@@ -709,9 +730,24 @@ __global__ __launch_bounds__(kNW * kWave, 2) void shared_attn_kernel(PagedShared
   // arrays of their own, so that reads of one need not wait for loads into another
   __shared__ __attribute__((aligned(1024))) unsigned char a0[area_bytes<T, D>()], a1[area_bytes<T, D>()],
       a2[area_bytes<T, D>()], a3[area_bytes<T, D>()];
-  const int id = blockIdx.x;
-  if (id < p.common_wgs) attend_common<T, D>(p, id, a0, a1, a2, a3);
-  else attend_own<T, D>(p, id - p.common_wgs, a0, a1, a2, a3);
+  // Common and own workgroups take turns, kMix on each XCD: the ones wait for products, the
+  // others for memory.
+  const int xcd = blockIdx.x % kXcds;
+  int slot = blockIdx.x / kXcds;
+  bool common;
+  const int turns = min(p.common_wgs, p.own_wgs) / (kXcds * kMix);
+  if (slot < 2 * kMix * turns) {
+    const int t = slot / kMix;
+    common = t % 2 == 0;
+    slot = t / 2 * kMix + slot % kMix;
+  } else {
+    slot -= kMix * turns;
+    common = slot < p.common_wgs / kXcds;
+    if (!common) slot -= p.common_wgs / kXcds - kMix * turns;
+  }
+  const int id = slot * kXcds + xcd;
+  if (common) attend_common<T, D>(p, id, a0, a1, a2, a3);
+  else if (id < p.own_wgs) attend_own<T, D>(p, id, a0, a1, a2, a3);
 }
 
 // ------------------------------------------------------------------ the join
@@ -841,11 +877,11 @@ hipError_t launch_join(const PagedSharedParams &p, hipStream_t s) {
 
 template <typename T, int D>
 hipError_t launch_typed(const PagedSharedParams &p, hipStream_t s) {
-  const int units = p.c.n_layers * p.c.batch * p.c.hkv;
-  hipLaunchKernelGGL((shared_attn_kernel<T, D>), dim3(p.common_wgs + units * p.own_splits), dim3(kNW * kWave), 0, s, p);
+  const int wgs = p.common_wgs + (p.own_wgs + kXcds - 1) / kXcds * kXcds;
+  hipLaunchKernelGGL((shared_attn_kernel<T, D>), dim3(wgs), dim3(kNW * kWave), 0, s, p);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  if (p.splits + p.own_splits > 8) return launch_join<T, D, kJoinThreads / (D / 4)>(p, s);
+  if (p.splits + p.own_splits > 8 && p.rows < 2048) return launch_join<T, D, kJoinThreads / (D / 4)>(p, s);
   return launch_join<T, D, 1>(p, s);
 }
 
