@@ -322,7 +322,7 @@ reco_status_t reco_paged_shared_decode_attn(const reco_paged_cache_t *cache, int
   p.scale_log2 = scale * 1.4426950408889634f;
   const int span = reco::shared_span_rows(p.c.cap, sinks, window);
   p.blocks = reco::shared_blocks(cache->batch, G, n_groups);
-  p.splits = reco::shared_splits(jobs, p.blocks, units, span, cache->dtype, cus);
+  p.splits = reco::shared_splits(jobs, p.blocks, span, cache->dtype, cus);
   p.own_splits = reco::shared_own_splits(units, span, cus);
   p.by_splits = reco::FastDiv(p.splits);
   p.by_own = reco::FastDiv(p.own_splits);

@@ -128,12 +128,13 @@ struct PagedSharedParams {
   int group, groups, rows;
   int blocks;             // most blocks of kSharedRows query rows that all groups have
   int splits, own_splits;
-  int common_wgs, own_wgs;   // workgroups of the rows that groups see together (whole eights), and of the others
+  int own_items;          // units and splits of own rows
+  int common_wgs, own_wgs;   // workgroups of the rows that groups see together, and of the others: whole eights
   int sinks, window;
   float scale_log2;
 };
 int shared_blocks(int batch, int group, int groups);
-int shared_splits(int jobs, int blocks, int units, int span_rows, int dtype, int compute_units);
+int shared_splits(int jobs, int blocks, int span_rows, int dtype, int compute_units);
 int shared_own_splits(int units, int span_rows, int compute_units);
 int shared_span_rows(int capacity, int sinks, int window);
 size_t paged_shared_workspace_bytes(int jobs, int batch, int group, int groups, int capacity, int head_dim, int dtype,

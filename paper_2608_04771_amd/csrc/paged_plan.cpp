@@ -168,12 +168,11 @@ int shared_span_rows(int capacity, int sinks, int window) {
   return static_cast<int>(seen < capacity ? seen : capacity);
 }
 
-// Two workgroups on every compute unit, one where units' own rows take the other place, share
-// the common rows of `jobs` (layers and KV heads); a split keeps 256 rows of what a call may
-// see, of fp32, whose products take sixteen times as long, a tile.
-int shared_splits(int jobs, int blocks, int units, int span_rows, int dtype, int compute_units) {
-  const int64_t places = (units >= compute_units ? 1 : 2) * static_cast<int64_t>(compute_units);
-  int64_t splits = places / (static_cast<int64_t>(jobs) * blocks);
+// A workgroup for every compute unit shares the common rows of `jobs` (layers and KV heads);
+// a split keeps 256 rows of what a call may see, of fp32, whose products take sixteen times
+// as long, a tile.
+int shared_splits(int jobs, int blocks, int span_rows, int dtype, int compute_units) {
+  int64_t splits = compute_units / (static_cast<int64_t>(jobs) * blocks);
   const int least = dtype == 0 ? prefill_tile_rows(0) : 256;
   if (splits > span_rows / least) splits = span_rows / least;
   if (splits > kSharedMaxSplits) splits = kSharedMaxSplits;
@@ -191,7 +190,7 @@ size_t paged_shared_workspace_bytes(int jobs, int batch, int group, int groups, 
                                     int compute_units) {
   // a window takes no more splits than the whole cache does
   const int blocks = shared_blocks(batch, group, groups), units = jobs * batch;
-  const size_t parts = static_cast<size_t>(shared_splits(jobs, blocks, units, capacity, dtype, compute_units)) +
+  const size_t parts = static_cast<size_t>(shared_splits(jobs, blocks, capacity, dtype, compute_units)) +
                        shared_own_splits(units, capacity, compute_units);
   return parts * jobs * batch * group * (static_cast<size_t>(head_dim) + 2) * sizeof(float);
 }
@@ -199,7 +198,8 @@ size_t paged_shared_workspace_bytes(int jobs, int batch, int group, int groups, 
 void paged_shared_place(PagedSharedParams &p, int head_dim, void *ws) {
   const int64_t jobs = static_cast<int64_t>(p.c.n_layers) * p.c.hkv * p.splits;
   p.common_wgs = static_cast<int>((jobs + kXcds - 1) / kXcds * kXcds * p.blocks);
-  p.own_wgs = p.c.n_layers * p.c.batch * p.c.hkv * p.own_splits;
+  p.own_items = p.c.n_layers * p.c.batch * p.c.hkv * p.own_splits;
+  p.own_wgs = (p.own_items + kXcds - 1) / kXcds * kXcds;
   p.part_o = static_cast<float *>(ws);
   p.part_ml = p.part_o + static_cast<size_t>(p.splits + p.own_splits) * p.rows * head_dim;
 }

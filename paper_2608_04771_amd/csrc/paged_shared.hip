@@ -28,19 +28,16 @@ namespace {
 constexpr int kNW = 4;                       // waves of a workgroup
 constexpr int kRows = kSharedRows;           // query rows of one
 static_assert(kRows == 32 * kNW, "32 rows a wave");
-constexpr int kWaitLoads = 0x0f70;           // vmcnt(0)
 constexpr int kMix = 32;                     // compute units of an XCD
+constexpr int kWaitLoads = 0x0f70;           // vmcnt(0)
 constexpr float kSlack = 8.f;                // log2 units that a maximum may grow before O follows
 
-__device__ __forceinline__ int wave_all_min(int v) {
-#pragma unroll
-  for (int m = 1; m < kWave; m <<= 1) v = min(v, __shfl_xor(v, m, kWave));
-  return v;
-}
-__device__ __forceinline__ int wave_all_max(int v) {
-#pragma unroll
-  for (int m = 1; m < kWave; m <<= 1) v = max(v, __shfl_xor(v, m, kWave));
-  return v;
+// f over all 64 lanes, by the vector unit alone (a shuffle goes through the LDS unit, some
+// 100 cycles each, which every workgroup would wait for before its first load).
+template <typename F>
+__device__ __forceinline__ int wave_all(int v, F f) {
+  const float x = wave_fold(__int_as_float(v), [&](float a, float b) { return __int_as_float(f(__float_as_int(a), __float_as_int(b))); });
+  return __builtin_amdgcn_readfirstlane(__float_as_int(x));
 }
 
 // What a workgroup needs first, asked for at once where it fits a wave: the list of groups,
@@ -80,26 +77,19 @@ __device__ __forceinline__ Group find_group(const PagedSharedParams &p, const As
     const bool ok = !in || (from <= to && from >= 0 && to <= p.c.batch && (i > 0 || from == 0) &&
                             (i + 1 < p.groups || to == p.c.batch));
     g.ok = g.ok && __all(ok);
-    int mine = 0, until = 0;
-    if (block >= 0) {
-      mine = in && ok ? ((to - from) * p.group + kRows - 1) / kRows : 0;
-      until = mine;
-#pragma unroll
-      for (int m = 1; m < kWave; m <<= 1) {
-        const int other = __shfl_up(until, m, kWave);
-        until += lane >= m ? other : 0;
+    if (block < 0) {
+      const unsigned long long who = __ballot(in && b >= from && b < to);
+      if (who && g.id < 0) {
+        const int at = __builtin_ctzll(who);
+        g = Group{g0 + at, __builtin_amdgcn_readlane(from, at), __builtin_amdgcn_readlane(to, at), 0, g.ok};
       }
-      until += before;
-      before = __shfl(until, kWave - 1, kWave);
+      continue;
     }
-    const bool hit = block >= 0 ? block < until && block >= until - mine : in && b >= from && b < to;
-    const unsigned long long who = __ballot(hit);
-    if (who && g.id < 0) {
-      const int at = __builtin_ctzll(who);
-      g.id = g0 + at;
-      g.from = __builtin_amdgcn_readlane(from, at);
-      g.to = __builtin_amdgcn_readlane(to, at);
-      g.row0 = block >= 0 ? (block - __builtin_amdgcn_readlane(until - mine, at)) * kRows : 0;
+    for (int k = 0; k < min(p.groups - g0, kWave) && g.ok && g.id < 0; ++k) {
+      const int k0 = __builtin_amdgcn_readlane(from, k), k1 = __builtin_amdgcn_readlane(to, k);
+      const int mine = ((k1 - k0) * p.group + kRows - 1) / kRows;
+      if (block < before + mine) g = Group{g0 + k, k0, k1, (block - before) * kRows, true};
+      before += mine;
     }
   }
   return g;
@@ -122,39 +112,40 @@ __device__ __forceinline__ Common common_rows(const PagedSharedParams &p, const 
   };
   if (lane >= g.from && lane < g.to) count(asked.len);
   for (int b = max(g.from, kWave) + lane; b < g.to; b += kWave) count(ask_len(p, layer, head, b));
-  least = wave_all_min(least);
+  least = wave_all(least, [](int a, int b) { return min(a, b); });
   const int given = g.id < kWave ? __builtin_amdgcn_readlane(asked.shared, g.id) : p.shared[layer * p.shared_stride + g.id];
   Common c;
   c.rows = max(0, min(given, least));
   if (reporting && c.rows != given) report(p.c.dev_err, kDevBadLength);
-  c.start = p.window > 0 ? min(wave_all_max(start), c.rows) : 0;
+  c.start = p.window > 0 ? min(wave_all(start, [](int a, int b) { return max(a, b); }), c.rows) : 0;
   c.sinks = min(p.sinks, c.start);
   return c;
 }
 
-// A list of tiles of KT rows that covers ranges of rows one after the other.
+// A list of tiles of KT rows that covers N ranges of rows, two or three, one after the other.
+// Its bounds are the same in all lanes.
 template <int KT, int N>
 struct Tiles {
-  int from[N], to[N], until[N];              // until: tiles of the ranges up to this one
-  int total;
+  int from0, to0, from1, to1, from2, to2;
+  int until0, until1, total;                 // tiles of the ranges up to this one
 
-  __device__ __forceinline__ void set(int i, int a, int b) {
-    from[i] = a;
-    to[i] = b;
-    const int n = b > a ? (b + KT - 1) / KT - a / KT : 0;
-    until[i] = (i > 0 ? until[i > 0 ? i - 1 : 0] : 0) + n;
-    total = until[i];
-  }
+  __device__ __forceinline__ static int count(int a, int b) { return b > a ? (b + KT - 1) / KT - a / KT : 0; }
+  __device__ __forceinline__ Tiles(int a0, int b0, int a1, int b1, int a2 = 0, int b2 = 0)
+      : from0(a0), to0(b0), from1(a1), to1(b1), from2(a2), to2(b2), until0(count(a0, b0)), until1(until0 + count(a1, b1)),
+        total(until1 + (N > 2 ? count(a2, b2) : 0)) {}
   struct At {
     int row, from, to, range;                // the tile's first row, its range's rows
   };
   __device__ __forceinline__ At at(int i) const {
-    At a{(from[0] / KT + i) * KT, from[0], to[0], 0};
-#pragma unroll
-    for (int r = 1; r < N; ++r) {
-      if (i >= until[r - 1]) a = At{(from[r] / KT + i - until[r - 1]) * KT, from[r], to[r], r};
-    }
-    return a;
+    // (readfirstlane keeps the choice one of values: of addresses, it would be made in memory)
+    const auto value = [](int v) { return __builtin_amdgcn_readfirstlane(v); };
+    const int f0 = value(from0), f1 = value(from1), t0 = value(to0), t1 = value(to1), u0 = value(until0);
+    const int f2 = N > 2 ? value(from2) : 0, t2 = N > 2 ? value(to2) : 0, u1 = N > 2 ? value(until1) : 0;
+    const bool past0 = i >= u0, past1 = N > 2 && i >= u1;
+    const int from = past1 ? f2 : past0 ? f1 : f0;
+    const int to = past1 ? t2 : past0 ? t1 : t0;
+    const int before = past1 ? u1 : past0 ? u0 : 0;
+    return At{(from / KT + i - before) * KT, from, to, past1 ? 2 : past0 ? 1 : 0};
   }
 };
 
@@ -283,9 +274,7 @@ __device__ __forceinline__ void attend_common(const PagedSharedParams &p, int id
   if (!g.ok || g.id < 0) return;
   const int rows = (g.to - g.from) * p.group;
   const Common seen = common_rows(p, asked, g, layer, head, lane, threadIdx.x == 0 && split == 0 && g.row0 == 0);
-  typename In::List list;
-  list.set(0, 0, seen.sinks);
-  list.set(1, seen.start, seen.rows);
+  const typename In::List list(0, seen.sinks, seen.start, seen.rows);
   const int per_split = p.by_splits.of(list.total + p.splits - 1);
   const int i0 = split * per_split;
   const int i1 = min(list.total, i0 + per_split);
@@ -344,8 +333,8 @@ __device__ __forceinline__ void attend_common(const PagedSharedParams &p, int id
 #pragma unroll
       for (int e = 0; e < 16; ++e) s[kb][e] = 0.f;
     }
-    constexpr int kSteps = C::blocks * C::qk_steps, kAhead = M::kpl == 8 ? 8 : 16, kEach = kSteps / C::insts;
-    frag kf[2][kAhead];
+    constexpr int kSteps = C::blocks * C::qk_steps, kMost = M::kpl == 8 ? 8 : 16, kAhead = kMost < kSteps ? kMost : kSteps, kEach = kSteps / C::insts;
+    frag kf[kSteps > kAhead ? 2 : 1][kAhead];
     const auto read_k = [&](int q) {
 #pragma unroll
       for (int c = 0; c < kAhead; ++c) {
@@ -482,7 +471,6 @@ __device__ __forceinline__ void attend_own(const PagedSharedParams &p, int id, u
   using C = tiles16::Cfg<T, D>;
   using MF = Mfma<T>;
   using frag = typename MF::frag;
-  constexpr int kThreads = kNW * kWave;
   const int lane = threadIdx.x & (kWave - 1);
   const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) / kWave);
   const int col = lane & 15;
@@ -494,7 +482,7 @@ __device__ __forceinline__ void attend_own(const PagedSharedParams &p, int id, u
   const size_t part0 = ((static_cast<size_t>(layer) * p.c.hkv + head) * p.c.batch + b) * p.group;
 
   const Asked asked = ask_first(p, layer, head, lane);
-  const int len_in = p.c.len[cunit];
+  const int len_in = __builtin_amdgcn_readfirstlane(p.c.len[cunit]);
   const int n_cache = max(0, min(len_in, p.c.cap));
   const bool append = p.k_new != nullptr;
   const int n = n_cache + (append ? 1 : 0);
@@ -504,9 +492,9 @@ __device__ __forceinline__ void attend_own(const PagedSharedParams &p, int id, u
   if (g.ok) seen = common_rows(p, asked, g, layer, head, lane, false);
   const bool alone = !g.ok;                               // no sharing at all
   const size_t lead = alone ? cunit : p.c.unit((layer * p.c.batch + g.from) * p.c.hkv + head);
-  if (alone && split == 0) {
-    if (threadIdx.x == 0) report(p.c.dev_err, kDevBadGroup);
-    for (int i = threadIdx.x; i < p.splits * p.group; i += kThreads) {
+  if (alone && split == 0 && wave == 0) {
+    if (lane == 0) report(p.c.dev_err, kDevBadGroup);
+    for (int i = lane; i < p.splits * p.group; i += kWave) {
       const size_t part = static_cast<size_t>(i / p.group) * p.rows + part0 + i % p.group;
       p.part_ml[2 * part] = -INFINITY;
       p.part_ml[2 * part + 1] = 0.f;
@@ -514,10 +502,9 @@ __device__ __forceinline__ void attend_own(const PagedSharedParams &p, int id, u
   }
 
   using List = Tiles<kTile, 3>;
-  List list;
-  list.set(0, max(lo, seen.sinks), seen.start);           // shared rows that not all see
-  list.set(1, seen.rows, min(p.sinks, lo));               // sinks behind them
-  list.set(2, max(seen.rows, lo), n);
+  const List list(max(lo, seen.sinks), seen.start,        // shared rows that not all see
+                  seen.rows, min(p.sinks, lo),            // sinks behind them
+                  max(seen.rows, lo), n);
   const int per_split = p.by_own.of(list.total + p.own_splits - 1);
   const int i0 = split * per_split;
   const int i1 = min(list.total, i0 + per_split);
@@ -532,6 +519,7 @@ __device__ __forceinline__ void attend_own(const PagedSharedParams &p, int id, u
   f32x4_t o[C::dtiles];
 #pragma unroll
   for (int dt = 0; dt < C::dtiles; ++dt) o[dt] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+
   unsigned char *stage = wave < 2 ? (wave == 0 ? a0 : a1) : (wave == 2 ? a2 : a3);
 
   // Where the wave's tiles lie: each lane holds the place of 16 rows, so 32 tiles at a
@@ -699,7 +687,7 @@ __device__ __forceinline__ void attend_own(const PagedSharedParams &p, int id, u
   __syncthreads();
   const auto area = [&](int w) { return reinterpret_cast<const float *>(w < 2 ? (w == 0 ? a0 : a1) : (w == 2 ? a2 : a3)); };
   const size_t part = static_cast<size_t>(p.splits + split) * p.rows + part0;
-  for (int idx = threadIdx.x; idx < p.group * (D / 4); idx += kThreads) {
+  for (int idx = threadIdx.x; idx < p.group * (D / 4); idx += kNW * kWave) {
     const int qi = idx / (D / 4);
     const int d = (idx - qi * (D / 4)) * 4;
     float M = -INFINITY, L = 0.f;
@@ -747,7 +735,7 @@ __global__ __launch_bounds__(kNW * kWave, 2) void shared_attn_kernel(PagedShared
   }
   const int id = slot * kXcds + xcd;
   if (common) attend_common<T, D>(p, id, a0, a1, a2, a3);
-  else if (id < p.own_wgs) attend_own<T, D>(p, id, a0, a1, a2, a3);
+  else if (id < p.own_items) attend_own<T, D>(p, id, a0, a1, a2, a3);
 }
 
 // ------------------------------------------------------------------ the join
@@ -877,8 +865,7 @@ hipError_t launch_join(const PagedSharedParams &p, hipStream_t s) {
 
 template <typename T, int D>
 hipError_t launch_typed(const PagedSharedParams &p, hipStream_t s) {
-  const int wgs = p.common_wgs + (p.own_wgs + kXcds - 1) / kXcds * kXcds;
-  hipLaunchKernelGGL((shared_attn_kernel<T, D>), dim3(wgs), dim3(kNW * kWave), 0, s, p);
+  hipLaunchKernelGGL((shared_attn_kernel<T, D>), dim3(p.common_wgs + p.own_wgs), dim3(kNW * kWave), 0, s, p);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   if (p.splits + p.own_splits > 8 && p.rows < 2048) return launch_join<T, D, kJoinThreads / (D / 4)>(p, s);
