@@ -323,9 +323,12 @@ reco_status_t reco_paged_shared_decode_attn(const reco_paged_cache_t *cache, int
   const int span = reco::shared_span_rows(p.c.cap, sinks, window);
   p.blocks = reco::shared_blocks(cache->batch, G, n_groups);
   p.splits = reco::shared_splits(jobs, p.blocks, span, cache->dtype, cus);
-  p.own_splits = reco::shared_own_splits(units, span, cus);
+  const int chunks = (cache->batch + reco::kSharedCell - 1) / reco::kSharedCell;
+  p.cell_wgs = reco::shared_cell_wgs(jobs * chunks, cus);
+  p.own_parts = reco::shared_own_parts(cache->batch, p.cell_wgs);
   p.by_splits = reco::FastDiv(p.splits);
-  p.by_own = reco::FastDiv(p.own_splits);
+  p.by_cell = reco::FastDiv(p.cell_wgs);
+  p.by_chunks = reco::FastDiv(chunks);
   p.by_blocks = reco::FastDiv(p.blocks);
   p.by_group = reco::FastDiv(G);
   if (!reco::paged_shared_fits_grid(p)) return RECO_ERR_UNSUPPORTED;

@@ -110,7 +110,8 @@ hipError_t launch_paged_prefill(const PagedPrefillParams &p, int dtype, int head
 
 // ---- attention of one new token over shared first rows -----------------------------
 constexpr int kSharedRows = 128;         // query rows of a workgroup
-constexpr int kSharedMaxSplits = 64;     // of the shared rows, and of a unit's own ones
+constexpr int kSharedMaxSplits = 64;     // of the shared rows, and parts of a sequence's own ones
+constexpr int kSharedCell = 512;         // sequences whose own rows are dealt out together
 constexpr int kSharedMaxParts = 2 * kSharedMaxSplits;
 struct PagedSharedParams {
   PagedCache c;
@@ -122,20 +123,23 @@ struct PagedSharedParams {
   const int32_t *first;   // [groups + 1]  first sequence of each group, and the batch
   const int32_t *shared;  // [groups], or [n_layers][groups] with shared_stride = groups
   int64_t shared_stride;
-  float *part_o;          // [splits, own_splits][rows][D], rows (layer, KV head, sequence, query head)
-  float *part_ml;         // [splits, own_splits][rows][2]  (maximum, sum)
-  FastDiv by_splits, by_own, by_blocks, by_group;
+  float *part_o;          // [splits, own_parts][rows][D], rows (layer, KV head, sequence, query head)
+  float *part_ml;         // [splits, own_parts][rows][2]  (maximum, sum)
+  FastDiv by_splits, by_cell, by_chunks, by_blocks, by_group;
   int group, groups, rows;
   int blocks;             // most blocks of kSharedRows query rows that all groups have
-  int splits, own_splits;
-  int own_items;          // units and splits of own rows
+  int splits;             // of the rows that a group sees together
+  int cell_wgs;           // workgroups of a cell
+  int own_parts;          // most parts of a sequence's own rows, 2 at least
+  int own_items;          // cells and their workgroups
   int common_wgs, own_wgs;   // workgroups of the rows that groups see together, and of the others: whole eights
   int sinks, window;
   float scale_log2;
 };
 int shared_blocks(int batch, int group, int groups);
 int shared_splits(int jobs, int blocks, int span_rows, int dtype, int compute_units);
-int shared_own_splits(int units, int span_rows, int compute_units);
+int shared_cell_wgs(int cells, int compute_units);
+int shared_own_parts(int batch, int cell_wgs);
 int shared_span_rows(int capacity, int sinks, int window);
 size_t paged_shared_workspace_bytes(int jobs, int batch, int group, int groups, int capacity, int head_dim, int dtype,
                                     int compute_units);

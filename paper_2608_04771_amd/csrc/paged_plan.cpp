@@ -179,36 +179,43 @@ int shared_splits(int jobs, int blocks, int span_rows, int dtype, int compute_un
   return splits < 1 ? 1 : static_cast<int>(splits);
 }
 
-int shared_own_splits(int units, int span_rows, int compute_units) {
-  int splits = compute_units / units;
-  if (splits > span_rows / 256) splits = span_rows / 256;
-  if (splits > kSharedMaxSplits) splits = kSharedMaxSplits;
-  return splits < 1 ? 1 : splits;
+// A workgroup for every compute unit shares the sequences' own rows, too.
+int shared_cell_wgs(int cells, int compute_units) { return (compute_units + cells - 1) / cells; }
+
+// A sequence's even share of its cell's waves, twice that, for longer ones, and two more for
+// the waves that it has in part.
+int shared_own_parts(int batch, int cell_wgs) {
+  const int sequences = batch < kSharedCell ? batch : kSharedCell;
+  const int64_t parts = 2 * ((4 * static_cast<int64_t>(cell_wgs) + sequences - 1) / sequences) + 2;
+  return parts < kSharedMaxSplits ? static_cast<int>(parts) : kSharedMaxSplits;
 }
 
 size_t paged_shared_workspace_bytes(int jobs, int batch, int group, int groups, int capacity, int head_dim, int dtype,
                                     int compute_units) {
   // a window takes no more splits than the whole cache does
-  const int blocks = shared_blocks(batch, group, groups), units = jobs * batch;
+  const int blocks = shared_blocks(batch, group, groups), cells = jobs * ((batch + kSharedCell - 1) / kSharedCell);
   const size_t parts = static_cast<size_t>(shared_splits(jobs, blocks, capacity, dtype, compute_units)) +
-                       shared_own_splits(units, capacity, compute_units);
+                       shared_own_parts(batch, shared_cell_wgs(cells, compute_units));
   return parts * jobs * batch * group * (static_cast<size_t>(head_dim) + 2) * sizeof(float);
 }
 
 void paged_shared_place(PagedSharedParams &p, int head_dim, void *ws) {
   const int64_t jobs = static_cast<int64_t>(p.c.n_layers) * p.c.hkv * p.splits;
   p.common_wgs = static_cast<int>((jobs + kXcds - 1) / kXcds * kXcds * p.blocks);
-  p.own_items = p.c.n_layers * p.c.batch * p.c.hkv * p.own_splits;
+  p.own_items = p.c.n_layers * p.c.hkv * p.by_chunks.d * p.cell_wgs;
   p.own_wgs = (p.own_items + kXcds - 1) / kXcds * kXcds;
   p.part_o = static_cast<float *>(ws);
-  p.part_ml = p.part_o + static_cast<size_t>(p.splits + p.own_splits) * p.rows * head_dim;
+  p.part_ml = p.part_o + static_cast<size_t>(p.splits + p.own_parts) * p.rows * head_dim;
 }
 
-// Workgroups of 256 threads, and what FastDiv divides.
+// Workgroups of 256 threads, what FastDiv divides, and a cell's tiles.
 bool paged_shared_fits_grid(const PagedSharedParams &p) {
   const int64_t most = int64_t{1} << 24, units = static_cast<int64_t>(p.c.n_layers) * p.c.batch * p.c.hkv;
   const int64_t jobs = static_cast<int64_t>(p.c.n_layers) * p.c.hkv * p.splits + kXcds;
-  return jobs * p.blocks + units * p.own_splits < most && units * p.group < most;
+  const int64_t cells = static_cast<int64_t>(p.c.n_layers) * p.c.hkv * p.by_chunks.d;
+  const int64_t sequences = p.c.batch < kSharedCell ? p.c.batch : kSharedCell;
+  return jobs * p.blocks + cells * p.cell_wgs < most && units * p.group < most &&
+         sequences * (p.c.cap / kPagedTile + 4) < (int64_t{1} << 31);
 }
 
 // A run of up to eight tokens is one workgroup's, which then sets the lengths itself.

@@ -64,9 +64,9 @@ struct Group {
   bool ok;              // the list ascends from 0 to the batch
 };
 
-// The group of block `block` (of kRows query rows each, groups in order), or with
-// block < 0 that of sequence b.  id is -1 where there is none.
-__device__ __forceinline__ Group find_group(const PagedSharedParams &p, const Asked &asked, int block, int b, int lane) {
+// The group of block `block` (of kRows query rows each, groups in order); id is -1 where
+// there is none.
+__device__ __forceinline__ Group find_group(const PagedSharedParams &p, const Asked &asked, int block, int lane) {
   Group g{-1, 0, 0, 0, true};
   int before = 0;
   for (int g0 = 0; g0 < p.groups; g0 += kWave) {
@@ -77,14 +77,6 @@ __device__ __forceinline__ Group find_group(const PagedSharedParams &p, const As
     const bool ok = !in || (from <= to && from >= 0 && to <= p.c.batch && (i > 0 || from == 0) &&
                             (i + 1 < p.groups || to == p.c.batch));
     g.ok = g.ok && __all(ok);
-    if (block < 0) {
-      const unsigned long long who = __ballot(in && b >= from && b < to);
-      if (who && g.id < 0) {
-        const int at = __builtin_ctzll(who);
-        g = Group{g0 + at, __builtin_amdgcn_readlane(from, at), __builtin_amdgcn_readlane(to, at), 0, g.ok};
-      }
-      continue;
-    }
     for (int k = 0; k < min(p.groups - g0, kWave) && g.ok && g.id < 0; ++k) {
       const int k0 = __builtin_amdgcn_readlane(from, k), k1 = __builtin_amdgcn_readlane(to, k);
       const int mine = ((k1 - k0) * p.group + kRows - 1) / kRows;
@@ -122,30 +114,34 @@ __device__ __forceinline__ Common common_rows(const PagedSharedParams &p, const 
   return c;
 }
 
-// A list of tiles of KT rows that covers N ranges of rows, two or three, one after the other.
-// Its bounds are the same in all lanes.
-template <int KT, int N>
-struct Tiles {
-  int from0, to0, from1, to1, from2, to2;
-  int until0, until1, total;                 // tiles of the ranges up to this one
+// A tile of KT rows in a list that covers ranges of rows, one after the other: its first row,
+// its range's rows, and which range that is.
+struct TileAt {
+  int row, from, to, range;
+};
+template <int KT>
+__device__ __forceinline__ int tiles_of(int from, int to) { return to > from ? (to + KT - 1) / KT - from / KT : 0; }
+template <int KT>
+__device__ __forceinline__ TileAt tile_at(int i, int from0, int to0, int from1, int to1, int from2, int to2) {
+  const int until0 = tiles_of<KT>(from0, to0), until1 = until0 + tiles_of<KT>(from1, to1);
+  const bool past0 = i >= until0, past1 = i >= until1;
+  const int from = past1 ? from2 : past0 ? from1 : from0;
+  const int to = past1 ? to2 : past0 ? to1 : to0;
+  return TileAt{(from / KT + i - (past1 ? until1 : past0 ? until0 : 0)) * KT, from, to, past1 ? 2 : past0 ? 1 : 0};
+}
 
-  __device__ __forceinline__ static int count(int a, int b) { return b > a ? (b + KT - 1) / KT - a / KT : 0; }
-  __device__ __forceinline__ Tiles(int a0, int b0, int a1, int b1, int a2 = 0, int b2 = 0)
-      : from0(a0), to0(b0), from1(a1), to1(b1), from2(a2), to2(b2), until0(count(a0, b0)), until1(until0 + count(a1, b1)),
-        total(until1 + (N > 2 ? count(a2, b2) : 0)) {}
-  struct At {
-    int row, from, to, range;                // the tile's first row, its range's rows
-  };
-  __device__ __forceinline__ At at(int i) const {
+// What a group sees together: the rows [0, sinks) and [start, rows).
+template <int KT>
+struct CommonTiles {
+  int sinks, start, rows, total;
+
+  __device__ __forceinline__ explicit CommonTiles(const Common &c)
+      : sinks(c.sinks), start(c.start), rows(c.rows), total(tiles_of<KT>(0, c.sinks) + tiles_of<KT>(c.start, c.rows)) {}
+  __device__ __forceinline__ TileAt at(int i) const {
     // (readfirstlane keeps the choice one of values: of addresses, it would be made in memory)
-    const auto value = [](int v) { return __builtin_amdgcn_readfirstlane(v); };
-    const int f0 = value(from0), f1 = value(from1), t0 = value(to0), t1 = value(to1), u0 = value(until0);
-    const int f2 = N > 2 ? value(from2) : 0, t2 = N > 2 ? value(to2) : 0, u1 = N > 2 ? value(until1) : 0;
-    const bool past0 = i >= u0, past1 = N > 2 && i >= u1;
-    const int from = past1 ? f2 : past0 ? f1 : f0;
-    const int to = past1 ? t2 : past0 ? t1 : t0;
-    const int before = past1 ? u1 : past0 ? u0 : 0;
-    return At{(from / KT + i - before) * KT, from, to, past1 ? 2 : past0 ? 1 : 0};
+    const int s = __builtin_amdgcn_readfirstlane(sinks), a = __builtin_amdgcn_readfirstlane(start),
+              r = __builtin_amdgcn_readfirstlane(rows);
+    return tile_at<KT>(i, 0, s, a, r, r, r);
   }
 };
 
@@ -159,7 +155,7 @@ struct Feed {
   static constexpr int KT = C::keys;
   static constexpr int kGroups = KT / 16;
   static constexpr int kBatch = kWave / kGroups;         // tiles
-  using List = Tiles<KT, 2>;
+  using List = CommonTiles<KT>;
   const unsigned char *k, *v;
   const int32_t *table;
   const List &list;
@@ -185,7 +181,7 @@ struct Feed {
   __device__ __forceinline__ int piece(int i) const { return (i * kNW + wave) * C::wave_rows; }
   // The first of this lane's 16 rows in the batch that starts at tile i, and whether any is seen.
   __device__ __forceinline__ int row_of(int i, bool &seen) const {
-    const typename List::At a = list.at(min(i + lane / kGroups, end - 1));
+    const TileAt a = list.at(min(i + lane / kGroups, end - 1));
     const int row = a.row + lane % kGroups * 16;
     seen = row < a.to && row + 16 > a.from;
     return row;
@@ -228,7 +224,7 @@ struct Feed {
     if (i < end && (i & (kBatch - 1)) == 0) batch(i);
   }
   // Rows of V outside the range count for nothing, whatever they hold.
-  __device__ __forceinline__ void clean(const typename List::At &a, unsigned char *vbuf) const {
+  __device__ __forceinline__ void clean(const TileAt &a, unsigned char *vbuf) const {
 #pragma unroll
     for (int j = 0; j < C::insts; ++j) {
       const int row = a.row + piece(j) + lane / C::lanes_per_row;
@@ -242,9 +238,8 @@ struct Feed {
 // wave's tile each.
 template <typename T, int D>
 constexpr int area_bytes() {
-  const int a = tiles32::Cfg<T, D, kNW>::stage, b = tiles16::Cfg<T, D>::wave_stage,
-            c = 16 * (2 + tiles16::Cfg<T, D>::merge_pitch) * 4;
-  return a > b ? (a > c ? a : c) : (b > c ? b : c);
+  const int a = tiles32::Cfg<T, D, kNW>::stage, b = tiles16::Cfg<T, D>::wave_stage;
+  return a > b ? a : b;
 }
 
 template <typename T, int D>
@@ -270,11 +265,11 @@ __device__ __forceinline__ void attend_common(const PagedSharedParams &p, int id
   const int layer = p.c.by_hkv.of(lh), head = p.c.by_hkv.rest(lh);
   if (layer >= p.c.n_layers) return;
   const Asked asked = ask_first(p, layer, head, lane);
-  const Group g = find_group(p, asked, block, 0, lane);
+  const Group g = find_group(p, asked, block, lane);
   if (!g.ok || g.id < 0) return;
   const int rows = (g.to - g.from) * p.group;
   const Common seen = common_rows(p, asked, g, layer, head, lane, threadIdx.x == 0 && split == 0 && g.row0 == 0);
-  const typename In::List list(0, seen.sinks, seen.start, seen.rows);
+  const typename In::List list(seen);
   const int per_split = p.by_splits.of(list.total + p.splits - 1);
   const int i0 = split * per_split;
   const int i1 = min(list.total, i0 + per_split);
@@ -310,7 +305,7 @@ __device__ __forceinline__ void attend_common(const PagedSharedParams &p, int id
   const auto step = [&](int i, unsigned char *kbuf, unsigned char *vbuf, unsigned char *kto, unsigned char *vto)
                         __attribute__((always_inline)) {
     in.turn(i + 1);
-    const typename In::List::At tile = list.at(i);
+    const TileAt tile = list.at(i);
     const bool whole = tile.row >= tile.from && tile.row + KT <= tile.to;
     __builtin_amdgcn_s_waitcnt(kWaitLoads);
     if (!whole) in.clean(tile, vbuf);                     // each wave looks after what it loaded
@@ -463,10 +458,149 @@ __device__ __forceinline__ void attend_common(const PagedSharedParams &p, int id
   }
 }
 
-// ------------------------------------------------------------------ a unit's own rows
+// ------------------------------------------------------------------ units' own rows
+// A cell is up to kSharedCell sequences of one layer and KV head.  Their own tiles, one
+// sequence after the other, are dealt evenly to the cell's waves, so that ragged sequences
+// leave no wave behind; a sequence's part of a wave is a part of its own for the join.
+struct Cell {
+  int n[kSharedCell];           // rows with the new one
+  int rows[kSharedCell];        // shared ones
+  int start[kSharedCell];       // of the rows that the sequence's group sees together
+  int lead[kSharedCell];        // the group's first sequence
+  int until[kSharedCell];       // tiles of the sequences up to this one
+  int sums[kNW], most;
+};
+
+// The rows of a sequence with n of them that are not its group's common ones: shared rows that
+// not all see, sinks behind the shared rows, and its own.
+struct OwnRows {
+  int from0, to0, from1, to1, from2, to2;
+
+  __device__ __forceinline__ OwnRows(const PagedSharedParams &p, int n, int rows, int start) {
+    const int lo = p.window > 0 && n > p.window ? n - p.window : 0;
+    from0 = max(lo, min(p.sinks, start));
+    to0 = start;
+    from1 = rows;
+    to1 = min(p.sinks, lo);
+    from2 = max(rows, lo);
+    to2 = n;
+  }
+  __device__ __forceinline__ int tiles() const {
+    return tiles_of<kPagedTile>(from0, to0) + tiles_of<kPagedTile>(from1, to1) + tiles_of<kPagedTile>(from2, to2);
+  }
+  __device__ __forceinline__ TileAt at(int i) const { return tile_at<kPagedTile>(i, from0, to0, from1, to1, from2, to2); }
+};
+
+// Fills the cell; returns whether the list of groups is good (without it every sequence's
+// rows are its own).  All tiles and the most of a sequence come with it.
+__device__ __forceinline__ bool fill_cell(const PagedSharedParams &p, Cell &cell, int layer, int head, int b0, int nb,
+                                          int *total) {
+  constexpr int kEach = kSharedCell / (kNW * kWave);
+  const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid / kWave;
+  const int extra = p.k_new ? 1 : 0;
+  const Asked asked = ask_first(p, layer, head, lane);
+  for (int i = tid; i < kSharedCell; i += kNW * kWave) {
+    cell.rows[i] = p.c.cap;
+    cell.start[i] = 0;
+  }
+  if (tid == 0) cell.most = 0;
+  __syncthreads();
+
+  // The group of sequence b: how many end before it or with it.
+  const auto group_of = [&](int b, int &from, int &to) {
+    int id = 0;
+    from = 0;
+    to = p.c.batch;
+    for (int g0 = 0; g0 < p.groups; g0 += kWave) {
+      const int f = g0 == 0 ? asked.from : p.first[min(g0 + lane, p.groups)];
+      const int t = g0 == 0 ? asked.to : p.first[min(g0 + lane + 1, p.groups)];
+      for (int k = 0; k < min(p.groups - g0, kWave); ++k) {
+        const int k0 = __builtin_amdgcn_readlane(f, k), k1 = __builtin_amdgcn_readlane(t, k);
+        id += k1 <= b ? 1 : 0;
+        if (k0 <= b && b < k1) {
+          from = k0;
+          to = k1;
+        }
+      }
+    }
+    return id;
+  };
+  bool ok = true;
+  for (int g0 = 0; g0 < p.groups; g0 += kWave) {
+    const int i = g0 + lane;
+    const int f = g0 == 0 ? asked.from : p.first[min(i, p.groups)];
+    const int t = g0 == 0 ? asked.to : p.first[min(i + 1, p.groups)];
+    ok = ok && __all(i >= p.groups || (f <= t && f >= 0 && t <= p.c.batch && (i > 0 || f == 0) && (i + 1 < p.groups || t == p.c.batch)));
+  }
+  // Sequences of groups that reach into the cell, also those outside of it, by the place of
+  // their group's first sequence in it.
+  for (int base = 0; ok && base < p.c.batch; base += kNW * kWave) {
+    const int b = min(base + tid, p.c.batch - 1);
+    const int len = base == 0 && wave == 0 ? asked.len : ask_len(p, layer, head, b);
+    int from, to;
+    group_of(b, from, to);
+    if (base + tid < p.c.batch && from < b0 + nb && to > b0) {
+      const int at = max(from, b0) - b0, n = max(0, min(len, p.c.cap));
+      atomicMin(&cell.rows[at], n);
+      if (p.window > 0) atomicMax(&cell.start[at], n + extra - p.window);
+    }
+  }
+  __syncthreads();
+  int n[kEach], rows[kEach], start[kEach], lead[kEach], tiles[kEach], sum = 0, most = 0;
+#pragma unroll
+  for (int i = 0; i < kEach; ++i) {
+    const int at = tid * kEach + i, b = b0 + at;
+    n[i] = rows[i] = start[i] = tiles[i] = 0;
+    lead[i] = b;
+    int from = 0, to = 0, id = 0;
+    if (ok) id = group_of(min(b, p.c.batch - 1), from, to);   // by all lanes
+    if (at < nb) {
+      n[i] = max(0, min(ask_len(p, layer, head, b), p.c.cap)) + extra;
+      if (ok) {
+        const int given = p.shared[layer * p.shared_stride + id], place = max(from, b0) - b0;
+        lead[i] = from;
+        rows[i] = max(0, min(given, cell.rows[place]));
+        start[i] = p.window > 0 ? min(cell.start[place], rows[i]) : 0;
+      }
+      tiles[i] = OwnRows(p, n[i], rows[i], start[i]).tiles();
+    }
+    sum += tiles[i];
+    most = max(most, tiles[i]);
+  }
+  // tiles up to each sequence: over the lanes, then the waves
+  int until = sum;
+#pragma unroll
+  for (int m = 1; m < kWave; m <<= 1) {
+    const int other = __shfl_up(until, m, kWave);
+    until += lane >= m ? other : 0;
+  }
+  if (lane == kWave - 1) cell.sums[wave] = until;
+  if (most > 0) atomicMax(&cell.most, most);
+  __syncthreads();
+  *total = 0;
+#pragma unroll
+  for (int w = 0; w < kNW; ++w) {
+    until += w < wave ? cell.sums[w] : 0;
+    *total += cell.sums[w];
+  }
+  until -= sum;
+#pragma unroll
+  for (int i = 0; i < kEach; ++i) {
+    const int at = tid * kEach + i;
+    until += tiles[i];
+    cell.n[at] = n[i];
+    cell.rows[at] = rows[i];
+    cell.start[at] = start[i];
+    cell.lead[at] = lead[i];
+    cell.until[at] = until;
+  }
+  __syncthreads();
+  return ok;
+}
+
 template <typename T, int D>
 __device__ __forceinline__ void attend_own(const PagedSharedParams &p, int id, unsigned char *a0, unsigned char *a1,
-                                           unsigned char *a2, unsigned char *a3) {
+                                           unsigned char *a2, unsigned char *a3, Cell &cell) {
   using namespace tiles16;
   using C = tiles16::Cfg<T, D>;
   using MF = Mfma<T>;
@@ -475,76 +609,77 @@ __device__ __forceinline__ void attend_own(const PagedSharedParams &p, int id, u
   const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) / kWave);
   const int col = lane & 15;
   const int grp = lane >> 4;
-  const int unit = p.by_own.of(id), split = p.by_own.rest(id);
-  const int lb = p.c.by_hkv.of(unit), head = p.c.by_hkv.rest(unit);
-  const int layer = p.c.by_batch.of(lb), b = p.c.by_batch.rest(lb);
-  const size_t cunit = p.c.unit(unit);
-  const size_t part0 = ((static_cast<size_t>(layer) * p.c.hkv + head) * p.c.batch + b) * p.group;
+  const int cid = p.by_cell.of(id), turn_of = p.by_cell.rest(id);     // the cell, and which of its workgroups
+  const int lh = p.by_chunks.of(cid), b0 = p.by_chunks.rest(cid) * kSharedCell;
+  const int layer = p.c.by_hkv.of(lh), head = p.c.by_hkv.rest(lh);
+  const int nb = min(kSharedCell, p.c.batch - b0);
+  int total;
+  const bool ok = fill_cell(p, cell, layer, head, b0, nb, &total);
+  total = __builtin_amdgcn_readfirstlane(total);
+  const size_t row0 = (static_cast<size_t>(lh) * p.c.batch + b0) * p.group;       // of the parts
 
-  const Asked asked = ask_first(p, layer, head, lane);
-  const int len_in = __builtin_amdgcn_readfirstlane(p.c.len[cunit]);
-  const int n_cache = max(0, min(len_in, p.c.cap));
-  const bool append = p.k_new != nullptr;
-  const int n = n_cache + (append ? 1 : 0);
-  const int lo = p.window > 0 && n > p.window ? n - p.window : 0;
-  const Group g = find_group(p, asked, -1, b, lane);
-  Common seen{0, 0, 0};
-  if (g.ok) seen = common_rows(p, asked, g, layer, head, lane, false);
-  const bool alone = !g.ok;                               // no sharing at all
-  const size_t lead = alone ? cunit : p.c.unit((layer * p.c.batch + g.from) * p.c.hkv + head);
-  if (alone && split == 0 && wave == 0) {
-    if (lane == 0) report(p.c.dev_err, kDevBadGroup);
-    for (int i = lane; i < p.splits * p.group; i += kWave) {
-      const size_t part = static_cast<size_t>(i / p.group) * p.rows + part0 + i % p.group;
-      p.part_ml[2 * part] = -INFINITY;
-      p.part_ml[2 * part + 1] = 0.f;
+  // Even shares, and of no sequence more parts than there are places.
+  const int most = __builtin_amdgcn_readfirstlane(cell.most);
+  const int waves = p.cell_wgs * kNW, w = turn_of * kNW + wave;
+  const int share = max(max((total + waves - 1) / waves, (most + p.own_parts - 2) / (p.own_parts - 1)), 1);
+  const auto no_part = [&](int slot, int b, int g) {
+    float *ml = p.part_ml + 2 * (static_cast<size_t>(slot) * p.rows + row0 + static_cast<size_t>(b) * p.group + g);
+    ml[0] = -INFINITY;
+    ml[1] = 0.f;
+  };
+  if (turn_of == 0) {
+    if (!ok && threadIdx.x == 0) report(p.c.dev_err, kDevBadGroup);
+    // places without a part: of sequences without tiles, and the common ones where there are no groups
+    for (int i = threadIdx.x; i < nb * p.group; i += kNW * kWave) {
+      const int b = p.by_group.of(i), g = p.by_group.rest(i);
+      if (cell.until[b] == (b > 0 ? cell.until[b - 1] : 0))
+        for (int k = 0; k < p.own_parts; ++k) no_part(p.splits + k, b, g);
+      if (!ok)
+        for (int k = 0; k < p.splits; ++k) no_part(k, b, g);
     }
   }
-
-  using List = Tiles<kTile, 3>;
-  const List list(max(lo, seen.sinks), seen.start,        // shared rows that not all see
-                  seen.rows, min(p.sinks, lo),            // sinks behind them
-                  max(seen.rows, lo), n);
-  const int per_split = p.by_own.of(list.total + p.own_splits - 1);
-  const int i0 = split * per_split;
-  const int i1 = min(list.total, i0 + per_split);
-
-  frag qf[C::qk_steps];
-  {
-    const T *qrow = reinterpret_cast<const T *>(p.q) + (static_cast<size_t>(unit) * p.group + col) * D + grp * C::dq;
-#pragma unroll
-    for (int c = 0; c < C::qk_steps; ++c) qf[c] = col < p.group ? load_frag(qrow + c * C::kpl) : zero_frag(frag{});
-  }
-  float m_run = -INFINITY, l_run = 0.f;
-  f32x4_t o[C::dtiles];
-#pragma unroll
-  for (int dt = 0; dt < C::dtiles; ++dt) o[dt] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-
+  const int x0 = w * share, x1 = min(total, x0 + share);
+  const int mine = x1 - x0;                               // tiles of the wave
+  if (mine <= 0) return;
   unsigned char *stage = wave < 2 ? (wave == 0 ? a0 : a1) : (wave == 2 ? a2 : a3);
 
   // Where the wave's tiles lie: each lane holds the place of 16 rows, so 32 tiles at a
   // time; the table's entries of the batch after are on their way meanwhile.
   constexpr int kBatch = kWave / 2;
-  const int mine = i1 - i0 - wave > 0 ? (i1 - i0 - wave + kNW - 1) / kNW : 0;   // tiles of the wave
-  const int32_t *own_table = p.c.pages + cunit * static_cast<size_t>(p.c.max_pages);
-  const int32_t *lead_table = p.c.pages + lead * static_cast<size_t>(p.c.max_pages);
-  const auto tile_of = [&](int k) { return list.at(i0 + wave + kNW * min(k, mine - 1)); };
+  struct Tile {
+    int b, row, from, to;       // the sequence and, from bit 16 on, the range of its list; rows
+  };
+  const auto locate = [&](int k) {
+    const int x = x0 + min(k, mine - 1);
+    int b = 0, end = nb - 1;                              // the first sequence whose tiles reach past x
+    while (__any(b < end)) {
+      const int mid = (b + end) >> 1;
+      const bool past = cell.until[mid] > x;
+      end = past ? mid : end;
+      b = past ? b : min(mid + 1, end);
+    }
+    const TileAt at = OwnRows(p, cell.n[b], cell.rows[b], cell.start[b]).at(x - (b > 0 ? cell.until[b - 1] : 0));
+    return Tile{b | at.range << 16, at.row, at.from, at.to};
+  };
+  Tile here, next;
   unsigned worst = 0;
   int coming = 0;
   uint64_t place = 0;
+  const int extra = p.k_new ? 1 : 0;
   const auto ask = [&](int batch) {
-    const typename List::At a = tile_of(batch * kBatch + lane / 2);
-    const int row = a.row + lane % 2 * 16;
-    const bool cached = row < min(a.to, n_cache) && row + 16 > a.from;
-    coming = cached ? (a.range == 0 ? lead_table : own_table)[row >> p.c.page_shift] : 0;
+    next = locate(batch * kBatch + lane / 2);
+    const int b = next.b & 0xffff, row = next.row + lane % 2 * 16;
+    const bool cached = row < min(next.to, cell.n[b] - extra) && row + 16 > next.from;
+    const size_t cunit = p.c.unit((layer * p.c.batch + (next.b >> 16 == 0 ? cell.lead[b] : b0 + b)) * p.c.hkv + head);
+    coming = cached ? p.c.pages[cunit * static_cast<size_t>(p.c.max_pages) + (row >> p.c.page_shift)] : 0;
   };
   const auto turn = [&](int batch) {
-    const typename List::At a = tile_of(batch * kBatch + lane / 2);
-    const int row = a.row + lane % 2 * 16;
+    here = next;
+    const int row = here.row + lane % 2 * 16;
     const unsigned page = min(static_cast<unsigned>(coming), static_cast<unsigned>(p.c.n_pages - 1));
     worst = max(worst, static_cast<unsigned>(coming));
     place = ((static_cast<uint64_t>(page) << p.c.page_shift) + (row & ((1 << p.c.page_shift) - 1))) * C::row_bytes;
-    ask(batch + 1);
+    if (mine > (batch + 1) * kBatch) ask(batch + 1);
   };
   struct Where {
     uint64_t at[2];
@@ -567,28 +702,68 @@ __device__ __forceinline__ void attend_own(const PagedSharedParams &p, int id, u
       reg[j] = __builtin_nontemporal_load(reinterpret_cast<const u32x4v *>(
           static_cast<const unsigned char *>(pool) + w.at[j / (C::insts / 2)] + j % (C::insts / 2) * (kWave * 16) + lane * 16));
   };
-  const auto fresh_row = [&](const void *rows) {
-    return append ? *reinterpret_cast<const uint4 *>(static_cast<const unsigned char *>(rows) +
-                                                     static_cast<size_t>(unit) * C::row_bytes + lane % C::lanes_per_row * 16)
-                  : make_uint4(0, 0, 0, 0);
+
+  // The sequence that the wave is at, and its softmax.
+  int seq = -1, n_cache = 0;
+  frag qf[C::qk_steps];
+  float m_run, l_run;
+  f32x4_t o[C::dtiles];
+  const auto begin = [&](int b) {
+    seq = b;
+    n_cache = __builtin_amdgcn_readfirstlane(cell.n[b]) - extra;
+    const size_t unit = static_cast<size_t>(layer * p.c.batch + b0 + b) * p.c.hkv + head;
+    const T *qrow = reinterpret_cast<const T *>(p.q) + (unit * p.group + col) * D + grp * C::dq;
+#pragma unroll
+    for (int c = 0; c < C::qk_steps; ++c) qf[c] = col < p.group ? load_frag(qrow + c * C::kpl) : zero_frag(frag{});
+    m_run = -INFINITY;
+    l_run = 0.f;
+#pragma unroll
+    for (int dt = 0; dt < C::dtiles; ++dt) o[dt] = f32x4_t{0.f, 0.f, 0.f, 0.f};
   };
-  const uint4 kfresh = fresh_row(p.k_new), vfresh = fresh_row(p.v_new);
+  const auto finish = [&]() {
+    const int first_tile = seq > 0 ? cell.until[seq - 1] : 0;
+    const int w0 = first_tile / share, k = w - w0;        // the sequence's first wave; the part's number
+    const float l_tot = group4_sum(l_run);
+    if (col >= p.group) return;
+    const size_t part = static_cast<size_t>(p.splits + k) * p.rows + row0 + static_cast<size_t>(seq) * p.group + col;
+    if (grp == 0) {
+      p.part_ml[2 * part] = m_run;
+      p.part_ml[2 * part + 1] = l_tot;
+      if (k == 0)
+        for (int i = (cell.until[seq] - 1) / share - w0 + 1; i < p.own_parts; ++i) no_part(p.splits + i, seq, col);
+    }
+#pragma unroll
+    for (int dt = 0; dt < C::dtiles; ++dt)
+      *reinterpret_cast<float4 *>(p.part_o + part * D + dt * 16 + 4 * grp) =
+          make_float4(o[dt][0], o[dt][1], o[dt][2], o[dt][3]);
+  };
 
   Rows<T, D> kreg, vreg;
   const auto attend = [&](int k) {
-    const typename List::At tile = tile_of(k);
-    const int kb = tile.row;
-    const bool holds_new = append && tile.range == 2 && kb <= n_cache && n_cache < kb + kTile;
-    const bool whole = kb >= tile.from && kb + kTile <= tile.to && !holds_new;
+    const int from_lane = (k & (kBatch - 1)) * 2;
+    const int kb = __builtin_amdgcn_readlane(here.row, from_lane), from = __builtin_amdgcn_readlane(here.from, from_lane),
+              to = __builtin_amdgcn_readlane(here.to, from_lane), b = __builtin_amdgcn_readlane(here.b, from_lane);
+    if ((b & 0xffff) != seq) {
+      if (seq >= 0) finish();
+      begin(b & 0xffff);
+    }
+    const bool holds_new = extra && b >> 16 == 2 && kb <= n_cache && n_cache < kb + kTile;
+    const bool whole = kb >= from && kb + kTile <= to && !holds_new;
     const bool more = k + 1 < mine;
-    if (((k + 1) & (kBatch - 1)) == 0) turn((k + 1) / kBatch);
-    const Where next = find(k + 1);
+    if (((k + 1) & (kBatch - 1)) == 0 && more) turn((k + 1) / kBatch);
+    const Where then = find(k + 1);
+    uint4 kfresh, vfresh;
+    if (holds_new && lane < C::lanes_per_row) {
+      const size_t at = (static_cast<size_t>(layer * p.c.batch + b0 + seq) * p.c.hkv + head) * C::lanes_per_row + lane;
+      kfresh = reinterpret_cast<const uint4 *>(p.k_new)[at];
+      vfresh = reinterpret_cast<const uint4 *>(p.v_new)[at];
+    }
 #pragma unroll
     for (int j = 0; j < C::insts; ++j) {
       const int r = j * C::rows_per_inst + lane / C::lanes_per_row;
       *reinterpret_cast<u32x4v *>(stage + r * C::k_stride + (lane % C::lanes_per_row) * 16) = kreg[j];
     }
-    if (more) load(kreg, p.c.k, next);
+    if (more) load(kreg, p.c.k, then);
     if (holds_new && lane < C::lanes_per_row)
       *reinterpret_cast<uint4 *>(stage + (n_cache - kb) * C::k_stride + lane * 16) = kfresh;
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
@@ -611,7 +786,7 @@ __device__ __forceinline__ void attend_own(const PagedSharedParams &p, int id, u
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         const int row = kb + (e >> 2) * 16 + 4 * grp + (e & 3);
-        x[e] = row >= tile.from && row < tile.to ? x[e] : -INFINITY;
+        x[e] = row >= from && row < to ? x[e] : -INFINITY;
       }
     }
     float top = x[0];
@@ -638,7 +813,7 @@ __device__ __forceinline__ void attend_own(const PagedSharedParams &p, int id, u
 #pragma unroll
       for (int j = 0; j < C::insts; ++j) {
         const int row = kb + j * C::rows_per_inst + lane / C::lanes_per_row;
-        const unsigned keep = row >= tile.from && row < tile.to ? ~0u : 0u;
+        const unsigned keep = row >= from && row < to ? ~0u : 0u;
         vreg[j] &= u32x4v{keep, keep, keep, keep};
       }
     }
@@ -649,7 +824,7 @@ __device__ __forceinline__ void attend_own(const PagedSharedParams &p, int id, u
       dst[0] = make_uint2(vreg[j][0], vreg[j][1]);
       dst[1] = make_uint2(vreg[j][2], vreg[j][3]);
     }
-    if (more) load(vreg, p.c.v, next);
+    if (more) load(vreg, p.c.v, then);
     if (holds_new && lane < C::lanes_per_row) {
       uint2 *dst = reinterpret_cast<uint2 *>(stage + (n_cache - kb) * C::v_stride + lane * 16);
       dst[0] = make_uint2(vfresh.x, vfresh.y);
@@ -663,54 +838,14 @@ __device__ __forceinline__ void attend_own(const PagedSharedParams &p, int id, u
     }
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
   };
-  if (mine > 0) {
-    ask(0);
-    turn(0);
-    const Where first = find(0);
-    load(kreg, p.c.k, first);
-    load(vreg, p.c.v, first);
-    for (int k = 0; k < mine; ++k) attend(k);
-  }
+  ask(0);
+  turn(0);
+  const Where first = find(0);
+  load(kreg, p.c.k, first);
+  load(vreg, p.c.v, first);
+  for (int k = 0; k < mine; ++k) attend(k);
+  finish();
   if (worst >= static_cast<unsigned>(p.c.n_pages)) report(p.c.dev_err, kDevBadPage);
-
-  // The waves' parts meet in LDS: outputs [16][merge_pitch], maxima, sums.
-  const float l_tot = group4_sum(l_run);
-  float *ow = reinterpret_cast<float *>(stage);
-  if (grp == 0) {
-    ow[16 * C::merge_pitch + col] = m_run;
-    ow[16 * C::merge_pitch + 16 + col] = l_tot;
-  }
-#pragma unroll
-  for (int dt = 0; dt < C::dtiles; ++dt)
-    *reinterpret_cast<float4 *>(ow + col * C::merge_pitch + dt * 16 + 4 * grp) =
-        make_float4(o[dt][0], o[dt][1], o[dt][2], o[dt][3]);
-  __syncthreads();
-  const auto area = [&](int w) { return reinterpret_cast<const float *>(w < 2 ? (w == 0 ? a0 : a1) : (w == 2 ? a2 : a3)); };
-  const size_t part = static_cast<size_t>(p.splits + split) * p.rows + part0;
-  for (int idx = threadIdx.x; idx < p.group * (D / 4); idx += kNW * kWave) {
-    const int qi = idx / (D / 4);
-    const int d = (idx - qi * (D / 4)) * 4;
-    float M = -INFINITY, L = 0.f;
-#pragma unroll
-    for (int w = 0; w < kNW; ++w) M = fmaxf(M, area(w)[16 * C::merge_pitch + qi]);
-    const float ref = M == -INFINITY ? 0.f : M;
-    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-    for (int w = 0; w < kNW; ++w) {
-      const float e = fast_exp2(area(w)[16 * C::merge_pitch + qi] - ref);
-      const float4 x = *reinterpret_cast<const float4 *>(area(w) + qi * C::merge_pitch + d);
-      acc.x += x.x * e;
-      acc.y += x.y * e;
-      acc.z += x.z * e;
-      acc.w += x.w * e;
-      L += area(w)[16 * C::merge_pitch + 16 + qi] * e;
-    }
-    *reinterpret_cast<float4 *>(p.part_o + (part + qi) * D + d) = acc;
-    if (d == 0) {
-      p.part_ml[2 * (part + qi)] = M;
-      p.part_ml[2 * (part + qi) + 1] = L;
-    }
-  }
 }
 
 template <typename T, int D>
@@ -718,6 +853,7 @@ __global__ __launch_bounds__(kNW * kWave, 2) void shared_attn_kernel(PagedShared
   // arrays of their own, so that reads of one need not wait for loads into another
   __shared__ __attribute__((aligned(1024))) unsigned char a0[area_bytes<T, D>()], a1[area_bytes<T, D>()],
       a2[area_bytes<T, D>()], a3[area_bytes<T, D>()];
+  __shared__ Cell cell;
   // Common and own workgroups take turns, kMix on each XCD: the ones wait for products, the
   // others for memory.
   const int xcd = blockIdx.x % kXcds;
@@ -735,7 +871,7 @@ __global__ __launch_bounds__(kNW * kWave, 2) void shared_attn_kernel(PagedShared
   }
   const int id = slot * kXcds + xcd;
   if (common) attend_common<T, D>(p, id, a0, a1, a2, a3);
-  else if (id < p.own_items) attend_own<T, D>(p, id, a0, a1, a2, a3);
+  else if (id < p.own_items) attend_own<T, D>(p, id, a0, a1, a2, a3, cell);
 }
 
 // ------------------------------------------------------------------ the join
@@ -753,11 +889,12 @@ __global__ __launch_bounds__(kJoinThreads) void shared_join_kernel(PagedSharedPa
   const int lane = tid % kLanes, sub = tid / kLanes % kSub, in = tid / kEach;
   const size_t row = static_cast<size_t>(blockIdx.x) * kPer + in;
   const bool real = row < p.rows;
-  const int S = p.splits + p.own_splits;
+  const int S = p.splits + p.own_parts;
 
-  // the parts are asked for together with their statistics
-  float4 x[kMost < 8 ? kMost : 8];
-  constexpr int kAhead = kMost < 8 ? kMost : 8;
+  // Few rows' parts are asked for together with their statistics; of many, whose places are
+  // mostly empty, those alone that there are.
+  constexpr int kAhead = kSub > 1 ? (kMost < 8 ? kMost : 8) : 0;
+  float4 x[kAhead + 1];
   const float *po = p.part_o + row * D + lane * 4;
 #pragma unroll
   for (int i = 0; i < kAhead; ++i) {
@@ -806,7 +943,7 @@ __global__ __launch_bounds__(kJoinThreads) void shared_join_kernel(PagedSharedPa
   }
 #pragma unroll 4
   for (int s = sub + kAhead * kSub; s < S; s += kSub)
-    if (real) add(s, *reinterpret_cast<const float4 *>(po + static_cast<size_t>(s) * p.rows * D));
+    if (real && s_w[in][s] != 0.f) add(s, *reinterpret_cast<const float4 *>(po + static_cast<size_t>(s) * p.rows * D));
   if constexpr (kSub > 1) {
     *reinterpret_cast<float4 *>(&s_acc[sub][lane * 4]) = acc;
     __syncthreads();
@@ -868,7 +1005,7 @@ hipError_t launch_typed(const PagedSharedParams &p, hipStream_t s) {
   hipLaunchKernelGGL((shared_attn_kernel<T, D>), dim3(p.common_wgs + p.own_wgs), dim3(kNW * kWave), 0, s, p);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  if (p.splits + p.own_splits > 8 && p.rows < 2048) return launch_join<T, D, kJoinThreads / (D / 4)>(p, s);
+  if (p.splits + p.own_parts > 8 && p.rows < 2048) return launch_join<T, D, kJoinThreads / (D / 4)>(p, s);
   return launch_join<T, D, 1>(p, s);
 }
 

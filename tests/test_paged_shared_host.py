@@ -43,7 +43,7 @@ SHIM = r'''
 extern "C" {
 int blocks(int b, int g, int n) { return reco::shared_blocks(b, g, n); }
 int splits(int jobs, int blocks, int span, int dt, int cus) { return reco::shared_splits(jobs, blocks, span, dt, cus); }
-int own(int units, int span, int cus) { return reco::shared_own_splits(units, span, cus); }
+int own(int jobs, int b, int cus) { return reco::shared_own_parts(b, reco::shared_cell_wgs(jobs * ((b + reco::kSharedCell - 1) / reco::kSharedCell), cus)); }
 int span(int cap, int sinks, int window) { return reco::shared_span_rows(cap, sinks, window); }
 size_t bytes(int jobs, int b, int g, int n, int cap, int d, int dt, int cus) { return reco::paged_shared_workspace_bytes(jobs, b, g, n, cap, d, dt, cus); }
 int rows() { return reco::kSharedRows; }
@@ -83,10 +83,10 @@ def test_splits_fit_the_workspace(plan):
                         for groups in {1, max(1, batch // 3), batch}:
                             blocks, units = plan.blocks(batch, G, groups), jobs * batch
                             for dt in (0, 1):
-                                whole = plan.splits(jobs, blocks, cap, dt, cus) + plan.own(units, cap, cus)
+                                whole = plan.splits(jobs, blocks, cap, dt, cus) + plan.own(jobs, batch, cus)
                                 assert plan.bytes(jobs, batch, G, groups, cap, 128, dt, cus) == whole * units * G * 130 * 4
                                 for sinks, window in ((0, 0), (4, 1), (4, 64), (2 ** 31 - 1, 2 ** 31 - 1), (100, 5000)):
                                     span = plan.span(cap, sinks, window)
-                                    a, b = plan.splits(jobs, blocks, span, dt, cus), plan.own(units, span, cus)
-                                    assert 1 <= a <= plan.most() and 1 <= b <= plan.most() and a + b <= whole
+                                    a, b = plan.splits(jobs, blocks, span, dt, cus), plan.own(jobs, batch, cus)
+                                    assert 1 <= a <= plan.most() and 2 <= b <= plan.most() and a + b <= whole
                                     assert a == 1 or a * jobs * blocks <= 2 * cus
