@@ -29,8 +29,28 @@ constexpr int kNW = 4;                       // waves of a workgroup
 constexpr int kRows = kSharedRows;           // query rows of one
 static_assert(kRows == 32 * kNW, "32 rows a wave");
 constexpr int kMix = 32;                     // compute units of an XCD
-constexpr int kWaitLoads = 0x0f70;           // vmcnt(0)
+constexpr int wait_loads(int n) { return 0x0f70 | (n & 15) | (n >> 4) << 14; }   // vmcnt(n)
 constexpr float kSlack = 8.f;                // log2 units that a maximum may grow before O follows
+
+// Loads to LDS of 16 or 4 bytes a lane, from `from` (the same in all lanes) + `at`, to the LDS
+// address `to` on.  In assembly, because the compiler makes reads of LDS wait for all loads
+// of its own kind that are on their way there; these are waited for by their number, and its
+// own waits for other loads only become longer by them.  No register receives anything.
+__device__ __forceinline__ void load_to_lds16(const void *from, unsigned at, unsigned to) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(at), "s"(from) : "m0");
+}
+__device__ __forceinline__ void load_to_lds4(const void *from, unsigned at, unsigned to) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(to), "v"(at), "s"(from) : "m0", "memory");
+}
+__device__ __forceinline__ unsigned lds_address(const void *p) {
+  return __builtin_amdgcn_readfirstlane(static_cast<unsigned>(reinterpret_cast<uintptr_t>((const __attribute__((address_space(3))) unsigned char *)p)));
+}
+// A barrier for what waves have waited for themselves (__syncthreads waits for all loads).
+__device__ __forceinline__ void barrier() {
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
 
 // f over all 64 lanes, by the vector unit alone (a shuffle goes through the LDS unit, some
 // 100 cycles each, which every workgroup would wait for before its first load).
@@ -147,8 +167,8 @@ struct CommonTiles {
 
 // ------------------------------------------------------------------ common rows
 // Key tiles on their way to LDS, which loads fill without registers between.  Each lane
-// holds the place of 16 rows of the list's tiles; the table's entries of the batch after
-// are on their way meanwhile.
+// holds the place of 16 rows of the list's tiles; the table's entries of the batch after go
+// to LDS meanwhile (a load to a register would have to wait for all rows on their way).
 template <typename T, int D>
 struct Feed {
   using C = tiles32::Cfg<T, D, kNW>;
@@ -159,17 +179,20 @@ struct Feed {
   const unsigned char *k, *v;
   const int32_t *table;
   const List &list;
-  int n_pages, shift, end, wave, lane;
+  int n_pages, shift, begin, end, wave, lane;
+  int *entries;                              // [kWave] in LDS, the wave's own
+  unsigned entries_at;
   unsigned worst;                            // id, of rows that are seen
   uint64_t place;                            // of this lane's 16 rows: a byte offset
-  int coming;                                // the entry for the same lane of the next batch
   unsigned koff[C::insts], voff[C::insts];   // within 16 rows
 
-  // Tiles [.., end) of the list.
-  __device__ __forceinline__ Feed(const PagedSharedParams &p, size_t cunit, const List &list_, int end_, int wave_, int lane_)
+  // Tiles [begin, end) of the list.
+  __device__ __forceinline__ Feed(const PagedSharedParams &p, size_t cunit, const List &list_, int begin_, int end_,
+                                  int *entries_, int wave_, int lane_)
       : k(static_cast<const unsigned char *>(p.c.k)), v(static_cast<const unsigned char *>(p.c.v)),
         table(p.c.pages + cunit * static_cast<size_t>(p.c.max_pages)), list(list_), n_pages(p.c.n_pages),
-        shift(p.c.page_shift), end(end_), wave(wave_), lane(lane_), worst(0) {
+        shift(p.c.page_shift), begin(begin_), end(end_), wave(wave_), lane(lane_), entries(entries_),
+        entries_at(lds_address(entries_)), worst(0) {
 #pragma unroll
     for (int i = 0; i < C::insts; ++i) {
       const int row = piece(i) + lane / C::lanes_per_row, c = lane % C::lanes_per_row;
@@ -186,42 +209,50 @@ struct Feed {
     seen = row < a.to && row + 16 > a.from;
     return row;
   }
-  __device__ __forceinline__ void ask(int i) {
+  __device__ __forceinline__ unsigned entry_of(int i) const {
     bool seen;
     const int row = row_of(i, seen);
-    coming = seen ? table[row >> shift] : 0;
+    return seen ? static_cast<unsigned>(row >> shift) * 4u : 0u;
   }
-  // The batch that starts at tile i, whose entries were asked for, and the one after.
-  __device__ __forceinline__ void batch(int i) {
+  __device__ __forceinline__ void ask(int i) { load_to_lds4(table, entry_of(i), entries_at); }
+  // The batch that starts at tile i, by its entries, and the one after.
+  __device__ __forceinline__ void batch(int i, int entry) {
     bool seen;
     const int row = row_of(i, seen);
-    worst = max(worst, static_cast<unsigned>(coming));
-    const unsigned id = min(static_cast<unsigned>(coming), static_cast<unsigned>(n_pages - 1));
+    if (seen) worst = max(worst, static_cast<unsigned>(entry));
+    const unsigned id = min(static_cast<unsigned>(entry), static_cast<unsigned>(n_pages - 1));
     place = ((static_cast<uint64_t>(id) << shift) + (row & ((1u << shift) - 1u))) * C::row_bytes;
     ask(i + kBatch);
   }
+  __device__ __forceinline__ void first() {
+    batch(begin, *reinterpret_cast<const int32_t *>(reinterpret_cast<const char *>(table) + entry_of(begin)));
+  }
+  __device__ __forceinline__ void turn(int i) {
+    if (i < end && ((i - begin) & (kBatch - 1)) == 0) batch(i, entries[lane]);
+  }
+  // Where tile i's loads begin.  Past the end they are made all the same, so that what is on
+  // its way can be counted, but of one piece.
   struct Place {
     uint64_t at[C::insts];
+    unsigned lanes;
   };
   __device__ __forceinline__ Place find(int i) const {
     const int at_i = min(i, end - 1);
     Place w;
+    w.lanes = i < end ? ~0u : 0u;
 #pragma unroll
     for (int j = 0; j < C::insts; ++j) {
-      const int from = (at_i & (kBatch - 1)) * kGroups + piece(j) / 16;
+      const int from = ((at_i - begin) & (kBatch - 1)) * kGroups + piece(j) / 16;
       w.at[j] = static_cast<uint64_t>(static_cast<unsigned>(__builtin_amdgcn_readlane(static_cast<int>(place >> 32), from))) << 32 |
                 static_cast<unsigned>(__builtin_amdgcn_readlane(static_cast<int>(place), from));
     }
     return w;
   }
-  __device__ __forceinline__ void load_k(const Place &w, int j, unsigned char *buf) const {
-    __builtin_amdgcn_global_load_lds((tiles32::global_u32 *)(k + w.at[j] + koff[j]), (tiles32::lds_u32 *)(buf + piece(j) * C::row_bytes), 16, 0, 0);
+  __device__ __forceinline__ void load_k(const Place &w, int j, unsigned to) const {
+    load_to_lds16(k + w.at[j], koff[j] & w.lanes, to + piece(j) * C::row_bytes);
   }
-  __device__ __forceinline__ void load_v(const Place &w, int j, unsigned char *buf) const {
-    __builtin_amdgcn_global_load_lds((tiles32::global_u32 *)(v + w.at[j] + voff[j]), (tiles32::lds_u32 *)(buf + piece(j) * C::row_bytes), 16, 0, 0);
-  }
-  __device__ __forceinline__ void turn(int i) {
-    if (i < end && (i & (kBatch - 1)) == 0) batch(i);
+  __device__ __forceinline__ void load_v(const Place &w, int j, unsigned to) const {
+    load_to_lds16(v + w.at[j], voff[j] & w.lanes, to + piece(j) * C::row_bytes);
   }
   // Rows of V outside the range count for nothing, whatever they hold.
   __device__ __forceinline__ void clean(const TileAt &a, unsigned char *vbuf) const {
@@ -244,7 +275,7 @@ constexpr int area_bytes() {
 
 template <typename T, int D>
 __device__ __forceinline__ void attend_common(const PagedSharedParams &p, int id, unsigned char *k0, unsigned char *v0,
-                                              unsigned char *k1, unsigned char *v1) {
+                                              unsigned char *k1, unsigned char *v1, int *entries) {
   using namespace tiles32;
   using C = tiles32::Cfg<T, D, kNW>;
   using In = Feed<T, D>;
@@ -291,7 +322,7 @@ __device__ __forceinline__ void attend_common(const PagedSharedParams &p, int id
   }
   const float scale = fmaxf(fabsf(p.scale_log2), 0x1p-126f);   // times a hidden row's -inf, 0 would be NaN
 
-  In in(p, p.c.unit((layer * p.c.batch + g.from) * p.c.hkv + head), list, i1, wave, lane);
+  In in(p, p.c.unit((layer * p.c.batch + g.from) * p.c.hkv + head), list, i0, i1, entries + wave * kWave, wave, lane);
   float m_run = -INFINITY, l_run = 0.f;                  // m in units of the scaled logits
   f32x16_t o[C::dtiles];
 #pragma unroll
@@ -301,53 +332,93 @@ __device__ __forceinline__ void attend_common(const PagedSharedParams &p, int id
   }
   const int kat = k_base<T, D>(lane), vat = v_base<T, D>(lane);
 
-  // Tile i, in kbuf and vbuf once its loads are done; tile i + 1 goes to kto and vto.
-  const auto step = [&](int i, unsigned char *kbuf, unsigned char *vbuf, unsigned char *kto, unsigned char *vto)
+  // Tile i, in kbuf and vbuf once its loads are done.  The next tile's V goes to vto, where the
+  // last tile's was, while S is formed, and the K of the one after to kbuf, while O is: so
+  // each has a tile and a half's time to come in two buffers.  `ahead`: the next tile's place,
+  // then that of the one after.
+  constexpr int kHalf = C::insts;                         // a wave's loads of a tile's K or V
+  typename In::Place ahead;
+  const auto step = [&](int i, unsigned char *kbuf, unsigned char *vbuf, unsigned kto, unsigned vto, bool turning)
                         __attribute__((always_inline)) {
-    in.turn(i + 1);
     const TileAt tile = list.at(i);
     const bool whole = tile.row >= tile.from && tile.row + KT <= tile.to;
-    __builtin_amdgcn_s_waitcnt(kWaitLoads);
-    if (!whole) in.clean(tile, vbuf);                     // each wave looks after what it loaded
-    __syncthreads();                                      // tile i is there, and no one reads tile i - 1
-    const typename In::Place from = in.find(i + 1);
+    __builtin_amdgcn_s_waitcnt(wait_loads(2 * kHalf));    // K
+    barrier();                                            // is there, and no one reads the last tile's V
+    f32x16_t s[C::blocks];
+    constexpr int kSteps = C::blocks * C::qk_steps, kAhead = M::kpl == 8 ? 8 : 16, kEach = kSteps / C::insts;
+    float ref = 0.f;
     if (!active) {
 #pragma unroll
-      for (int j = 0; j < C::insts; ++j) {
-        in.load_k(from, j, kto);
-        in.load_v(from, j, vto);
+      for (int j = 0; j < C::insts; ++j) in.load_v(ahead, j, vto);
+    } else {
+      // S^T, with operands read ahead of their products, and between the products the next
+      // V asked for, piece by piece.  The blocks take turns, so that a product does not wait
+      // for the one before.
+#pragma unroll
+      for (int kb = 0; kb < C::blocks; ++kb) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) s[kb][e] = 0.f;
       }
+      frag kf[2][kAhead];
+      const auto read_k = [&](int q) {
+#pragma unroll
+        for (int c = 0; c < kAhead; ++c) {
+          const int z = q * kAhead + c, byte = z / C::blocks * M::kpl * (int)sizeof(T);
+          kf[q & 1][c] = load_frag(reinterpret_cast<const T *>(kbuf + (kat ^ (byte & ~15)) + (byte & 15) + z % C::blocks * 32 * C::row_bytes));
+        }
+      };
+      read_k(0);
+#pragma unroll
+      for (int z = 0; z < kSteps; ++z) {
+        if (z % kAhead == 0 && z + kAhead < kSteps) read_k(z / kAhead + 1);
+        if (z % kAhead == 0) __builtin_amdgcn_sched_barrier(0);
+        s[z % C::blocks] = M::mma(kf[z / kAhead & 1][z % kAhead], qf[z / C::blocks], s[z % C::blocks]);
+        if (z % kEach == 0) in.load_v(ahead, z / kEach, vto);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      if (!whole) {
+        const int low = tile.from - tile.row - 4 * half, high = tile.to - tile.row - 4 * half;
+#pragma unroll
+        for (int kb = 0; kb < C::blocks; ++kb) {
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            const int c = kb * 32 + acc_row(e, 0);
+            s[kb][e] = c < low || c >= high ? -INFINITY : s[kb][e];
+          }
+        }
+      }
+      float top = -INFINITY;
+#pragma unroll
+      for (int kb = 0; kb < C::blocks; ++kb) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) top = fmaxf(top, s[kb][e]);
+      }
+      top = fmaxf(top, shfl_xor(top, 32)) * scale;
+      // The reference of the exponentials follows the maximum only where it grew by more
+      // than kSlack (P then stays below 2^kSlack, with the same relative precision), so
+      // that O is seldom rescaled.
+      if (__any(top > m_run + kSlack)) {
+        const float m_new = fmaxf(m_run, top);
+        const float alpha = fast_exp2(m_run - (m_new == -INFINITY ? 0.f : m_new));
+        l_run *= alpha;
+        m_run = m_new;
+#pragma unroll
+        for (int dt = 0; dt < C::dtiles; ++dt) {
+#pragma unroll
+          for (int e = 0; e < 16; ++e) o[dt][e] *= alpha;
+        }
+      }
+      ref = m_run == -INFINITY ? 0.f : m_run;
+    }
+    __builtin_amdgcn_s_waitcnt(wait_loads(2 * kHalf));    // V
+    if (!whole) in.clean(tile, vbuf);                     // each wave looks after what it loaded
+    barrier();                                            // is there, and no one reads K any more
+    if (turning) in.turn(i + 2);
+    ahead = in.find(i + 2);
+    if (!active) {
+#pragma unroll
+      for (int j = 0; j < C::insts; ++j) in.load_k(ahead, j, kto);
       return;
-    }
-
-    // S^T, with operands read ahead of their products, and between the products the
-    // next tile asked for, piece by piece.
-    f32x16_t s[C::blocks];
-#pragma unroll
-    for (int kb = 0; kb < C::blocks; ++kb) {
-#pragma unroll
-      for (int e = 0; e < 16; ++e) s[kb][e] = 0.f;
-    }
-    constexpr int kSteps = C::blocks * C::qk_steps, kMost = M::kpl == 8 ? 8 : 16, kAhead = kMost < kSteps ? kMost : kSteps, kEach = kSteps / C::insts;
-    frag kf[kSteps > kAhead ? 2 : 1][kAhead];
-    const auto read_k = [&](int q) {
-#pragma unroll
-      for (int c = 0; c < kAhead; ++c) {
-        const int z = q * kAhead + c, byte = z % C::qk_steps * M::kpl * (int)sizeof(T);
-        kf[q & 1][c] = load_frag(reinterpret_cast<const T *>(kbuf + (kat ^ (byte & ~15)) + (byte & 15) + z / C::qk_steps * 32 * C::row_bytes));
-      }
-    };
-    read_k(0);
-#pragma unroll
-    for (int z = 0; z < kSteps; ++z) {
-      if (z % kAhead == 0 && z + kAhead < kSteps) read_k(z / kAhead + 1);
-      if (z % kAhead == 0) __builtin_amdgcn_sched_barrier(0);
-      s[z / C::qk_steps] = M::mma(kf[z / kAhead & 1][z % kAhead], qf[z % C::qk_steps], s[z / C::qk_steps]);
-      if (z % kEach == 0) {
-        in.load_k(from, z / kEach, kto);
-        in.load_v(from, z / kEach, vto);
-      }
-      __builtin_amdgcn_sched_barrier(0);
     }
     constexpr int kParts = C::blocks * C::pv_steps;
     frag vf[2][C::dtiles];
@@ -359,42 +430,9 @@ __device__ __forceinline__ void attend_common(const PagedSharedParams &p, int id
     };
     read_v(0);
 
-    if (!whole) {
-      const int low = tile.from - tile.row - 4 * half, high = tile.to - tile.row - 4 * half;
-#pragma unroll
-      for (int kb = 0; kb < C::blocks; ++kb) {
-#pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          const int c = kb * 32 + acc_row(e, 0);
-          s[kb][e] = c < low || c >= high ? -INFINITY : s[kb][e];
-        }
-      }
-    }
-    float top = -INFINITY;
-#pragma unroll
-    for (int kb = 0; kb < C::blocks; ++kb) {
-#pragma unroll
-      for (int e = 0; e < 16; ++e) top = fmaxf(top, s[kb][e]);
-    }
-    top = fmaxf(top, shfl_xor(top, 32)) * scale;
-    // The reference of the exponentials follows the maximum only where it grew by more
-    // than kSlack (P then stays below 2^kSlack, with the same relative precision), so
-    // that O is seldom rescaled.
-    if (__any(top > m_run + kSlack)) {
-      const float m_new = fmaxf(m_run, top);
-      const float alpha = fast_exp2(m_run - (m_new == -INFINITY ? 0.f : m_new));
-      l_run *= alpha;
-      m_run = m_new;
-#pragma unroll
-      for (int dt = 0; dt < C::dtiles; ++dt) {
-#pragma unroll
-        for (int e = 0; e < 16; ++e) o[dt][e] *= alpha;
-      }
-    }
     // O^T: part q takes kpl elements of every lane, slot j of which is row
     // 8 (e / 4) + 4 half + e % 4 of S^T for e = q * kpl + j; the exponentials of a part
-    // lie between the products of the part before.
-    const float ref = m_run == -INFINITY ? 0.f : m_run;
+    // lie between the products of the part before, as the loads do.
     const auto weigh = [&](int q, int j) {
       const int e = q * M::kpl + j;
       const float w = fast_exp2(fmaf(s[e / 16][e % 16], scale, -ref));
@@ -412,9 +450,14 @@ __device__ __forceinline__ void attend_common(const PagedSharedParams &p, int id
     for (int q = 0; q < kParts; ++q) {
       if (q + 1 < kParts) read_v(q + 1);
       __builtin_amdgcn_sched_barrier(0);
+      constexpr int kApart = kParts / C::insts > 0 ? kParts / C::insts : 1, kTogether = kApart * C::insts > kParts ? 2 : 1;
 #pragma unroll
       for (int dt = 0; dt < C::dtiles; ++dt) {
         o[dt] = M::mma(vf[q & 1][dt], pf[q & 1], o[dt]);
+        if (dt == 0 && q % kApart == 0) {
+#pragma unroll
+          for (int j = q / kApart * kTogether; j < (q / kApart + 1) * kTogether && j < C::insts; ++j) in.load_k(ahead, j, kto);
+        }
         if (q + 1 < kParts) {
 #pragma unroll
           for (int j = dt * M::kpl / C::dtiles; j < (dt + 1) * M::kpl / C::dtiles; ++j) put(q + 1, j);
@@ -424,20 +467,23 @@ __device__ __forceinline__ void attend_common(const PagedSharedParams &p, int id
     }
   };
   if (i0 < i1) {
-    in.ask(i0 & -In::kBatch);
-    in.batch(i0 & -In::kBatch);
-    const typename In::Place from = in.find(i0);
+    in.first();
+    const unsigned at_k0 = lds_address(k0), at_v0 = lds_address(v0), at_k1 = lds_address(k1), at_v1 = lds_address(v1);
+    ahead = in.find(i0);
 #pragma unroll
-    for (int j = 0; j < C::insts; ++j) {
-      in.load_k(from, j, k0);
-      in.load_v(from, j, v0);
-    }
+    for (int j = 0; j < C::insts; ++j) in.load_k(ahead, j, at_k0);
+#pragma unroll
+    for (int j = 0; j < C::insts; ++j) in.load_v(ahead, j, at_v0);
+    ahead = in.find(i0 + 1);
+#pragma unroll
+    for (int j = 0; j < C::insts; ++j) in.load_k(ahead, j, at_k1);
+    static_assert(In::kBatch % 2 == 0, "batches begin at an even step");
     for (int i = i0; i < i1; i += 2) {
-      step(i, k0, v0, k1, v1);
-      if (i + 1 < i1) step(i + 1, k1, v1, k0, v0);
+      step(i, k0, v0, at_k0, at_v1, true);
+      if (i + 1 < i1) step(i + 1, k1, v1, at_k1, at_v0, false);
     }
   }
-  __builtin_amdgcn_s_waitcnt(kWaitLoads);
+  __builtin_amdgcn_s_waitcnt(wait_loads(0));              // LDS is another workgroup's afterwards
   if (in.worst >= static_cast<unsigned>(p.c.n_pages)) report(p.c.dev_err, kDevBadPage);
 
   const float l_tot = l_run + shfl_xor(l_run, 32);
@@ -491,10 +537,64 @@ struct OwnRows {
   __device__ __forceinline__ TileAt at(int i) const { return tile_at<kPagedTile>(i, from0, to0, from1, to1, from2, to2); }
 };
 
-// Fills the cell; returns whether the list of groups is good (without it every sequence's
-// rows are its own).  All tiles and the most of a sequence come with it.
-__device__ __forceinline__ bool fill_cell(const PagedSharedParams &p, Cell &cell, int layer, int head, int b0, int nb,
-                                          int *total) {
+// Inclusive sums over the lanes: within sixteens, then over them.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int dpp_add(int v) {
+  return v + __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xf, false);
+}
+__device__ __forceinline__ int wave_sums(int v) {
+  v = dpp_add<0x111, 0xf>(v);                             // the lane 1, 2, 4, 8 before
+  v = dpp_add<0x112, 0xf>(v);
+  v = dpp_add<0x114, 0xf>(v);
+  v = dpp_add<0x118, 0xf>(v);
+  v = dpp_add<0x142, 0xa>(v);                             // lane 15 to the next sixteen, 31 to the next two
+  return dpp_add<0x143, 0xc>(v);
+}
+
+// Whether the list of groups is good (without it every sequence's rows are its own), all
+// tiles, and the most of a sequence.
+struct CellSum {
+  bool ok;
+  int total, most;
+};
+
+// Fills the cell of up to a wave's sequences, which are the whole batch.  Every wave writes
+// what it reads, the same as the others, so that none has to wait for another.
+__device__ __forceinline__ CellSum fill_small_cell(const PagedSharedParams &p, Cell &cell, int layer, int head, int lane) {
+  const int extra = p.k_new ? 1 : 0;
+  const Asked asked = ask_first(p, layer, head, lane);
+  const bool in = lane < p.c.batch;
+  const int cached = max(0, min(asked.len, p.c.cap)), n = cached + extra;
+  CellSum sum;
+  sum.ok = __all(lane >= p.groups || (asked.from <= asked.to && asked.from >= 0 && asked.to <= p.c.batch &&
+                                      (lane > 0 || asked.from == 0) && (lane + 1 < p.groups || asked.to == p.c.batch)));
+  int rows = 0, start = 0, lead = lane;
+  for (int k = 0; sum.ok && k < p.groups; ++k) {
+    const int from = __builtin_amdgcn_readlane(asked.from, k), to = __builtin_amdgcn_readlane(asked.to, k);
+    const bool here = lane >= from && lane < to;
+    const int least = wave_all(here ? cached : p.c.cap, [](int a, int b) { return min(a, b); });
+    const int most = p.window > 0 ? wave_all(here ? n - p.window : 0, [](int a, int b) { return max(a, b); }) : 0;
+    const int r = max(0, min(__builtin_amdgcn_readlane(asked.shared, k), least));
+    rows = here ? r : rows;
+    start = here ? max(0, min(most, r)) : start;
+    lead = here ? from : lead;
+  }
+  const int tiles = in ? OwnRows(p, n, rows, start).tiles() : 0;
+  const int until = wave_sums(tiles);
+  if (in) {
+    cell.n[lane] = n;
+    cell.rows[lane] = rows;
+    cell.start[lane] = start;
+    cell.lead[lane] = lead;
+    cell.until[lane] = until;
+  }
+  sum.total = __builtin_amdgcn_readlane(until, kWave - 1);
+  sum.most = wave_all(tiles, [](int a, int b) { return max(a, b); });
+  return sum;
+}
+
+// Fills any cell, by all waves together.
+__device__ __forceinline__ CellSum fill_cell(const PagedSharedParams &p, Cell &cell, int layer, int head, int b0, int nb) {
   constexpr int kEach = kSharedCell / (kNW * kWave);
   const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid / kWave;
   const int extra = p.k_new ? 1 : 0;
@@ -568,20 +668,15 @@ __device__ __forceinline__ bool fill_cell(const PagedSharedParams &p, Cell &cell
     most = max(most, tiles[i]);
   }
   // tiles up to each sequence: over the lanes, then the waves
-  int until = sum;
-#pragma unroll
-  for (int m = 1; m < kWave; m <<= 1) {
-    const int other = __shfl_up(until, m, kWave);
-    until += lane >= m ? other : 0;
-  }
+  int until = wave_sums(sum);
   if (lane == kWave - 1) cell.sums[wave] = until;
   if (most > 0) atomicMax(&cell.most, most);
   __syncthreads();
-  *total = 0;
+  int total = 0;
 #pragma unroll
   for (int w = 0; w < kNW; ++w) {
     until += w < wave ? cell.sums[w] : 0;
-    *total += cell.sums[w];
+    total += cell.sums[w];
   }
   until -= sum;
 #pragma unroll
@@ -595,7 +690,7 @@ __device__ __forceinline__ bool fill_cell(const PagedSharedParams &p, Cell &cell
     cell.until[at] = until;
   }
   __syncthreads();
-  return ok;
+  return CellSum{ok, __builtin_amdgcn_readfirstlane(total), __builtin_amdgcn_readfirstlane(cell.most)};
 }
 
 template <typename T, int D>
@@ -613,32 +708,29 @@ __device__ __forceinline__ void attend_own(const PagedSharedParams &p, int id, u
   const int lh = p.by_chunks.of(cid), b0 = p.by_chunks.rest(cid) * kSharedCell;
   const int layer = p.c.by_hkv.of(lh), head = p.c.by_hkv.rest(lh);
   const int nb = min(kSharedCell, p.c.batch - b0);
-  int total;
-  const bool ok = fill_cell(p, cell, layer, head, b0, nb, &total);
-  total = __builtin_amdgcn_readfirstlane(total);
+  const CellSum sum = p.c.batch <= kWave ? fill_small_cell(p, cell, layer, head, lane) : fill_cell(p, cell, layer, head, b0, nb);
   const size_t row0 = (static_cast<size_t>(lh) * p.c.batch + b0) * p.group;       // of the parts
 
   // Even shares, and of no sequence more parts than there are places.
-  const int most = __builtin_amdgcn_readfirstlane(cell.most);
   const int waves = p.cell_wgs * kNW, w = turn_of * kNW + wave;
-  const int share = max(max((total + waves - 1) / waves, (most + p.own_parts - 2) / (p.own_parts - 1)), 1);
+  const int share = max(max((sum.total + waves - 1) / waves, (sum.most + p.own_parts - 2) / (p.own_parts - 1)), 1);
   const auto no_part = [&](int slot, int b, int g) {
     float *ml = p.part_ml + 2 * (static_cast<size_t>(slot) * p.rows + row0 + static_cast<size_t>(b) * p.group + g);
     ml[0] = -INFINITY;
     ml[1] = 0.f;
   };
   if (turn_of == 0) {
-    if (!ok && threadIdx.x == 0) report(p.c.dev_err, kDevBadGroup);
+    if (!sum.ok && threadIdx.x == 0) report(p.c.dev_err, kDevBadGroup);
     // places without a part: of sequences without tiles, and the common ones where there are no groups
     for (int i = threadIdx.x; i < nb * p.group; i += kNW * kWave) {
       const int b = p.by_group.of(i), g = p.by_group.rest(i);
       if (cell.until[b] == (b > 0 ? cell.until[b - 1] : 0))
         for (int k = 0; k < p.own_parts; ++k) no_part(p.splits + k, b, g);
-      if (!ok)
+      if (!sum.ok)
         for (int k = 0; k < p.splits; ++k) no_part(k, b, g);
     }
   }
-  const int x0 = w * share, x1 = min(total, x0 + share);
+  const int x0 = w * share, x1 = min(sum.total, x0 + share);
   const int mine = x1 - x0;                               // tiles of the wave
   if (mine <= 0) return;
   unsigned char *stage = wave < 2 ? (wave == 0 ? a0 : a1) : (wave == 2 ? a2 : a3);
@@ -703,69 +795,93 @@ __device__ __forceinline__ void attend_own(const PagedSharedParams &p, int id, u
           static_cast<const unsigned char *>(pool) + w.at[j / (C::insts / 2)] + j % (C::insts / 2) * (kWave * 16) + lane * 16));
   };
 
-  // The sequence that the wave is at, and its softmax.
-  int seq = -1, n_cache = 0;
-  frag qf[C::qk_steps];
+  // The sequence that the wave is at, its part's number, and its softmax; what the next tile
+  // needs beside its rows (another sequence's queries, the new row) comes with them.
+  struct Uniform {
+    int b, range, row, from, to;
+    bool fresh;                 // the new row is in it
+  };
+  const auto info = [&](int k) {
+    const int from_lane = (k & (kBatch - 1)) * 2, b = __builtin_amdgcn_readlane(here.b, from_lane);
+    Uniform u{b & 0xffff, b >> 16, __builtin_amdgcn_readlane(here.row, from_lane), __builtin_amdgcn_readlane(here.from, from_lane),
+              __builtin_amdgcn_readlane(here.to, from_lane), false};
+    u.fresh = extra && u.range == 2 && u.row + kTile >= u.to;      // a sequence's last tile holds it
+    return u;
+  };
+  // (fp32 has no registers for the next queries beside the present ones and waits for them)
+  constexpr bool kQueriesAhead = sizeof(T) == 2;
+  frag qf[C::qk_steps], q_next[kQueriesAhead ? C::qk_steps : 1];
+  uint4 kfresh, vfresh;
+  const auto unit_of = [&](const Uniform &u) { return static_cast<size_t>(layer * p.c.batch + b0 + u.b) * p.c.hkv + head; };
+  const auto load_queries = [&](auto &to, const Uniform &u) {
+    const T *qrow = reinterpret_cast<const T *>(p.q) + (unit_of(u) * p.group + min(col, p.group - 1)) * D + grp * C::dq;
+#pragma unroll
+    for (int c = 0; c < C::qk_steps; ++c) to[c] = load_frag(qrow + c * C::kpl);
+  };
+  const auto load_more = [&](const Uniform &u, bool queries) {
+    if constexpr (kQueriesAhead) {
+      if (queries) load_queries(q_next, u);
+    }
+    if (u.fresh) {
+      const size_t at = unit_of(u) * C::lanes_per_row + lane % C::lanes_per_row;
+      kfresh = reinterpret_cast<const uint4 *>(p.k_new)[at];
+      vfresh = reinterpret_cast<const uint4 *>(p.v_new)[at];
+    }
+  };
   float m_run, l_run;
   f32x4_t o[C::dtiles];
-  const auto begin = [&](int b) {
-    seq = b;
-    n_cache = __builtin_amdgcn_readfirstlane(cell.n[b]) - extra;
-    const size_t unit = static_cast<size_t>(layer * p.c.batch + b0 + b) * p.c.hkv + head;
-    const T *qrow = reinterpret_cast<const T *>(p.q) + (unit * p.group + col) * D + grp * C::dq;
+  int number = 0;
+  const auto begin = [&](const Uniform &u) {
+    if constexpr (kQueriesAhead) {
 #pragma unroll
-    for (int c = 0; c < C::qk_steps; ++c) qf[c] = col < p.group ? load_frag(qrow + c * C::kpl) : zero_frag(frag{});
+      for (int c = 0; c < C::qk_steps; ++c) qf[c] = q_next[c];
+    } else {
+      load_queries(qf, u);
+    }
     m_run = -INFINITY;
     l_run = 0.f;
 #pragma unroll
     for (int dt = 0; dt < C::dtiles; ++dt) o[dt] = f32x4_t{0.f, 0.f, 0.f, 0.f};
   };
-  const auto finish = [&]() {
-    const int first_tile = seq > 0 ? cell.until[seq - 1] : 0;
-    const int w0 = first_tile / share, k = w - w0;        // the sequence's first wave; the part's number
+  const auto finish = [&](int seq) {
     const float l_tot = group4_sum(l_run);
-    if (col >= p.group) return;
-    const size_t part = static_cast<size_t>(p.splits + k) * p.rows + row0 + static_cast<size_t>(seq) * p.group + col;
-    if (grp == 0) {
-      p.part_ml[2 * part] = m_run;
-      p.part_ml[2 * part + 1] = l_tot;
-      if (k == 0)
-        for (int i = (cell.until[seq] - 1) / share - w0 + 1; i < p.own_parts; ++i) no_part(p.splits + i, seq, col);
-    }
+    if (col < p.group) {
+      const size_t part = static_cast<size_t>(p.splits + number) * p.rows + row0 + static_cast<size_t>(seq) * p.group + col;
+      if (grp == 0) {
+        p.part_ml[2 * part] = m_run;
+        p.part_ml[2 * part + 1] = l_tot;
+      }
 #pragma unroll
-    for (int dt = 0; dt < C::dtiles; ++dt)
-      *reinterpret_cast<float4 *>(p.part_o + part * D + dt * 16 + 4 * grp) =
-          make_float4(o[dt][0], o[dt][1], o[dt][2], o[dt][3]);
+      for (int dt = 0; dt < C::dtiles; ++dt)
+        *reinterpret_cast<float4 *>(p.part_o + part * D + dt * 16 + 4 * grp) =
+            make_float4(o[dt][0], o[dt][1], o[dt][2], o[dt][3]);
+      if (number == 0) {                                  // the places of parts that there are not
+        const int until = cell.until[seq], parts = until <= x1 ? 1 : (until - 1) / share - w + 1;
+        for (int i = parts + grp; i < p.own_parts; i += 4) no_part(p.splits + i, seq, col);
+      }
+    }
+    number = 0;
   };
 
   Rows<T, D> kreg, vreg;
+  Uniform now, then;
   const auto attend = [&](int k) {
-    const int from_lane = (k & (kBatch - 1)) * 2;
-    const int kb = __builtin_amdgcn_readlane(here.row, from_lane), from = __builtin_amdgcn_readlane(here.from, from_lane),
-              to = __builtin_amdgcn_readlane(here.to, from_lane), b = __builtin_amdgcn_readlane(here.b, from_lane);
-    if ((b & 0xffff) != seq) {
-      if (seq >= 0) finish();
-      begin(b & 0xffff);
-    }
-    const bool holds_new = extra && b >> 16 == 2 && kb <= n_cache && n_cache < kb + kTile;
-    const bool whole = kb >= from && kb + kTile <= to && !holds_new;
     const bool more = k + 1 < mine;
     if (((k + 1) & (kBatch - 1)) == 0 && more) turn((k + 1) / kBatch);
-    const Where then = find(k + 1);
-    uint4 kfresh, vfresh;
-    if (holds_new && lane < C::lanes_per_row) {
-      const size_t at = (static_cast<size_t>(layer * p.c.batch + b0 + seq) * p.c.hkv + head) * C::lanes_per_row + lane;
-      kfresh = reinterpret_cast<const uint4 *>(p.k_new)[at];
-      vfresh = reinterpret_cast<const uint4 *>(p.v_new)[at];
-    }
+    const Where place_of = find(k + 1);
+    then = info(k + 1);
+    if (!more) then.b = now.b;
+    const int kb = now.row, from = now.from, to = now.to, n_cache = to - 1;   // of a tile with the new row
+    const bool whole = kb >= from && kb + kTile <= to && !now.fresh;
 #pragma unroll
     for (int j = 0; j < C::insts; ++j) {
       const int r = j * C::rows_per_inst + lane / C::lanes_per_row;
       *reinterpret_cast<u32x4v *>(stage + r * C::k_stride + (lane % C::lanes_per_row) * 16) = kreg[j];
     }
-    if (more) load(kreg, p.c.k, then);
-    if (holds_new && lane < C::lanes_per_row)
+    if (now.fresh && lane < C::lanes_per_row)
       *reinterpret_cast<uint4 *>(stage + (n_cache - kb) * C::k_stride + lane * 16) = kfresh;
+    const uint4 v_row = vfresh;
+    if (more) load(kreg, p.c.k, place_of);
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     f32x4_t s[2];
 #pragma unroll
@@ -792,22 +908,24 @@ __device__ __forceinline__ void attend_own(const PagedSharedParams &p, int id, u
     float top = x[0];
 #pragma unroll
     for (int e = 1; e < 8; ++e) top = fmaxf(top, x[e]);
-    const float m_new = fmaxf(m_run, group4_max(top));
-    const float ref = m_new == -INFINITY ? 0.f : m_new;   // logits of -inf alone have no weight
-    const float alpha = fast_exp2(m_run - ref);
+    top = group4_max(top);
+    if (__any(top > m_run + kSlack)) {                    // as in the common part
+      const float m_new = fmaxf(m_run, top);
+      const float alpha = fast_exp2(m_run - (m_new == -INFINITY ? 0.f : m_new));
+      l_run *= alpha;
+      m_run = m_new;
+#pragma unroll
+      for (int dt = 0; dt < C::dtiles; ++dt) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[dt][e] *= alpha;
+      }
+    }
+    const float ref = m_run == -INFINITY ? 0.f : m_run;   // logits of -inf alone have no weight
     float pv[8];
-    float sum = 0.f;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       pv[e] = fast_exp2(x[e] - ref);
-      sum += pv[e];
-    }
-    l_run = l_run * alpha + sum;
-    m_run = m_new;
-#pragma unroll
-    for (int dt = 0; dt < C::dtiles; ++dt) {
-#pragma unroll
-      for (int e = 0; e < 4; ++e) o[dt][e] *= alpha;
+      l_run += pv[e];
     }
     if (!whole) {                                         // a NaN that is not seen, times 0, would be NaN
 #pragma unroll
@@ -824,11 +942,14 @@ __device__ __forceinline__ void attend_own(const PagedSharedParams &p, int id, u
       dst[0] = make_uint2(vreg[j][0], vreg[j][1]);
       dst[1] = make_uint2(vreg[j][2], vreg[j][3]);
     }
-    if (more) load(vreg, p.c.v, then);
-    if (holds_new && lane < C::lanes_per_row) {
+    if (now.fresh && lane < C::lanes_per_row) {
       uint2 *dst = reinterpret_cast<uint2 *>(stage + (n_cache - kb) * C::v_stride + lane * 16);
-      dst[0] = make_uint2(vfresh.x, vfresh.y);
-      dst[1] = make_uint2(vfresh.z, vfresh.w);
+      dst[0] = make_uint2(v_row.x, v_row.y);
+      dst[1] = make_uint2(v_row.z, v_row.w);
+    }
+    if (more) {
+      load(vreg, p.c.v, place_of);
+      load_more(then, then.b != now.b);
     }
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
 #pragma unroll
@@ -843,8 +964,19 @@ __device__ __forceinline__ void attend_own(const PagedSharedParams &p, int id, u
   const Where first = find(0);
   load(kreg, p.c.k, first);
   load(vreg, p.c.v, first);
-  for (int k = 0; k < mine; ++k) attend(k);
-  finish();
+  now = info(0);
+  load_more(now, true);
+  number = w - (now.b > 0 ? __builtin_amdgcn_readfirstlane(cell.until[now.b - 1]) : 0) / share;   // waves before that had some of it
+  begin(now);
+  for (int k = 0; k < mine; ++k) {
+    attend(k);
+    if (then.b != now.b) {
+      finish(now.b);
+      begin(then);
+    }
+    now = then;
+  }
+  finish(now.b);
   if (worst >= static_cast<unsigned>(p.c.n_pages)) report(p.c.dev_err, kDevBadPage);
 }
 
@@ -870,7 +1002,7 @@ __global__ __launch_bounds__(kNW * kWave, 2) void shared_attn_kernel(PagedShared
     if (!common) slot -= p.common_wgs / kXcds - kMix * turns;
   }
   const int id = slot * kXcds + xcd;
-  if (common) attend_common<T, D>(p, id, a0, a1, a2, a3);
+  if (common) attend_common<T, D>(p, id, a0, a1, a2, a3, cell.n);
   else if (id < p.own_items) attend_own<T, D>(p, id, a0, a1, a2, a3, cell);
 }
 
