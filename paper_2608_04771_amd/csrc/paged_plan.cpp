@@ -168,11 +168,12 @@ int shared_span_rows(int capacity, int sinks, int window) {
   return static_cast<int>(seen < capacity ? seen : capacity);
 }
 
-// A workgroup for every compute unit shares the common rows of `jobs` (layers and KV heads);
+// A workgroup for every compute unit, up to two, shares the common rows of `jobs` (layers and KV heads);
 // a split keeps 256 rows of what a call may see, of fp32, whose products take sixteen times
 // as long, a tile.
 int shared_splits(int jobs, int blocks, int span_rows, int dtype, int compute_units) {
-  int64_t splits = compute_units / (static_cast<int64_t>(jobs) * blocks);
+  const int64_t each = static_cast<int64_t>(jobs) * blocks;
+  int64_t splits = (compute_units + each - 1) / each;
   const int least = dtype == 0 ? prefill_tile_rows(0) : 256;
   if (splits > span_rows / least) splits = span_rows / least;
   if (splits > kSharedMaxSplits) splits = kSharedMaxSplits;

@@ -558,38 +558,75 @@ struct CellSum {
   int total, most;
 };
 
-// Fills the cell of up to a wave's sequences, which are the whole batch.  Every wave writes
-// what it reads, the same as the others, so that none has to wait for another.
-__device__ __forceinline__ CellSum fill_small_cell(const PagedSharedParams &p, Cell &cell, int layer, int head, int lane) {
-  const int extra = p.k_new ? 1 : 0;
-  const Asked asked = ask_first(p, layer, head, lane);
-  const bool in = lane < p.c.batch;
-  const int cached = max(0, min(asked.len, p.c.cap)), n = cached + extra;
+// Fills the cell that is the whole batch, in few groups.  Every wave writes what it reads,
+// the same as the others, so that none has to wait for another: 1.4 us, by all waves
+// together 5 us, but the groups take their turns here (some 100 cycles each).
+__device__ __forceinline__ CellSum fill_whole_cell(const PagedSharedParams &p, Cell &cell, int layer, int head, int lane) {
+  constexpr int kEach = kSharedCell / kWave;
+  const int extra = p.k_new ? 1 : 0, per = (p.c.batch + kWave - 1) / kWave;      // sequences of a lane, neighbours
+  Asked asked;
+  asked.from = p.first[min(lane, p.groups)];
+  asked.to = p.first[min(lane + 1, p.groups)];
+  asked.shared = p.shared[layer * p.shared_stride + min(lane, p.groups - 1)];
+  int cached[kEach], rows[kEach], start[kEach], lead[kEach], tiles[kEach];
+#pragma unroll
+  for (int j = 0; j < kEach; ++j) cached[j] = j < per ? ask_len(p, layer, head, min(lane * per + j, p.c.batch - 1)) : 0;
   CellSum sum;
   sum.ok = __all(lane >= p.groups || (asked.from <= asked.to && asked.from >= 0 && asked.to <= p.c.batch &&
                                       (lane > 0 || asked.from == 0) && (lane + 1 < p.groups || asked.to == p.c.batch)));
-  int rows = 0, start = 0, lead = lane;
+#pragma unroll
+  for (int j = 0; j < kEach; ++j) {
+    cached[j] = max(0, min(cached[j], p.c.cap));
+    rows[j] = start[j] = 0;
+    lead[j] = lane * per + j;
+  }
   for (int k = 0; sum.ok && k < p.groups; ++k) {
     const int from = __builtin_amdgcn_readlane(asked.from, k), to = __builtin_amdgcn_readlane(asked.to, k);
-    const bool here = lane >= from && lane < to;
-    const int least = wave_all(here ? cached : p.c.cap, [](int a, int b) { return min(a, b); });
-    const int most = p.window > 0 ? wave_all(here ? n - p.window : 0, [](int a, int b) { return max(a, b); }) : 0;
+    int least = p.c.cap, most = 0;
+#pragma unroll
+    for (int j = 0; j < kEach; ++j) {
+      const int b = lane * per + j;
+      if (j < per && b >= from && b < to) {
+        least = min(least, cached[j]);
+        most = max(most, cached[j] + extra - p.window);
+      }
+    }
+    least = wave_all(least, [](int a, int b) { return min(a, b); });
+    if (p.window > 0) most = wave_all(most, [](int a, int b) { return max(a, b); });
     const int r = max(0, min(__builtin_amdgcn_readlane(asked.shared, k), least));
-    rows = here ? r : rows;
-    start = here ? max(0, min(most, r)) : start;
-    lead = here ? from : lead;
+#pragma unroll
+    for (int j = 0; j < kEach; ++j) {
+      const int b = lane * per + j;
+      const bool here = b >= from && b < to;
+      rows[j] = here ? r : rows[j];
+      start[j] = here && p.window > 0 ? max(0, min(most, r)) : start[j];
+      lead[j] = here ? from : lead[j];
+    }
   }
-  const int tiles = in ? OwnRows(p, n, rows, start).tiles() : 0;
-  const int until = wave_sums(tiles);
-  if (in) {
-    cell.n[lane] = n;
-    cell.rows[lane] = rows;
-    cell.start[lane] = start;
-    cell.lead[lane] = lead;
-    cell.until[lane] = until;
+  int all = 0, most = 0;
+#pragma unroll
+  for (int j = 0; j < kEach; ++j) {
+    tiles[j] = j < per && lane * per + j < p.c.batch ? OwnRows(p, cached[j] + extra, rows[j], start[j]).tiles() : 0;
+    all += tiles[j];
+    most = max(most, tiles[j]);
   }
+  int until = wave_sums(all);
   sum.total = __builtin_amdgcn_readlane(until, kWave - 1);
-  sum.most = wave_all(tiles, [](int a, int b) { return max(a, b); });
+  sum.most = wave_all(most, [](int a, int b) { return max(a, b); });
+  until -= all;
+#pragma unroll
+  for (int j = 0; j < kEach; ++j) {
+    const int b = lane * per + j;
+    if (j >= per) break;
+    until += tiles[j];
+    if (b < p.c.batch) {
+      cell.n[b] = cached[j] + extra;
+      cell.rows[b] = rows[j];
+      cell.start[b] = start[j];
+      cell.lead[b] = lead[j];
+      cell.until[b] = until;
+    }
+  }
   return sum;
 }
 
@@ -708,7 +745,8 @@ __device__ __forceinline__ void attend_own(const PagedSharedParams &p, int id, u
   const int lh = p.by_chunks.of(cid), b0 = p.by_chunks.rest(cid) * kSharedCell;
   const int layer = p.c.by_hkv.of(lh), head = p.c.by_hkv.rest(lh);
   const int nb = min(kSharedCell, p.c.batch - b0);
-  const CellSum sum = p.c.batch <= kWave ? fill_small_cell(p, cell, layer, head, lane) : fill_cell(p, cell, layer, head, b0, nb);
+  const CellSum sum = p.c.batch <= kSharedCell && p.groups <= 16 ? fill_whole_cell(p, cell, layer, head, lane)
+                                                                 : fill_cell(p, cell, layer, head, b0, nb);
   const size_t row0 = (static_cast<size_t>(lh) * p.c.batch + b0) * p.group;       // of the parts
 
   // Even shares, and of no sequence more parts than there are places.
@@ -1011,6 +1049,21 @@ __global__ __launch_bounds__(kNW * kWave, 2) void shared_attn_kernel(PagedShared
 // commits the append.
 constexpr int kJoinThreads = 256;
 
+// f over each 16 or 32 lanes, in every lane.
+template <int LANES, typename F>
+__device__ __forceinline__ float lanes_fold(float v, F f) {
+  static_assert(LANES == 16 || LANES == 32, "a row's lanes");
+  v = f(v, dpp<kDppXor1>(v));
+  v = f(v, dpp<kDppXor2>(v));
+  v = f(v, dpp<kDppHalfMirror>(v));
+  v = f(v, dpp<kDppMirror>(v));
+  if (LANES == 32) {
+    const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = f(__uint_as_float(a[0]), __uint_as_float(a[1]));
+  }
+  return v;
+}
+
 template <typename T, int D, int kSub>
 __global__ __launch_bounds__(kJoinThreads) void shared_join_kernel(PagedSharedParams p) {
   constexpr int kLanes = D / 4, kEach = kLanes * kSub, kPer = kJoinThreads / kEach;   // rows of a workgroup
@@ -1046,8 +1099,7 @@ __global__ __launch_bounds__(kJoinThreads) void shared_join_kernel(PagedSharedPa
       l[i] = ml.y;
       M = fmaxf(M, m[i]);
     }
-#pragma unroll
-    for (int d = 1; d < kLanes; d <<= 1) M = fmaxf(M, shfl_xor(M, d));
+    M = lanes_fold<kLanes>(M, [](float a, float b) { return fmaxf(a, b); });
     const float ref = M == -INFINITY ? 0.f : M;
 #pragma unroll
     for (int i = 0; i < kTurns; ++i) {
@@ -1056,8 +1108,7 @@ __global__ __launch_bounds__(kJoinThreads) void shared_join_kernel(PagedSharedPa
       // a part without rows has no output
       if (sub == 0 && lane + i * kLanes < kSharedMaxParts) s_w[in][lane + i * kLanes] = l[i] == 0.f ? 0.f : m[i];
     }
-#pragma unroll
-    for (int d = 1; d < kLanes; d <<= 1) L += shfl_xor(L, d);
+    L = lanes_fold<kLanes>(L, [](float a, float b) { return a + b; });
   }
   __syncthreads();
   const float inv = L == 0.f ? 0.f : 1.f / L;
