@@ -692,7 +692,7 @@ class PreparedPagedSharedDecode:
         self.cache, self.out, self.lse = cache, out, lse
         self._keep = (first, shared, ws, dev_err)
         self._fn = load_library().reco_paged_shared_decode_attn
-        self._dev, self._dt = cache.k.device, cache.k.dtype
+        self._dev, self._dt, self._index = cache.k.device, cache.k.dtype, cache.k.get_device()
         self._q_shape, self._kv_shape = (nl, Bsz, hq, D), (nl, Bsz, H, D)
         scale = 1.0 / math.sqrt(D) if scale is None else float(scale)
         self._head = (cache.ref(), layer0, nl)
@@ -700,7 +700,7 @@ class PreparedPagedSharedDecode:
         self._tail = (_ptr(out), _ptr(lse), _ptr(ws), _nbytes(ws), _ptr(dev_err))
 
     def _check_t(self, t: torch.Tensor, what: str, shape):
-        if tuple(t.shape) != shape or t.dtype != self._dt or t.device != self._dev or not t.is_contiguous():
+        if t.shape != shape or t.dtype != self._dt or t.get_device() != self._index or not t.is_contiguous():
             raise ValueError(f"{what} must be a contiguous {_DT[self._dt]} {list(shape)} tensor on {self._dev}")
 
     def __call__(self, q: torch.Tensor, k_new: Optional[torch.Tensor] = None, v_new: Optional[torch.Tensor] = None):
@@ -710,8 +710,8 @@ class PreparedPagedSharedDecode:
         if k_new is not None:
             self._check_t(k_new, "k_new", self._kv_shape)
             self._check_t(v_new, "v_new", self._kv_shape)
-        with _on(q):
-            st = self._fn(*self._head, _ptr(q), *self._mid, _ptr(k_new), _ptr(v_new), *self._tail, _stream(self._dev))
+        st = _launch(self._index, self._fn, *self._head, q.data_ptr(), *self._mid, None if k_new is None else k_new.data_ptr(),
+                     None if v_new is None else v_new.data_ptr(), *self._tail)
         if st != RECO_OK:
             _check(st, "reco_paged_shared_decode_attn")
         return self.out, self.lse
@@ -841,39 +841,55 @@ class _Rows:
     """A tensor's rows as the C ABI takes them: [n_layers][B][heads][T][D], or without T
     for one token, in any order of memory whose rows are contiguous and 16-byte aligned."""
 
-    __slots__ = ("shape", "dtype", "device", "what", "struct", "_strides", "_piece", "_token", "_write")
+    __slots__ = ("what", "shape", "dtype", "index", "struct", "ref", "_strides", "_piece", "_write")
 
     def __init__(self, what: str, shape, dtype: torch.dtype, device, write: bool = False):
-        self.what, self.shape, self.dtype, self.device, self._write = what, tuple(shape), dtype, device, write
-        self._token = len(self.shape) == 4
+        self.what, self.shape, self.dtype, self._write = what, tuple(shape), dtype, write
+        self.index = device.index if device.type == "cuda" else -1
         self._piece = 4 if dtype == torch.float32 else 8
         self._strides = None
         self.struct = RecoRows()
+        self.ref = ctypes.byref(self.struct)
 
     def take(self, t: torch.Tensor):
-        if tuple(t.shape) != self.shape or t.dtype != self.dtype or t.device != self.device:
-            raise ValueError(f"{self.what} must be {_DT.get(self.dtype, self.dtype)} {list(self.shape)} on {self.device}, "
+        if t.shape != self.shape or t.dtype != self.dtype or t.get_device() != self.index:
+            raise ValueError(f"{self.what} must be {_DT.get(self.dtype, self.dtype)} {list(self.shape)} on GPU {self.index}, "
                              f"got {_DT.get(t.dtype, t.dtype)} {list(t.shape)} on {t.device}")
         st = t.stride()
         if st != self._strides:
-            if st[-1] != 1 or any(n > 1 and x % self._piece for n, x in zip(self.shape[:-1], st[:-1])):
-                raise ValueError(f"{self.what}: rows must be contiguous and multiples of 16 bytes apart")
-            st4 = [x if n > 1 else 0 for n, x in zip(self.shape[:-1], st[:-1])]      # those of one are not used
-            if self._write:
-                end = self.shape[-1]
-                for x, n in sorted((x, n) for n, x in zip(self.shape[:-1], st4) if n > 1):
-                    if x < end:
-                        raise ValueError(f"{self.what}: rows must not overlap")
-                    end = x * (n - 1) + end
-            s = self.struct
-            s.layer, s.seq, s.head = st4[:3]
-            s.token = 0 if self._token else st4[3]
-            self._strides = st
+            self._take_strides(st)
         p = t.data_ptr()
         if p & 15:
             raise ValueError(f"{self.what} must be 16-byte aligned")
         self.struct.data = p
-        return ctypes.byref(self.struct)
+        return self.ref
+
+    def _take_strides(self, st):
+        if st[-1] != 1 or any(n > 1 and x % self._piece for n, x in zip(self.shape[:-1], st[:-1])):
+            raise ValueError(f"{self.what}: rows must be contiguous and multiples of 16 bytes apart")
+        used = [x if n > 1 else 0 for n, x in zip(self.shape[:-1], st[:-1])]      # those of one are not used
+        if self._write:
+            end = self.shape[-1]
+            for x, n in sorted((x, n) for n, x in zip(self.shape[:-1], used) if n > 1):
+                if x < end:
+                    raise ValueError(f"{self.what}: rows must not overlap")
+                end = x * (n - 1) + end
+        s = self.struct
+        s.layer, s.seq, s.head = used[:3]
+        s.token = used[3] if len(used) == 4 else 0
+        self._strides = st
+
+
+def _launch(index: int, fn, *args) -> int:
+    """fn's status, with its GPU as the current one and that one's stream behind the arguments."""
+    if torch.cuda.current_device() == index:
+        return fn(*args, _stream_of(index))
+    with torch.cuda.device(index):
+        return fn(*args, _stream_of(index))
+
+
+def _stream_of(index: int) -> int:
+    return _raw_stream(index) if _raw_stream is not None else torch.cuda.current_stream(index).cuda_stream
 
 
 def _no_partial_overlap(x: torch.Tensor, out: torch.Tensor, what: str):
@@ -912,9 +928,9 @@ class PreparedRope:
         self.out = out
         self._keep = (rope, pos, n_new, dev_err)
         self._fn = load_library().reco_rope
-        self._dev = out.device
         self._struct = rope._struct(pos)
         self._in = _Rows("x", out.shape, out.dtype, out.device)
+        self._checked = None
         self._head = ctypes.byref(self._struct)
         self._out = _Rows("out", out.shape, out.dtype, out.device, write=True).take(out)
         self._tail = (NL, Bsz, H, T, D, RECO_F32 if out.dtype == torch.float32 else RECO_BF16, _ptr(n_new),
@@ -922,9 +938,10 @@ class PreparedRope:
 
     def __call__(self, x: torch.Tensor) -> torch.Tensor:
         xr = self._in.take(x)
-        _no_partial_overlap(x, self.out, "out")
-        with _on(x):
-            st = self._fn(self._head, xr, self._out, *self._tail, _stream(self._dev))
+        if self._checked != (x.data_ptr(), self._in._strides):
+            _no_partial_overlap(x, self.out, "out")
+            self._checked = x.data_ptr(), self._in._strides
+        st = _launch(self._in.index, self._fn, self._head, xr, self._out, *self._tail)
         if st != RECO_OK:
             _check(st, "reco_rope")
         return self.out
@@ -976,7 +993,7 @@ class PreparedPagedAppend:
         self.cache, self.q_out = cache, q_out
         self._keep = (rope, pos, n_new, dev_err)
         self._fn = load_library().reco_paged_append
-        self._dev = dev
+        self._checked = None
         self._k, self._v = (_Rows(what, (nl, Bsz, H, *run, D), dt, dev) for what in ("k_new", "v_new"))
         self._q = self._qo = None
         if q_out is not None:
@@ -994,9 +1011,10 @@ class PreparedPagedAppend:
         qr = None
         if q is not None:
             qr = self._q.take(q)
-            _no_partial_overlap(q, self.q_out, "q_out")
-        with _on(k_new):
-            st = self._fn(*self._head, k, v, qr, self._qo, *self._tail, _stream(self._dev))
+            if self._checked != (q.data_ptr(), self._q._strides):
+                _no_partial_overlap(q, self.q_out, "q_out")
+                self._checked = q.data_ptr(), self._q._strides
+        st = _launch(self._k.index, self._fn, *self._head, k, v, qr, self._qo, *self._tail)
         if st != RECO_OK:
             _check(st, "reco_paged_append")
         return self.q_out

@@ -112,7 +112,6 @@ reco_status_t rope_params(reco::RopeParams &p, const reco_rope_t *rope, int32_t 
     for (int i = 0; rope->axis && i < rope->rot_dim / 2; ++i)
       p.axis[i / 32] |= static_cast<uint64_t>(rope->axis[i]) << (2 * (i % 32));
   }
-  p.block = reco::rope_block(n_tokens);
   p.n_new = n_new;
   p.dev_err = dev_err;
   p.layers = n_layers;
@@ -138,6 +137,7 @@ reco_status_t reco_rope(const reco_rope_t *rope, const reco_rows_t *x, const rec
   p.q = rows_of(x);
   p.q_out = rows_of(out);
   p.heads = n_heads;
+  reco::rope_plan(p, head_dim * elem);
   return reco::hip_status(reco::launch_rope(p, dtype, head_dim, stream));
 }
 
@@ -168,6 +168,7 @@ reco_status_t reco_paged_append(const reco_paged_cache_t *cache, int32_t layer0,
     p.q_out = rows_of(q_out);
     p.heads = n_q_heads;
   }
+  reco::rope_plan(p, row_bytes_of(cache));
   return reco::hip_status(reco::launch_rope(p, cache->dtype, cache->head_dim, stream));
 }
 

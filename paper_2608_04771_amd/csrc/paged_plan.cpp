@@ -219,11 +219,18 @@ bool paged_shared_fits_grid(const PagedSharedParams &p) {
          sequences * (p.c.cap / kPagedTile + 4) < (int64_t{1} << 31);
 }
 
-// A run of up to eight tokens is one workgroup's, which then sets the lengths itself.
-int rope_block(int tokens) {
-  int block = 1;
-  while (block < tokens && block < kRopeMaxBlock) block *= 2;
-  return block;
+// An appended run of up to eight tokens is one workgroup's, which then sets the lengths itself
+// and is as wide as one can be (5 tokens of 4 sequences, 32 layers of 48 rows: 16.0 us with
+// 256 threads, 12 with 1,024); other runs go by fours.  Rows that the kernel before has left
+// are in the last cache, and what is made of them fits beside them, unless they are many
+// (36 heads, past the caches and through them: 2,848 tokens 15.6 and 12.0 us, 8,192 27.1 and
+// 26.0, 12,000 36.1 and 42.1).
+void rope_plan(RopeParams &p, int row_bytes) {
+  const int most = p.c.k && p.tokens <= kRopeMaxBlock ? kRopeMaxBlock : kRopeBlock;
+  p.block = 1;
+  while (p.block < p.tokens && p.block < most) p.block *= 2;
+  const int64_t rows = static_cast<int64_t>(p.layers) * p.batch * p.tokens * (p.heads + (p.c.k ? 2 * p.c.hkv : 0));
+  p.far = rows * row_bytes > (int64_t{64} << 20);
 }
 
 static int64_t evict_state_pitch(int capacity, int row_bytes) {

@@ -18,8 +18,10 @@ struct RowsOf {
 };
 
 constexpr int kRopeThreads = 256;
+constexpr int kRopeWide = 1024;      // of a workgroup that has a sequence's whole run
 constexpr int kRopeMaxAxes = 4;      // two bits a pair
-constexpr int kRopeMaxBlock = 8;     // tokens of a workgroup
+constexpr int kRopeBlock = 4;        // tokens of a workgroup
+constexpr int kRopeMaxBlock = 8;     // of one that has a whole run
 
 struct RopeParams {
   const float *freq;      // [rot / 2]
@@ -35,9 +37,11 @@ struct RopeParams {
   int32_t *dev_err;
   int heads, layers, batch, tokens;
   int block;              // tokens of a workgroup, a power of two
+  bool far;               // the rows are not in a cache
 };
 
-int rope_block(int tokens);
+// Sets block and far; the rows' numbers are set.
+void rope_plan(RopeParams &p, int row_bytes);
 hipError_t launch_rope(const RopeParams &p, int dtype, int head_dim, hipStream_t s);
 
 }  // namespace reco

@@ -16,11 +16,11 @@ namespace reco {
 
 namespace {
 
-template <typename T, int D>
+template <typename T, int D, int THREADS>
 struct Cfg {
   static constexpr int vec = 16 / (int)sizeof(T);        // elements of a load, pairs of a thread
   static constexpr int per_row = D / (2 * vec);          // threads of a row
-  static constexpr int rows = kRopeThreads / per_row;    // of a turn of the workgroup
+  static constexpr int rows = THREADS / per_row;         // of a turn of the workgroup
 };
 
 template <typename T>
@@ -31,6 +31,13 @@ template <typename T>
 __device__ __forceinline__ Vec<T> unpack(u32x4v w) { return __builtin_bit_cast(Vec<T>, w); }
 template <typename T>
 __device__ __forceinline__ u32x4v pack(const Vec<T> &v) { return __builtin_bit_cast(u32x4v, v); }
+
+template <typename T>
+__device__ __forceinline__ void turn_pair(T x, T y, float2 turn, T &u, T &w) {
+  const float g = to_f32(x), o = to_f32(y);
+  u = from_f32<T>(g * turn.x - o * turn.y);
+  w = from_f32<T>(g * turn.y + o * turn.x);
+}
 
 // Real tokens of a sequence; a bad count is none.
 __device__ __forceinline__ int new_tokens(const RopeParams &p, int b, bool &bad) {
@@ -46,9 +53,9 @@ __device__ __forceinline__ int append_code(const PagedCache &c, int L, int n, bo
   return bad_page && n > 0 ? kDevBadPage : 0;
 }
 
-template <typename T, int D, bool kAppend>
-__global__ __launch_bounds__(kRopeThreads) void rope_kernel(RopeParams p) {
-  using C = Cfg<T, D>;
+template <typename T, int D, bool kAppend, int THREADS, bool kFar>
+__global__ __launch_bounds__(THREADS) void rope_kernel(RopeParams p) {
+  using C = Cfg<T, D, THREADS>;
   __shared__ __attribute__((aligned(16))) float2 s_turn[kRopeMaxBlock][D / 2];
   extern __shared__ __attribute__((aligned(16))) int64_t s_to[];     // [hkv][block]  element of the pool, or -1
   const int tid = threadIdx.x;
@@ -66,9 +73,13 @@ __global__ __launch_bounds__(kRopeThreads) void rope_kernel(RopeParams p) {
   const int at_t = slot & (p.block - 1);
   const int t = t0 + at_t;
   const int step = C::rows / p.block;                     // heads of a turn
-  const bool turns = sub * 2 * C::vec < p.rot;
-  const int e0 = turns && !p.pairs ? sub * C::vec : sub * 2 * C::vec;
-  const int e1 = turns && !p.pairs ? e0 + p.rot / 2 : e0 + C::vec;
+  // Two pieces of the row, of neighbouring threads beside each other: of halves the two ends
+  // of the same pairs, or two of what passes; of neighbouring pairs any two.
+  const int half = p.pairs ? D / 2 : p.rot / 2;
+  const bool low = sub * C::vec < half;
+  const int e0 = low ? sub * C::vec : p.rot + sub * C::vec - half;
+  const int e1 = low ? half + e0 : e0 + (D - p.rot) / 2;
+  const bool turns0 = e0 < p.rot, turns1 = e1 < p.rot;
   const int rows = p.heads + (kAppend ? 2 * p.c.hkv : 0);
   const bool real = t < n;
 
@@ -85,23 +96,26 @@ __global__ __launch_bounds__(kRopeThreads) void rope_kernel(RopeParams p) {
     }
     return q + r * p.q.head;
   };
-  constexpr int kAhead = 4;
-  u32x4v lo[kAhead], hi[kAhead];
-  const auto load = [&](int r0) {
+  // One row of a thread comes while another goes.  More of them on their way made long runs
+  // slower (16,384 tokens of 36 heads: 71 us by ones, 80 by twos, 82 by fours without turns).
+  constexpr int kAhead = 1;
+  u32x4v lo_a[kAhead], hi_a[kAhead], lo_b[kAhead], hi_b[kAhead];
+  const auto load = [&](int r0, u32x4v (&lo)[kAhead], u32x4v (&hi)[kAhead]) {
 #pragma unroll
     for (int i = 0; i < kAhead; ++i) {
       const int r = r0 + i * step;
       if (real && r < rows) {
         const T *src = source(r);
-        lo[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4v *>(src + e0));
-        hi[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4v *>(src + e1));
+        const u32x4v *x = reinterpret_cast<const u32x4v *>(src + e0), *y = reinterpret_cast<const u32x4v *>(src + e1);
+        lo[i] = kFar ? __builtin_nontemporal_load(x) : *x;
+        hi[i] = kFar ? __builtin_nontemporal_load(y) : *y;
       }
     }
   };
   const int first = slot / p.block;
-  load(first);
+  load(first, lo_a, hi_a);
 
-  for (int i = tid; i < p.block * (p.rot / 2); i += kRopeThreads) {
+  for (int i = tid; i < p.block * (p.rot / 2); i += THREADS) {
     const int pair = i % (p.rot / 2), tt = i / (p.rot / 2);
     if (t0 + tt >= n) break;
     const int axis = static_cast<int>(p.axis[pair / 32] >> (2 * (pair % 32))) & 3;
@@ -114,7 +128,7 @@ __global__ __launch_bounds__(kRopeThreads) void rope_kernel(RopeParams p) {
   }
   if (kAppend) {
     const int shift = p.c.page_shift;
-    for (int i = tid; i < p.c.hkv * p.block; i += kRopeThreads) {
+    for (int i = tid; i < p.c.hkv * p.block; i += THREADS) {
       const int tt = i & (p.block - 1), h = i / p.block;
       const size_t cunit = p.c.unit((l * p.batch + b) * p.c.hkv + h);
       const int L = p.c.len[cunit], row = L + t0 + tt;
@@ -130,7 +144,7 @@ __global__ __launch_bounds__(kRopeThreads) void rope_kernel(RopeParams p) {
   }
   __syncthreads();
   if (kAppend && all) {
-    for (int h = tid; h < p.c.hkv; h += kRopeThreads) {
+    for (int h = tid; h < p.c.hkv; h += THREADS) {
       const size_t cunit = p.c.unit((l * p.batch + b) * p.c.hkv + h);
       const int L = p.c.len[cunit];
       bool bad_page = false;
@@ -140,24 +154,28 @@ __global__ __launch_bounds__(kRopeThreads) void rope_kernel(RopeParams p) {
       else if (n > 0) p.c.len[cunit] = L + n;
     }
   }
+  // The angles of this thread's pairs; with neighbouring pairs half of them are its second piece's.
   float2 turn[C::vec];
 #pragma unroll
-  for (int j = 0; j < C::vec; ++j) turn[j] = turns && real ? s_turn[at_t][sub * C::vec + j] : make_float2(1.f, 0.f);
+  for (int j = 0; j < C::vec; ++j) {
+    const int pair = !p.pairs ? e0 + j : j < C::vec / 2 ? e0 / 2 + j : e1 / 2 + j - C::vec / 2;
+    turn[j] = s_turn[at_t][min(pair, D / 2 - 1)];
+  }
 
-  for (int r0 = first; r0 < rows; r0 += kAhead * step) {
+  const auto put = [&](int r0, const u32x4v (&lo)[kAhead], const u32x4v (&hi)[kAhead]) {
 #pragma unroll
     for (int i = 0; i < kAhead; ++i) {
       const int r = r0 + i * step;
       if (!real || r >= rows) break;
       const int h = r - p.heads;
       T *dst;
-      bool turned = turns;
+      bool turned = true;
       if (kAppend && h >= 0) {
         const bool key = h < p.c.hkv;
         const int64_t to = s_to[(key ? h : h - p.c.hkv) * p.block + at_t];
         if (to < 0) continue;
         dst = static_cast<T *>(key ? p.c.k : p.c.v) + to;
-        turned = turned && key;
+        turned = key;
       } else {
         dst = p.q_out.at<T>(l, b, t) + r * p.q_out.head;
       }
@@ -167,35 +185,34 @@ __global__ __launch_bounds__(kRopeThreads) void rope_kernel(RopeParams p) {
         Vec<T> u, w;
         if (p.pairs) {
 #pragma unroll
-          for (int j = 0; j < C::vec; ++j) {              // pair j: elements 2 j and 2 j + 1 of the two loads
-            const Vec<T> &from = j < C::vec / 2 ? x : y;
-            Vec<T> &to = j < C::vec / 2 ? u : w;
-            const int e = 2 * j % C::vec;
-            const float g = to_f32(from.x[e]), o = to_f32(from.x[e + 1]);
-            to.x[e] = from_f32<T>(g * turn[j].x - o * turn[j].y);
-            to.x[e + 1] = from_f32<T>(g * turn[j].y + o * turn[j].x);
+          for (int j = 0; j < C::vec / 2; ++j) {
+            turn_pair(x.x[2 * j], x.x[2 * j + 1], turn[j], u.x[2 * j], u.x[2 * j + 1]);
+            turn_pair(y.x[2 * j], y.x[2 * j + 1], turn[C::vec / 2 + j], w.x[2 * j], w.x[2 * j + 1]);
           }
         } else {
 #pragma unroll
-          for (int j = 0; j < C::vec; ++j) {
-            const float g = to_f32(x.x[j]), o = to_f32(y.x[j]);
-            u.x[j] = from_f32<T>(g * turn[j].x - o * turn[j].y);
-            w.x[j] = from_f32<T>(g * turn[j].y + o * turn[j].x);
-          }
+          for (int j = 0; j < C::vec; ++j) turn_pair(x.x[j], y.x[j], turn[j], u.x[j], w.x[j]);
         }
-        a = pack<T>(u);
-        z = pack<T>(w);
+        a = turns0 ? pack<T>(u) : a;
+        z = turns1 ? pack<T>(w) : z;
       }
       *reinterpret_cast<u32x4v *>(dst + e0) = a;
       *reinterpret_cast<u32x4v *>(dst + e1) = z;
     }
-    load(r0 + kAhead * step);
+  };
+  for (int r0 = first; r0 < rows; r0 += 2 * kAhead * step) {
+    load(r0 + kAhead * step, lo_b, hi_b);
+    put(r0, lo_a, hi_a);
+    load(r0 + 2 * kAhead * step, lo_a, hi_a);
+    put(r0 + kAhead * step, lo_b, hi_b);
   }
 }
 
 // The lengths after a run of more tokens than a workgroup's, whose rows the other kernel
 // has put where their pages are good.
-__global__ __launch_bounds__(kWave) void rope_len_kernel(RopeParams p) {
+constexpr int kRopeLenThreads = 256;
+
+__global__ __launch_bounds__(kRopeLenThreads) void rope_len_kernel(RopeParams p) {
   const int unit = blockIdx.x;
   const size_t cunit = p.c.unit(unit);
   bool bad;
@@ -203,28 +220,38 @@ __global__ __launch_bounds__(kWave) void rope_len_kernel(RopeParams p) {
   bool bad_page = false;
   if (L >= 0 && L <= p.c.cap && n <= p.c.cap - L && n > 0) {
     const int32_t *table = p.c.pages + cunit * static_cast<size_t>(p.c.max_pages);
-    for (int g = (L >> p.c.page_shift) + threadIdx.x; g <= (L + n - 1) >> p.c.page_shift; g += kWave)
+#pragma unroll 4
+    for (int g = (L >> p.c.page_shift) + threadIdx.x; g <= (L + n - 1) >> p.c.page_shift; g += kRopeLenThreads)
       bad_page |= static_cast<unsigned>(table[g]) >= static_cast<unsigned>(p.c.n_pages);
   }
-  bad_page = __any(bad_page);
+  bad_page = __syncthreads_or(bad_page);
   if (threadIdx.x) return;
   const int code = append_code(p.c, L, n, bad_page);
   if (code) report(p.dev_err, code);
   else if (n > 0) p.c.len[cunit] = L + n;
 }
 
+template <typename T, int D, bool kAppend>
+hipError_t launch_rows(const RopeParams &p, hipStream_t s) {
+  const dim3 grid((p.tokens + p.block - 1) / p.block, p.batch, p.layers);
+  const size_t lds = kAppend ? static_cast<size_t>(p.c.hkv) * p.block * sizeof(int64_t) : 0;
+  if constexpr (kAppend) {
+    if (p.tokens <= p.block) {
+      hipLaunchKernelGGL((rope_kernel<T, D, true, kRopeWide, false>), grid, dim3(kRopeWide), lds, s, p);
+      return hipGetLastError();
+    }
+  }
+  if (p.far) hipLaunchKernelGGL((rope_kernel<T, D, kAppend, kRopeThreads, true>), grid, dim3(kRopeThreads), lds, s, p);
+  else hipLaunchKernelGGL((rope_kernel<T, D, kAppend, kRopeThreads, false>), grid, dim3(kRopeThreads), lds, s, p);
+  return hipGetLastError();
+}
+
 template <typename T, int D>
 hipError_t launch_typed(const RopeParams &p, hipStream_t s) {
-  const dim3 grid((p.tokens + p.block - 1) / p.block, p.batch, p.layers);
-  if (!p.c.k) {
-    hipLaunchKernelGGL((rope_kernel<T, D, false>), grid, dim3(kRopeThreads), 0, s, p);
-    return hipGetLastError();
-  }
-  const size_t lds = static_cast<size_t>(p.c.hkv) * p.block * sizeof(int64_t);
-  hipLaunchKernelGGL((rope_kernel<T, D, true>), grid, dim3(kRopeThreads), lds, s, p);
-  const hipError_t e = hipGetLastError();
+  if (!p.c.k) return launch_rows<T, D, false>(p, s);
+  const hipError_t e = launch_rows<T, D, true>(p, s);
   if (e != hipSuccess || p.tokens <= p.block) return e;
-  hipLaunchKernelGGL(rope_len_kernel, dim3(p.layers * p.batch * p.c.hkv), dim3(kWave), 0, s, p);
+  hipLaunchKernelGGL(rope_len_kernel, dim3(p.layers * p.batch * p.c.hkv), dim3(kRopeLenThreads), 0, s, p);
   return hipGetLastError();
 }
 
