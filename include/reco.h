@@ -450,7 +450,8 @@ reco_status_t reco_rope(const reco_rope_t *rope, const reco_rows_t *x, const rec
  * rotated in the same pass.
  *   rope         : nullable: rows are taken as they are
  *   k_new, v_new : rows of n_kv_heads heads, cache dtype
- *   q, q_out     : both NULL or rows of n_q_heads heads, cache dtype; q_out may be q
+ *   q, q_out     : both NULL or rows of n_q_heads heads, cache dtype; q_out may be q,
+ *                  and meets none of the other rows
  * Decode attention without an append (k_new = NULL) then sees the rows.  A unit whose
  * length is bad (RECO_DEV_BAD_LENGTH), whose run does not fit its capacity
  * (RECO_DEV_APPEND_OVERFLOW) or whose rows' page ids are bad (RECO_DEV_BAD_PAGE) keeps

@@ -892,19 +892,43 @@ def _stream_of(index: int) -> int:
     return _raw_stream(index) if _raw_stream is not None else torch.cuda.current_stream(index).cuda_stream
 
 
-def _no_partial_overlap(x: torch.Tensor, out: torch.Tensor, what: str):
-    """``out`` is x itself, or none of its rows meet x's."""
-    def span(t):
-        return t.data_ptr(), t.data_ptr() + t.element_size() * (1 + sum((n - 1) * s for n, s in zip(t.shape, t.stride())))
-    (a, a1), (b, b1) = span(x), span(out)
-    if a1 <= b or b1 <= a or (a == b and x.stride() == out.stride()):
+class _Span:
+    """Where a call's output lies, to tell quickly that an input is elsewhere."""
+
+    __slots__ = ("begin", "end")
+
+    def __init__(self, out: torch.Tensor):
+        self.begin, self.end = _span(out)
+
+    def misses(self, x: torch.Tensor) -> bool:
+        at = x.data_ptr()
+        # of a tensor that starts before the output, its strides say where it ends
+        return at >= self.end or (at < self.begin and _span(x)[1] <= self.begin)
+
+
+def _span(t: torch.Tensor):
+    at = t.data_ptr()
+    return at, at + t.element_size() * (1 + sum((n - 1) * s for n, s in zip(t.shape, t.stride())))
+
+
+def _no_partial_overlap(x: torch.Tensor, out: torch.Tensor, what: str, same: bool = True):
+    """``out`` is x itself (where that is ``same``), or none of its rows meet x's."""
+    (a, a1), (b, b1) = _span(x), _span(out)
+    if a1 <= b or b1 <= a or (same and x.shape == out.shape and a == b and x.stride() == out.stride()):
         return
-    d, e = abs(a - b), x.element_size()
-    heads = x.shape[2] * x.stride(2) * e
-    others = [s * e for i, (n, s) in enumerate(zip(x.shape, x.stride())) if i not in (2, x.dim() - 1) and n > 1]
-    if x.stride() == out.stride() and heads <= d and all(d + heads <= s for s in others):
-        return                                             # other heads of the same tokens
-    raise ValueError(f"{what} must be the same rows as its input or meet none of them")
+    # heads beside each other, of the same tokens
+    d, e, i = b - a, x.element_size(), 2
+    others = [j for j in range(x.dim() - 1) if j != i]
+    if all(x.shape[j] == out.shape[j] and (x.shape[j] == 1 or x.stride(j) == out.stride(j)) for j in others):
+        x1, o1 = (e * ((t.shape[i] - 1) * t.stride(i) + t.shape[-1]) for t in (x, out))
+        low, high = (x1, d + o1) if d >= 0 else (o1, x1 - d)      # the lower one's end, the higher one's from the lower's start
+        nested = low <= abs(d)
+        for st, n in sorted((x.stride(j) * e, x.shape[j]) for j in others if x.shape[j] > 1):
+            nested, high = nested and high <= st, st * (n - 1) + high
+        if nested:
+            return
+    raise ValueError(f"{what} must be the same rows as its input or meet none of them" if same else
+                     f"{what} must not meet k_new or v_new")
 
 
 class PreparedRope:
@@ -930,7 +954,7 @@ class PreparedRope:
         self._fn = load_library().reco_rope
         self._struct = rope._struct(pos)
         self._in = _Rows("x", out.shape, out.dtype, out.device)
-        self._checked = None
+        self._out_span = _Span(out)
         self._head = ctypes.byref(self._struct)
         self._out = _Rows("out", out.shape, out.dtype, out.device, write=True).take(out)
         self._tail = (NL, Bsz, H, T, D, RECO_F32 if out.dtype == torch.float32 else RECO_BF16, _ptr(n_new),
@@ -938,9 +962,8 @@ class PreparedRope:
 
     def __call__(self, x: torch.Tensor) -> torch.Tensor:
         xr = self._in.take(x)
-        if self._checked != (x.data_ptr(), self._in._strides):
+        if not self._out_span.misses(x):
             _no_partial_overlap(x, self.out, "out")
-            self._checked = x.data_ptr(), self._in._strides
         st = _launch(self._in.index, self._fn, self._head, xr, self._out, *self._tail)
         if st != RECO_OK:
             _check(st, "reco_rope")
@@ -993,13 +1016,13 @@ class PreparedPagedAppend:
         self.cache, self.q_out = cache, q_out
         self._keep = (rope, pos, n_new, dev_err)
         self._fn = load_library().reco_paged_append
-        self._checked = None
         self._k, self._v = (_Rows(what, (nl, Bsz, H, *run, D), dt, dev) for what in ("k_new", "v_new"))
         self._q = self._qo = None
         if q_out is not None:
             shape = (nl, Bsz, hq, *run, D)
             self._q = _Rows("q", shape, dt, dev)
             self._qo = _Rows("q_out", shape, dt, dev, write=True).take(q_out)
+            self._out_span = _Span(q_out)
         self._struct = None if rope is None else rope._struct(pos)
         self._head = (cache.ref(), layer0, nl, None if rope is None else ctypes.byref(self._struct), T, _ptr(n_new))
         self._tail = (hq, _ptr(dev_err))
@@ -1011,9 +1034,11 @@ class PreparedPagedAppend:
         qr = None
         if q is not None:
             qr = self._q.take(q)
-            if self._checked != (q.data_ptr(), self._q._strides):
+            if not self._out_span.misses(q):
                 _no_partial_overlap(q, self.q_out, "q_out")
-                self._checked = q.data_ptr(), self._q._strides
+            for x in (k_new, v_new):
+                if not self._out_span.misses(x):
+                    _no_partial_overlap(x, self.q_out, "q_out", same=False)
         st = _launch(self._k.index, self._fn, *self._head, k, v, qr, self._qo, *self._tail)
         if st != RECO_OK:
             _check(st, "reco_paged_append")

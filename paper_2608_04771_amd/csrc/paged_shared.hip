@@ -77,33 +77,46 @@ __device__ __forceinline__ Asked ask_first(const PagedSharedParams &p, int layer
   return a;
 }
 
+// Whether the list of groups ascends from 0 to the batch.
+__device__ __forceinline__ bool groups_ascend(const PagedSharedParams &p, int from0, int to0, int lane) {
+  const auto good = [&](int i, int from, int to) {
+    return i >= p.groups || (from <= to && from >= 0 && to <= p.c.batch && (i > 0 || from == 0) && (i + 1 < p.groups || to == p.c.batch));
+  };
+  bool ok = good(lane, from0, to0);
+#pragma unroll 4
+  for (int i = kWave + lane; i < p.groups; i += kWave) ok = ok & good(i, p.first[i], p.first[i + 1]);
+  return __all(ok);
+}
+
 // One group of sequences [from, to), and its place in the list.
 struct Group {
   int id, from, to;
   int row0;             // of the block that was looked for
-  bool ok;              // the list ascends from 0 to the batch
 };
 
-// The group of block `block` (of kRows query rows each, groups in order); id is -1 where
-// there is none.
+// The group of block `block` (of kRows query rows each, groups in order) of a list that ascends;
+// id is -1 where there is none.  A group's blocks begin where all before it would end, had each
+// kRows - 1 rows more, so that no one has to count them.
 __device__ __forceinline__ Group find_group(const PagedSharedParams &p, const Asked &asked, int block, int lane) {
-  Group g{-1, 0, 0, 0, true};
-  int before = 0;
-  for (int g0 = 0; g0 < p.groups; g0 += kWave) {
-    const int i = g0 + lane;
-    const int from = g0 == 0 ? asked.from : p.first[min(i, p.groups)];
-    const int to = g0 == 0 ? asked.to : p.first[min(i + 1, p.groups)];
-    const bool in = i < p.groups;
-    const bool ok = !in || (from <= to && from >= 0 && to <= p.c.batch && (i > 0 || from == 0) &&
-                            (i + 1 < p.groups || to == p.c.batch));
-    g.ok = g.ok && __all(ok);
-    for (int k = 0; k < min(p.groups - g0, kWave) && g.ok && g.id < 0; ++k) {
-      const int k0 = __builtin_amdgcn_readlane(from, k), k1 = __builtin_amdgcn_readlane(to, k);
-      const int mine = ((k1 - k0) * p.group + kRows - 1) / kRows;
-      if (block < before + mine) g = Group{g0 + k, k0, k1, (block - before) * kRows, true};
-      before += mine;
+  const auto begins = [&](int id, int from) { return (from * p.group + id * (kRows - 1)) / kRows; };
+  Group g;
+  if (p.groups <= kWave) {
+    const uint64_t here = __ballot(lane < p.groups && block >= begins(lane, asked.from) && block < begins(lane + 1, asked.to));
+    if (here == 0) return Group{-1, 0, 0, 0};
+    g.id = __builtin_ctzll(here);
+    g.from = __builtin_amdgcn_readlane(asked.from, g.id);
+    g.to = __builtin_amdgcn_readlane(asked.to, g.id);
+  } else {
+    int low = 0, high = p.groups - 1;                     // the last group that begins here or before
+    while (low < high) {
+      const int mid = (low + high + 1) / 2;
+      if (begins(mid, p.first[mid]) <= block) low = mid;
+      else high = mid - 1;
     }
+    g = Group{low, p.first[low], p.first[low + 1], 0};
   }
+  g.row0 = (block - begins(g.id, g.from)) * kRows;
+  if (g.row0 >= (g.to - g.from) * p.group) g.id = -1;
   return g;
 }
 
@@ -296,8 +309,9 @@ __device__ __forceinline__ void attend_common(const PagedSharedParams &p, int id
   const int layer = p.c.by_hkv.of(lh), head = p.c.by_hkv.rest(lh);
   if (layer >= p.c.n_layers) return;
   const Asked asked = ask_first(p, layer, head, lane);
+  if (!groups_ascend(p, asked.from, asked.to, lane)) return;
   const Group g = find_group(p, asked, block, lane);
-  if (!g.ok || g.id < 0) return;
+  if (g.id < 0) return;
   const int rows = (g.to - g.from) * p.group;
   const Common seen = common_rows(p, asked, g, layer, head, lane, threadIdx.x == 0 && split == 0 && g.row0 == 0);
   const typename In::List list(seen);
@@ -572,8 +586,7 @@ __device__ __forceinline__ CellSum fill_whole_cell(const PagedSharedParams &p, C
 #pragma unroll
   for (int j = 0; j < kEach; ++j) cached[j] = j < per ? ask_len(p, layer, head, min(lane * per + j, p.c.batch - 1)) : 0;
   CellSum sum;
-  sum.ok = __all(lane >= p.groups || (asked.from <= asked.to && asked.from >= 0 && asked.to <= p.c.batch &&
-                                      (lane > 0 || asked.from == 0) && (lane + 1 < p.groups || asked.to == p.c.batch)));
+  sum.ok = groups_ascend(p, asked.from, asked.to, lane);
 #pragma unroll
   for (int j = 0; j < kEach; ++j) {
     cached[j] = max(0, min(cached[j], p.c.cap));
@@ -643,43 +656,33 @@ __device__ __forceinline__ CellSum fill_cell(const PagedSharedParams &p, Cell &c
   if (tid == 0) cell.most = 0;
   __syncthreads();
 
-  // The group of sequence b: how many end before it or with it.
-  const auto group_of = [&](int b, int &from, int &to) {
-    int id = 0;
-    from = 0;
-    to = p.c.batch;
-    for (int g0 = 0; g0 < p.groups; g0 += kWave) {
-      const int f = g0 == 0 ? asked.from : p.first[min(g0 + lane, p.groups)];
-      const int t = g0 == 0 ? asked.to : p.first[min(g0 + lane + 1, p.groups)];
-      for (int k = 0; k < min(p.groups - g0, kWave); ++k) {
-        const int k0 = __builtin_amdgcn_readlane(f, k), k1 = __builtin_amdgcn_readlane(t, k);
-        id += k1 <= b ? 1 : 0;
-        if (k0 <= b && b < k1) {
-          from = k0;
-          to = k1;
-        }
-      }
+  // The group of sequence b: the last one that begins there or before.
+  const auto group_of = [&](int b) {
+    int low = 0, high = p.groups - 1;
+    while (low < high) {
+      const int mid = (low + high + 1) / 2;
+      if (p.first[mid] <= b) low = mid;
+      else high = mid - 1;
     }
-    return id;
+    return low;
   };
-  bool ok = true;
-  for (int g0 = 0; g0 < p.groups; g0 += kWave) {
-    const int i = g0 + lane;
-    const int f = g0 == 0 ? asked.from : p.first[min(i, p.groups)];
-    const int t = g0 == 0 ? asked.to : p.first[min(i + 1, p.groups)];
-    ok = ok && __all(i >= p.groups || (f <= t && f >= 0 && t <= p.c.batch && (i > 0 || f == 0) && (i + 1 < p.groups || t == p.c.batch)));
-  }
+  const bool ok = groups_ascend(p, asked.from, asked.to, lane);
   // Sequences of groups that reach into the cell, also those outside of it, by the place of
   // their group's first sequence in it.
-  for (int base = 0; ok && base < p.c.batch; base += kNW * kWave) {
-    const int b = min(base + tid, p.c.batch - 1);
-    const int len = base == 0 && wave == 0 ? asked.len : ask_len(p, layer, head, b);
-    int from, to;
-    group_of(b, from, to);
-    if (base + tid < p.c.batch && from < b0 + nb && to > b0) {
-      const int at = max(from, b0) - b0, n = max(0, min(len, p.c.cap));
-      atomicMin(&cell.rows[at], n);
-      if (p.window > 0) atomicMax(&cell.start[at], n + extra - p.window);
+  int begin = 0, end = p.c.batch;
+  if (ok && nb < p.c.batch) {
+    begin = p.first[group_of(b0)];
+    end = p.first[group_of(b0 + nb - 1) + 1];
+  }
+  for (int b = begin + tid; ok && b < end; b += kNW * kWave) {
+    const int len = b < kWave && wave == 0 ? asked.len : ask_len(p, layer, head, b);
+    const int id = group_of(b), from = p.first[id];
+    const int at = max(from, b0) - b0, n = max(0, min(len, p.c.cap));
+    atomicMin(&cell.rows[at], n);
+    if (p.window > 0) atomicMax(&cell.start[at], n + extra - p.window);
+    if (b >= b0 && b < b0 + nb) {
+      cell.lead[b - b0] = from;
+      cell.until[b - b0] = id;
     }
   }
   __syncthreads();
@@ -689,13 +692,11 @@ __device__ __forceinline__ CellSum fill_cell(const PagedSharedParams &p, Cell &c
     const int at = tid * kEach + i, b = b0 + at;
     n[i] = rows[i] = start[i] = tiles[i] = 0;
     lead[i] = b;
-    int from = 0, to = 0, id = 0;
-    if (ok) id = group_of(min(b, p.c.batch - 1), from, to);   // by all lanes
     if (at < nb) {
       n[i] = max(0, min(ask_len(p, layer, head, b), p.c.cap)) + extra;
       if (ok) {
-        const int given = p.shared[layer * p.shared_stride + id], place = max(from, b0) - b0;
-        lead[i] = from;
+        lead[i] = cell.lead[at];
+        const int given = p.shared[layer * p.shared_stride + cell.until[at]], place = max(lead[i], b0) - b0;
         rows[i] = max(0, min(given, cell.rows[place]));
         start[i] = p.window > 0 ? min(cell.start[place], rows[i]) : 0;
       }
@@ -745,7 +746,7 @@ __device__ __forceinline__ void attend_own(const PagedSharedParams &p, int id, u
   const int lh = p.by_chunks.of(cid), b0 = p.by_chunks.rest(cid) * kSharedCell;
   const int layer = p.c.by_hkv.of(lh), head = p.c.by_hkv.rest(lh);
   const int nb = min(kSharedCell, p.c.batch - b0);
-  const CellSum sum = p.c.batch <= kSharedCell && p.groups <= 16 ? fill_whole_cell(p, cell, layer, head, lane)
+  const CellSum sum = p.c.batch <= kSharedCell && p.groups <= 8 ? fill_whole_cell(p, cell, layer, head, lane)
                                                                  : fill_cell(p, cell, layer, head, b0, nb);
   const size_t row0 = (static_cast<size_t>(lh) * p.c.batch + b0) * p.group;       // of the parts
 

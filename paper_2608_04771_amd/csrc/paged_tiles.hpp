@@ -109,10 +109,10 @@ struct Mma32<float> {
   __device__ __forceinline__ static frag negated(frag a) { return -a; }
 };
 
-template <typename T, int D, int NW = kWaves, int KEYS = Mma32<T>::keys>
+template <typename T, int D, int NW = kWaves>
 struct Cfg {
   using M = Mma32<T>;
-  static constexpr int keys = KEYS;
+  static constexpr int keys = M::keys;
   static constexpr int blocks = keys / 32;               // S^T blocks of a tile
   static constexpr int qk_steps = D / 2 / M::kpl;
   static constexpr int dtiles = D / 32;

@@ -234,3 +234,41 @@ def test_captured_beside_eager():
         assert torch.equal(a.length, b.length) and a.length.eq(20 + 10 * (i + 1)).all()
         for y, z in ((a.k, b.k), (a.v, b.v), (qa, qb)):
             assert torch.equal(y.view(torch.int16), z.view(torch.int16)), f"replay {i}"
+
+
+@pytest.mark.parametrize("T", [1, 8, 9])
+def test_the_most_heads(T):
+    H, D = 1024, 64
+    g = torch.Generator().manual_seed(T)
+    c = Paged(np.arange(H)[None, None] % 40, 16, D, F32, spare=T, seed=T)
+    kn, vn = (torch.randn((1, 1, H, T, D), generator=g) for _ in "kv")
+    freq, axes, rope = _rope(D, False, 1)
+    pos = torch.arange(100, 100 + T, dtype=torch.int32)[None]
+    cache = c.upload()
+    err = torch.zeros(1, dtype=torch.int32, device="cuda")
+    B.reco_paged_append(cache, kn.cuda(), vn.cuda(), rope, pos.cuda(), dev_err=err)
+    assert err.item() == 0
+    want, off = turned(kn, pos[None], freq)
+    _check(c, cache, want, vn, off, [T], "heads")
+
+
+def test_pages_past_four_gibibytes():
+    # 4,200 pages of 1 MiB in each pool, of which the last are in use
+    page, n_pages, T = 4096, 4200, 30
+    c = Paged(np.array([[[4090, 0]]]), page, 128, BF, spare=T, seed=3)
+    have = c.k.shape[0]
+    pools = [torch.empty((n_pages, page, 128), dtype=BF, device="cuda") for _ in "kv"]
+    for pool, x in zip(pools, (c.k, c.v)):
+        pool[n_pages - have:] = x.cuda()
+    table = torch.where((c.pages >= 0) & (c.pages < have), c.pages + (n_pages - have), c.pages)
+    g = torch.Generator().manual_seed(1)
+    kn, vn = (torch.randn((1, 1, 2, T, 128), generator=g).to(BF) for _ in "kv")
+    freq, axes, rope = _rope(128, False, 1)
+    pos = torch.arange(T, dtype=torch.int32)[None]
+    for some in (slice(0, T), slice(0, 1)):                # a long run, and one that is a workgroup's
+        cache = B.PagedKVCache(*pools, table.cuda(), c.length.cuda())
+        k, v, p = kn[:, :, :, some].contiguous(), vn[:, :, :, some].contiguous(), pos[:, some].contiguous()
+        B.reco_paged_append(cache, k.cuda(), v.cuda(), rope, p.cuda())
+        want, off = turned(k, p[None], freq)
+        after = B.PagedKVCache(pools[0][n_pages - have:].clone(), pools[1][n_pages - have:].clone(), c.pages.cuda(), cache.length)
+        _check(c, after, want, v, off, [k.shape[3]], str(some))

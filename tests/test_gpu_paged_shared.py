@@ -233,3 +233,113 @@ def test_bits_repeat_and_graphs_follow_their_inputs():
             assert torch.equal(a.view(torch.int8), b.view(torch.int8)), f"replay {i}"
         assert torch.equal(caches[0].k.view(torch.int16), caches[1].k.view(torch.int16))
         assert torch.isfinite(outs[0][1]).all()
+
+
+def _big(B_, groups, seed, most=40):
+    """first and shared of `groups` groups over B_ sequences, and lengths, some of them of nothing."""
+    rng = np.random.RandomState(seed)
+    first = np.sort(np.concatenate([[0, B_], rng.randint(0, B_ + 1, groups - 1)]))
+    shared = rng.randint(0, 50, groups)
+    group = np.searchsorted(first[1:], np.arange(B_), side="right")
+    return first, shared, (shared[group] + rng.randint(0, most, B_))[None, :, None], rng
+
+
+@pytest.mark.parametrize("sinks,window", [(0, 0), (3, 20)])
+@pytest.mark.parametrize("batch,groups", [(65, 2), (200, 16), (200, 17), (512, 1), (512, 16), (512, 64), (512, 65), (512, 400),
+                                          (513, 3), (700, 16), (1100, 2), (1100, 65), (1100, 1000)])
+def test_large_batches(batch, groups, sinks, window):
+    # cells of whole batches and of parts of one, groups that cross their borders, lists past a wave's lanes
+    first, shared, lens, rng = _big(batch, groups, batch + groups)
+    c, q, kn, vn = make(lens, first, shared, 16, 64, BF, 2, True, seed=groups)
+    cache = c.upload()
+    err = torch.zeros(1, dtype=torch.int32, device="cuda")
+    out, lse = call(c, cache, q, kn, vn, err, sinks=sinks, window=window)
+    assert err.item() == 0
+    some = sorted({0, 63, 64, batch - 1} | {b for b in (511, 512, 1023, 1024) if b < batch} | set(rng.choice(batch, 60).tolist()))
+    check_attention(c, q, kn, vn, out, lse, sinks, window, units=[(0, b, 0) for b in some])
+    # the others' as a call of another split of work has them: sequences in groups of one
+    ones = torch.arange(batch + 1, dtype=torch.int32).cuda()
+    if window == 0:
+        check_append(c, cache, kn, vn)
+    else:
+        for u in np.ndindex(lens.shape):                   # shared rows in every list
+            lead, P = (0, int(c.first[c.group[u[1]]]), 0), int(c.shared[0, c.group[u[1]]])
+            rows = torch.arange(P)
+            if u != lead and P:
+                kept = P // 16
+                c.pages[u][:kept] = c.pages[lead][:kept]
+                at, of = c.where(u, rows[kept * 16:]), c.where(lead, rows[kept * 16:])
+                c.k[at], c.v[at] = c.k[of], c.v[of]
+        alone = c.upload()
+        a, za = B.reco_paged_shared_decode_attn(alone, q.cuda(), ones, torch.zeros(batch, dtype=torch.int32).cuda(), kn.cuda(), vn.cuda(),
+                                                sinks, window, dev_err=err)
+        top = max(c.v.float().nan_to_num(0).abs().max().item(), vn.float().abs().max().item())
+        assert err.item() == 0 and (a.cpu().float() - out.float()).abs().max().item() <= 2 * 2.0 ** -7 * top   # each within 2^-7
+        assert (za.cpu() - lse).abs().max().item() <= 2e-4
+
+
+def test_lists_of_many_groups_that_do_not_ascend():
+    first, shared, lens, _ = _big(600, 300, 1)
+    shared[:] = 0
+    for at, x in ((70, -1), (299, 601), (300, 599), (150, 2 ** 31 - 1), (0, 1)):
+        c, q, kn, vn = make(lens, first, shared, 16, 64, F32, 1, True)
+        cache = c.upload()
+        bad = torch.from_numpy(first.astype(np.int64).copy())
+        bad[at] = x
+        err = torch.zeros(1, dtype=torch.int32, device="cuda")
+        out, lse = B.reco_paged_shared_decode_attn(cache, q.cuda(), bad.int().cuda(), torch.ones(300, dtype=torch.int32).cuda(), kn.cuda(),
+                                                   vn.cuda(), dev_err=err)
+        assert err.item() == 10
+        check_attention(c, q, kn, vn, out.cpu(), lse.cpu(), units=[(0, b, 0) for b in range(0, 600, 13)], what=str(at))
+        check_append(c, cache, kn, vn)
+
+
+def test_pages_past_four_gibibytes():
+    # 4,200 pages of 1 MiB in each pool; those in use are the last ones
+    page, n_pages = 4096, 4200
+    c, q, kn, vn = make(np.array([[[5000], [5040], [4999]]]), [0, 3], [4990], page, 128, BF, 4, True, seed=9)
+    have = c.k.shape[0]
+    pools = [torch.empty((n_pages, page, 128), dtype=BF, device="cuda") for _ in "kv"]
+    for pool, x in zip(pools, (c.k, c.v)):
+        pool[n_pages - have:] = x.cuda()
+    table = torch.where((c.pages >= 0) & (c.pages < have), c.pages + (n_pages - have), c.pages)
+    cache = B.PagedKVCache(*pools, table.cuda(), c.length.cuda())
+    for sinks, window in ((0, 0), (4, 700)):
+        out, lse = call(c, cache, q, kn, vn, sinks=sinks, window=window)
+        check_attention(c, q, kn, vn, out, lse, sinks, window)
+        cache.length.copy_(c.length)
+    for pool, x in zip(pools, (kn, vn)):
+        for u in np.ndindex(c.lens.shape):
+            L = int(c.lens[u])
+            at = table[u][L // page].item()
+            assert at >= 4190 and torch.equal(pool[at, L % page].cpu(), x[u])
+
+
+def test_graphs_that_share_a_workspace():
+    # two calls of other sizes, captured with one workspace and replayed in turn
+    made = [make(_lens(100, [3, 40, 9, 70], 2), [0, 4], [100], 16, 128, BF, 4, False, seed=1),
+            make(_lens(300, [80, 2], 1, NL=3), [0, 1, 2], [300, 290], 16, 128, BF, 7, False, seed=2)]
+    caches = [m[0].upload() for m in made]
+    sizes = [B.paged_shared_decode_attn_workspace_size(x, m[1].shape[2], len(m[0].first) - 1) for x, m in zip(caches, made)]
+    ws = torch.empty(max(sizes), dtype=torch.uint8, device="cuda")
+    calls, graphs, s = [], [], torch.cuda.Stream()
+    for x, (c, q, _, _) in zip(caches, made):
+        out = torch.zeros(q.shape, dtype=BF, device="cuda")
+        calls.append((B.PreparedPagedSharedDecode(x, q.shape[2], *c.groups(), out, torch.zeros(q.shape[:3], device="cuda"), ws), q.cuda()))
+    torch.cuda.synchronize()
+    for f, q in calls:
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1], stream=s):
+            f(q)
+    for i in range(3):
+        for f, q in calls:
+            f.out.zero_()
+            q.mul_(-1 if i else 1)
+        torch.cuda.synchronize()
+        with torch.cuda.stream(s):
+            for _ in range(2):
+                for g in graphs:
+                    g.replay()
+        torch.cuda.synchronize()
+        for (f, q), (c, _, _, _) in zip(calls, made):
+            check_attention(c, q.cpu(), None, None, f.out.cpu(), f.lse.cpu(), what=f"turn {i}")

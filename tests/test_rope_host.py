@@ -104,3 +104,24 @@ def test_binding_refuses_outputs_over_inputs():
                  (x[:, :, :, :3], x[:, :, :, 1:]), (x[:, :1], x[:, :1].transpose(2, 3)[:, :, :, :4])):
         with pytest.raises(ValueError, match="out"):
             B._no_partial_overlap(a, b, "out")
+
+
+def test_rotated_queries_meet_no_keys_or_values():
+    x = torch.zeros(1, 2, 4, 10, 64).transpose(2, 3)       # six heads of queries, two of keys, two of values
+    q, k, v = x[:, :, :6], x[:, :, 6:8], x[:, :, 8:]
+    for t in (k, v):
+        B._no_partial_overlap(t, q, "q_out", same=False)
+        B._no_partial_overlap(t, torch.zeros(1, 2, 6, 4, 64), "q_out", same=False)
+    one = torch.zeros(1, 2, 2, 1, 64)                      # one token: a stride of its dimension is not one
+    B._no_partial_overlap(one[:, :, :1], one[:, :, 1:], "q_out", same=False)
+    flat = x.transpose(2, 3).reshape(-1)
+    skew = torch.zeros(2000).as_strided((1, 2, 1, 2, 64), (0, 200, 64, 192, 1))      # rows 0, 192, 200, 392
+    for t, out in ((k, x[:, :, 1:7]), (k, k), (v, x[:, :, 4:]), (k, flat[:2 * 6 * 4 * 64].view(1, 2, 6, 4, 64)),
+                   (k, x[:, :, 6:8].transpose(2, 3)), (x[:, :, 6:8, 1:], x[:, :, :6, :3]),
+                   (skew, torch.as_strided(skew, skew.shape, skew.stride(), 64))):
+        with pytest.raises(ValueError, match="q_out must not meet"):
+            B._no_partial_overlap(t, out, "q_out", same=False)
+    buf = torch.zeros(4000)
+    out, below, above = buf[1000:2000], buf[:1000], buf[2000:]
+    span = B._Span(out)
+    assert span.misses(below) and span.misses(above) and not span.misses(buf[:1001]) and not span.misses(buf[1999:]) and not span.misses(out)
