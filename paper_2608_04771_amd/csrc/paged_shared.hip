@@ -1076,6 +1076,15 @@ __global__ __launch_bounds__(kJoinThreads) void shared_join_kernel(PagedSharedPa
   const size_t row = static_cast<size_t>(blockIdx.x) * kPer + in;
   const bool real = row < p.rows;
   const int S = p.splits + p.own_parts;
+  // rows are (layer, KV head, sequence, query head); units (layer, sequence, KV head)
+  const int flat = static_cast<int>(real ? row : 0);
+  const int lhb = p.by_group.of(flat), qi = p.by_group.rest(flat);
+  const int lh = p.c.by_batch.of(lhb), b = p.c.by_batch.rest(lhb);
+  const int layer = p.c.by_hkv.of(lh), head = p.c.by_hkv.rest(lh);
+  const int unit = (layer * p.c.batch + b) * p.c.hkv + head;
+  const size_t cunit = p.c.unit(unit);
+  const bool commits = real && sub == 0 && qi == 0;
+  const int len_in = commits ? p.c.len[cunit] : 0;        // (asked for first: its page waits for it)
 
   // Few rows' parts are asked for together with their statistics; of many, whose places are
   // mostly empty, those alone that there are.
@@ -1087,30 +1096,38 @@ __global__ __launch_bounds__(kJoinThreads) void shared_join_kernel(PagedSharedPa
     const int s = sub + i * kSub;
     x[i] = real && s < S ? *reinterpret_cast<const float4 *>(po + static_cast<size_t>(s) * p.rows * D) : make_float4(0.f, 0.f, 0.f, 0.f);
   }
-  float M = -INFINITY, L = 0.f;
-  {
-    constexpr int kTurns = (kSharedMaxParts + kLanes - 1) / kLanes;
-    float m[kTurns], l[kTurns];
+  constexpr int kTurns = (kSharedMaxParts + kLanes - 1) / kLanes;
+  float m[kTurns], l[kTurns];
 #pragma unroll
-    for (int i = 0; i < kTurns; ++i) {
-      const int s = lane + i * kLanes;
-      const bool there = real && s < S;
-      const float2 ml = there ? reinterpret_cast<const float2 *>(p.part_ml)[static_cast<size_t>(s) * p.rows + row] : make_float2(-INFINITY, 0.f);
-      m[i] = ml.x;
-      l[i] = ml.y;
-      M = fmaxf(M, m[i]);
-    }
-    M = lanes_fold<kLanes>(M, [](float a, float b) { return fmaxf(a, b); });
-    const float ref = M == -INFINITY ? 0.f : M;
-#pragma unroll
-    for (int i = 0; i < kTurns; ++i) {
-      m[i] = fast_exp2(m[i] - ref);
-      L += l[i] * m[i];
-      // a part without rows has no output
-      if (sub == 0 && lane + i * kLanes < kSharedMaxParts) s_w[in][lane + i * kLanes] = l[i] == 0.f ? 0.f : m[i];
-    }
-    L = lanes_fold<kLanes>(L, [](float a, float b) { return a + b; });
+  for (int i = 0; i < kTurns; ++i) {
+    const int s = lane + i * kLanes;
+    const bool there = real && s < S;
+    const float2 ml = there ? reinterpret_cast<const float2 *>(p.part_ml)[static_cast<size_t>(s) * p.rows + row] : make_float2(-INFINITY, 0.f);
+    m[i] = ml.x;
+    l[i] = ml.y;
   }
+  using Four = std::conditional_t<sizeof(T) == 2, uint2, uint4>;           // elements of a thread
+  Four k_row{}, v_row{};
+  int page = 0;
+  if (commits && p.k_new) {
+    const size_t from = static_cast<size_t>(unit) * kLanes + lane;
+    k_row = reinterpret_cast<const Four *>(p.k_new)[from];
+    v_row = reinterpret_cast<const Four *>(p.v_new)[from];
+    page = p.c.pages[cunit * static_cast<size_t>(p.c.max_pages) + (max(0, min(len_in, p.c.cap - 1)) >> p.c.page_shift)];
+  }
+  float M = -INFINITY, L = 0.f;
+#pragma unroll
+  for (int i = 0; i < kTurns; ++i) M = fmaxf(M, m[i]);
+  M = lanes_fold<kLanes>(M, [](float a, float b) { return fmaxf(a, b); });
+  const float ref = M == -INFINITY ? 0.f : M;
+#pragma unroll
+  for (int i = 0; i < kTurns; ++i) {
+    m[i] = fast_exp2(m[i] - ref);
+    L += l[i] * m[i];
+    // a part without rows has no output
+    if (sub == 0 && lane + i * kLanes < kSharedMaxParts) s_w[in][lane + i * kLanes] = l[i] == 0.f ? 0.f : m[i];
+  }
+  L = lanes_fold<kLanes>(L, [](float a, float b) { return a + b; });
   __syncthreads();
   const float inv = L == 0.f ? 0.f : 1.f / L;
   float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -1142,38 +1159,20 @@ __global__ __launch_bounds__(kJoinThreads) void shared_join_kernel(PagedSharedPa
     }
   }
   if (!real) return;
-  // rows are (layer, KV head, sequence, query head); units (layer, sequence, KV head)
-  const int flat = static_cast<int>(row);
-  const int lhb = p.by_group.of(flat), qi = p.by_group.rest(flat);
-  const int lh = p.c.by_batch.of(lhb), b = p.c.by_batch.rest(lhb);
-  const int layer = p.c.by_hkv.of(lh), head = p.c.by_hkv.rest(lh);
-  const int unit = (layer * p.c.batch + b) * p.c.hkv + head;
   const size_t oq = static_cast<size_t>(unit) * p.group + qi;
-  T *dst = reinterpret_cast<T *>(p.out) + oq * D + lane * 4;
-  dst[0] = from_f32<T>(acc.x);
-  dst[1] = from_f32<T>(acc.y);
-  dst[2] = from_f32<T>(acc.z);
-  dst[3] = from_f32<T>(acc.w);
+  const T y[4] = {from_f32<T>(acc.x), from_f32<T>(acc.y), from_f32<T>(acc.z), from_f32<T>(acc.w)};
+  reinterpret_cast<Four *>(p.out)[oq * kLanes + lane] = __builtin_bit_cast(Four, y);
   if (p.lse && lane == 0) p.lse[oq] = L == 0.f ? -INFINITY : (M + log2f(L)) * kLn2;
-  if (qi != 0) return;
-  const size_t cunit = p.c.unit(unit);
-  const int len_in = p.c.len[cunit];
-  int code = 0, page = 0;
+  if (!commits) return;
+  int code = 0;
   if (len_in < 0 || len_in > p.c.cap) code = kDevBadLength;
   else if (p.k_new && len_in == p.c.cap) code = kDevAppendOverflow;
-  if (code == 0 && p.k_new) {
-    page = p.c.pages[cunit * static_cast<size_t>(p.c.max_pages) + (len_in >> p.c.page_shift)];
-    if (static_cast<unsigned>(page) >= static_cast<unsigned>(p.c.n_pages)) code = kDevBadPage;
-  }
+  else if (p.k_new && static_cast<unsigned>(page) >= static_cast<unsigned>(p.c.n_pages)) code = kDevBadPage;
   if (code && lane == 0) report(p.c.dev_err, code);
   if (code || !p.k_new) return;
-  const size_t at = ((static_cast<size_t>(page) << p.c.page_shift) + (len_in & ((1 << p.c.page_shift) - 1))) * D + lane * 4;
-  const size_t from = static_cast<size_t>(unit) * D + lane * 4;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    reinterpret_cast<T *>(p.c.k)[at + i] = reinterpret_cast<const T *>(p.k_new)[from + i];
-    reinterpret_cast<T *>(p.c.v)[at + i] = reinterpret_cast<const T *>(p.v_new)[from + i];
-  }
+  const size_t at = ((static_cast<size_t>(page) << p.c.page_shift) + (len_in & ((1 << p.c.page_shift) - 1))) * kLanes + lane;
+  reinterpret_cast<Four *>(p.c.k)[at] = k_row;
+  reinterpret_cast<Four *>(p.c.v)[at] = v_row;
   if (lane == 0) p.c.len[cunit] = len_in + 1;
 }
 
