@@ -168,12 +168,19 @@ int shared_span_rows(int capacity, int sinks, int window) {
   return static_cast<int>(seen < capacity ? seen : capacity);
 }
 
-// A workgroup for every compute unit, up to two, shares the common rows of `jobs` (layers and KV heads);
-// a split keeps 256 rows of what a call may see, of fp32, whose products take sixteen times
-// as long, a tile.
+// A workgroup for every compute unit shares the common rows of `jobs` (layers and KV heads), nine
+// tenths of them at least, and no number where few units have a second one: up to 1.4 for
+// each one split more is taken (32 sequences in 8 groups, 4 layers, 144 blocks: 288 workgroups
+// 325 us, 432 of them 282; two for every unit write and join more parts: 128 rows of 28 heads a
+// group, 8 layers, 64 blocks: 256 workgroups 170 us, 512 of them 195).  A split keeps 256 rows
+// of what a call may see, of fp32, whose products take sixteen times as long, a tile.
 int shared_splits(int jobs, int blocks, int span_rows, int dtype, int compute_units) {
   const int64_t each = static_cast<int64_t>(jobs) * blocks;
-  int64_t splits = (compute_units + each - 1) / each;
+  int64_t splits = compute_units / each;
+  if (splits < 1 || 10 * each * splits < 9 * compute_units) {
+    ++splits;
+    if (each * splits > compute_units && 10 * each * splits < 14 * compute_units) ++splits;
+  }
   const int least = dtype == 0 ? prefill_tile_rows(0) : 256;
   if (splits > span_rows / least) splits = span_rows / least;
   if (splits > kSharedMaxSplits) splits = kSharedMaxSplits;

@@ -89,4 +89,4 @@ def test_splits_fit_the_workspace(plan):
                                     span = plan.span(cap, sinks, window)
                                     a, b = plan.splits(jobs, blocks, span, dt, cus), plan.own(jobs, batch, cus)
                                     assert 1 <= a <= plan.most() and 2 <= b <= plan.most() and a + b <= whole
-                                    assert a == 1 or a * jobs * blocks < 2 * cus
+                                    assert a == 1 or a * jobs * blocks < 3 * cus
