@@ -841,7 +841,8 @@ class _Rows:
     """A tensor's rows as the C ABI takes them: [n_layers][B][heads][T][D], or without T
     for one token, in any order of memory whose rows are contiguous and 16-byte aligned."""
 
-    __slots__ = ("what", "shape", "dtype", "index", "struct", "ref", "_strides", "_piece", "_write")
+    __slots__ = ("what", "shape", "dtype", "index", "struct", "ref", "at", "extent", "_strides",
+                 "_piece", "_write")
 
     def __init__(self, what: str, shape, dtype: torch.dtype, device, write: bool = False):
         self.what, self.shape, self.dtype, self._write = what, tuple(shape), dtype, write
@@ -861,8 +862,12 @@ class _Rows:
         p = t.data_ptr()
         if p & 15:
             raise ValueError(f"{self.what} must be 16-byte aligned")
-        self.struct.data = p
+        self.at = self.struct.data = p
         return self.ref
+
+    def meets(self, span) -> bool:
+        """Whether the rows taken may lie in ``span`` (addresses)."""
+        return self.at < span[1] and span[0] < self.at + self.extent
 
     def _take_strides(self, st):
         if st[-1] != 1 or any(n > 1 and x % self._piece for n, x in zip(self.shape[:-1], st[:-1])):
@@ -875,6 +880,7 @@ class _Rows:
                     raise ValueError(f"{self.what}: rows must not overlap")
                 end = x * (n - 1) + end
         s = self.struct
+        self.extent = (16 // self._piece) * (1 + sum((n - 1) * x for n, x in zip(self.shape, st)))
         s.layer, s.seq, s.head = used[:3]
         s.token = used[3] if len(used) == 4 else 0
         self._strides = st
@@ -890,20 +896,6 @@ def _launch(index: int, fn, *args) -> int:
 
 def _stream_of(index: int) -> int:
     return _raw_stream(index) if _raw_stream is not None else torch.cuda.current_stream(index).cuda_stream
-
-
-class _Span:
-    """Where a call's output lies, to tell quickly that an input is elsewhere."""
-
-    __slots__ = ("begin", "end")
-
-    def __init__(self, out: torch.Tensor):
-        self.begin, self.end = _span(out)
-
-    def misses(self, x: torch.Tensor) -> bool:
-        at = x.data_ptr()
-        # of a tensor that starts before the output, its strides say where it ends
-        return at >= self.end or (at < self.begin and _span(x)[1] <= self.begin)
 
 
 def _span(t: torch.Tensor):
@@ -954,7 +946,7 @@ class PreparedRope:
         self._fn = load_library().reco_rope
         self._struct = rope._struct(pos)
         self._in = _Rows("x", out.shape, out.dtype, out.device)
-        self._out_span = _Span(out)
+        self._span = _span(out)
         self._head = ctypes.byref(self._struct)
         self._out = _Rows("out", out.shape, out.dtype, out.device, write=True).take(out)
         self._tail = (NL, Bsz, H, T, D, RECO_F32 if out.dtype == torch.float32 else RECO_BF16, _ptr(n_new),
@@ -962,7 +954,7 @@ class PreparedRope:
 
     def __call__(self, x: torch.Tensor) -> torch.Tensor:
         xr = self._in.take(x)
-        if not self._out_span.misses(x):
+        if self._in.meets(self._span):
             _no_partial_overlap(x, self.out, "out")
         st = _launch(self._in.index, self._fn, self._head, xr, self._out, *self._tail)
         if st != RECO_OK:
@@ -1022,7 +1014,7 @@ class PreparedPagedAppend:
             shape = (nl, Bsz, hq, *run, D)
             self._q = _Rows("q", shape, dt, dev)
             self._qo = _Rows("q_out", shape, dt, dev, write=True).take(q_out)
-            self._out_span = _Span(q_out)
+            self._span = _span(q_out)
         self._struct = None if rope is None else rope._struct(pos)
         self._head = (cache.ref(), layer0, nl, None if rope is None else ctypes.byref(self._struct), T, _ptr(n_new))
         self._tail = (hq, _ptr(dev_err))
@@ -1034,11 +1026,12 @@ class PreparedPagedAppend:
         qr = None
         if q is not None:
             qr = self._q.take(q)
-            if not self._out_span.misses(q):
+            if self._q.meets(self._span):
                 _no_partial_overlap(q, self.q_out, "q_out")
-            for x in (k_new, v_new):
-                if not self._out_span.misses(x):
-                    _no_partial_overlap(x, self.q_out, "q_out", same=False)
+            if self._k.meets(self._span):
+                _no_partial_overlap(k_new, self.q_out, "q_out", same=False)
+            if self._v.meets(self._span):
+                _no_partial_overlap(v_new, self.q_out, "q_out", same=False)
         st = _launch(self._k.index, self._fn, *self._head, k, v, qr, self._qo, *self._tail)
         if st != RECO_OK:
             _check(st, "reco_paged_append")

@@ -121,7 +121,8 @@ def test_rotated_queries_meet_no_keys_or_values():
                    (skew, torch.as_strided(skew, skew.shape, skew.stride(), 64))):
         with pytest.raises(ValueError, match="q_out must not meet"):
             B._no_partial_overlap(t, out, "q_out", same=False)
-    buf = torch.zeros(4000)
-    out, below, above = buf[1000:2000], buf[:1000], buf[2000:]
-    span = B._Span(out)
-    assert span.misses(below) and span.misses(above) and not span.misses(buf[:1001]) and not span.misses(buf[1999:]) and not span.misses(out)
+    buf = torch.zeros(4096)
+    r, span = B._Rows("x", (1, 1, 1, 2, 64), torch.float32, torch.device("cpu")), B._span(buf[1024:2048])
+    for at, met in ((0, False), (1024 - 128, False), (1024 - 124, True), (1024, True), (2044, True), (2048, False)):
+        r.take(buf[at:at + 128].view(1, 1, 1, 2, 64))
+        assert r.meets(span) == met, at
