@@ -12,12 +12,30 @@
 // One launch has both kinds of workgroups, so that neither kind's last ones leave the
 // device idle; the second joins their parts and commits the append.
 //
-// The common part is the prefill kernel's: 128 query rows a workgroup, 32 a wave, key tiles
-// that the waves share through LDS,
+// The common part has 128 query rows a workgroup, 32 a wave, and key tiles (64 rows of bf16, 32 of
+// fp32) that the waves share through LDS,
 //   S^T = K_tile . Q^T (32 keys x 32 rows),   O^T += V_tile^T . P^T.
-// The own part is the decode kernel's: 16 padded query heads, tiles of 32 keys that are a
-// wave's own.  Statistics and outputs are fp32; P alone is rounded to the cache's type, as
-// its operand has to be.
+// The own part has 16 padded query heads and tiles of 32 keys that are a wave's own.
+// Statistics and outputs are fp32; P alone is rounded to the cache's type, as its operand
+// has to be: a weight is off by half a step, 2^-8 of it at most.
+//
+// What bounds it, per call (both kernels, and the least time of its bytes at 6.6 TB/s):
+//   32 sequences of 28 heads on 4, 16,384 common rows and 256 to 2,048 own ones, 8 layers: 877 MB,
+//   163 + 8 us, 133: memory.  The two blocks of query rows read the common rows at 1.0 times
+//   their bytes from memory and again from L2, 7 TB/s into the units together; the matrix
+//   units work in 19% of the cycles, the vector units in 23, both in 5.
+//   16 sequences in 4 groups, window 4,096, 4 layers: 368 MB, 75 + 5 us, 56: the ends of ragged
+//   groups, each of whose tiles waits for a load from memory.
+//   128 sequences of 32 heads, 4,096 common rows and up to 400 own ones: 125 MB and 9 GFLOP,
+//   32 + 7 us, 19: products, exponentials and loads in turn, and 4,096 rows of 8 parts and more.
+//   8 sequences, 8,190 common rows: 62 MB, 16 + 5 us, 9.3: the way to the first tile (lengths,
+//   page ids, keys: three round trips, 4 us) and the last one's way out.
+// fp32 is bound by its products, a sixteenth of bf16's rate, and a group of up to 32 query rows
+// has one of four waves at work.  Of fp32 rows of 128, 26 registers are kept in memory.
+// Not kept: 256 query rows and 8 waves a workgroup with four stages (200 us for the first call, 188
+// then), 32-key tiles in bf16 and three waves a SIMD (410, by registers in memory), own rows two
+// tiles ahead (233, likewise), one wave's own rows as items of their own (181 to 185), and a
+// priority of its own for either kind of workgroup (no difference).
 #include "paged_device.hpp"
 #include "paged_tiles.hpp"
 
@@ -28,7 +46,7 @@ namespace {
 constexpr int kNW = 4;                       // waves of a workgroup
 constexpr int kRows = kSharedRows;           // query rows of one
 static_assert(kRows == 32 * kNW, "32 rows a wave");
-constexpr int kMix = 32;                     // compute units of an XCD
+constexpr int kMix = 32;                     // compute units of an XCD (by 1: 217 us, by 16 or 64: the same)
 constexpr int wait_loads(int n) { return 0x0f70 | (n & 15) | (n >> 4) << 14; }   // vmcnt(n)
 constexpr float kSlack = 8.f;                // log2 units that a maximum may grow before O follows
 
@@ -573,8 +591,9 @@ struct CellSum {
 };
 
 // Fills the cell that is the whole batch, in few groups.  Every wave writes what it reads,
-// the same as the others, so that none has to wait for another: 1.4 us, by all waves
-// together 5 us, but the groups take their turns here (some 100 cycles each).
+// the same as the others, so that none has to wait for another (128 sequences in one group:
+// 42.5 us a call, 47.7 with all waves together), but the groups take their turns here, some
+// 100 cycles each (64 sequences in 16 groups: 17.9 us, 14.3 together; 8 groups: the same).
 __device__ __forceinline__ CellSum fill_whole_cell(const PagedSharedParams &p, Cell &cell, int layer, int head, int lane) {
   constexpr int kEach = kSharedCell / kWave;
   const int extra = p.k_new ? 1 : 0, per = (p.c.batch + kWave - 1) / kWave;      // sequences of a lane, neighbours
@@ -1188,6 +1207,7 @@ hipError_t launch_typed(const PagedSharedParams &p, hipStream_t s) {
   hipLaunchKernelGGL((shared_attn_kernel<T, D>), dim3(p.common_wgs + p.own_wgs), dim3(kNW * kWave), 0, s, p);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
+  // Few rows of many parts have a workgroup each.
   if (p.splits + p.own_parts > 8 && p.rows < 2048) return launch_join<T, D, kJoinThreads / (D / 4)>(p, s);
   return launch_join<T, D, 1>(p, s);
 }
