@@ -30,8 +30,9 @@
 //   32 + 7 us, 19: products, exponentials and loads in turn, and 4,096 rows of 8 parts and more.
 //   8 sequences, 8,190 common rows: 62 MB, 16 + 5 us, 9.3: the way to the first tile (lengths,
 //   page ids, keys: three round trips, 4 us) and the last one's way out.
-// fp32 is bound by its products, a sixteenth of bf16's rate, and a group of up to 32 query rows
-// has one of four waves at work.  Of fp32 rows of 128, 26 registers are kept in memory.
+// fp32 is bound by its products, a sixteenth of bf16's rate: where a block has up to 64 query rows, the
+// waves that would have none share the others' (21 sequences in 8 groups, 15,366 rows: 596 us with
+// one wave at work, 367).  Of fp32 rows of 128, 43 registers are kept in memory.
 // Not kept: 256 query rows and 8 waves a workgroup with four stages (200 us for the first call, 188
 // then), 32-key tiles in bf16 and three waves a SIMD (410, by registers in memory), own rows two
 // tiles ahead (233, likewise), one wave's own rows as items of their own (181 to 185), and a
@@ -304,50 +305,54 @@ constexpr int area_bytes() {
   return a > b ? a : b;
 }
 
-template <typename T, int D>
-__device__ __forceinline__ void attend_common(const PagedSharedParams &p, int id, unsigned char *k0, unsigned char *v0,
-                                              unsigned char *k1, unsigned char *v1, int *entries) {
+// A split of a block of query rows.
+struct Block {
+  int layer, head, lh, split;
+  Group g;
+  Common seen;
+};
+
+// kWays waves have 32 query rows together: each forms S from its part of D, all add them up through
+// LDS and weigh the same rows, and each forms its columns of O (of two with the same ones,
+// from half of the tile's rows).
+template <typename T, int D, int kWays>
+__device__ __forceinline__ void attend_block(const PagedSharedParams &p, const Block &at, unsigned char *k0, unsigned char *v0,
+                                             unsigned char *k1, unsigned char *v1, int *entries) {
   using namespace tiles32;
   using C = tiles32::Cfg<T, D, kNW>;
   using In = Feed<T, D>;
   using M = Mma32<T>;
   using frag = typename M::frag;
   constexpr int KT = C::keys;
+  constexpr int kQk = C::qk_steps / kWays;                // a wave's, of a block of S
+  constexpr int kD = C::dtiles > kWays ? C::dtiles / kWays : 1, kColumns = C::dtiles / kD, kHalves = kWays / kColumns > 1 ? 2 : 1;
+  static_assert(kWays == 1 || (C::blocks == 1 && M::kpl == 1), "fp32's tiles");
   const int lane = threadIdx.x & (kWave - 1);
   const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) / kWave);
   const int half = lane >> 5;
   const int col = lane & 31;
-
-  // The blocks of a layer, KV head and split take their turn on one XCD, beside each other,
-  // so that those of a group share the keys' way through its L2.
-  const int slot = id / kXcds;
-  const int turn = p.by_blocks.of(slot), block = p.by_blocks.rest(slot);
-  const int job = turn * kXcds + id % kXcds;
-  const int lh = p.by_splits.of(job), split = p.by_splits.rest(job);
-  const int layer = p.c.by_hkv.of(lh), head = p.c.by_hkv.rest(lh);
-  if (layer >= p.c.n_layers) return;
-  const Asked asked = ask_first(p, layer, head, lane);
-  if (!groups_ascend(p, asked.from, asked.to, lane)) return;
-  const Group g = find_group(p, asked, block, lane);
-  if (g.id < 0) return;
+  const int part = wave % kWays;                          // of D
+  const int dt0 = kWays > 1 ? part % kColumns * kD : 0, key_half = kHalves > 1 ? part / kColumns : 0;
+  const int layer = at.layer, head = at.head, lh = at.lh, split = at.split;
+  const Group &g = at.g;
   const int rows = (g.to - g.from) * p.group;
-  const Common seen = common_rows(p, asked, g, layer, head, lane, threadIdx.x == 0 && split == 0 && g.row0 == 0);
-  const typename In::List list(seen);
+
+  const typename In::List list(at.seen);
   const int per_split = p.by_splits.of(list.total + p.splits - 1);
   const int i0 = split * per_split;
   const int i1 = min(list.total, i0 + per_split);
 
   // This lane's query row.
-  const int wave_row = g.row0 + wave * 32;
+  const int wave_row = g.row0 + wave / kWays * 32;
   const bool active = wave_row < rows;
   const int r = min(wave_row + col, rows - 1);
   const int b = g.from + p.by_group.of(r);
   const size_t qrow = (static_cast<size_t>(layer * p.c.batch + b) * p.c.hkv + head) * p.group + p.by_group.rest(r);
-  frag qf[C::qk_steps];
+  frag qf[kQk];
   {
-    const T *src = reinterpret_cast<const T *>(p.q) + qrow * D + half * (D / 2);
+    const T *src = reinterpret_cast<const T *>(p.q) + qrow * D + half * (D / 2) + part * kQk * M::kpl;
 #pragma unroll
-    for (int c = 0; c < C::qk_steps; ++c) {
+    for (int c = 0; c < kQk; ++c) {
       qf[c] = load_frag(src + c * M::kpl);
       if (p.scale_log2 < 0.f) qf[c] = M::negated(qf[c]);   // so that the largest product is the largest logit
     }
@@ -356,13 +361,14 @@ __device__ __forceinline__ void attend_common(const PagedSharedParams &p, int id
 
   In in(p, p.c.unit((layer * p.c.batch + g.from) * p.c.hkv + head), list, i0, i1, entries + wave * kWave, wave, lane);
   float m_run = -INFINITY, l_run = 0.f;                  // m in units of the scaled logits
-  f32x16_t o[C::dtiles];
+  f32x16_t o[kD];
 #pragma unroll
-  for (int dt = 0; dt < C::dtiles; ++dt) {
+  for (int dt = 0; dt < kD; ++dt) {
 #pragma unroll
     for (int i = 0; i < 16; ++i) o[dt][i] = 0.f;
   }
-  const int kat = k_base<T, D>(lane), vat = v_base<T, D>(lane);
+  const int kat = k_base<T, D>(lane) ^ (part * kQk * M::kpl * (int)sizeof(T));
+  const int vat = (v_base<T, D>(lane) ^ (dt0 * 32 * (int)sizeof(T))) + key_half * (16 * C::row_bytes);
 
   // Tile i, in kbuf and vbuf once its loads are done.  The next tile's V goes to vto, where the
   // last tile's was, while S is formed, and the K of the one after to kbuf, while O is: so
@@ -377,7 +383,7 @@ __device__ __forceinline__ void attend_common(const PagedSharedParams &p, int id
     __builtin_amdgcn_s_waitcnt(wait_loads(2 * kHalf));    // K
     barrier();                                            // is there, and no one reads the last tile's V
     f32x16_t s[C::blocks];
-    constexpr int kSteps = C::blocks * C::qk_steps, kAhead = M::kpl == 8 ? 8 : 16, kEach = kSteps / C::insts;
+    constexpr int kSteps = C::blocks * kQk, kAhead = M::kpl == 8 || kSteps < 16 ? 8 : 16, kEach = kSteps / C::insts;
     float ref = 0.f;
     if (!active) {
 #pragma unroll
@@ -408,6 +414,32 @@ __device__ __forceinline__ void attend_common(const PagedSharedParams &p, int id
         if (z % kEach == 0) in.load_v(ahead, z / kEach, vto);
         __builtin_amdgcn_sched_barrier(0);
       }
+      if constexpr (kWays > 1) {
+        // All waves are past their reads of K, whose place the parts of S take; their sum has one order.
+        constexpr int kRounds = kNW * kWave * 64 / C::stage > 1 ? kNW * kWave * 64 / C::stage : 1, kRegs = 16 / kRounds;
+        float4 *parts = reinterpret_cast<float4 *>(kbuf);
+#pragma unroll
+        for (int rd = 0; rd < kRounds; ++rd) {
+          barrier();
+#pragma unroll
+          for (int e = rd * kRegs; e < (rd + 1) * kRegs; e += 4)
+            parts[(wave * (kRegs / 4) + e / 4 % (kRegs / 4)) * kWave + lane] = make_float4(s[0][e], s[0][e + 1], s[0][e + 2], s[0][e + 3]);
+          barrier();
+#pragma unroll
+          for (int e = rd * kRegs; e < (rd + 1) * kRegs; e += 4) {
+            float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+            for (int w = 0; w < kWays; ++w) {
+              const float4 x = parts[((wave - part + w) * (kRegs / 4) + e / 4 % (kRegs / 4)) * kWave + lane];
+              sum = w == 0 ? x : make_float4(sum.x + x.x, sum.y + x.y, sum.z + x.z, sum.w + x.w);
+            }
+            s[0][e] = sum.x;
+            s[0][e + 1] = sum.y;
+            s[0][e + 2] = sum.z;
+            s[0][e + 3] = sum.w;
+          }
+        }
+      }
       if (!whole) {
         const int low = tile.from - tile.row - 4 * half, high = tile.to - tile.row - 4 * half;
 #pragma unroll
@@ -435,7 +467,7 @@ __device__ __forceinline__ void attend_common(const PagedSharedParams &p, int id
         l_run *= alpha;
         m_run = m_new;
 #pragma unroll
-        for (int dt = 0; dt < C::dtiles; ++dt) {
+        for (int dt = 0; dt < kD; ++dt) {
 #pragma unroll
           for (int e = 0; e < 16; ++e) o[dt][e] *= alpha;
         }
@@ -452,12 +484,12 @@ __device__ __forceinline__ void attend_common(const PagedSharedParams &p, int id
       for (int j = 0; j < C::insts; ++j) in.load_k(ahead, j, kto);
       return;
     }
-    constexpr int kParts = C::blocks * C::pv_steps;
-    frag vf[2][C::dtiles];
+    constexpr int kParts = C::blocks * C::pv_steps / kHalves;
+    frag vf[2][kD];
     const auto read_v = [&](int q) {
       const int row = M::kpl == 8 ? 16 * q : 8 * (q / 4) + q % 4;
 #pragma unroll
-      for (int dt = 0; dt < C::dtiles; ++dt)
+      for (int dt = 0; dt < kD; ++dt)
         vf[q & 1][dt] = v_frag32<T, D>(vbuf + (vat ^ (dt * 32 * (int)sizeof(T))) + row * C::row_bytes);
     };
     read_v(0);
@@ -473,7 +505,10 @@ __device__ __forceinline__ void attend_common(const PagedSharedParams &p, int id
     };
     frag pf[2];
     const auto put = [&](int q, int j) {
-      if constexpr (M::kpl == 1) pf[q & 1] = weigh(q, j);
+      if constexpr (kHalves > 1) {
+        const float low = weigh(q, j), high = weigh(q + kParts, j);
+        pf[q & 1] = key_half ? high : low;
+      } else if constexpr (M::kpl == 1) pf[q & 1] = weigh(q, j);
       else pf[q & 1][j] = static_cast<__bf16>(weigh(q, j));
     };
 #pragma unroll
@@ -484,7 +519,7 @@ __device__ __forceinline__ void attend_common(const PagedSharedParams &p, int id
       __builtin_amdgcn_sched_barrier(0);
       constexpr int kApart = kParts / C::insts > 0 ? kParts / C::insts : 1, kTogether = kApart * C::insts > kParts ? 2 : 1;
 #pragma unroll
-      for (int dt = 0; dt < C::dtiles; ++dt) {
+      for (int dt = 0; dt < kD; ++dt) {
         o[dt] = M::mma(vf[q & 1][dt], pf[q & 1], o[dt]);
         if (dt == 0 && q % kApart == 0) {
 #pragma unroll
@@ -492,7 +527,7 @@ __device__ __forceinline__ void attend_common(const PagedSharedParams &p, int id
         }
         if (q + 1 < kParts) {
 #pragma unroll
-          for (int j = dt * M::kpl / C::dtiles; j < (dt + 1) * M::kpl / C::dtiles; ++j) put(q + 1, j);
+          for (int j = dt * M::kpl / kD; j < (dt + 1) * M::kpl / kD; ++j) put(q + 1, j);
         }
         __builtin_amdgcn_sched_barrier(0);
       }
@@ -519,21 +554,67 @@ __device__ __forceinline__ void attend_common(const PagedSharedParams &p, int id
   if (in.worst >= static_cast<unsigned>(p.c.n_pages)) report(p.c.dev_err, kDevBadPage);
 
   const float l_tot = l_run + shfl_xor(l_run, 32);
+  if constexpr (kHalves > 1) {
+    if (i0 < i1) {
+      float4 *halves = reinterpret_cast<float4 *>(k0);
+      barrier();                                          // of all waves' loads and reads
+#pragma unroll
+      for (int e = 0; e < 4 && key_half; ++e)
+        halves[(part % kColumns * 4 + e) * kWave + lane] = make_float4(o[0][4 * e], o[0][4 * e + 1], o[0][4 * e + 2], o[0][4 * e + 3]);
+      barrier();
+#pragma unroll
+      for (int e = 0; e < 4 && !key_half; ++e) {
+        const float4 x = halves[(part % kColumns * 4 + e) * kWave + lane];
+        o[0][4 * e] += x.x;
+        o[0][4 * e + 1] += x.y;
+        o[0][4 * e + 2] += x.z;
+        o[0][4 * e + 3] += x.w;
+      }
+    }
+    if (key_half) return;
+  }
   if (wave_row + col >= rows) return;
-  const size_t part = static_cast<size_t>(split) * p.rows +
+  const size_t to = static_cast<size_t>(split) * p.rows +
                       (static_cast<size_t>(lh) * p.c.batch + g.from) * p.group + wave_row + col;
-  if (half == 0) {
-    p.part_ml[2 * part] = m_run;
-    p.part_ml[2 * part + 1] = l_tot;
+  if (half == 0 && part == 0) {
+    p.part_ml[2 * to] = m_run;
+    p.part_ml[2 * to + 1] = l_tot;
   }
   if (i0 >= i1) return;                                   // without tiles, sum 0: not read
-  float4 *po = reinterpret_cast<float4 *>(p.part_o + part * D) + half;
+  float4 *po = reinterpret_cast<float4 *>(p.part_o + to * D) + half + dt0 * 8;
 #pragma unroll
-  for (int dt = 0; dt < C::dtiles; ++dt) {
+  for (int dt = 0; dt < kD; ++dt) {
 #pragma unroll
     for (int e = 0; e < 4; ++e)
       po[dt * 8 + 2 * e] = make_float4(o[dt][4 * e], o[dt][4 * e + 1], o[dt][4 * e + 2], o[dt][4 * e + 3]);
   }
+}
+
+template <typename T, int D>
+__device__ __forceinline__ void attend_common(const PagedSharedParams &p, int id, unsigned char *k0, unsigned char *v0,
+                                              unsigned char *k1, unsigned char *v1, int *entries) {
+  const int lane = threadIdx.x & (kWave - 1);
+  // The blocks of a layer, KV head and split take their turn on one XCD, beside each other,
+  // so that those of a group share the keys' way through its L2.
+  const int slot = id / kXcds;
+  const int turn = p.by_blocks.of(slot), block = p.by_blocks.rest(slot);
+  const int job = turn * kXcds + id % kXcds;
+  const int lh = p.by_splits.of(job), split = p.by_splits.rest(job);
+  const int layer = p.c.by_hkv.of(lh), head = p.c.by_hkv.rest(lh);
+  if (layer >= p.c.n_layers) return;
+  const Asked asked = ask_first(p, layer, head, lane);
+  if (!groups_ascend(p, asked.from, asked.to, lane)) return;
+  const Group g = find_group(p, asked, block, lane);
+  if (g.id < 0) return;
+  const Block at{layer, head, lh, split, g, common_rows(p, asked, g, layer, head, lane, threadIdx.x == 0 && split == 0 && g.row0 == 0)};
+  // fp32's products take so long that few rows' ones are dealt to all waves; of bf16 one wave keeps up
+  // with memory.
+  if constexpr (sizeof(T) == 4) {
+    const int here = (g.to - g.from) * p.group - g.row0;
+    if (here <= 32) return attend_block<T, D, 4>(p, at, k0, v0, k1, v1, entries);
+    if (here <= 64) return attend_block<T, D, 2>(p, at, k0, v0, k1, v1, entries);
+  }
+  attend_block<T, D, 1>(p, at, k0, v0, k1, v1, entries);
 }
 
 // ------------------------------------------------------------------ units' own rows
@@ -844,15 +925,6 @@ __device__ __forceinline__ void attend_own(const PagedSharedParams &p, int id, u
     }
     return w;
   };
-  // Rows outside the range are others of the pool and are masked where they are used; the
-  // new row is put where it belongs in LDS.
-  const auto load = [&](Rows<T, D> &reg, const void *pool, const Where &w) {
-#pragma unroll
-    for (int j = 0; j < C::insts; ++j)
-      reg[j] = __builtin_nontemporal_load(reinterpret_cast<const u32x4v *>(
-          static_cast<const unsigned char *>(pool) + w.at[j / (C::insts / 2)] + j % (C::insts / 2) * (kWave * 16) + lane * 16));
-  };
-
   // The sequence that the wave is at, its part's number, and its softmax; what the next tile
   // needs beside its rows (another sequence's queries, the new row) comes with them.
   struct Uniform {
@@ -865,6 +937,21 @@ __device__ __forceinline__ void attend_own(const PagedSharedParams &p, int id, u
               __builtin_amdgcn_readlane(here.to, from_lane), false};
     u.fresh = extra && u.range == 2 && u.row + kTile >= u.to;      // a sequence's last tile holds it
     return u;
+  };
+  // Rows outside the range are masked where they are used; loads take one of its rows in
+  // their place, so that short ranges cost what they hold (of sixteen that are all outside,
+  // one; 167 sequences of 20 own rows, 3 layers, window 368: 65 us with all rows loaded, 55).
+  // The new row is put where it belongs in LDS.
+  const auto load = [&](Rows<T, D> &reg, const void *pool, const Where &w, const Uniform &u) {
+    const int low = u.from - u.row, high = u.to - u.row - (u.fresh ? 2 : 1);
+#pragma unroll
+    for (int j = 0; j < C::insts; ++j) {
+      constexpr int kHalf = C::insts / 2;
+      const int hf = j / kHalf, row = j % kHalf * C::rows_per_inst + lane / C::lanes_per_row;
+      const int from = max(0, min(low - 16 * hf, 15)), to = max(0, min(high - 16 * hf, 15));
+      reg[j] = __builtin_nontemporal_load(reinterpret_cast<const u32x4v *>(
+          static_cast<const unsigned char *>(pool) + w.at[hf] + max(from, min(row, to)) * C::row_bytes + lane % C::lanes_per_row * 16));
+    }
   };
   // (fp32 has no registers for the next queries beside the present ones and waits for them)
   constexpr bool kQueriesAhead = sizeof(T) == 2;
@@ -939,7 +1026,7 @@ __device__ __forceinline__ void attend_own(const PagedSharedParams &p, int id, u
     if (now.fresh && lane < C::lanes_per_row)
       *reinterpret_cast<uint4 *>(stage + (n_cache - kb) * C::k_stride + lane * 16) = kfresh;
     const uint4 v_row = vfresh;
-    if (more) load(kreg, p.c.k, place_of);
+    if (more) load(kreg, p.c.k, place_of, then);
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     f32x4_t s[2];
 #pragma unroll
@@ -1006,7 +1093,7 @@ __device__ __forceinline__ void attend_own(const PagedSharedParams &p, int id, u
       dst[1] = make_uint2(v_row.z, v_row.w);
     }
     if (more) {
-      load(vreg, p.c.v, place_of);
+      load(vreg, p.c.v, place_of, then);
       load_more(then, then.b != now.b);
     }
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
@@ -1020,9 +1107,9 @@ __device__ __forceinline__ void attend_own(const PagedSharedParams &p, int id, u
   ask(0);
   turn(0);
   const Where first = find(0);
-  load(kreg, p.c.k, first);
-  load(vreg, p.c.v, first);
   now = info(0);
+  load(kreg, p.c.k, first, now);
+  load(vreg, p.c.v, first, now);
   load_more(now, true);
   number = w - (now.b > 0 ? __builtin_amdgcn_readfirstlane(cell.until[now.b - 1]) : 0) / share;   // waves before that had some of it
   begin(now);

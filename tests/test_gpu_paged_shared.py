@@ -343,3 +343,32 @@ def test_graphs_that_share_a_workspace():
         torch.cuda.synchronize()
         for (f, q), (c, _, _, _) in zip(calls, made):
             check_attention(c, q.cpu(), None, None, f.out.cpu(), f.lse.cpu(), what=f"turn {i}")
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("sequences", [1, 4, 5, 8, 9, 17, 20, 21])
+def test_blocks_of_fp32_rows(D, sequences):
+    # 8 query heads: blocks of up to 32 rows, up to 64 and more, alone and behind whole ones
+    own = [i * 7 % 50 for i in range(sequences)]
+    for P, sinks, window in ((0, 0, 0), (31, 0, 0), (300, 0, 0), (1000, 3, 700)):
+        c, q, kn, vn = make(_lens(P, own, 2), [0, sequences], [P], 16, D, F32, 8, True, seed=P)
+        cache = c.upload()
+        err = torch.zeros(1, dtype=torch.int32, device="cuda")
+        out, lse = call(c, cache, q, kn, vn, err, sinks=sinks, window=window)
+        assert err.item() == 0
+        check_attention(c, q, kn, vn, out, lse, sinks, window, what=f"{P} rows")
+        again = c.upload()
+        o2, z2 = call(c, again, q, kn, vn, err, sinks=sinks, window=window)
+        assert torch.equal(o2.view(torch.int32), out.view(torch.int32)) and torch.equal(z2, lse)
+
+
+def test_short_own_rows_beside_odd_ones():
+    # ranges of few rows in their tiles, pages that are full of infinities around them
+    for dtype, D, G in ((BF, 128, 4), (BF, 64, 1), (F32, 128, 7)):
+        for P, sinks, window in ((47, 0, 0), (64, 0, 0), (64, 2, 21), (100, 5, 33)):
+            c, q, kn, vn = make(_lens(P, [0, 1, 2, 15, 16, 17], 2), [0, 6], [P], 64, D, dtype, G, True, seed=P)
+            for x in (c.k, c.v):
+                x[torch.isnan(x)] = float("inf")
+            cache = c.upload()
+            out, lse = call(c, cache, q, kn, vn, sinks=sinks, window=window)
+            check_attention(c, q, kn, vn, out, lse, sinks, window, what=f"{dtype} {P}")
