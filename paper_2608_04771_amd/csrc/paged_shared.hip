@@ -21,7 +21,7 @@
 //
 // What bounds it, per call (both kernels, and the least time of its bytes at 6.6 TB/s):
 //   32 sequences of 28 heads on 4, 16,384 common rows and 256 to 2,048 own ones, 8 layers: 877 MB,
-//   163 + 8 us, 133: memory.  The two blocks of query rows read the common rows at 1.0 times
+//   161 + 8 us, 133: memory.  The two blocks of query rows read the common rows at 1.0 times
 //   their bytes from memory and again from L2, 7 TB/s into the units together; the matrix
 //   units work in 19% of the cycles, the vector units in 23, both in 5.
 //   16 sequences in 4 groups, window 4,096, 4 layers: 368 MB, 75 + 5 us, 56: the ends of ragged
