@@ -24,8 +24,9 @@
 //   161 + 8 us, 133: memory.  The two blocks of query rows read the common rows at 1.0 times
 //   their bytes from memory and again from L2, 7 TB/s into the units together; the matrix
 //   units work in 19% of the cycles, the vector units in 23, both in 5.
-//   16 sequences in 4 groups, window 4,096, 4 layers: 368 MB, 75 + 5 us, 56: the ends of ragged
-//   groups, each of whose tiles waits for a load from memory.
+//   16 sequences in 4 groups, window 4,096, 4 layers: 368 MB, 75 + 5 us, 56: 426 MB, since each
+//   sequence reads alone what lies between its window's start and its group's last one, and the
+//   ends of ragged groups.
 //   128 sequences of 32 heads, 4,096 common rows and up to 400 own ones: 125 MB and 9 GFLOP,
 //   32 + 7 us, 19: products, exponentials and loads in turn, and 4,096 rows of 8 parts and more.
 //   8 sequences, 8,190 common rows: 62 MB, 16 + 5 us, 9.3: the way to the first tile (lengths,

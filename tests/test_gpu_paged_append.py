@@ -272,3 +272,30 @@ def test_pages_past_four_gibibytes():
         want, off = turned(k, p[None], freq)
         after = B.PagedKVCache(pools[0][n_pages - have:].clone(), pools[1][n_pages - have:].clone(), c.pages.cuda(), cache.length)
         _check(c, after, want, v, off, [k.shape[3]], str(some))
+
+
+@pytest.mark.parametrize("dtype,D", [(BF, 128), (F32, 64)])
+@pytest.mark.parametrize("T", [None, 1, 8, 21])
+def test_a_projection_rotated_where_it_lies(dtype, D, T):
+    # queries in place, keys and values from the heads beside them, which stay as they are
+    NL, Bs, H, G = 2, 3, 2, 3
+    g = torch.Generator().manual_seed(5)
+    n = T or 1
+    fused = torch.randn((NL, Bs, n, H * (G + 2), D), generator=g).to(dtype)
+    dev = fused.cuda().transpose(2, 3)
+    x = dev if T else dev[:, :, :, 0]
+    c = Paged(np.array([[[3, 15], [0, 40], [16, 1]]] * NL), 16, D, dtype, spare=n, seed=2)
+    cache = c.upload()
+    freq, axes, rope = _rope(D, True, 1)
+    pos = torch.randint(-50, 5000, (Bs, n), generator=g, dtype=torch.int32)
+    q, kn, vn = x[:, :, :H * G], x[:, :, H * G:H * (G + 1)], x[:, :, H * (G + 1):]
+    for bad in (kn, x[:, :, 1:1 + H * G], x[:, :, 2 * H:2 * H + H * G]):
+        if bad.shape == q.shape:
+            with pytest.raises(ValueError, match="q_out"):
+                B.reco_paged_append(cache, kn, vn, rope, pos.cuda(), q, q_out=bad)
+    got = B.reco_paged_append(cache, kn, vn, rope, pos.cuda(), q, q_out=q)
+    assert got.data_ptr() == q.data_ptr()
+    want, off = turned(fused.transpose(2, 3), pos[None], freq, pairs=True)
+    close_rows(dev[:, :, :H * G].cpu(), want[:, :, :H * G], off[:, :, :H * G], "queries")
+    assert torch.equal(dev[:, :, H * G:].cpu(), fused.transpose(2, 3)[:, :, H * G:])
+    _check(c, cache, want[:, :, H * G:H * (G + 1)], fused.transpose(2, 3)[:, :, H * (G + 1):], off[:, :, H * G:H * (G + 1)], [n] * Bs, "fused")

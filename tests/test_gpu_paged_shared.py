@@ -372,3 +372,19 @@ def test_short_own_rows_beside_odd_ones():
             cache = c.upload()
             out, lse = call(c, cache, q, kn, vn, sinks=sinks, window=window)
             check_attention(c, q, kn, vn, out, lse, sinks, window, what=f"{dtype} {P}")
+
+
+def test_without_lse_and_on_another_stream():
+    c, q, kn, vn = make(_lens(90, [3, 40, 9], 2), [0, 3], [90], 16, 128, BF, 4, True, seed=6)
+    cache, (first, shared), s = c.upload(), c.groups(), torch.cuda.Stream()
+    dev = [x.cuda() for x in (q, kn, vn)]
+    torch.cuda.synchronize()
+    with torch.cuda.stream(s):
+        out, none = B.reco_paged_shared_decode_attn(cache, dev[0], first, shared, *dev[1:], want_lse=False)
+    s.synchronize()
+    assert none is None
+    again = c.upload()
+    o2, z2 = B.reco_paged_shared_decode_attn(again, dev[0], first, shared, *dev[1:])
+    assert torch.equal(o2.view(torch.int16), out.view(torch.int16))
+    check_attention(c, q, kn, vn, out.cpu(), z2.cpu())
+    check_append(c, cache, kn, vn)
