@@ -345,13 +345,14 @@ def test_graphs_that_share_a_workspace():
             check_attention(c, q.cpu(), None, None, f.out.cpu(), f.lse.cpu(), what=f"turn {i}")
 
 
+@pytest.mark.parametrize("dtype", [F32, BF])
 @pytest.mark.parametrize("D", [64, 128])
 @pytest.mark.parametrize("sequences", [1, 4, 5, 8, 9, 17, 20, 21])
-def test_blocks_of_fp32_rows(D, sequences):
+def test_blocks_of_few_rows(dtype, D, sequences):
     # 8 query heads: blocks of up to 32 rows, up to 64 and more, alone and behind whole ones
     own = [i * 7 % 50 for i in range(sequences)]
     for P, sinks, window in ((0, 0, 0), (31, 0, 0), (300, 0, 0), (1000, 3, 700)):
-        c, q, kn, vn = make(_lens(P, own, 2), [0, sequences], [P], 16, D, F32, 8, True, seed=P)
+        c, q, kn, vn = make(_lens(P, own, 2), [0, sequences], [P], 16, D, dtype, 8, True, seed=P)
         cache = c.upload()
         err = torch.zeros(1, dtype=torch.int32, device="cuda")
         out, lse = call(c, cache, q, kn, vn, err, sinks=sinks, window=window)
@@ -359,7 +360,7 @@ def test_blocks_of_fp32_rows(D, sequences):
         check_attention(c, q, kn, vn, out, lse, sinks, window, what=f"{P} rows")
         again = c.upload()
         o2, z2 = call(c, again, q, kn, vn, err, sinks=sinks, window=window)
-        assert torch.equal(o2.view(torch.int32), out.view(torch.int32)) and torch.equal(z2, lse)
+        assert torch.equal(o2.view(torch.uint8), out.view(torch.uint8)) and torch.equal(z2, lse)
 
 
 def test_short_own_rows_beside_odd_ones():
