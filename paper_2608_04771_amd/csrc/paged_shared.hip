@@ -777,7 +777,7 @@ __device__ __forceinline__ CellSum fill_cell(const PagedSharedParams &p, Cell &c
     end = p.first[group_of(b0 + nb - 1) + 1];
   }
   for (int b = begin + tid; ok && b < end; b += kNW * kWave) {
-    const int len = b < kWave && wave == 0 ? asked.len : ask_len(p, layer, head, b);
+    const int len = wave == 0 && b == lane ? asked.len : ask_len(p, layer, head, b);   // (not where begin > 0)
     const int id = group_of(b), from = p.first[id];
     const int at = max(from, b0) - b0, n = max(0, min(len, p.c.cap));
     atomicMin(&cell.rows[at], n);
