@@ -255,6 +255,9 @@ struct Feed {
     if (seen) worst = max(worst, static_cast<unsigned>(entry));
     const unsigned id = min(static_cast<unsigned>(entry), static_cast<unsigned>(n_pages - 1));
     place = ((static_cast<uint64_t>(id) << shift) + (row & ((1u << shift) - 1u))) * C::row_bytes;
+    // The entry has come from LDS before the load that overwrites it there is sent, which
+    // the compiler does not know to write LDS.
+    asm volatile("s_waitcnt lgkmcnt(0)" : "+v"(entry));
     ask(i + kBatch);
   }
   __device__ __forceinline__ void first() {
