@@ -12,6 +12,7 @@ import contextlib
 import ctypes
 import math
 import os
+import threading
 from typing import Optional, Sequence
 
 import torch
@@ -926,7 +927,7 @@ def _no_partial_overlap(x: torch.Tensor, out: torch.Tensor, what: str, same: boo
 class PreparedRope:
     """reco_rope for a loop that calls it again and again with the same positions
     tensor, output and counts (whose contents may change): those are checked once
-    here, each call checks its input."""
+    here, each call checks its input.  Calls of several threads take their turns."""
 
     def __init__(self, rope: Rope, pos: torch.Tensor, out: torch.Tensor, n_new: Optional[torch.Tensor] = None,
                  dev_err: Optional[torch.Tensor] = None):
@@ -951,12 +952,14 @@ class PreparedRope:
         self._out = _Rows("out", out.shape, out.dtype, out.device, write=True).take(out)
         self._tail = (NL, Bsz, H, T, D, RECO_F32 if out.dtype == torch.float32 else RECO_BF16, _ptr(n_new),
                       _ptr(dev_err))
+        self._lock = threading.Lock()      # of _in, which the library reads without Python's own
 
     def __call__(self, x: torch.Tensor) -> torch.Tensor:
-        xr = self._in.take(x)
-        if self._in.meets(self._span):
-            _no_partial_overlap(x, self.out, "out")
-        st = _launch(self._in.index, self._fn, self._head, xr, self._out, *self._tail)
+        with self._lock:
+            xr = self._in.take(x)
+            if self._in.meets(self._span):
+                _no_partial_overlap(x, self.out, "out")
+            st = _launch(self._in.index, self._fn, self._head, xr, self._out, *self._tail)
         if st != RECO_OK:
             _check(st, "reco_rope")
         return self.out
@@ -978,7 +981,7 @@ class PreparedPagedAppend:
     """reco_paged_append for a loop that calls it again and again with the same cache,
     positions tensor, rotated queries and counts (whose contents may change): those are
     checked once here, each call checks the new rows.  ``n_tokens`` None: rows without
-    the dimension T, one token each."""
+    the dimension T, one token each.  Calls of several threads take their turns."""
 
     def __init__(self, cache: PagedKVCache, n_tokens: Optional[int] = None, rope: Optional[Rope] = None,
                  pos: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None,
@@ -1018,21 +1021,23 @@ class PreparedPagedAppend:
         self._struct = None if rope is None else rope._struct(pos)
         self._head = (cache.ref(), layer0, nl, None if rope is None else ctypes.byref(self._struct), T, _ptr(n_new))
         self._tail = (hq, _ptr(dev_err))
+        self._lock = threading.Lock()      # of _k, _v and _q, which the library reads without Python's own
 
     def __call__(self, k_new: torch.Tensor, v_new: torch.Tensor, q: Optional[torch.Tensor] = None):
         if (q is None) != (self._q is None):
             raise ValueError("q and q_out must be given together")
-        k, v = self._k.take(k_new), self._v.take(v_new)
-        qr = None
-        if q is not None:
-            qr = self._q.take(q)
-            if self._q.meets(self._span):
-                _no_partial_overlap(q, self.q_out, "q_out")
-            if self._k.meets(self._span):
-                _no_partial_overlap(k_new, self.q_out, "q_out", same=False)
-            if self._v.meets(self._span):
-                _no_partial_overlap(v_new, self.q_out, "q_out", same=False)
-        st = _launch(self._k.index, self._fn, *self._head, k, v, qr, self._qo, *self._tail)
+        with self._lock:
+            k, v = self._k.take(k_new), self._v.take(v_new)
+            qr = None
+            if q is not None:
+                qr = self._q.take(q)
+                if self._q.meets(self._span):
+                    _no_partial_overlap(q, self.q_out, "q_out")
+                if self._k.meets(self._span):
+                    _no_partial_overlap(k_new, self.q_out, "q_out", same=False)
+                if self._v.meets(self._span):
+                    _no_partial_overlap(v_new, self.q_out, "q_out", same=False)
+            st = _launch(self._k.index, self._fn, *self._head, k, v, qr, self._qo, *self._tail)
         if st != RECO_OK:
             _check(st, "reco_paged_append")
         return self.q_out
