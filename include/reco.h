@@ -355,11 +355,16 @@ reco_status_t reco_paged_prefill_attn(const reco_paged_cache_t *cache, int32_t l
  *              1 <= n_groups <= batch
  *   shared   : int32; [n_groups] with shared_layer_stride = 0 or [n_layers][n_groups]
  *              with stride = n_groups; at most the shortest len of a group's units
- * A shared count outside that is clamped (RECO_DEV_BAD_LENGTH); a list of groups that does
- * not ascend from 0 to batch counts as none, each unit's rows then being all its own
- * (RECO_DEV_BAD_GROUP).  Appended rows go to each unit's own pages, so a page that shared
- * rows fill in part is a unit's own from there on.  cache->weight must be NULL
- * (RECO_ERR_UNSUPPORTED otherwise): a row that several sequences see cannot be evicted from one. */
+ * A shared count outside that is clamped (RECO_DEV_BAD_LENGTH), and each unit's rows are its
+ * own from there on; a list of groups that does not ascend from 0 to batch counts as none,
+ * each unit's rows then being all its own (RECO_DEV_BAD_GROUP).  A bad len is clamped, too, as
+ * for reco_paged_decode_attn: one below 0 leaves the units of its layer, head and group without
+ * shared rows, which they then look for in their own lists (RECO_DEV_BAD_PAGE may be what is
+ * reported).  Outputs of that group are unspecified there; those of other groups, layers and
+ * heads, and the appends of all units of good length, are not.
+ * Appended rows go to each unit's own pages, so a page that shared rows fill in part is a
+ * unit's own from there on.  cache->weight must be NULL (RECO_ERR_UNSUPPORTED otherwise): a
+ * row that several sequences see cannot be evicted from one. */
 size_t reco_paged_shared_decode_attn_workspace_size(const reco_paged_cache_t *cache, int32_t n_layers,
                                                     int32_t n_q_heads, int32_t n_groups);
 reco_status_t reco_paged_shared_decode_attn(const reco_paged_cache_t *cache, int32_t layer0,
