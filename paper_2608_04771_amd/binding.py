@@ -907,7 +907,9 @@ def _span(t: torch.Tensor):
 def _no_partial_overlap(x: torch.Tensor, out: torch.Tensor, what: str, same: bool = True):
     """``out`` is x itself (where that is ``same``), or none of its rows meet x's."""
     (a, a1), (b, b1) = _span(x), _span(out)
-    if a1 <= b or b1 <= a or (same and x.shape == out.shape and a == b and x.stride() == out.stride()):
+    if a1 <= b or b1 <= a:
+        return
+    if same and a == b and x.shape == out.shape and all(n == 1 or s == t for n, s, t in zip(x.shape, x.stride(), out.stride())):
         return
     # heads beside each other, of the same tokens
     d, e, i = b - a, x.element_size(), 2
