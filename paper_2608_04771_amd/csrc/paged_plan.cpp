@@ -191,7 +191,7 @@ int shared_splits(int jobs, int blocks, int span_rows, int dtype, int compute_un
 int shared_cell_wgs(int cells, int compute_units) { return (compute_units + cells - 1) / cells; }
 
 // A sequence's even share of its cell's waves, twice that, for longer ones, and two more for
-// the waves that it has in part.
+// the waves that it has in part.  Still longer ones make all waves' shares larger.
 int shared_own_parts(int batch, int cell_wgs) {
   const int sequences = batch < kSharedCell ? batch : kSharedCell;
   const int64_t parts = 2 * ((4 * static_cast<int64_t>(cell_wgs) + sequences - 1) / sequences) + 2;

@@ -24,9 +24,10 @@
 //   161 + 8 us, 133: memory.  The two blocks of query rows read the common rows at 1.0 times
 //   their bytes from memory and again from L2, 7 TB/s into the units together; the matrix
 //   units work in 19% of the cycles, the vector units in 23, both in 5.
-//   16 sequences in 4 groups, window 4,096, 4 layers: 368 MB, 75 + 5 us, 56: 426 MB, since each
-//   sequence reads alone what lies between its window's start and its group's last one, and the
-//   ends of ragged groups.
+//   16 sequences in 4 groups, window 4,096, 4 layers: 368 MB, 75 + 5 us, 56: 426 MB, since the
+//   common rows begin at the group's last window start, and what lies between a sequence's own
+//   start and that one it reads alone (a choice: rows that some do not see would have to be
+//   masked by each query row's start, and kept from its sums in V); and the ends of ragged groups.
 //   128 sequences of 32 heads, 4,096 common rows and up to 400 own ones: 125 MB and 9 GFLOP,
 //   32 + 7 us, 19: products, exponentials and loads in turn, and 4,096 rows of 8 parts and more.
 //   8 sequences, 8,190 common rows: 62 MB, 16 + 5 us, 9.3: the way to the first tile (lengths,
@@ -624,8 +625,12 @@ __device__ __forceinline__ void attend_common(const PagedSharedParams &p, int id
 
 // ------------------------------------------------------------------ units' own rows
 // A cell is up to kSharedCell sequences of one layer and KV head.  Their own tiles, one
-// sequence after the other, are dealt evenly to the cell's waves, so that ragged sequences
-// leave no wave behind; a sequence's part of a wave is a part of its own for the join.
+// sequence after the other, are dealt evenly to the cell's waves, also of ragged sequences; a
+// sequence's part of a wave is a part of its own for the join.  Of one sequence there are
+// own_parts of them at most, 4 where a cell has as many sequences as waves: one that is longer
+// than 3 even shares makes every wave's share a third of itself, and leaves some waves nothing
+// (8 heads, 128 sequences of 20 own rows, one of 2,048: 69 us a call, 17 with as many rows dealt
+// evenly; one of 8,192: 198 and 20).
 struct Cell {
   int n[kSharedCell];           // rows with the new one
   int rows[kSharedCell];        // shared ones

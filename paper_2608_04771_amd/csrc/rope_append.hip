@@ -10,7 +10,8 @@
 // stores.  A thread holds 16 bytes of each end of its pairs, of one token, and goes
 // through the heads.  Bound by the rows' bytes: 16,384 tokens of 32 heads in bf16, 269 MB in 48 us
 // (5.6 TB/s; a copy reaches 4.9), with K and V of 16,384 tokens appended besides, 302 MB in 68 us
-// (4.5 TB/s: writes go to pages) and 5 us for the lengths.  One token takes 2.6 us, of 32
+// (4.5 TB/s: writes go to pages) and 5 us for the lengths; fp32, half as many tokens: 50 us, and
+// 70 and 5.  One token takes 2.6 us, of 32
 // sequences with its append 5.8: a launch and the round trips to positions, page ids and rows.
 // Blocks of 2, 8, 16 or 32 tokens and 512 or 1,024 threads were slower on long runs.
 #include "paged_device.hpp"
